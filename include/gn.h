@@ -453,6 +453,114 @@ gn_status gn_thin_m_gemm_noalloc(int M, int N, int64_t rows, const float* dA, in
                                  int64_t ldb, float* dD, int64_t ldd, void* cuda_stream, char* errbuf,
                                  int64_t errbuf_len);
 
+/* ======================================================================================================
+ * THE FEED-FORWARD BLOCK OF A LANGUAGE MODEL: layer norm, gated feed-forward layer, dropout
+ *
+ * The fully-connected networks above have z^m = sigma((W^m)^T z^{m-1} + b^m).  These calls evaluate and differentiate the form that a
+ * language model gives to a pair of such layers,
+ *     out = x + dropout(ffn(norm(x))),   ffn(x) = (act(x Wg^T) * (x Wu^T)) Wd^T,
+ * each part by a call of its own.  They need no context.
+ *
+ * MATRICES are row-major with unit stride inside a row and a leading dimension >= the row's length; weights keep the layout of
+ * W^m in theta, one row per neuron of the layer above.  gn_dtype names the type of all matrices of a call.  Any alignment that the
+ * type itself asks for is taken; 16-byte aligned bases and rows are the fast case.  Sums, row statistics and products
+ * are accumulated in FP32 whatever the type; results are rounded once, to nearest.
+ * STREAMS.  A call enqueues on the given stream (NULL: the legacy default stream) and never synchronises, so it can be captured;
+ * the device that holds the pointers is to be the current one.  The first call of each kind on a device loads its kernels: make it
+ * outside a capture.  WORKSPACES are the caller's: 16-byte aligned device memory of the size that the *_workspace call gives, free for
+ * any use before and after; two calls, or two captured graphs, that may run at the same time must not share one.  Nothing
+ * is kept in it from one call to the next.
+ * Inputs and outputs do not overlap unless a call says so.  Rows behind the last, and what lies between a row's end and the next row, is
+ * neither read into a result nor written.  rows == 0 is a call without rows: sums over rows are zero.
+ * ERRORS.  Arguments are checked before anything is launched; a failure's reason goes to errbuf (optional, errbuf_len bytes).
+ * Results are the same bits from one call to the next on the same operands.
+ * ====================================================================================================== */
+
+typedef enum { GN_F32 = 0, GN_BF16 = 1, GN_F16 = 2 } gn_dtype;
+
+/*
+ * gn_layer_norm - y = (x - mean) rstd w + b for each row of x [rows][cols]: mean = sum x / cols, rstd = 1 / sqrt(var + eps),
+ * var = sum (x - mean)^2 / cols.
+ *   wtype            type of d_weight and d_bias: `type` or GN_F32.
+ *   d_weight, d_bias [cols], each may be NULL (1 and 0).
+ *   eps              >= 0.  (0 and a row of equal elements give NaN.)
+ *   d_y              [rows][ldy]; may be d_x (with ldy == ldx).
+ *   d_mean, d_rstd   [rows] floats for the backward pass, each may be NULL.
+ * 1 <= cols <= 2^20.
+ */
+gn_status gn_layer_norm(gn_dtype type, gn_dtype wtype, int64_t rows, int32_t cols, const void* d_x, int64_t ldx, const void* d_weight,
+                        const void* d_bias, double eps, void* d_y, int64_t ldy, float* d_mean, float* d_rstd, void* cuda_stream,
+                        char* errbuf, int64_t errbuf_len);
+
+/*
+ * gn_layer_norm_grad - backward pass of gn_layer_norm.  With xhat = (x - mean) rstd and g = dy w:
+ *     dx = rstd (g - avg(g) - xhat avg(g xhat)) + add,   dw = sum_rows dy xhat,   db = sum_rows dy.
+ *   d_mean, d_rstd       what the forward call has written.
+ *   d_weight             as in the forward call, or NULL.
+ *   d_add                [rows][ld_add] or NULL: the gradient that reaches x past the norm (the residual path).
+ *   d_dx                 [rows][ld_dx] or NULL (not wanted); may be d_dy or d_add (with the same leading dimension).
+ *   d_dweight, d_dbias   [cols] of type wtype, each may be NULL.  Rows are summed in a fixed order.
+ *   d_ws                 workspace of gn_layer_norm_grad_workspace(rows, cols) bytes.
+ */
+int64_t gn_layer_norm_grad_workspace(int64_t rows, int32_t cols);
+gn_status gn_layer_norm_grad(gn_dtype type, gn_dtype wtype, int64_t rows, int32_t cols, const void* d_dy, int64_t ld_dy,
+                             const void* d_x, int64_t ldx, const float* d_mean, const float* d_rstd, const void* d_weight,
+                             const void* d_add, int64_t ld_add, void* d_dx, int64_t ld_dx, void* d_dweight, void* d_dbias,
+                             void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+
+/*
+ * gn_dropout - y = keep ? x / (1 - p) : 0, plus the residual where there is one.  No mask is stored: element (r, c) of a matrix of
+ * `cols` columns is element i = r cols + c of the call, and is kept iff
+ *     word i mod 4 of Philox4x32-10(counter = (low and high word of i / 4, low and high word of step), key)  >=  round(p 2^32)
+ * (Salmon et al. 2011, "Parallel random numbers: as easy as 1, 2, 3").  The same key and step give the same mask whatever the type,
+ * leading dimensions and device, so the backward pass is this call on the gradient, without the residual.  What is dropped is zero
+ * even where x is infinite or NaN.
+ *   p            0 <= p <= 1; p = 1 drops everything.
+ *   key, step    any 64-bit numbers: a run's seed and, say, the number of the training step and layer.
+ *   d_step       NULL, or a device word that is added to step when the kernel runs: a captured training step draws a new mask at
+ *                every replay if the graph, or the caller between replays, advances that word.
+ *   d_residual   [rows][ld_res] or NULL.
+ *   d_y          [rows][ldy]; may be d_x or d_residual (with the same leading dimension).
+ */
+gn_status gn_dropout(gn_dtype type, int64_t rows, int32_t cols, const void* d_x, int64_t ldx, const void* d_residual, int64_t ld_res,
+                     void* d_y, int64_t ldy, double p, uint64_t key, uint64_t step, const uint64_t* d_step, void* cuda_stream,
+                     char* errbuf, int64_t errbuf_len);
+
+typedef enum {
+  GN_ACT_SIGMOID = 0,   /* 1 / (1 + exp(-g)), the network's own */
+  GN_ACT_SILU = 1,      /* g sigmoid(g) */
+  GN_ACT_GELU = 2,      /* g Phi(g), Phi by the error function */
+  GN_ACT_GELU_TANH = 3, /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+  GN_ACT_RELU = 4       /* max(g, 0), derivative 0 at 0 */
+} gn_act;
+
+typedef struct { void* p; int64_t ld; } gn_mat;
+
+/*
+ * gn_gated_ffn - y = (act(x Wg^T) * (x Wu^T)) Wd^T.
+ *   type, act, rows, cols, inner   x, y [rows][cols]; w_gate, w_up [inner][cols]; w_down [cols][inner]; all other members as needed:
+ *   gate, up                       [rows][inner], each with p == NULL or an output: x Wg^T and x Wu^T, for the backward pass.
+ * gn_gated_ffn_grad - its backward pass.  With h = act(gate) * up, dh = dy Wd, dup = dh act(gate), dgate = dh up act'(gate):
+ *     dx = dgate Wg + dup Wu,   dWg = dgate^T x,   dWu = dup^T x,   dWd = dy^T h.
+ *   dy [rows][cols], x, gate, up, and the three weights are inputs; dx, dw_gate, dw_up, dw_down are outputs of the shapes of x and the
+ *   weights, each with p == NULL where it is not wanted.
+ * GN_BF16 and GN_F16: operands go to the tensor cores as they are; h, dup and dgate are rounded to the type on their way into the next
+ * product.  GN_F32: every product at FP32 accuracy (see gn_set_accurate_method).
+ * Workspace: gn_gated_ffn_workspace(args, backward) bytes for the same args; it depends on sizes, types, leading dimensions
+ * and on the alignment of the pointers, and is negative for bad arguments.
+ * 1 <= cols, inner <= 2^24 with cols * inner < 2^31; rows < 2^31.
+ */
+typedef struct {
+  int32_t type, act;          /* gn_dtype, gn_act */
+  int64_t rows;
+  int32_t cols, inner;
+  gn_mat x, w_gate, w_up, w_down, y, gate, up, dy, dx, dw_gate, dw_up, dw_down;
+} gn_ffn;
+
+int64_t gn_gated_ffn_workspace(const gn_ffn* args, int32_t backward);
+gn_status gn_gated_ffn(const gn_ffn* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+gn_status gn_gated_ffn_grad(const gn_ffn* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+
 #ifdef __cplusplus
 }
 #endif

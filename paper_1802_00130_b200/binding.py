@@ -54,6 +54,15 @@ _SIGNATURES = {
     "gn_debug_gemm": (_i32, [_vp, _i32, _i32, _i32, _i32, _vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64]),
     "gn_debug_gemm_epilogue": (_i32, [_vp, _i32, _i32, _i32, _i32, _vp, _i64, _i32, _vp, _i64, _i32, _vp, _i64,
                                       _vp, _i32, _vp, _i64, C.c_float, _vp, _i64, C.c_float]),
+    "gn_layer_norm": (_i32, [_i32, _i32, _i64, _i32, _vp, _i64, _vp, _vp, _dbl, _vp, _i64, _vp, _vp, _vp, C.c_char_p, _i64]),
+    "gn_layer_norm_grad_workspace": (_i64, [_i64, _i32]),
+    "gn_layer_norm_grad": (_i32, [_i32, _i32, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp,
+                                  _vp, _i64, _vp, C.c_char_p, _i64]),
+    "gn_dropout": (_i32, [_i32, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _dbl, C.c_uint64, C.c_uint64, _vp, _vp, C.c_char_p,
+                          _i64]),
+    "gn_gated_ffn_workspace": (_i64, [_vp, _i32]),
+    "gn_gated_ffn": (_i32, [_vp, _vp, _i64, _vp, C.c_char_p, _i64]),
+    "gn_gated_ffn_grad": (_i32, [_vp, _vp, _i64, _vp, C.c_char_p, _i64]),
 }
 
 

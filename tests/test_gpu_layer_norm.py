@@ -1,0 +1,236 @@
+"""Layer norm and its backward pass against a plain form in 64 bits."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_1802_00130_b200 as gn
+from feedforward_common import E, TYPES, rand, tiny, u, vec, within
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [(1, 1), (5, 2), (3, 7), (131, 8), (33, 33), (257, 64), (1, 100), (700, 127), (64, 256), (300, 617), (19, 1000), (4001, 1024),
+          (7, 1201), (40, 4096), (3, 8200), (2, 16384), (2, 16385), (3, 32768), (2, 70001), (1, 300000)]
+
+
+def norm64(x, w, b, eps):
+    x = x.double()
+    mean = x.mean(1, keepdim=True)
+    d = x - mean
+    rstd = (d.square().mean(1, keepdim=True) + eps) ** -0.5
+    y = d * rstd * (1 if w is None else w.double()) + (0 if b is None else b.double())
+    return y, mean[:, 0], rstd[:, 0]
+
+
+def norm_bounds(x, w, b, y, mean, rstd, t):
+    """FP32 arithmetic on a row: sums of up to cols / 32 terms a thread in sequence and a tree of 10 steps after it (each term of the sums
+    carries one or two roundings), rstd of a quotient, a root and a reciprocal, and the four operations of y."""
+    n = x.shape[1]
+    rel = E * (n / 32 + 24)
+    x = x.double()
+    spread = x.abs().mean(1)                                       # what the sum's roundings are relative to
+    m_err = rel * (x - mean[:, None]).abs().mean(1) + 2 * E * mean.abs() + (E * (n / 32 + 24)) ** 2 * spread
+    r_err = rel * rstd
+    W = torch.ones_like(x) if w is None else w.double().expand_as(x)
+    B = torch.zeros_like(x) if b is None else b.double().expand_as(x)
+    scaled = (x - mean[:, None]).abs() * rstd[:, None] * W.abs()
+    y_err = u(t) * y.abs() + tiny(t) + (rel + 4 * E) * scaled + 2 * E * B.abs() + (m_err - 2 * E * mean.abs())[:, None] * rstd[:, None] * W.abs() \
+        + E * (x.abs() + mean.abs()[:, None]) * rstd[:, None] * W.abs() * (E * n)
+    return y_err, m_err + 1e-30, r_err
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("t,wt", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32")])
+def test_forward(t, wt, shape):
+    rows, cols = shape
+    t, wt = TYPES[t], TYPES[wt]
+    x = rand(shape, t, rows + cols, 1.5, 0.3)
+    w, b = vec(cols, wt, 1, 0.2, 1.0), vec(cols, wt, 2, 0.3)
+    y, mean, rstd = gn.layer_norm(x, w, b, 1e-5, save=True)
+    ry, rm, rr = norm64(x, w, b, 1e-5)
+    by, bm, br = norm_bounds(x, w, b, ry, rm, rr, t)
+    within(y, ry, by, "y")
+    within(mean, rm, bm, "mean")
+    within(rstd, rr, br, "rstd")
+    assert torch.equal(gn.layer_norm(x, w, b, 1e-5), y)
+
+
+@pytest.mark.parametrize("pad", [1, 3, 8])
+@pytest.mark.parametrize("w,b", [(True, False), (False, True), (False, False)])
+@pytest.mark.parametrize("t", TYPES)
+def test_forward_strides_and_no_weights(t, w, b, pad):
+    t = TYPES[t]
+    x = rand((57, 520), t, 3, 1.0, -0.5, pad)
+    w, b = vec(520, t, 1) if w else None, vec(520, t, 2) if b else None
+    y, mean, rstd = gn.layer_norm(x, w, b, 0.0, save=True)
+    ry, rm, rr = norm64(x, w, b, 0.0)
+    by, _, _ = norm_bounds(x, w, b, ry, rm, rr, t)
+    within(y, ry, by, "y")
+
+
+@pytest.mark.parametrize("offset", range(1, 8))
+def test_forward_misaligned_bases(offset):
+    flat = vec(64 * 1024 + 8, torch.bfloat16, 4)
+    w = vec(1024 + 8, torch.bfloat16, 5)
+    x = flat[offset: offset + 64 * 1024].view(64, 1024)
+    y = gn.layer_norm(x, w[offset: offset + 1024], w[8 - offset: 8 - offset + 1024])
+    assert torch.equal(y, gn.layer_norm(x.clone(), w[offset: offset + 1024].clone(), w[8 - offset: 8 - offset + 1024].clone()))
+
+
+def test_forward_of_a_large_mean():
+    """mean / spread = 10^4: the corrected sums keep y to FP32 accuracy of the values x - mean, which are exact to 2^-24 |x|."""
+    x = rand((40, 3000), torch.float32, 6, 1.0, 1e4)
+    y, mean, rstd = gn.layer_norm(x, save=True)
+    ry, rm, rr = norm64(x, None, None, 1e-5)
+    # x - m is exact (Sterbenz) and the correction removes m's own error; what is left is rel of the spread
+    within(y, ry, E * (3000 / 32 + 40) * (ry.abs() + 1), "y")
+    within(mean, rm, 2 * E * rm.abs(), "mean")
+    within(rstd, rr, E * (3000 / 32 + 40) * rr, "rstd")
+
+
+@pytest.mark.parametrize("cols", [5, 640, 4096, 20000])
+def test_forward_rows_of_equal_elements_and_bad_rows(cols):
+    x = rand((6, cols), torch.float32, 7)
+    good = gn.layer_norm(x)
+    x[1] = 3.25
+    x[3, cols // 2] = float("nan")
+    x[4, cols - 1] = float("inf")
+    y, mean, rstd = gn.layer_norm(x, save=True)
+    assert torch.equal(y[[0, 2, 5]], good[[0, 2, 5]])
+    assert bool((y[1] == 0).all()) and float(mean[1]) == 3.25 and abs(float(rstd[1]) - 1e-5 ** -0.5) < 1e-3
+    assert bool(y[3].isnan().all()) and bool(y[4].isnan().any())
+
+
+def grads64(dy, x, mean, rstd, w, add):
+    dy, xh = dy.double(), (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    g = dy if w is None else dy * w.double()
+    dx = rstd.double()[:, None] * (g - g.mean(1, keepdim=True) - xh * (g * xh).mean(1, keepdim=True))
+    return dx + (0 if add is None else add.double()), (dy * xh).sum(0), dy.sum(0)
+
+
+def check_grads(got, dy, x, mean, rstd, w, add, t, wt):
+    n, rows = x.shape[1], x.shape[0]
+    ref = grads64(dy, x, mean, rstd, w, add)
+    xh = ((x.double() - mean.double()[:, None]) * rstd.double()[:, None]).abs()
+    g = dy.double().abs() * (1 if w is None else w.double().abs())
+    rel, rs = E * (n / 32 + 24), rstd.double()[:, None]
+    x_err = E * (x.double().abs() + mean.double().abs()[:, None]) * rs          # of (x - mean) rstd, absolute
+    # every term of dx with the roundings that went into it, the sums with theirs
+    b_dx = u(t) * ref[0].abs() + tiny(t) + 6 * E * rs * g + rs * rel * (g.mean(1, keepdim=True) + xh * (g * xh).mean(1, keepdim=True)) \
+        + rs * (x_err * (g * xh).mean(1, keepdim=True) + xh * (g * x_err).mean(1, keepdim=True)) + 2 * E * (0 if add is None else add.double().abs())
+    within(got[0], ref[0], b_dx, "dx")
+    # sums over rows: every addition is off by at most E of a partial sum, in sequence over the rows of a block and then over the blocks
+    terms = dy.double().abs() * xh
+    acc = 7 * E * max(rows, 1) ** 0.5 + 8 * E
+    spread = lambda v: (v * v).sum(0).sqrt()
+    b_dw = u(wt) * ref[1].abs() + tiny(wt) + acc * (ref[1].abs() + 7 * spread(terms)) + (dy.double().abs() * x_err).sum(0) + 4 * E * terms.sum(0)
+    within(got[1], ref[1], b_dw, "dweight")
+    b_db = u(wt) * ref[2].abs() + tiny(wt) + acc * (ref[2].abs() + 7 * spread(dy.double()))
+    within(got[2], ref[2], b_db, "dbias")
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("shape", SHAPES + [(20000, 96), (9000, 24), (5000, 520)])
+@pytest.mark.parametrize("t,wt", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32")])
+def test_backward(t, wt, shape, add):
+    rows, cols = shape
+    t, wt = TYPES[t], TYPES[wt]
+    x = rand(shape, t, rows + 3 * cols, 1.5, 0.3)
+    dy = rand(shape, t, rows + 5 * cols, 0.5)
+    w = vec(cols, wt, 1, 0.2, 1.0)
+    a = rand(shape, t, 9) if add else None
+    _, mean, rstd = gn.layer_norm(x, w, save=True)
+    got = gn.layer_norm_grad(dy, x, mean, rstd, w, add=a)
+    assert got[0].dtype == t and got[1].dtype == wt and got[2].dtype == wt
+    check_grads(got, dy, x, mean, rstd, w, a, t, wt)
+    again = gn.layer_norm_grad(dy, x, mean, rstd, w, add=a)
+    assert all(torch.equal(p, q) for p, q in zip(got, again))          # sums in a fixed order
+
+
+@pytest.mark.parametrize("cols", [24, 521, 5000])
+@pytest.mark.parametrize("t", TYPES)
+def test_backward_strides_and_no_weight(t, cols):
+    t = TYPES[t]
+    x, dy, add = rand((77, cols), t, 1, pad=3), rand((77, cols), t, 2, pad=1), rand((77, cols), t, 3, pad=8)
+    _, mean, rstd = gn.layer_norm(x, save=True)
+    check_grads(gn.layer_norm_grad(dy, x, mean, rstd, None, add=add), dy, x, mean, rstd, None, add, t, t)
+
+
+def test_backward_against_differences():
+    """d/dx of sum(c * norm(x)) by central differences of the 64-bit form."""
+    x, w, c = rand((3, 17), torch.float32, 1), vec(17, torch.float32, 2, 0.2, 1.0), rand((3, 17), torch.float32, 3)
+    _, mean, rstd = gn.layer_norm(x, w, save=True)
+    dx, dw, db = gn.layer_norm_grad(c, x, mean, rstd, w)
+    h, x64 = 1e-5, x.double()
+    f = lambda x, w: (norm64(x, w, None, 1e-5)[0] * c.double()).sum()
+    for i in range(3):
+        for j in range(17):
+            d = torch.zeros_like(x64)
+            d[i, j] = h
+            # the difference's own error is of the order h^2 = 1e-10 and 1e-16 / h = 1e-11; the call's is FP32 rounding
+            assert abs(float((f(x64 + d, w) - f(x64 - d, w)) / (2 * h)) - float(dx[i, j])) < 2e-5
+    for j in range(17):
+        d = torch.zeros(17, dtype=torch.float64, device="cuda")
+        d[j] = h
+        assert abs(float((f(x64, w.double() + d) - f(x64, w.double() - d)) / (2 * h)) - float(dw[j])) < 2e-5
+
+
+def test_no_rows():
+    x = torch.empty(0, 40, dtype=torch.bfloat16, device="cuda")
+    w = vec(40, torch.float32, 1)
+    y, mean, rstd = gn.layer_norm(x, w, save=True)
+    assert y.shape == (0, 40) and mean.shape == (0,)
+    dx, dw, db = gn.layer_norm_grad(x, x, mean, rstd, w)
+    assert dx.shape == (0, 40) and not dw.any() and not db.any()
+
+
+@pytest.mark.parametrize("cols", [12, 600, 4096, 9000, 40000])
+def test_in_place_and_what_is_left_alone(cols):
+    """y in x's place, dx in dy's and in add's; columns past the row's end and rows behind the last keep what they hold."""
+    rows, ld = 9, cols + 5
+    err = C.create_string_buffer(200)
+    x, dy, add = rand((rows, cols), torch.float16, 1), rand((rows, cols), torch.float16, 2), rand((rows, cols), torch.float16, 3)
+    w = vec(cols, torch.float16, 4)
+    y, mean, rstd = gn.layer_norm(x, w, save=True)
+    want = gn.layer_norm_grad(dy, x, mean, rstd, w, add=add)
+
+    def wide(m):
+        b = torch.full((rows + 2, ld), 7.0, dtype=torch.float16, device="cuda")
+        b[:rows, :cols] = m
+        return b
+
+    def kept(b):
+        assert bool((b[rows:] == 7).all()) and bool((b[:, cols:] == 7).all())
+        return b[:rows, :cols]
+
+    bx = wide(x)
+    assert gn.lib().gn_layer_norm(2, 2, rows, cols, bx.data_ptr(), ld, w.data_ptr(), None, 1e-5, bx.data_ptr(), ld, None, None,
+                                  torch.cuda.current_stream().cuda_stream, err, 200) == 0, err.value
+    assert torch.equal(kept(bx), y)
+    n = gn.lib().gn_layer_norm_grad_workspace(rows, cols)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    for place in range(2):
+        b = [wide(dy), wide(add)]
+        assert gn.lib().gn_layer_norm_grad(2, 2, rows, cols, b[0].data_ptr(), ld, x.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), w.data_ptr(),
+                                           b[1].data_ptr(), ld, b[place].data_ptr(), ld, None, None, ws.data_ptr(), n,
+                                           torch.cuda.current_stream().cuda_stream, err, 200) == 0, err.value
+        assert torch.equal(kept(b[place]), want[0])
+        kept(b[1 - place])
+
+
+def test_refusals():
+    x = rand((4, 16), torch.bfloat16, 1)
+    _, mean, rstd = gn.layer_norm(x, save=True)
+    for bad in (lambda: gn.layer_norm(x.double()), lambda: gn.layer_norm(x, vec(16, torch.float16, 1)),
+                lambda: gn.layer_norm(x, vec(16, torch.float32, 1), vec(16, torch.bfloat16, 1)),
+                lambda: gn.layer_norm_grad(x.float(), x, mean, rstd), lambda: gn.layer_norm_grad(x, x, mean.double(), rstd),
+                lambda: gn.layer_norm_grad(x, x, None, rstd)):
+        with pytest.raises(TypeError):
+            bad()
+    for bad in (lambda: gn.layer_norm(x[0]), lambda: gn.layer_norm(x, vec(15, torch.bfloat16, 1)), lambda: gn.layer_norm(x.T),
+                lambda: gn.layer_norm(x[:1].expand(4, 16)), lambda: gn.layer_norm(x[:, :0]), lambda: gn.layer_norm_grad(x[:3], x, mean, rstd),
+                lambda: gn.layer_norm_grad(x, x, mean[:3], rstd), lambda: gn.layer_norm_grad(x, x, mean, rstd, add=x[:, :8])):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(gn.GnError, match="eps"):
+        gn.layer_norm(x, eps=-1.0)

@@ -548,7 +548,9 @@ typedef struct { void* p; int64_t ld; } gn_mat;
  * product.  GN_F32: every product at FP32 accuracy (see gn_set_accurate_method).
  * Workspace: gn_gated_ffn_workspace(args, backward) bytes for the same args; it depends on sizes, types, leading dimensions
  * and on the alignment of the pointers, and is negative for bad arguments.
- * 1 <= cols, inner <= 2^24 with cols * inner < 2^31; rows < 2^31.
+ * 1 <= cols, inner <= 2^24 with cols * inner < 2^31; rows < 2^30.
+ * gn_gated_ffn_status - synchronises the stream and returns GN_ETIMEOUT if a bounded wait of one of these calls' tensor-core kernels has
+ * run out on the current device since the last look (results are invalid then), else GN_OK.
  */
 typedef struct {
   int32_t type, act;          /* gn_dtype, gn_act */
@@ -560,6 +562,7 @@ typedef struct {
 int64_t gn_gated_ffn_workspace(const gn_ffn* args, int32_t backward);
 gn_status gn_gated_ffn(const gn_ffn* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 gn_status gn_gated_ffn_grad(const gn_ffn* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+gn_status gn_gated_ffn_status(void* cuda_stream, char* errbuf, int64_t errbuf_len);
 
 #ifdef __cplusplus
 }

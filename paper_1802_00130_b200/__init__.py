@@ -5,7 +5,7 @@ path runs in the library's CUDA kernels.  PyTorch supplies device memory and str
 """
 from .binding import (GN_FP32_ACCURATE, GN_TF32, GnContext, GnError, NewtonParams, NewtonReport, exported_symbols, lib, lib_path,
                       plan_group, thin_m_gemm_noalloc)
-from .feedforward import dropout, gated_ffn, gated_ffn_grad, layer_norm, layer_norm_grad
+from .feedforward import dropout, gated_ffn, gated_ffn_grad, gated_ffn_status, layer_norm, layer_norm_grad
 
 __all__ = ["GnContext", "GnError", "GN_TF32", "GN_FP32_ACCURATE", "lib", "lib_path", "exported_symbols", "NewtonParams", "NewtonReport", "thin_m_gemm_noalloc", "plan_group",
-           "layer_norm", "layer_norm_grad", "dropout", "gated_ffn", "gated_ffn_grad"]
+           "layer_norm", "layer_norm_grad", "dropout", "gated_ffn", "gated_ffn_grad", "gated_ffn_status"]

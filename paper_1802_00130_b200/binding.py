@@ -63,6 +63,7 @@ _SIGNATURES = {
     "gn_gated_ffn_workspace": (_i64, [_vp, _i32]),
     "gn_gated_ffn": (_i32, [_vp, _vp, _i64, _vp, C.c_char_p, _i64]),
     "gn_gated_ffn_grad": (_i32, [_vp, _vp, _i64, _vp, C.c_char_p, _i64]),
+    "gn_gated_ffn_status": (_i32, [_vp, C.c_char_p, _i64]),
 }
 
 

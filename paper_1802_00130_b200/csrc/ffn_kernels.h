@@ -1,0 +1,30 @@
+// Launch interface between the gated feed-forward block's calls (gated_ffn.cu) and its tensor-core kernels.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace gn {
+
+// A stored matrix of 16-bit elements, 16-byte aligned with a leading dimension that is a multiple of 8 where TMA is to read it.
+struct Mat16 { const void* p = nullptr; int64_t ld = 0; };
+struct Out16 { void* p = nullptr; int64_t ld = 0; };
+
+// What becomes of the sums acc(m, n) = sum_k A(m, k) B(k, n) (+ the same of a second operand pair):
+//   FFN_STORE  d[0] = acc
+//   FFN_GATE   two right operands, B[0] and B[1], one sum each: gate and up.  d[0] = act(gate) * up; d[1], d[2] = gate, up (optional)
+//   FFN_GRAD   acc = dh: d[0] = act(gate) * up, d[1] = dh up act'(gate), d[2] = dh act(gate), from the stored gate and up
+enum FfnKind { FFN_STORE = 0, FFN_GATE = 1, FFN_GRAD = 2 };
+struct FfnGemm {
+  int M = 0, N = 0;
+  int K[2] = {0, 0};             // K[1] > 0: a second operand pair (FFN_STORE)
+  bool a_mn = false, b_mn = false;   // stored [K][M], [K][N] instead of [M][K], [N][K]
+  Mat16 A[2], B[2];
+  Out16 d[3];
+  Mat16 gate, up;
+};
+constexpr int kFfnGroup = 4;     // problems of one launch (FFN_STORE)
+
+// CTA-pair kernel (gemm_pair16.cu).  Returns cudaSuccess, or what the launch or the maps failed with.
+cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, int* err, cudaStream_t st);
+
+}  // namespace gn

@@ -1,95 +1,75 @@
 // Gated feed-forward block and its backward pass: the calls, their workspaces and the order of their products.
+//
+// 16-bit types: two tensor-core launches forward (both projections with the gate, then the product with Wd), two backward (dh with the
+// gate's gradient, then dx and the three weight gradients as one launch).  TMA reads the operands, so one with a base or a leading
+// dimension that is no multiple of 16 bytes is copied to the workspace first.
+// FP32: the FP32-accurate products of the rest of the library (gemm_f16x3.cu, gemm_ffma.cu), with the gate as a pass of its own.
 #include <math.h>
 
-#include "op_common.cuh"
+#include <atomic>
+
+#include "ffn_act.cuh"
+#include "ffn_kernels.h"
+#include "gn_kernels.h"
 
 namespace gn {
 namespace {
 
-// 1 / (1 + exp(-v)) and 1 / (1 + exp(v)), each to full relative accuracy: one minus the other would lose it where it is small.
-__device__ __forceinline__ void sigmoids(float v, float& z, float& nz) {
-  const float e = expf(-fabsf(v)), r = 1.f / (1.f + e);
-  z = v < 0.f ? e * r : r; nz = v < 0.f ? r : e * r;
-}
-// act(v) and its derivative.  A NaN stays one: comparisons with it fall to the branch that computes with it.
-__device__ __forceinline__ void activation(int act, float v, float& a, float& da) {
-  float z, nz;
-  switch (act) {
-    case GN_ACT_RELU: a = v < 0.f ? 0.f : v; da = v > 0.f ? 1.f : 0.f; break;
-    case GN_ACT_GELU: {
-      const float cdf = 0.5f * erfcf(-0.70710678118654752f * v);
-      a = v * cdf; da = cdf + v * 0.39894228040143268f * expf(-0.5f * v * v);
-      break;
-    }
-    case GN_ACT_GELU_TANH: {                   // (1 + tanh q) / 2 = 1 / (1 + exp(-2 q))
-      const float k = 1.5957691216057308f;     // 2 sqrt(2 / pi)
-      sigmoids(k * (v + 0.044715f * v * v * v), z, nz);
-      a = v * z; da = z + v * z * nz * k * (1.f + 0.134145f * v * v);
-      break;
-    }
-    case GN_ACT_SIGMOID: sigmoids(v, z, nz); a = z; da = z * nz; break;
-    default: sigmoids(v, z, nz); a = v * z; da = z + v * z * nz;
+__device__ int ffn_error;        // code of a bounded wait that ran out; looked at, and cleared, by gn_gated_ffn_status
+
+int* error_word() {
+  static std::atomic<void*> at[64];
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+  void* p = at[dev].load(std::memory_order_acquire);
+  if (!p) {
+    if (cudaGetSymbolAddress(&p, ffn_error) != cudaSuccess) return nullptr;
+    at[dev].store(p, std::memory_order_release);
   }
+  return static_cast<int*>(p);
 }
 
-// D(m, n) = sum over the operand pairs of sum_k A(m, k) B(k, n), element (i, j) of an operand at i s0 + j s1.
-struct Operand { const void* p; int64_t s0, s1; };
-struct PlainGemm { int64_t M, N, K; int pairs; Operand a[2], b[2]; void* d; int64_t ldd; };
-template <class T, class D>
-__global__ void plain_gemm_kernel(const PlainGemm g) {
-  __shared__ float sa[16][65], sb[16][65];
-  const int64_t m0 = (int64_t)blockIdx.x * 64, n0 = (int64_t)blockIdx.y * 64;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[4][4] = {};
-  for (int q = 0; q < g.pairs; ++q)
-    for (int64_t k0 = 0; k0 < g.K; k0 += 16) {
-      for (int e = threadIdx.x; e < 1024; e += 256) {
-        const int i = e >> 4, k = e & 15;
-        sa[k][i] = m0 + i < g.M && k0 + k < g.K ? to_f(((const T*)g.a[q].p)[(m0 + i) * g.a[q].s0 + (k0 + k) * g.a[q].s1]) : 0.f;
-        sb[k][i] = n0 + i < g.N && k0 + k < g.K ? to_f(((const T*)g.b[q].p)[(k0 + k) * g.b[q].s0 + (n0 + i) * g.b[q].s1]) : 0.f;
-      }
-      __syncthreads();
-      for (int k = 0; k < 16; ++k)
-        for (int i = 0; i < 4; ++i)
-          for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[k][ty + 16 * i], sb[k][tx + 16 * j], acc[i][j]);
-      __syncthreads();
-    }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int64_t m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-      if (m < g.M && n < g.N) ((D*)g.d)[m * g.ldd + n] = from_f<D>(acc[i][j]);
-    }
-}
-
-// h = act(gate) * up, and with dh the two gradients.
-struct Gates { int64_t rows; int cols, act; const void *gate, *up; int64_t ld_gate, ld_up; const float* dh; void *h, *dgate, *dup; };
-template <class T>
+// h = act(gate) * up, and with dh the two gradients, in FP32.
+struct Gates { int64_t rows; int cols, act; const float *gate, *up; int64_t ld_gate, ld_up; const float* dh; float *h, *dgate, *dup; int64_t ld; };
 __global__ void gate_kernel(const Gates g) {
   const int64_t n = g.rows * g.cols;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
-    const int64_t r = i / g.cols, c = i % g.cols;
-    float a, da;
-    const float u = to_f(((const T*)g.up)[r * g.ld_up + c]);
-    activation(g.act, to_f(((const T*)g.gate)[r * g.ld_gate + c]), a, da);
-    if (g.h) ((T*)g.h)[i] = from_f<T>(a * u);
-    if (g.dh) {
-      ((T*)g.dup)[i] = from_f<T>(g.dh[i] * a);
-      ((T*)g.dgate)[i] = from_f<T>(g.dh[i] * u * da);
+  with_activation(g.act, [&](auto act) {
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+      const int64_t r = i / g.cols, c = i % g.cols, o = r * g.ld + c;
+      float a, da;
+      const float u = g.up[r * g.ld_up + c];
+      activation<decltype(act)::value, false>(g.gate[r * g.ld_gate + c], a, da);
+      g.h[o] = a * u;
+      if (g.dh) { g.dup[o] = g.dh[o] * a; g.dgate[o] = g.dh[o] * u * da; }
     }
-  }
+  });
 }
-template <class T, class D = T>
-cudaError_t plain_gemm(const PlainGemm& g, cudaStream_t st) {
-  if (g.M == 0 || g.N == 0) return cudaSuccess;
-  plain_gemm_kernel<T, D><<<dim3((unsigned)((g.M + 63) / 64), (unsigned)((g.N + 63) / 64)), 256, 0, st>>>(g);
-  return cudaGetLastError();
+
+// Copies of 16-bit matrices with rows that TMA can address.
+constexpr int kPackMax = 5;
+struct PackJob { const uint16_t* src; uint16_t* dst; int64_t rows, ld, ld_out; int cols; };
+struct PackList { PackJob j[kPackMax]; };
+__global__ void pack_kernel(const PackList list) {
+  const PackJob& j = list.j[blockIdx.y];
+  const int units = (j.cols + 7) / 8;
+  const int64_t n = j.rows * units;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+    const int64_t r = i / units;
+    const int c = (int)(i - r * units) * 8;
+    const uint16_t* const s = j.src + r * j.ld + c;
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e < j.cols) w[e >> 1] |= (uint32_t)s[e] << (16 * (e & 1));
+    *reinterpret_cast<uint4*>(j.dst + r * j.ld_out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
 }
 
 const char* ffn_args(const gn_ffn* f, bool backward) {
   if (!f) return "no arguments";
   if (!type_ok(f->type)) return "type is not a gn_dtype";
   if (f->act < GN_ACT_SIGMOID || f->act > GN_ACT_RELU) return "act is not a gn_act";
-  if (f->rows < 0 || f->rows >= (int64_t(1) << 31)) return "rows must be in [0, 2^31)";
+  if (f->rows < 0 || f->rows >= (int64_t(1) << 30)) return "rows must be in [0, 2^30)";
   if (f->cols < 1 || f->inner < 1 || f->cols > (1 << 24) || f->inner > (1 << 24) || (int64_t)f->cols * f->inner >= (int64_t(1) << 31))
     return "cols and inner must be in [1, 2^24] with a product below 2^31";
   const struct { const gn_mat* m; int64_t cols; bool needed, rows; const char* why; } list[] = {
@@ -114,57 +94,255 @@ const char* ffn_args(const gn_ffn* f, bool backward) {
   return nullptr;
 }
 
-struct Workspace {               // hands out 256-byte aligned pieces, or only counts them
+
+inline int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+
+struct Workspace {               // hands out 256-byte aligned pieces (of no memory at all where a call is only measured)
   char* p; int64_t used = 0;
-  void* take(int64_t bytes) { void* r = p ? p + used : nullptr; used += (bytes + 255) / 256 * 256; return r; }
+  void* take(int64_t bytes) { void* r = p + used; used += (bytes + 255) / 256 * 256; return r; }
 };
-struct Pieces { void *gate, *up, *h, *dgate, *dup; float* dh; };
-int64_t lay_out(const gn_ffn& f, bool backward, char* base, Pieces& w) {
+char* const kNowhere = reinterpret_cast<char*>(256);
+
+// ---- 16-bit types ------------------------------------------------------------------------------
+struct Half {
+  Mat16 x, w_gate, w_up, w_down, dy;      // as TMA reads them
+  PackList packs; int n_packs; int64_t pack_units;
+  Out16 h, dgate, dup;
+};
+Mat16 addressable(const gn_mat& m, int64_t rows, int cols, Workspace& ws, Half& w) {
+  if (((uintptr_t)m.p & 15) == 0 && m.ld % 8 == 0) return {m.p, m.ld};
+  const int64_t ld = up8(cols);
+  void* const dst = ws.take(rows * ld * 2);
+  w.packs.j[w.n_packs++] = {(const uint16_t*)m.p, (uint16_t*)dst, rows, m.ld, ld, cols};
+  if (rows * (ld / 8) > w.pack_units) w.pack_units = rows * (ld / 8);
+  return {dst, ld};
+}
+int64_t lay_out_half(const gn_ffn& f, bool backward, char* base, Half& w) {
   Workspace ws{base};
-  const int64_t hidden = f.rows * f.inner * type_bytes(f.type);
-  w = Pieces{};
-  w.h = ws.take(hidden);
-  if (backward) { w.dgate = ws.take(hidden); w.dup = ws.take(hidden); w.dh = (float*)ws.take(f.rows * f.inner * 4); }
-  else { w.gate = ws.take(f.gate.p ? 0 : hidden); w.up = ws.take(f.up.p ? 0 : hidden); }
-  return ws.used + 256;
+  w = Half{};
+  const int64_t ld = up8(f.inner);
+  w.x = addressable(f.x, f.rows, f.cols, ws, w);
+  w.w_gate = addressable(f.w_gate, f.inner, f.cols, ws, w);
+  w.w_up = addressable(f.w_up, f.inner, f.cols, ws, w);
+  w.w_down = addressable(f.w_down, f.cols, f.inner, ws, w);
+  if (backward) w.dy = addressable(f.dy, f.rows, f.cols, ws, w);
+  for (Out16* o : {&w.h, &w.dgate, &w.dup}) {
+    if (o != &w.h && !backward) break;
+    *o = {ws.take(f.rows * ld * 2), ld};
+  }
+  return ws.used;
 }
+cudaError_t pack(const Half& w, cudaStream_t st) {
+  if (w.n_packs == 0) return cudaSuccess;
+  const int64_t blocks = (w.pack_units + 255) / 256;
+  pack_kernel<<<dim3((unsigned)(blocks < 1184 ? blocks : 1184), (unsigned)w.n_packs), 256, 0, st>>>(w.packs);
+  return cudaGetLastError();
+}
+inline Mat16 in16(const Out16& m) { return {m.p, m.ld}; }
+inline Out16 out16(const gn_mat& m) { return {m.p, m.ld}; }
 
-template <class T>
-cudaError_t forward(const gn_ffn& f, const Pieces& w, cudaStream_t st) {
-  const int64_t R = f.rows, C = f.cols, F = f.inner;
-  const gn_mat gate = f.gate.p ? f.gate : gn_mat{w.gate, F}, up = f.up.p ? f.up : gn_mat{w.up, F};
-  cudaError_t e = plain_gemm<T>({R, F, C, 1, {{f.x.p, f.x.ld, 1}}, {{f.w_gate.p, 1, f.w_gate.ld}}, gate.p, gate.ld}, st);
-  if (e == cudaSuccess) e = plain_gemm<T>({R, F, C, 1, {{f.x.p, f.x.ld, 1}}, {{f.w_up.p, 1, f.w_up.ld}}, up.p, up.ld}, st);
-  if (e == cudaSuccess) gate_kernel<T><<<1184, 256, 0, st>>>({R, f.inner, f.act, gate.p, up.p, gate.ld, up.ld, nullptr, w.h, nullptr, nullptr});
-  if (e == cudaSuccess) e = plain_gemm<T>({R, C, F, 1, {{w.h, F, 1}}, {{f.w_down.p, 1, f.w_down.ld}}, f.y.p, f.y.ld}, st);
+cudaError_t forward_half(const gn_ffn& f, const Half& w, int* err, cudaStream_t st) {
+  const bool bf16 = f.type == GN_BF16;
+  FfnGemm a, b;
+  a.M = (int)f.rows; a.N = f.inner; a.K[0] = f.cols;
+  a.A[0] = w.x; a.B[0] = w.w_gate; a.B[1] = w.w_up;
+  a.d[0] = w.h; a.d[1] = out16(f.gate); a.d[2] = out16(f.up);
+  b.M = (int)f.rows; b.N = f.cols; b.K[0] = f.inner;
+  b.A[0] = in16(w.h); b.B[0] = w.w_down; b.d[0] = out16(f.y);
+  cudaError_t e = pack(w, st);
+  if (e == cudaSuccess) e = launch_ffn_pair(FFN_GATE, bf16, f.act, &a, 1, err, st);
+  if (e == cudaSuccess) e = launch_ffn_pair(FFN_STORE, bf16, f.act, &b, 1, err, st);
   return e;
 }
 
-template <class T>
-cudaError_t backward(const gn_ffn& f, const Pieces& w, cudaStream_t st) {
-  const int64_t R = f.rows, C = f.cols, F = f.inner;
-  cudaError_t e = plain_gemm<T, float>({R, F, C, 1, {{f.dy.p, f.dy.ld, 1}}, {{f.w_down.p, f.w_down.ld, 1}}, w.dh, F}, st);
-  if (e == cudaSuccess && R) gate_kernel<T><<<1184, 256, 0, st>>>({R, f.inner, f.act, f.gate.p, f.up.p, f.gate.ld, f.up.ld, w.dh, w.h, w.dgate, w.dup});
-  if (e == cudaSuccess && f.dx.p) e = plain_gemm<T>({R, C, F, 2, {{w.dgate, F, 1}, {w.dup, F, 1}}, {{f.w_gate.p, f.w_gate.ld, 1}, {f.w_up.p, f.w_up.ld, 1}}, f.dx.p, f.dx.ld}, st);
-  if (e == cudaSuccess && f.dw_gate.p) e = plain_gemm<T>({F, C, R, 1, {{w.dgate, 1, F}}, {{f.x.p, f.x.ld, 1}}, f.dw_gate.p, f.dw_gate.ld}, st);
-  if (e == cudaSuccess && f.dw_up.p) e = plain_gemm<T>({F, C, R, 1, {{w.dup, 1, F}}, {{f.x.p, f.x.ld, 1}}, f.dw_up.p, f.dw_up.ld}, st);
-  if (e == cudaSuccess && f.dw_down.p) e = plain_gemm<T>({C, F, R, 1, {{f.dy.p, 1, f.dy.ld}}, {{w.h, F, 1}}, f.dw_down.p, f.dw_down.ld}, st);
+cudaError_t backward_half(const gn_ffn& f, const Half& w, int* err, cudaStream_t st) {
+  const bool bf16 = f.type == GN_BF16;
+  const int R = (int)f.rows;
+  FfnGemm a;
+  a.M = R; a.N = f.inner; a.K[0] = f.cols; a.b_mn = true;
+  a.A[0] = w.dy; a.B[0] = w.w_down;
+  a.d[0] = w.h; a.d[1] = w.dgate; a.d[2] = w.dup;
+  a.gate = {f.gate.p, f.gate.ld}; a.up = {f.up.p, f.up.ld};
+  FfnGemm list[kFfnGroup];
+  int n = 0;
+  if (f.dx.p) {
+    FfnGemm& q = list[n++];
+    q.M = R; q.N = f.cols; q.K[0] = q.K[1] = f.inner; q.b_mn = true;
+    q.A[0] = in16(w.dgate); q.B[0] = w.w_gate; q.A[1] = in16(w.dup); q.B[1] = w.w_up; q.d[0] = out16(f.dx);
+  }
+  auto weights = [&](int M, int N, const Mat16& A, const Mat16& B, const gn_mat& d) {
+    if (!d.p) return;
+    FfnGemm& q = list[n++];
+    q.M = M; q.N = N; q.K[0] = R; q.a_mn = q.b_mn = true; q.A[0] = A; q.B[0] = B; q.d[0] = out16(d);
+  };
+  weights(f.inner, f.cols, in16(w.dgate), w.x, f.dw_gate);
+  weights(f.inner, f.cols, in16(w.dup), w.x, f.dw_up);
+  weights(f.cols, f.inner, w.dy, in16(w.h), f.dw_down);
+  if (n == 0) return cudaSuccess;
+  cudaError_t e = pack(w, st);
+  if (e == cudaSuccess) e = launch_ffn_pair(FFN_GRAD, bf16, f.act, &a, 1, err, st);
+  if (e == cudaSuccess) e = launch_ffn_pair(FFN_STORE, bf16, f.act, list, n, err, st);
   return e;
+}
+
+// ---- FP32 --------------------------------------------------------------------------------------
+struct Single { float *gate, *up, *h, *dgate, *dup, *dh; int64_t ld; char* parts; int64_t parts_bytes; float* sums; };
+
+// Whether the tensor-core form is the faster way to FP32 accuracy (the rule of the contexts' contractions, see gn_context.cu).
+bool on_tensor_cores(const GemmArgs& g) {
+  if (!gemm_f16x3_usable()) return false;
+  const double K = (double)g.K1 + (g.A2 ? g.K2 : 0);
+  const double blocks = ((g.M + 127) / 128) * (double)((g.N + 127) / 128);
+  const double fma_us = 10.0 + (blocks <= 148.0 ? 1.0 : blocks / 148.0) * K * 0.12;
+  return gemm_f16x3_estimate_us(g) + 14.0 + (g.M + (double)g.N) * K * 8.0 / 4.0e6 * 0.5 < fma_us;
+}
+struct Stored { const float* p; int64_t rows; int cols; int64_t ld; };
+// The products of a call, one after another: their operands as stored, and what they need of the workspace.
+GemmArgs product(int64_t M, int64_t N, const Stored& A, bool a_k, const Stored& B, bool b_k, float* D, int64_t ldd) {
+  GemmArgs g;
+  g.M = (int)M; g.N = (int)N;
+  g.A1 = A.p; g.lda1 = A.ld; g.B1 = B.p; g.ldb1 = B.ld; g.K1 = a_k ? A.cols : (int)A.rows;
+  g.a_kmajor = a_k; g.b_kmajor = b_k; g.D = D; g.ldd = ldd;
+  g.chunk_kb = M > 128 && N >= 128 ? 2 : 1;
+  return g;
+}
+Stored stored_a(const GemmArgs& g, int s) {
+  const float* p = s ? g.A2 : g.A1; const int K = s ? g.K2 : g.K1; const int64_t ld = s ? g.lda2 : g.lda1;
+  return g.a_kmajor ? Stored{p, g.M, K, ld} : Stored{p, K, g.M, ld};
+}
+Stored stored_b(const GemmArgs& g, int s) {
+  const float* p = s ? g.B2 : g.B1; const int K = s ? g.K2 : g.K1; const int64_t ld = s ? g.ldb2 : g.ldb1;
+  return g.b_kmajor ? Stored{p, g.N, K, ld} : Stored{p, K, g.N, ld};
+}
+// Where the two FP16 parts of a product's operands, and their cells' exponents, go: counted and laid out by the same lines.
+int place_parts(const GemmArgs& g, Workspace& ws, SplitJob (&jobs)[4], SplitOperand (&ops)[4]) {
+  const int n = g.A2 ? 4 : 2;
+  for (int k = 0; k < n; ++k) {
+    const Stored m = k % 2 ? stored_b(g, k / 2) : stored_a(g, k / 2);
+    const int64_t ld = up8(m.cols), cells = (m.rows + 127) / 128 * ((m.cols + 127) / 128);
+    jobs[k] = {m.p, m.rows, m.cols, m.ld, ws.take(m.rows * ld * 2), ws.take(m.rows * ld * 2), ld, (int8_t*)ws.take(cells)};
+    ops[k].hi = jobs[k].hi; ops[k].lo = jobs[k].lo; ops[k].ld = ld; ops[k].cells = jobs[k].cells; ops[k].cells_ld = (m.cols + 127) / 128;
+  }
+  return n;
+}
+// What one product needs for the parts of its operands, and for the sums of K slices.
+void product_needs(const GemmArgs& g, int64_t& parts, int64_t& sums) {
+  Workspace ws{kNowhere};
+  SplitJob jobs[4];
+  SplitOperand ops[4];
+  place_parts(g, ws, jobs, ops);
+  parts = ws.used > parts ? ws.used : parts;
+  const int64_t w = gemm_f16x3_workspace_floats(g) * 4;
+  sums = w > sums ? w : sums;
+}
+cudaError_t run_product(const GemmArgs& g, const Single& w, int* err, cudaStream_t st) {
+  if (g.M < 1 || g.N < 1) return cudaSuccess;
+  if (!on_tensor_cores(g)) { launch_gemm_ffma(g, st); return cudaGetLastError(); }
+  Workspace ws{w.parts};
+  SplitJob jobs[4];
+  SplitOperand ops[4];
+  const int n = place_parts(g, ws, jobs, ops);
+  if (launch_split_f16(jobs, n, st) < 0 || launch_gemm_f16x3(g, ops, w.sums, err, st) < 0) {
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? cudaErrorInvalidValue : e;
+  }
+  return cudaSuccess;
+}
+
+struct SingleCall { GemmArgs g[6]; int n, gate_after; };   // products, the gate's pass after the first gate_after of them
+SingleCall single_products(const gn_ffn& f, bool backward, const Single& w) {
+  SingleCall c{};
+  const int64_t R = f.rows;
+  const int C = f.cols, F = f.inner;
+  const Stored x{(const float*)f.x.p, R, C, f.x.ld}, wg{(const float*)f.w_gate.p, F, C, f.w_gate.ld}, wu{(const float*)f.w_up.p, F, C, f.w_up.ld};
+  const Stored wd{(const float*)f.w_down.p, C, F, f.w_down.ld}, h{w.h, R, F, w.ld};
+  if (!backward) {
+    c.g[c.n++] = product(R, F, x, true, wg, true, w.gate, f.gate.p ? f.gate.ld : w.ld);
+    c.g[c.n++] = product(R, F, x, true, wu, true, w.up, f.up.p ? f.up.ld : w.ld);
+    c.gate_after = c.n;
+    c.g[c.n++] = product(R, C, h, true, wd, true, (float*)f.y.p, f.y.ld);
+    return c;
+  }
+  const Stored dy{(const float*)f.dy.p, R, C, f.dy.ld}, dg{w.dgate, R, F, w.ld}, du{w.dup, R, F, w.ld};
+  c.g[c.n++] = product(R, F, dy, true, wd, false, w.dh, w.ld);
+  c.gate_after = c.n;
+  if (f.dx.p) {
+    GemmArgs& g = c.g[c.n++] = product(R, C, dg, true, wg, false, (float*)f.dx.p, f.dx.ld);
+    g.A2 = du.p; g.lda2 = du.ld; g.B2 = wu.p; g.ldb2 = wu.ld; g.K2 = F;
+  }
+  if (f.dw_gate.p) c.g[c.n++] = product(F, C, dg, false, x, false, (float*)f.dw_gate.p, f.dw_gate.ld);
+  if (f.dw_up.p) c.g[c.n++] = product(F, C, du, false, x, false, (float*)f.dw_up.p, f.dw_up.ld);
+  if (f.dw_down.p) c.g[c.n++] = product(C, F, dy, false, h, false, (float*)f.dw_down.p, f.dw_down.ld);
+  return c;
+}
+int64_t lay_out_single(const gn_ffn& f, bool backward, char* base, Single& w) {
+  Workspace ws{base};
+  w = Single{};
+  w.ld = up8(f.inner);
+  const int64_t hidden = f.rows * w.ld * 4;
+  w.h = (float*)ws.take(hidden);
+  if (backward) {
+    w.dgate = (float*)ws.take(hidden); w.dup = (float*)ws.take(hidden); w.dh = (float*)ws.take(hidden);
+  } else {
+    w.gate = f.gate.p ? (float*)f.gate.p : (float*)ws.take(hidden);
+    w.up = f.up.p ? (float*)f.up.p : (float*)ws.take(hidden);
+  }
+  const SingleCall c = single_products(f, backward, w);
+  int64_t parts = 0, sums = 0;
+  for (int i = 0; i < c.n; ++i)
+    if (c.g[i].M > 0 && c.g[i].K1 > 0) product_needs(c.g[i], parts, sums);
+  w.parts = (char*)ws.take(parts);
+  w.sums = (float*)ws.take(sums);
+  return ws.used;
+}
+cudaError_t run_single(const gn_ffn& f, bool backward, const Single& w, int* err, cudaStream_t st) {
+  const SingleCall c = single_products(f, backward, w);
+  if (backward && c.n == 1) return cudaSuccess;
+  cudaError_t e = cudaSuccess;
+  for (int i = 0; i < c.n && e == cudaSuccess; ++i) {
+    if (i == c.gate_after) {
+      const Gates g = backward ? Gates{f.rows, f.inner, f.act, (const float*)f.gate.p, (const float*)f.up.p, f.gate.ld, f.up.ld, w.dh, w.h, w.dgate, w.dup, w.ld}
+                               : Gates{f.rows, f.inner, f.act, w.gate, w.up, f.gate.p ? f.gate.ld : w.ld, f.up.p ? f.up.ld : w.ld, nullptr, w.h, nullptr, nullptr, w.ld};
+      const int64_t blocks = (f.rows * f.inner + 255) / 256;
+      gate_kernel<<<(unsigned)(blocks < 1184 ? blocks : 1184), 256, 0, st>>>(g);
+      e = cudaGetLastError();
+    }
+    if (e == cudaSuccess) e = run_product(c.g[i], w, err, st);
+  }
+  return e;
+}
+
+cudaError_t clear(const gn_mat& m, int64_t rows, int64_t cols, int type, cudaStream_t st) {
+  const size_t b = (size_t)type_bytes(type);
+  return m.p ? cudaMemset2DAsync(m.p, (size_t)m.ld * b, 0, (size_t)cols * b, (size_t)rows, st) : cudaSuccess;
+}
+
+int64_t needed(const gn_ffn& f, bool backward, char* base, Half& h, Single& s) {
+  return (f.type == GN_F32 ? lay_out_single(f, backward, base, s) : lay_out_half(f, backward, base, h)) + 256;
 }
 
 gn_status run(const gn_ffn* f, bool back, void* d_ws, int64_t ws_bytes, void* stream, char* errbuf, int64_t errbuf_len) {
   const char* why = ffn_args(f, back);
   if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
-  Pieces w;
-  if (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < lay_out(*f, back, nullptr, w))
+  Half h;
+  Single s;
+  char* const base = (char*)(((uintptr_t)d_ws + 255) & ~(uintptr_t)255);
+  if (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < needed(*f, back, base, h, s))
     return op_fail(GN_EINVAL, "workspace: null, not 16-byte aligned or too small", errbuf, errbuf_len);
-  if (f->rows == 0 && !back) return op_done(cudaSuccess, errbuf, errbuf_len);
-  lay_out(*f, back, (char*)(((uintptr_t)d_ws + 255) & ~(uintptr_t)255), w);
   cudaStream_t st = (cudaStream_t)stream;
-  cudaError_t e;
-  if (f->type == GN_F32) e = back ? backward<float>(*f, w, st) : forward<float>(*f, w, st);
-  else if (f->type == GN_BF16) e = back ? backward<__nv_bfloat16>(*f, w, st) : forward<__nv_bfloat16>(*f, w, st);
-  else e = back ? backward<__half>(*f, w, st) : forward<__half>(*f, w, st);
+  cudaError_t e = cudaSuccess;
+  if (f->rows == 0) {
+    if (back) {
+      e = clear(f->dw_gate, f->inner, f->cols, f->type, st);
+      if (e == cudaSuccess) e = clear(f->dw_up, f->inner, f->cols, f->type, st);
+      if (e == cudaSuccess) e = clear(f->dw_down, f->cols, f->inner, f->type, st);
+    }
+    return op_done(e, errbuf, errbuf_len);
+  }
+  int* const err = error_word();
+  if (!err) return op_done(cudaErrorNoDevice, errbuf, errbuf_len);
+  if (f->type == GN_F32) e = run_single(*f, back, s, err, st);
+  else e = back ? backward_half(*f, h, err, st) : forward_half(*f, h, err, st);
   return op_done(e, errbuf, errbuf_len);
 }
 
@@ -174,12 +352,26 @@ gn_status run(const gn_ffn* f, bool back, void* d_ws, int64_t ws_bytes, void* st
 using namespace gn;
 
 extern "C" int64_t gn_gated_ffn_workspace(const gn_ffn* args, int32_t backward) {
-  Pieces w;
-  return ffn_args(args, backward != 0) ? -1 : lay_out(*args, backward != 0, nullptr, w);
+  Half h;
+  Single s;
+  return ffn_args(args, backward != 0) ? -1 : needed(*args, backward != 0, kNowhere, h, s);
 }
 extern "C" gn_status gn_gated_ffn(const gn_ffn* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
   return run(args, false, d_ws, ws_bytes, cuda_stream, errbuf, errbuf_len);
 }
 extern "C" gn_status gn_gated_ffn_grad(const gn_ffn* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
   return run(args, true, d_ws, ws_bytes, cuda_stream, errbuf, errbuf_len);
+}
+extern "C" gn_status gn_gated_ffn_status(void* cuda_stream, char* errbuf, int64_t errbuf_len) {
+  int* const err = error_word();
+  if (!err) return op_done(cudaErrorNoDevice, errbuf, errbuf_len);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  int code = 0;
+  cudaError_t e = cudaMemcpyAsync(&code, err, sizeof code, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess || code == 0) return op_done(e, errbuf, errbuf_len);
+  e = cudaMemsetAsync(err, 0, sizeof code, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) return op_done(e, errbuf, errbuf_len);
+  return op_fail(GN_ETIMEOUT, "a bounded wait of a tensor-core kernel ran out: results since the last look are invalid", errbuf, errbuf_len);
 }

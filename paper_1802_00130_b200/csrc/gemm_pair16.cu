@@ -1,0 +1,428 @@
+// Products of 16-bit matrices for the gated feed-forward block: a CTA pair per 256 x bn tile (tcgen05.mma.cta_group::2, operands by
+// TMA, accumulators in tensor memory), with the gate, its gradient or a plain rounding as the epilogue.
+//
+// Persistent: one pair for two SMs, tiles dealt in turn.  Warp roles in each CTA:
+//   warp 0      TMA producer: a ring of STAGES slots, each this CTA's 128 rows of A and its half of the B tile, 64 terms of K
+//   warp 1      MMA issuer (leader CTA only), one thread
+//   warps 2..9  epilogue: two warps per 32-lane quadrant of tensor memory, alternating over the tile's 64-column chunks
+// Two accumulators of 256 tensor-memory columns alternate, so a tile's epilogue runs under the next tile's products.
+//
+// FFN_GATE: the B tile is bn / 2 rows of the gate's weights, staged by the leader, and the same rows of the up projection's, staged by
+// the other CTA: one product gives both sums of bn / 2 hidden units, and a thread finds them in the same tensor-memory lane.
+//
+// A thread of the epilogue holds a row (a tensor-memory lane) of a chunk.  What goes to or comes from global memory passes a
+// staging tile of 32 rows x 128 bytes in shared memory, so that a warp's access covers whole lines: 16-byte units are permuted by the row's
+// low bits, which keeps both directions free of bank conflicts.
+//
+// Operand layouts are those of gemm_tf32.cu's FP16 copies: K-major rows of 128 bytes, or MN-major chunks of 64 columns x 64 rows, both
+// with the plain 128-byte swizzle.  Every wait is bounded; a role that gives up leaves a code in *err and the CTA drains.
+#include "ffn_act.cuh"
+#include "ffn_kernels.h"
+#include "tc_common.cuh"
+
+namespace gn {
+namespace {
+
+constexpr int P_BM = 128, P_BK = 64, P_BN = 256;
+constexpr int P_STAGES = 6, P_EPI_WARPS = 8, P_THREADS = 64 + 32 * P_EPI_WARPS;
+constexpr int P_A_BYTES = P_BM * P_BK * 2, P_STAGE_BYTES = 2 * P_A_BYTES;
+constexpr int P_STG_BYTES = 32 * 128;
+constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + P_EPI_WARPS * P_STG_BYTES + 1024 + 256;
+static_assert(P_SMEM <= 232448, "more shared memory than a block can have");
+constexpr int P_PANELS = 8;       // tiles are walked in strips of so many row panels: 74 tiles at a time read 8 panels of A and 9 of B
+
+struct PairProblem {
+  int M, N, bn, tiles_m, tiles_n, tiles;
+  int kb0, kb;                    // k-blocks of the first operand pair, of both
+  int a_mn, b_mn, vec;            // vec: every matrix of the epilogue takes 16-byte accesses
+  Out16 d[3];
+  Mat16 gate, up;
+};
+template <int NP> struct PairParams { PairProblem p[NP]; int n, act, pairs, tiles; int* err; };
+template <int NP> struct PairMaps { CUtensorMap m[NP][4]; };   // A0, B0, A1, B1 (FFN_GATE: A, gate weights, -, up weights)
+
+template <bool BF16>
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accum) : "memory");
+}
+
+// Two times 32 columns of this warp's quadrant (lane = row), waited for in the same statement: nothing may move a value before it is there.
+__device__ __forceinline__ void tmem_ld32_pair(uint32_t a, uint32_t b, float (&x)[32], float (&y)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%64];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%65];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]),
+        "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(x[16]), "=f"(x[17]), "=f"(x[18]),
+        "=f"(x[19]), "=f"(x[20]), "=f"(x[21]), "=f"(x[22]), "=f"(x[23]), "=f"(x[24]), "=f"(x[25]), "=f"(x[26]), "=f"(x[27]),
+        "=f"(x[28]), "=f"(x[29]), "=f"(x[30]), "=f"(x[31]), "=f"(y[0]), "=f"(y[1]), "=f"(y[2]), "=f"(y[3]), "=f"(y[4]), "=f"(y[5]),
+        "=f"(y[6]), "=f"(y[7]), "=f"(y[8]), "=f"(y[9]), "=f"(y[10]), "=f"(y[11]), "=f"(y[12]), "=f"(y[13]), "=f"(y[14]), "=f"(y[15]),
+        "=f"(y[16]), "=f"(y[17]), "=f"(y[18]), "=f"(y[19]), "=f"(y[20]), "=f"(y[21]), "=f"(y[22]), "=f"(y[23]), "=f"(y[24]),
+        "=f"(y[25]), "=f"(y[26]), "=f"(y[27]), "=f"(y[28]), "=f"(y[29]), "=f"(y[30]), "=f"(y[31])
+      : "r"(a), "r"(b) : "memory");
+}
+
+// Problem and tile of the t-th piece of work.
+template <int NP>
+__device__ __forceinline__ int find_tile(const PairParams<NP>& g, int t, int& m, int& n) {
+  int k = 0;
+  if (NP > 1)
+    while (k + 1 < g.n && t >= g.p[k].tiles) t -= g.p[k++].tiles;
+  const PairProblem& p = g.p[k];
+  const int strip = t / (P_PANELS * p.tiles_n), rest = t - strip * P_PANELS * p.tiles_n;
+  const int high = min(P_PANELS, p.tiles_m - strip * P_PANELS);
+  m = strip * P_PANELS + rest % high; n = rest / high;
+  return k;
+}
+
+__device__ __forceinline__ uint32_t stg_at(uint32_t stg, int row, int unit) { return stg + (uint32_t)(row * 128 + ((unit ^ (row & 7)) << 4)); }
+__device__ __forceinline__ void sts16(uint32_t a, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+
+// This thread's row of a chunk, 64 elements in 32 words, to rows m0.. (of M) and columns n0.. (of N) of a matrix, by way of the staging tile.
+__device__ __forceinline__ void put_chunk(const uint32_t (&w)[32], uint32_t stg, int lane, void* base, int64_t ld, int m0, int M, int n0, int N, int vec) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) sts16(stg_at(stg, lane, q), make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]));
+  __syncwarp();
+  const int unit = lane & 7, n = n0 + unit * 8;
+#pragma unroll
+  for (int it = 0; it < 8; ++it) {
+    const int row = it * 4 + (lane >> 3);
+    const uint4 v = lds16(stg_at(stg, row, unit));
+    if (m0 + row < M && n < N) {
+      uint16_t* const p = reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + row) * ld + n;
+      if (vec && n + 8 <= N) {
+        *reinterpret_cast<uint4*>(p) = v;
+      } else {
+        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (n + e < N) p[e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1)));
+      }
+    }
+  }
+  __syncwarp();
+}
+// The other way: eight units of the chunk, four rows apart, as a warp's accesses cover them; then by rows.
+__device__ __forceinline__ void fetch_chunk(uint4 (&v)[8], int lane, const void* base, int64_t ld, int m0, int M, int n0, int N, int vec) {
+  const int unit = lane & 7, n = n0 + unit * 8;
+#pragma unroll
+  for (int it = 0; it < 8; ++it) {
+    const int m = m0 + it * 4 + (lane >> 3);
+    v[it] = make_uint4(0u, 0u, 0u, 0u);
+    if (m < M && n < N) {
+      const uint16_t* const p = reinterpret_cast<const uint16_t*>(base) + (int64_t)m * ld + n;
+      if (vec && n + 8 <= N) {
+        v[it] = __ldg(reinterpret_cast<const uint4*>(p));
+      } else {
+        uint32_t x[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (n + e < N) x[e >> 1] |= (uint32_t)__ldg(p + e) << (16 * (e & 1));
+        v[it] = make_uint4(x[0], x[1], x[2], x[3]);
+      }
+    }
+  }
+}
+__device__ __forceinline__ void turn_chunk(const uint4 (&v)[8], uint32_t stg, int lane, uint32_t (&w)[32]) {
+#pragma unroll
+  for (int it = 0; it < 8; ++it) sts16(stg_at(stg, it * 4 + (lane >> 3), lane & 7), v[it]);
+  __syncwarp();
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const uint4 x = lds16(stg_at(stg, lane, q));
+    w[4 * q] = x.x; w[4 * q + 1] = x.y; w[4 * q + 2] = x.z; w[4 * q + 3] = x.w;
+  }
+  __syncwarp();
+}
+
+template <int KIND, class T, int NP>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
+ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant__ PairParams<NP> g) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* staging = smem + P_STAGES * P_STAGE_BYTES;
+  uint64_t* full = reinterpret_cast<uint64_t*>(staging + P_EPI_WARPS * P_STG_BYTES);
+  uint64_t* empty = full + P_STAGES;
+  uint64_t* acc_full = empty + P_STAGES;   // [2]
+  uint64_t* acc_empty = acc_full + 2;      // [2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < P_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 2 * P_EPI_WARPS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  grid_dep_wait();
+  grid_dep_launch();
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int s = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int t = pair; ok && t < g.tiles; t += g.pairs) {
+        int tm, tn;
+        const int k = find_tile(g, t, tm, tn);
+        const PairProblem& p = g.p[k];
+        const int hb = p.bn >> 1;                          // B rows staged by each CTA
+        const int m0 = tm * 2 * P_BM + (int)rank * P_BM;
+        const int n0 = KIND == FFN_GATE ? tn * hb : tn * p.bn + (int)rank * hb;
+        const uint32_t pair_tx = 2u * (P_A_BYTES + (uint32_t)hb * 128u);
+        for (int kb = 0; kb < p.kb; ++kb) {
+          if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, g.err, 1)) { ok = false; break; }
+          if (rank == 0) mbar_expect_tx(&full[s], pair_tx);
+          const uint32_t bar = map_to_cta(smem_u32(&full[s]), 0);
+          const int second = kb >= p.kb0 ? 1 : 0;
+          const int k0 = (second ? kb - p.kb0 : kb) * P_BK;
+          const CUtensorMap* ma = &maps.m[k][2 * second];
+          const CUtensorMap* mb = KIND == FFN_GATE ? &maps.m[k][rank ? 3 : 1] : ma + 1;
+          uint8_t* const sa = smem + s * P_STAGE_BYTES;
+          uint8_t* const sb = sa + P_A_BYTES;
+          if (!p.a_mn) {
+            tma2_load_2d(sa, ma, k0, m0, bar);
+          } else {
+            tma2_load_2d(sa, ma, m0, k0, bar);
+            tma2_load_2d(sa + 8192, ma, m0 + 64, k0, bar);
+          }
+          if (!p.b_mn) {
+            tma2_load_2d(sb, mb, k0, n0, bar);
+          } else {
+            tma2_load_2d(sb, mb, n0, k0, bar);
+            if (hb > 64) tma2_load_2d(sb + 8192, mb, n0 + 64, k0, bar);
+          }
+          if (++s == P_STAGES) { s = 0; ph ^= 1u; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (rank == 0 && lane == 0) {
+      constexpr bool BF16 = sizeof(T) == 2 && !__is_same(T, __half);
+      const uint32_t base = smem_u32(smem);
+      int s = 0, ti = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int t = pair; ok && t < g.tiles; t += g.pairs, ++ti) {
+        int tm, tn;
+        const PairProblem& p = g.p[find_tile(g, t, tm, tn)];
+        const int buf = ti & 1;
+        if (!wait_or_abort(&acc_empty[buf], ((ti >> 1) & 1) ^ 1, abort_flag, g.err, 4)) break;
+        tc_fence_after();
+        const uint32_t tmem_d = tmem_base + (uint32_t)(buf * P_BN);
+        const uint32_t idesc = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) |
+                               ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)((2 * P_BM) >> 4) << 24);
+        const uint64_t a_step = (p.a_mn ? 2048 : 32) >> 4, b_step = (p.b_mn ? 2048 : 32) >> 4;
+        const uint64_t a0 = make_desc(base, p.a_mn ? 8192 : 16, 1024, 2);
+        const uint64_t b0 = make_desc(base + P_A_BYTES, p.b_mn ? 8192 : 16, 1024, 2);
+        uint32_t acc = 0u;
+        const int kbs = p.kb;
+#pragma unroll 1
+        for (int kb = 0; kb < kbs; ++kb) {
+          if (!wait_or_abort(&full[s], ph, abort_flag, g.err, 2)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t ad = a0 + (uint64_t)(s * (P_STAGE_BYTES >> 4)), bd = b0 + (uint64_t)(s * (P_STAGE_BYTES >> 4));
+          pair_mma<BF16>(tmem_d, ad, bd, idesc, acc);
+          acc = 1u;
+          pair_mma<BF16>(tmem_d, ad + a_step, bd + b_step, idesc, 1u);
+          pair_mma<BF16>(tmem_d, ad + 2 * a_step, bd + 2 * b_step, idesc, 1u);
+          pair_mma<BF16>(tmem_d, ad + 3 * a_step, bd + 3 * b_step, idesc, 1u);
+          mma2_commit_both(&empty[s]);
+          if (++s == P_STAGES) { s = 0; ph ^= 1u; }
+        }
+        if (ok) mma2_commit_both(&acc_full[buf]);
+      }
+    }
+  } else {
+    const int quad = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t stg = smem_u32(staging + (warp - 2) * P_STG_BYTES);
+    int ti = 0;
+    for (int t = pair; t < g.tiles; t += g.pairs, ++ti) {
+      int tm, tn;
+      const PairProblem& p = g.p[find_tile(g, t, tm, tn)];
+      const int width = KIND == FFN_GATE ? p.bn >> 1 : p.bn;          // columns of the result
+      const int m0 = tm * 2 * P_BM + (int)rank * P_BM + quad * 32, n0 = tn * width;
+      const int buf = ti & 1;
+      int good = 1;
+      if (lane == 0) good = wait_or_abort(&acc_full[buf], (ti >> 1) & 1, abort_flag, g.err, 3) ? 1 : 0;
+      good = __shfl_sync(0xffffffffu, good, 0);
+      if (!good) break;
+      tc_fence_after();
+      const uint32_t tq = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * P_BN);
+      if (m0 < p.M) {
+        for (int c = half; c < width / 64; c += 2) {
+          const int nc = n0 + c * 64;
+          if (nc >= p.N) break;
+          uint32_t w[32];
+          if (KIND == FFN_STORE) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float v[32];
+              tmem_ld32(tq + (uint32_t)(c * 64 + h * 32), v);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) w[16 * h + i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+            }
+            put_chunk(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
+          } else if (KIND == FFN_GATE) {
+            uint32_t gw[32], uw[32];
+            with_activation(g.act, [&](auto act) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float gv[32], uv[32];
+                tmem_ld32_pair(tq + (uint32_t)(c * 64 + h * 32), tq + (uint32_t)(width + c * 64 + h * 32), gv, uv);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  float a0, a1, unused;
+                  activation<decltype(act)::value, true>(gv[2 * i], a0, unused);
+                  activation<decltype(act)::value, true>(gv[2 * i + 1], a1, unused);
+                  w[16 * h + i] = pack2<T>(a0 * uv[2 * i], a1 * uv[2 * i + 1]);
+                  gw[16 * h + i] = pack2<T>(gv[2 * i], gv[2 * i + 1]);
+                  uw[16 * h + i] = pack2<T>(uv[2 * i], uv[2 * i + 1]);
+                }
+              }
+            });
+            put_chunk(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
+            if (p.d[1].p) put_chunk(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
+            if (p.d[2].p) put_chunk(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
+          } else {
+            uint4 gx[8], ux[8];
+            fetch_chunk(gx, lane, dep(p.gate.p), p.gate.ld, m0, p.M, nc, p.N, p.vec);
+            fetch_chunk(ux, lane, dep(p.up.p), p.up.ld, m0, p.M, nc, p.N, p.vec);
+            uint32_t gw[32], uw[32];
+            turn_chunk(gx, stg, lane, gw);
+            turn_chunk(ux, stg, lane, uw);
+            with_activation(g.act, [&](auto act) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                float v[32];
+                tmem_ld32(tq + (uint32_t)(c * 64 + h * 32), v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  const float2 gt = unpack2<T>(gw[16 * h + i]), up = unpack2<T>(uw[16 * h + i]);
+                  float a0, a1, s0, s1;
+                  activation<decltype(act)::value, true>(gt.x, a0, s0);
+                  activation<decltype(act)::value, true>(gt.y, a1, s1);
+                  w[16 * h + i] = pack2<T>(a0 * up.x, a1 * up.y);
+                  gw[16 * h + i] = pack2<T>(v[2 * i] * up.x * s0, v[2 * i + 1] * up.y * s1);
+                  uw[16 * h + i] = pack2<T>(v[2 * i] * a0, v[2 * i + 1] * a1);
+                }
+              }
+            });
+            put_chunk(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
+            put_chunk(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
+            put_chunk(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&acc_empty[buf]), 0));
+    }
+  }
+  tc_fence_before();
+  cluster_sync_all();      // neither CTA leaves (or frees tensor memory) while the other may still use it
+  if (warp == 2) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+  }
+}
+
+// ---- host side ---------------------------------------------------------------------------------
+// 2-D map over a row-major [rows][cols] matrix of 16-bit elements; box = 64 columns x box_r rows.
+bool make_map16(CUtensorMap* m, const Mat16& a, long long rows, long long cols, int box_r, bool bf16) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)a.ld * 2};
+  cuuint32_t box[2] = {64, (cuuint32_t)box_r};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(a.p), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+template <class P> bool vec16(const P& m) { return !m.p || (((uintptr_t)m.p & 15) == 0 && m.ld % 8 == 0); }
+
+template <int KIND, class T, int NP>
+cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStream_t st) {
+  constexpr bool BF16 = !__is_same(T, __half);
+  static std::atomic<signed char> ready[64];
+  auto* const kernel = ffn_pair_kernel<KIND, T, NP>;
+  if (!once_per_device(ready, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, P_SMEM) == cudaSuccess; }))
+    return cudaErrorInvalidDevice;
+  PairMaps<NP> maps;
+  PairParams<NP> q = {};
+  q.n = n; q.act = act; q.err = err;
+  const int pairs = num_sms() / 2;
+  // width of the tiles: that of the fewer waves, a wave of narrow ones taking a little over half the time of one of wide ones
+  long long cost[2] = {0, 0};
+  for (int w = 0; w < 2; ++w) {
+    long long tiles = 0;
+    for (int i = 0; i < n; ++i) {
+      const int width = (w ? 128 : 256) / (KIND == FFN_GATE ? 2 : 1);
+      tiles += (long long)((g[i].M + 255) / 256) * ((g[i].N + width - 1) / width);
+    }
+    cost[w] = (tiles + pairs - 1) / pairs * (w ? 5 : 8);
+  }
+  const int bn = cost[1] < cost[0] ? 128 : 256;
+  long long tiles = 0;
+  for (int i = 0; i < n; ++i) {
+    PairProblem& p = q.p[i];
+    const int width = KIND == FFN_GATE ? bn / 2 : bn;
+    p.M = g[i].M; p.N = g[i].N; p.bn = bn;
+    p.tiles_m = (p.M + 255) / 256; p.tiles_n = (p.N + width - 1) / width;
+    tiles += (long long)p.tiles_m * p.tiles_n;
+    if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
+    p.tiles = p.tiles_m * p.tiles_n;
+    p.kb0 = (g[i].K[0] + P_BK - 1) / P_BK; p.kb = p.kb0 + (g[i].K[1] + P_BK - 1) / P_BK;
+    p.a_mn = g[i].a_mn; p.b_mn = g[i].b_mn;
+    for (int k = 0; k < 3; ++k) p.d[k] = g[i].d[k];
+    p.gate = g[i].gate; p.up = g[i].up;
+    p.vec = vec16(p.d[0]) && vec16(p.d[1]) && vec16(p.d[2]) && vec16(p.gate) && vec16(p.up);
+    for (int s = 0; s < 2; ++s) {
+      const int a = g[i].K[1] > 0 ? s : 0, b = KIND == FFN_GATE ? s : a, K = g[i].K[a];
+      const bool ok = (g[i].a_mn ? make_map16(&maps.m[i][2 * s], g[i].A[a], K, p.M, 64, BF16) : make_map16(&maps.m[i][2 * s], g[i].A[a], p.M, K, P_BM, BF16)) &&
+                      (g[i].b_mn ? make_map16(&maps.m[i][2 * s + 1], g[i].B[b], K, p.N, 64, BF16) : make_map16(&maps.m[i][2 * s + 1], g[i].B[b], p.N, K, bn / 2, BF16));
+      if (!ok) return cudaErrorInvalidValue;
+    }
+  }
+  q.tiles = (int)tiles;
+  q.pairs = (int)(tiles < pairs ? tiles : pairs);
+  return launch_pdl(kernel, 2 * q.pairs, P_THREADS, P_SMEM, st, maps, q);
+}
+
+}  // namespace
+
+cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, int* err, cudaStream_t st) {
+  if (kind == FFN_GATE) return bf16 ? launch_pair_as<FFN_GATE, __nv_bfloat16, 1>(act, g, n, err, st) : launch_pair_as<FFN_GATE, __half, 1>(act, g, n, err, st);
+  if (kind == FFN_GRAD) return bf16 ? launch_pair_as<FFN_GRAD, __nv_bfloat16, 1>(act, g, n, err, st) : launch_pair_as<FFN_GRAD, __half, 1>(act, g, n, err, st);
+  return bf16 ? launch_pair_as<FFN_STORE, __nv_bfloat16, kFfnGroup>(act, g, n, err, st) : launch_pair_as<FFN_STORE, __half, kFfnGroup>(act, g, n, err, st);
+}
+
+}  // namespace gn

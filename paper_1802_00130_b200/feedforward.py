@@ -208,3 +208,12 @@ def gated_ffn_grad(dy, x, gate, up, w_gate, w_up, w_down, act="silu", stream=Non
         mats += [(dx.data_ptr(), cols), (dwg.data_ptr(), cols), (dwu.data_ptr(), cols), (dwd.data_ptr(), inner)]
         _ffn_call(lib().gn_gated_ffn_grad, 1, x, a, kind, rows, cols, inner, mats, st)
     return dx, dwg, dwu, dwd
+
+
+def gated_ffn_status(device=None, stream=None):
+    """Synchronises and raises GnError (GN_ETIMEOUT) if a bounded wait of a gated_ffn call's kernels has run out on the device since the
+    last look; results since then are invalid."""
+    with torch.cuda.device(device if stream is None else stream.device):
+        st = stream if stream is not None else torch.cuda.current_stream()
+        err = C.create_string_buffer(160)
+        _checked(lib().gn_gated_ffn_status(st.cuda_stream, err, 160), err)

@@ -1,7 +1,17 @@
-// Layer norm and its backward pass.
+// Layer norm and its backward pass, each in one pass over the data: memory bound, so a row is read once, kept in registers as it is
+// stored, and written once.
+//
+// Forward: 8 or 32 threads a row up to 4096 columns of 16 bits (no barrier, a row's loads all in flight), a block a row above it.  The sums
+// of a row are taken twice from the registers, of x for the mean m and then of x - m and its square: the first of these two
+// is what m's rounding has left, which corrects the mean and the variance, so a mean far above the spread costs no accuracy.
+//
+// Backward: 8 columns a thread, kRows rows at a time.  With mean and rstd at hand a row needs one reduction, of g and g xhat; the sums
+// over rows of dy xhat and dy stay with the thread that owns the column, and each block leaves one row of partial sums, which a
+// second kernel adds in a fixed order.
 #include <math.h>
 
 #include "op_common.cuh"
+#include "tc_common.cuh"
 
 namespace gn {
 namespace {
@@ -23,10 +33,84 @@ __device__ __forceinline__ void block_sum(float (&v)[N]) {
     for (int o = 16; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
   }
 }
+// Sum over the TPR threads of a row, known to all of them.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N]) {
+  if constexpr (TPR > 32) {
+    block_sum(v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int o = TPR / 2; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+  }
+}
 
+// TPR threads a row, which hold NU units of 16 bytes each; rows of a block go through one after another only where the grid is full.
+template <class T, class W, int TPR, int NU, bool VEC>
+__global__ void __launch_bounds__(TPR > 32 ? TPR : 128) layer_norm_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, const W* b, float eps,
+                                                                          T* y, int64_t ldy, float* mean_out, float* rstd_out) {
+  constexpr int V = Pack<T>::V, WU = sizeof(W) / sizeof(T);      // units of the weights to a unit of x
+  constexpr int PER = TPR > 32 ? 1 : 128 / TPR;                  // rows of a block
+  const int thread = threadIdx.x % TPR;
+  grid_dep_wait();
+  grid_dep_launch();
+  x = dep(x); w = dep(w); b = dep(b);
+  const float inv_n = 1.f / (float)cols;
+  const int64_t r = (int64_t)blockIdx.x * PER + threadIdx.x / TPR;
+  const bool in = r < rows;                                      // (a warp's other rows still take part in the sums' exchanges)
+  const T* const xr = x + (in ? r : 0) * ldx;
+  Pack<T> v[NU];
+#pragma unroll
+  for (int u = 0; u < NU; ++u) v[u] = load_pack<VEC>(xr, (u * TPR + thread) * V, cols);
+  float s[1] = {0.f};
+#pragma unroll
+  for (int u = 0; u < NU; ++u)
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[0] += v[u].get(e);
+  row_sum<TPR>(s);
+  const float m = s[0] * inv_n;
+  float d[2] = {0.f, 0.f};
+#pragma unroll
+  for (int u = 0; u < NU; ++u)
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float t = v[u].get(e) - m;
+      if ((u * TPR + thread) * V + e < cols) { d[0] += t; d[1] = fmaf(t, t, d[1]); }
+    }
+  row_sum<TPR>(d);
+  const float off = d[0] * inv_n, rstd = 1.f / sqrtf(d[1] * inv_n - off * off + eps);
+#pragma unroll
+  for (int u = 0; u < NU; ++u) {
+    const int c = (u * TPR + thread) * V;
+    if (c >= cols) break;
+    float wv[V], bv[V];
+#pragma unroll
+    for (int q = 0; q < WU; ++q) {
+      constexpr int VW = Pack<W>::V;
+      Pack<W> pw, pb;
+      if (w) pw = load_pack<VEC>(w, c + q * VW, cols);
+      if (b) pb = load_pack<VEC>(b, c + q * VW, cols);
+#pragma unroll
+      for (int e = 0; e < VW; ++e) { wv[q * VW + e] = w ? pw.get(e) : 1.f; bv[q * VW + e] = b ? pb.get(e) : 0.f; }
+    }
+    float o[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = fmaf((v[u].get(e) - m - off) * rstd, wv[e], bv[e]);
+    Pack<T> p;
+    p.set(o);
+    if (in) store_pack<VEC>(y + r * ldy, p, c, cols);
+  }
+  if (in && thread == 0) {
+    if (mean_out) mean_out[r] = m + off;
+    if (rstd_out) rstd_out[r] = rstd;
+  }
+}
+
+// Rows too long for the registers of a block: the row is read three times, twice of them out of L2.
 template <class T, class W>
-__global__ void layer_norm_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, const W* b, float eps, T* y, int64_t ldy,
-                                  float* mean_out, float* rstd_out) {
+__global__ void __launch_bounds__(1024) layer_norm_long_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, const W* b, float eps, T* y,
+                                                               int64_t ldy, float* mean_out, float* rstd_out) {
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const T* xr = x + r * ldx;
     float s[1] = {0.f};
@@ -48,51 +132,252 @@ __global__ void layer_norm_kernel(int64_t rows, int cols, const T* x, int64_t ld
   }
 }
 
-template <class T, class W>
-__global__ void layer_norm_dx_kernel(int64_t rows, int cols, const T* dy, int64_t ld_dy, const T* x, int64_t ldx, const float* mean,
-                                     const float* rstd, const W* w, const T* add, int64_t ld_add, T* dx, int64_t ld_dx) {
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const float m = mean[r], rs = rstd[r];
-    float s[2] = {0.f, 0.f};
-    for (int c = threadIdx.x; c < cols; c += blockDim.x) {
-      const float g = to_f(dy[r * ld_dy + c]) * (w ? to_f(w[c]) : 1.f);
-      s[0] += g; s[1] += g * (to_f(x[r * ldx + c]) - m) * rs;
-    }
-    block_sum(s);
-    const float a = s[0] / cols, q = s[1] / cols;
-    for (int c = threadIdx.x; c < cols; c += blockDim.x) {
-      const float g = to_f(dy[r * ld_dy + c]) * (w ? to_f(w[c]) : 1.f), xh = (to_f(x[r * ldx + c]) - m) * rs;
-      dx[r * ld_dx + c] = from_f<T>(rs * (g - a - xh * q) + (add ? to_f(add[r * ld_add + c]) : 0.f));
+// ---- backward ----------------------------------------------------------------------------------
+constexpr int kOwn = 8;              // columns of a thread
+constexpr int kRows = 1;             // rows of a group of threads at a time
+
+struct NormGradArgs {
+  int64_t rows; int cols;
+  const void *dy, *x, *w, *add; void* dx;
+  int64_t ld_dy, ldx, ld_add, ld_dx;
+  const float *mean, *rstd;
+  float* part;                       // [blocks][2][cols]
+  float* stats;                      // long rows: [rows][2], the means of g and of g xhat
+  int sums;                          // whether the sums over rows are wanted
+};
+
+// The kOwn elements of a row that belong to a thread: units of 16 bytes, `threads` units apart.
+template <class T>
+__device__ __forceinline__ int own_col(int k, int thread, int threads) { return (k / Pack<T>::V * threads + thread) * Pack<T>::V + k % Pack<T>::V; }
+template <bool VEC, class T>
+struct Own {
+  Pack<T> p[kOwn / Pack<T>::V];
+  __device__ __forceinline__ void load(const T* row, int thread, int threads, int cols) {
+#pragma unroll
+    for (int u = 0; u < kOwn / Pack<T>::V; ++u) p[u] = load_pack<VEC>(row, (u * threads + thread) * Pack<T>::V, cols);
+  }
+  __device__ __forceinline__ float get(int k) const { return p[k / Pack<T>::V].get(k % Pack<T>::V); }
+  __device__ __forceinline__ void set_store(const float (&o)[kOwn], T* row, int thread, int threads, int cols) {
+#pragma unroll
+    for (int u = 0; u < kOwn / Pack<T>::V; ++u) {
+      float q[Pack<T>::V];
+#pragma unroll
+      for (int e = 0; e < Pack<T>::V; ++e) q[e] = o[u * Pack<T>::V + e];
+      p[u].set(q);
+      store_pack<VEC>(row, p[u], (u * threads + thread) * Pack<T>::V, cols);
     }
   }
+};
+
+// The columns that a thread owns, summed over the block's groups of threads, to the block's row of partial sums.
+template <class T, int TPR, int BLOCK>
+__device__ __forceinline__ void leave_sums(const NormGradArgs& a, float (&sw)[kOwn], float (&sb)[kOwn], float* buf, int64_t block, int first, int cols) {
+  constexpr int G = BLOCK / TPR;
+  const int thread = threadIdx.x % TPR, group = threadIdx.x / TPR;
+  if constexpr (G > 1) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) buf[k * BLOCK + threadIdx.x] = half ? sb[k] : sw[k];
+      __syncthreads();
+      if (group == 0)
+#pragma unroll
+        for (int k = 0; k < kOwn; ++k) {
+          float t = 0.f;
+          for (int q = 0; q < G; ++q) t += buf[k * BLOCK + q * TPR + thread];
+          if (half) sb[k] = t; else sw[k] = t;
+        }
+    }
+  }
+  if (group == 0)
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      const int c = own_col<T>(k, thread, TPR);
+      if (c < cols) {
+        a.part[(block * 2) * a.cols + first + c] = sw[k];
+        a.part[(block * 2 + 1) * a.cols + first + c] = sb[k];
+      }
+    }
 }
 
-constexpr int kChunkRows = 256;
-template <class T>
-__global__ void layer_norm_dw_kernel(int64_t rows, int cols, const T* dy, int64_t ld_dy, const T* x, int64_t ldx, const float* mean,
-                                     const float* rstd, float* part) {
-  const int c = blockIdx.x * blockDim.x + threadIdx.x;
-  if (c >= cols) return;
-  const int64_t r0 = (int64_t)blockIdx.y * kChunkRows, r1 = r0 + kChunkRows < rows ? r0 + kChunkRows : rows;
-  float sw = 0.f, sb = 0.f;
-  for (int64_t r = r0; r < r1; ++r) {
-    const float g = to_f(dy[r * ld_dy + c]);
-    sb += g; sw += g * (to_f(x[r * ldx + c]) - mean[r]) * rstd[r];
+template <class T, class W, int TPR, bool VEC>
+__global__ void __launch_bounds__(TPR > 256 ? TPR : 256, TPR > 256 ? 1024 / TPR : 4) layer_norm_grad_kernel(const NormGradArgs a) {
+  constexpr int BLOCK = TPR > 256 ? TPR : 256, G = BLOCK / TPR, WARPS = TPR / 32;
+  __shared__ float part[2][G][TPR > 32 ? WARPS : 1][2 * kRows];
+  __shared__ float buf[G > 1 ? kOwn * BLOCK : 1];
+  const int thread = threadIdx.x % TPR, group = threadIdx.x / TPR, lane = threadIdx.x & 31;
+  grid_dep_wait();
+  grid_dep_launch();
+  const T* const dy = (const T*)dep(a.dy);
+  const T* const x = (const T*)dep(a.x);
+  const T* const add = (const T*)dep(a.add);
+  const W* const w = (const W*)dep(a.w);
+  const float* const mean = dep(a.mean);
+  const float* const rstd = dep(a.rstd);
+  const int cols = a.cols;
+  const float inv_n = 1.f / (float)cols;
+  float wv[kOwn], sw[kOwn], sb[kOwn];
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {
+    const int c = own_col<T>(k, thread, TPR);
+    wv[k] = w && c < cols ? to_f(w[c]) : 1.f;
+    sw[k] = sb[k] = 0.f;
   }
-  part[((int64_t)blockIdx.y * 2) * cols + c] = sw;
-  part[((int64_t)blockIdx.y * 2 + 1) * cols + c] = sb;
+  const int64_t step = (int64_t)gridDim.x * G * kRows, rounds = (a.rows + step - 1) / step;
+  int flip = 0;
+  for (int64_t it = 0; it < rounds; ++it, flip ^= 1) {
+    const int64_t r0 = it * step + ((int64_t)blockIdx.x * G + group) * kRows;
+    Own<VEC, T> xo[kRows], go[kRows];
+    float m[kRows], rs[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const bool in = r0 + i < a.rows;
+      m[i] = in ? mean[r0 + i] : 0.f; rs[i] = in ? rstd[r0 + i] : 0.f;
+      const int n = in ? cols : 0;
+      xo[i].load(x + (in ? r0 + i : 0) * a.ldx, thread, TPR, n);
+      go[i].load(dy + (in ? r0 + i : 0) * a.ld_dy, thread, TPR, n);
+    }
+    float s[2 * kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      s[2 * i] = s[2 * i + 1] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) {
+        const float g = go[i].get(k), xh = (xo[i].get(k) - m[i]) * rs[i];
+        // (columns past the row's end: dy reads as zero there)
+        s[2 * i] = fmaf(g, wv[k], s[2 * i]);
+        s[2 * i + 1] = fmaf(g * wv[k], xh, s[2 * i + 1]);
+        sw[k] = fmaf(g, xh, sw[k]);
+        sb[k] += g;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * kRows; ++i)
+#pragma unroll
+      for (int o = (TPR < 32 ? TPR : 32) / 2; o; o >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+    if constexpr (TPR > 32) {
+      // (two sets of partial sums in turn: one barrier a round is enough)
+      if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < 2 * kRows; ++i) part[flip][group][thread >> 5][i] = s[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 2 * kRows; ++i) {
+        s[i] = lane < WARPS ? part[flip][group][lane % WARPS][i] : 0.f;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
+      }
+    }
+    if (a.dx)
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (r0 + i < a.rows) {
+          Own<VEC, T> ao;
+          if (add) ao.load(add + (r0 + i) * a.ld_add, thread, TPR, cols);
+          const float p = s[2 * i] * inv_n, q = s[2 * i + 1] * inv_n;
+          float o[kOwn];
+#pragma unroll
+          for (int k = 0; k < kOwn; ++k) {
+            const float xh = (xo[i].get(k) - m[i]) * rs[i];
+            o[k] = rs[i] * (go[i].get(k) * wv[k] - p - xh * q) + (add ? ao.get(k) : 0.f);
+          }
+          go[i].set_store(o, (T*)a.dx + (r0 + i) * a.ld_dx, thread, TPR, cols);
+        }
+  }
+  if (a.sums) leave_sums<T, TPR, BLOCK>(a, sw, sb, buf, blockIdx.x, 0, cols);
 }
+
+// Rows of more than 8192 columns: the two means of a row by a kernel of their own, then column blocks of 2048 that walk a share of the rows.
+template <class T, class W>
+__global__ void __launch_bounds__(1024) layer_norm_stats_kernel(const NormGradArgs a) {
+  const T* const dy = (const T*)a.dy;
+  const T* const x = (const T*)a.x;
+  const W* const w = (const W*)a.w;
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const float m = a.mean[r], rs = a.rstd[r];
+    float s[2] = {0.f, 0.f};
+    for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
+      const float g = to_f(dy[r * a.ld_dy + c]) * (w ? to_f(w[c]) : 1.f);
+      s[0] += g; s[1] += g * ((to_f(x[r * a.ldx + c]) - m) * rs);
+    }
+    block_sum(s);
+    if (threadIdx.x == 0) { a.stats[2 * r] = s[0] / a.cols; a.stats[2 * r + 1] = s[1] / a.cols; }
+  }
+}
+constexpr int kLongCols = 256 * kOwn;
+template <class T, class W, bool VEC>
+__global__ void __launch_bounds__(256) layer_norm_grad_long_kernel(const NormGradArgs a) {
+  const int first = blockIdx.x * kLongCols, cols = min(kLongCols, a.cols - first), thread = threadIdx.x;
+  const T* const dy = (const T*)a.dy + first;
+  const T* const x = (const T*)a.x + first;
+  const T* const add = a.add ? (const T*)a.add + first : nullptr;
+  const W* const w = a.w ? (const W*)a.w + first : nullptr;
+  float wv[kOwn], sw[kOwn], sb[kOwn];
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {
+    const int c = own_col<T>(k, thread, 256);
+    wv[k] = w && c < cols ? to_f(w[c]) : 1.f;
+    sw[k] = sb[k] = 0.f;
+  }
+  for (int64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
+    const float m = a.mean[r], rs = a.rstd[r], p = a.dx ? a.stats[2 * r] : 0.f, q = a.dx ? a.stats[2 * r + 1] : 0.f;
+    Own<VEC, T> xo, go, ao;
+    xo.load(x + r * a.ldx, thread, 256, cols);
+    go.load(dy + r * a.ld_dy, thread, 256, cols);
+    if (add) ao.load(add + r * a.ld_add, thread, 256, cols);
+    float o[kOwn];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      const float g = go.get(k), xh = (xo.get(k) - m) * rs;
+      sw[k] = fmaf(g, xh, sw[k]); sb[k] += g;
+      o[k] = rs * (g * wv[k] - p - xh * q) + (add ? ao.get(k) : 0.f);
+    }
+    if (a.dx) go.set_store(o, (T*)a.dx + first + r * a.ld_dx, thread, 256, cols);
+  }
+  if (a.sums) leave_sums<T, 256, 256>(a, sw, sb, nullptr, blockIdx.y, first, cols);
+}
+
+// dw, db = sums of the blocks' partial sums, in order of the blocks: 32 columns of either a block, a warp for every 32nd partial row.
 template <class W>
-__global__ void layer_norm_dw_final_kernel(int64_t chunks, int cols, const float* part, W* dw, W* db) {
-  const int c = blockIdx.x * blockDim.x + threadIdx.x;
-  if (c >= cols) return;
-  float sw = 0.f, sb = 0.f;
-  for (int64_t k = 0; k < chunks; ++k) { sw += part[2 * k * cols + c]; sb += part[(2 * k + 1) * cols + c]; }
-  if (dw) dw[c] = from_f<W>(sw);
-  if (db) db[c] = from_f<W>(sb);
+__global__ void __launch_bounds__(1024) layer_norm_sums_kernel(int blocks, int cols, const float* part, W* dw, W* db) {
+  __shared__ float buf[32][33];
+  grid_dep_wait();
+  grid_dep_launch();
+  part = dep(part);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  float s = 0.f;
+  if (c < cols)
+    for (int k = warp; k < blocks; k += 32) s += part[((int64_t)k * 2 + blockIdx.y) * cols + c];
+  buf[warp][lane] = s;
+  __syncthreads();
+  s = buf[lane][warp];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  W* const out = blockIdx.y ? db : dw;
+  if (lane == 0 && out && blockIdx.x * 32 + warp < cols) out[blockIdx.x * 32 + warp] = from_f<W>(s);
+}
+
+// How a backward pass is cut: threads a row (0: long rows), and the blocks that leave partial sums.  By sizes alone: the workspace
+// and the order of the sums are the same for all types and alignments.
+struct NormGradPlan { int tpr; int64_t blocks; };
+NormGradPlan norm_grad_plan(int64_t rows, int cols) {
+  NormGradPlan p{0, 0};
+  for (int t = 8; t <= 1024; t *= 2)
+    if (cols <= t * kOwn) { p.tpr = t; break; }
+  if (p.tpr) {
+    const int block = p.tpr > 256 ? p.tpr : 256, per = block / p.tpr * kRows;
+    const int64_t want = (rows + per - 1) / per, most = 148LL * (1024 / block);
+    p.blocks = want < most ? want : most;
+  } else {
+    const int64_t strips = (cols + kLongCols - 1) / kLongCols, most = (148 * 4 + strips - 1) / strips;
+    p.blocks = rows < most ? rows : most;
+  }
+  return p;
 }
 
 struct NormCall {
+  int type;
   int64_t rows; int cols;
   const void *dy, *x, *w, *b, *add; int64_t ld_dy, ldx, ld_add;
   void *y, *dw, *db; int64_t ldy;
@@ -100,32 +385,77 @@ struct NormCall {
   void* ws; cudaStream_t st;
 };
 
-template <class T, class W>
-void run_norm(const NormCall& a) {
-  const int grid = (int)(a.rows < 4096 ? a.rows : 4096);
-  layer_norm_kernel<T, W><<<grid, 256, 0, a.st>>>(a.rows, a.cols, (const T*)a.x, a.ldx, (const W*)a.w, (const W*)a.b, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
+template <class T, class W, int TPR, int NU>
+cudaError_t norm_as(const NormCall& a, bool vec) {
+  constexpr int PER = TPR > 32 ? 1 : 128 / TPR;
+  const int64_t blocks = (a.rows + PER - 1) / PER;
+  auto* const k = vec ? layer_norm_kernel<T, W, TPR, NU, true> : layer_norm_kernel<T, W, TPR, NU, false>;
+  return launch_pdl_grid(k, dim3((unsigned)blocks), TPR > 32 ? TPR : 128, 0, a.st, a.rows, a.cols, (const T*)a.x, a.ldx, (const W*)a.w, (const W*)a.b, a.eps,
+                         (T*)a.y, a.ldy, a.mean, a.rstd);
 }
 template <class T, class W>
-void run_norm_grad(const NormCall& a) {
-  const int64_t chunks = (a.rows + kChunkRows - 1) / kChunkRows;
-  if (a.dw || a.db) {
-    if (chunks) layer_norm_dw_kernel<T><<<dim3((a.cols + 127) / 128, (unsigned)chunks), 128, 0, a.st>>>(a.rows, a.cols, (const T*)a.dy, a.ld_dy, (const T*)a.x, a.ldx, a.mean, a.rstd, (float*)a.ws);
-    layer_norm_dw_final_kernel<W><<<(a.cols + 127) / 128, 128, 0, a.st>>>(chunks, a.cols, (const float*)a.ws, (W*)a.dw, (W*)a.db);
-  }
-  if (a.y && a.rows) {
-    const int grid = (int)(a.rows < 4096 ? a.rows : 4096);
-    layer_norm_dx_kernel<T, W><<<grid, 256, 0, a.st>>>(a.rows, a.cols, (const T*)a.dy, a.ld_dy, (const T*)a.x, a.ldx, a.mean, a.rstd, (const W*)a.w, (const T*)a.add, a.ld_add, (T*)a.y, a.ldy);
-  }
+cudaError_t run_norm(const NormCall& a) {
+  const bool vec = wide_ok(a.x, a.ldx, a.type) && wide_ok(a.y, a.ldy, a.type) && wide_ok(a.w, 0, GN_F32) && wide_ok(a.b, 0, GN_F32);
+  const int units = (a.cols + Pack<T>::V - 1) / Pack<T>::V;
+  if (units <= 8) return norm_as<T, W, 8, 1>(a, vec);
+  if (units <= 32) return norm_as<T, W, 32, 1>(a, vec);
+  if (units <= 64) return norm_as<T, W, 32, 2>(a, vec);
+  if (units <= 128) return norm_as<T, W, 32, 4>(a, vec);
+  if (units <= 256) return norm_as<T, W, 32, 8>(a, vec);
+  if (units <= 512) return norm_as<T, W, 32, 16>(a, vec);
+  if (units <= 1024) return norm_as<T, W, 256, 4>(a, vec);
+  if (units <= 2048) return norm_as<T, W, 256, 8>(a, vec);
+  if (units <= 4096) return norm_as<T, W, 1024, 4>(a, vec);
+  const int64_t most = 148 * 2;
+  layer_norm_long_kernel<T, W><<<(unsigned)(a.rows < most ? a.rows : most), 1024, 0, a.st>>>(
+      a.rows, a.cols, (const T*)a.x, a.ldx, (const W*)a.w, (const W*)a.b, a.eps, (T*)a.y, a.ldy, a.mean, a.rstd);
+  return cudaGetLastError();
 }
 
-template <template <class, class> class F, class... A>
-void by_types(int type, int wtype, const NormCall& a) {
-  if (type == GN_F32) F<float, float>::run(a);
-  else if (type == GN_BF16) { if (wtype == GN_F32) F<__nv_bfloat16, float>::run(a); else F<__nv_bfloat16, __nv_bfloat16>::run(a); }
-  else { if (wtype == GN_F32) F<__half, float>::run(a); else F<__half, __half>::run(a); }
+template <class T, class W, int TPR>
+cudaError_t norm_grad_as(const NormGradArgs& g, bool vec, int64_t blocks, cudaStream_t st) {
+  return launch_pdl_grid(vec ? layer_norm_grad_kernel<T, W, TPR, true> : layer_norm_grad_kernel<T, W, TPR, false>, dim3((unsigned)blocks),
+                         TPR > 256 ? TPR : 256, 0, st, g);
 }
-template <class T, class W> struct Norm { static void run(const NormCall& a) { run_norm<T, W>(a); } };
-template <class T, class W> struct NormGrad { static void run(const NormCall& a) { run_norm_grad<T, W>(a); } };
+template <class T, class W>
+cudaError_t run_norm_grad(const NormCall& a) {
+  const NormGradPlan plan = norm_grad_plan(a.rows, a.cols);
+  NormGradArgs g{a.rows, a.cols, a.dy, a.x, a.w, a.add, a.y, a.ld_dy, a.ldx, a.ld_add, a.ldy, a.mean, a.rstd, (float*)a.ws, nullptr, a.dw || a.db};
+  const bool vec = wide_ok(a.dy, a.ld_dy, a.type) && wide_ok(a.x, a.ldx, a.type) && wide_ok(a.add, a.ld_add, a.type) && wide_ok(a.y, a.ldy, a.type);
+  cudaError_t e = cudaSuccess;
+  if (a.rows > 0 && (g.sums || g.dx)) {
+    switch (plan.tpr) {
+      case 8: e = norm_grad_as<T, W, 8>(g, vec, plan.blocks, a.st); break;
+      case 16: e = norm_grad_as<T, W, 16>(g, vec, plan.blocks, a.st); break;
+      case 32: e = norm_grad_as<T, W, 32>(g, vec, plan.blocks, a.st); break;
+      case 64: e = norm_grad_as<T, W, 64>(g, vec, plan.blocks, a.st); break;
+      case 128: e = norm_grad_as<T, W, 128>(g, vec, plan.blocks, a.st); break;
+      case 256: e = norm_grad_as<T, W, 256>(g, vec, plan.blocks, a.st); break;
+      case 512: e = norm_grad_as<T, W, 512>(g, vec, plan.blocks, a.st); break;
+      case 1024: e = norm_grad_as<T, W, 1024>(g, vec, plan.blocks, a.st); break;
+      default: {
+        g.stats = g.part + plan.blocks * 2 * a.cols;
+        if (g.dx) layer_norm_stats_kernel<T, W><<<(unsigned)(a.rows < 296 ? a.rows : 296), 1024, 0, a.st>>>(g);
+        const dim3 grid((unsigned)((a.cols + kLongCols - 1) / kLongCols), (unsigned)plan.blocks);
+        if (vec) layer_norm_grad_long_kernel<T, W, true><<<grid, 256, 0, a.st>>>(g);
+        else layer_norm_grad_long_kernel<T, W, false><<<grid, 256, 0, a.st>>>(g);
+        e = cudaGetLastError();
+      }
+    }
+  }
+  if (e != cudaSuccess || !g.sums) return e;
+  return launch_pdl_grid(layer_norm_sums_kernel<W>, dim3((unsigned)((a.cols + 31) / 32), 2), 1024, 0, a.st, (int)plan.blocks, a.cols, (const float*)g.part,
+                         (W*)a.dw, (W*)a.db);
+}
+
+template <template <class, class> class F>
+cudaError_t by_types(int type, int wtype, const NormCall& a) {
+  if (type == GN_F32) return F<float, float>::run(a);
+  if (type == GN_BF16) return wtype == GN_F32 ? F<__nv_bfloat16, float>::run(a) : F<__nv_bfloat16, __nv_bfloat16>::run(a);
+  return wtype == GN_F32 ? F<__half, float>::run(a) : F<__half, __half>::run(a);
+}
+template <class T, class W> struct Norm { static cudaError_t run(const NormCall& a) { return run_norm<T, W>(a); } };
+template <class T, class W> struct NormGrad { static cudaError_t run(const NormCall& a) { return run_norm_grad<T, W>(a); } };
 
 constexpr int kMaxCols = 1 << 20;
 const char* norm_sizes(int type, int wtype, int64_t rows, int cols) {
@@ -156,15 +486,15 @@ extern "C" gn_status gn_layer_norm(gn_dtype type, gn_dtype wtype, int64_t rows, 
   if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
   if (rows == 0) return op_done(cudaSuccess, errbuf, errbuf_len);
   NormCall a = {};
-  a.rows = rows; a.cols = cols; a.x = d_x; a.ldx = ldx; a.w = d_weight; a.b = d_bias; a.eps = (float)eps;
+  a.type = type; a.rows = rows; a.cols = cols; a.x = d_x; a.ldx = ldx; a.w = d_weight; a.b = d_bias; a.eps = (float)eps;
   a.y = d_y; a.ldy = ldy; a.mean = d_mean; a.rstd = d_rstd; a.st = (cudaStream_t)cuda_stream;
-  by_types<Norm>(type, wtype, a);
-  return op_done(cudaSuccess, errbuf, errbuf_len);
+  return op_done(by_types<Norm>(type, wtype, a), errbuf, errbuf_len);
 }
 
 extern "C" int64_t gn_layer_norm_grad_workspace(int64_t rows, int32_t cols) {
   if (rows < 0 || cols < 1 || cols > kMaxCols) return -1;
-  return (rows + kChunkRows - 1) / kChunkRows * 2 * cols * 4 + 16;
+  const NormGradPlan p = norm_grad_plan(rows, cols);
+  return (p.blocks * 2 * cols + (p.tpr ? 0 : 2 * rows)) * 4 + 16;
 }
 
 extern "C" gn_status gn_layer_norm_grad(gn_dtype type, gn_dtype wtype, int64_t rows, int32_t cols, const void* d_dy, int64_t ld_dy,
@@ -184,9 +514,8 @@ extern "C" gn_status gn_layer_norm_grad(gn_dtype type, gn_dtype wtype, int64_t r
   if (!why && (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < gn_layer_norm_grad_workspace(rows, cols))) why = "workspace: null, not 16-byte aligned or too small";
   if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
   NormCall a = {};
-  a.rows = rows; a.cols = cols; a.dy = d_dy; a.ld_dy = ld_dy; a.x = d_x; a.ldx = ldx; a.w = d_weight; a.add = d_add; a.ld_add = ld_add;
+  a.type = type; a.rows = rows; a.cols = cols; a.dy = d_dy; a.ld_dy = ld_dy; a.x = d_x; a.ldx = ldx; a.w = d_weight; a.add = d_add; a.ld_add = ld_add;
   a.y = d_dx; a.ldy = ld_dx; a.dw = d_dweight; a.db = d_dbias; a.mean = const_cast<float*>(d_mean); a.rstd = const_cast<float*>(d_rstd);
   a.ws = d_ws; a.st = (cudaStream_t)cuda_stream;
-  by_types<NormGrad>(type, wtype, a);
-  return op_done(cudaSuccess, errbuf, errbuf_len);
+  return op_done(by_types<NormGrad>(type, wtype, a), errbuf, errbuf_len);
 }

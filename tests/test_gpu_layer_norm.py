@@ -73,8 +73,14 @@ def test_forward_misaligned_bases(offset):
     flat = vec(64 * 1024 + 8, torch.bfloat16, 4)
     w = vec(1024 + 8, torch.bfloat16, 5)
     x = flat[offset: offset + 64 * 1024].view(64, 1024)
-    y = gn.layer_norm(x, w[offset: offset + 1024], w[8 - offset: 8 - offset + 1024])
-    assert torch.equal(y, gn.layer_norm(x.clone(), w[offset: offset + 1024].clone(), w[8 - offset: 8 - offset + 1024].clone()))
+    b = w[8 - offset: 8 - offset + 1024]
+    w = w[offset: offset + 1024]
+    y, mean, rstd = gn.layer_norm(x, w, b, save=True)
+    ry, rm, rr = norm64(x, w, b, 1e-5)
+    by, bm, br = norm_bounds(x, w, b, ry, rm, rr, torch.bfloat16)          # (rows that 16-byte loads cannot read are summed in another order)
+    within(y, ry, by, "y")
+    within(mean, rm, bm, "mean")
+    within(rstd, rr, br, "rstd")
 
 
 def test_forward_of_a_large_mean():

@@ -5,7 +5,7 @@
 // of a row are taken twice from the registers, of x for the mean m and then of x - m and its square: the first of these two
 // is what m's rounding has left, which corrects the mean and the variance, so a mean far above the spread costs no accuracy.
 //
-// Backward: 8 columns a thread, kRows rows at a time.  With mean and rstd at hand a row needs one reduction, of g and g xhat; the sums
+// Backward: two units a thread.  With mean and rstd at hand a row needs one reduction, of g and g xhat; the sums
 // over rows of dy xhat and dy stay with the thread that owns the column, and each block leaves one row of partial sums, which a
 // second kernel adds in a fixed order.
 #include <math.h>
@@ -16,94 +16,116 @@
 namespace gn {
 namespace {
 
-template <int N>
-__device__ __forceinline__ void block_sum(float (&v)[N]) {
-  __shared__ float part[N][32];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+// Sum over the TPR threads of a row, known to all of them.  `part`: TPR / 32 words of shared memory for each value, which must not be written again
+// before every thread has passed another barrier.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sum(float (&v)[N], float* part) {
 #pragma unroll
   for (int k = 0; k < N; ++k)
-    for (int o = 16; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-  __syncthreads();
-  if (lane == 0)
-    for (int k = 0; k < N; ++k) part[k][warp] = v[k];
-  __syncthreads();
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    v[k] = lane < (blockDim.x >> 5) ? part[k][lane] : 0.f;
-    for (int o = 16; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-  }
-}
-// Sum over the TPR threads of a row, known to all of them.
-template <int TPR, int N>
-__device__ __forceinline__ void row_sum(float (&v)[N]) {
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
   if constexpr (TPR > 32) {
-    block_sum(v);
-  } else {
+    constexpr int WARPS = TPR / 32;
+    const int warp = threadIdx.x % TPR / 32, lane = threadIdx.x & 31;
+    if (lane == 0)
 #pragma unroll
-    for (int k = 0; k < N; ++k)
+      for (int k = 0; k < N; ++k) part[k * WARPS + warp] = v[k];
+    __syncthreads();
 #pragma unroll
-      for (int o = TPR / 2; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    for (int k = 0; k < N; ++k) {
+      v[k] = part[k * WARPS + lane % WARPS];
+#pragma unroll
+      for (int o = WARPS / 2; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    }
   }
 }
 
-// TPR threads a row, which hold NU units of 16 bytes each; rows of a block go through one after another only where the grid is full.
+// TPR threads a row, which hold NU units of 16 bytes each.  A block walks its rows with the next row's loads under way while it works on
+// one; the weights stay in registers where they are few.
+template <int TPR> constexpr int norm_block = TPR > 128 ? TPR : 128;
+// Blocks of an SM.  16384 x 4096 bf16 with two units a thread: 51.3 us at 768 threads an SM (80 registers), 52.6 at 1024, 74 at 1280.
+template <int TPR> constexpr int norm_blocks = TPR > 256 ? 1024 / TPR : 768 / norm_block<TPR>;
 template <class T, class W, int TPR, int NU, bool VEC>
-__global__ void __launch_bounds__(TPR > 32 ? TPR : 128) layer_norm_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, const W* b, float eps,
-                                                                          T* y, int64_t ldy, float* mean_out, float* rstd_out) {
-  constexpr int V = Pack<T>::V, WU = sizeof(W) / sizeof(T);      // units of the weights to a unit of x
-  constexpr int PER = TPR > 32 ? 1 : 128 / TPR;                  // rows of a block
+__global__ void __launch_bounds__(norm_block<TPR>, norm_blocks<TPR>)
+layer_norm_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, const W* b, float eps, T* y, int64_t ldy, float* mean_out, float* rstd_out) {
+  constexpr int V = Pack<T>::V, VW = Pack<W>::V, WU = sizeof(W) / sizeof(T);      // WU: units of the weights to a unit of x
+  constexpr int PER = norm_block<TPR> / TPR;                     // rows of a block
+  constexpr bool KEEP = NU * WU <= 2;
+  __shared__ float part[TPR > 32 ? PER : 1][3 * (TPR > 32 ? TPR / 32 : 1)];
   const int thread = threadIdx.x % TPR;
+  float* const mine = part[TPR > 32 ? threadIdx.x / TPR : 0];
   grid_dep_wait();
   grid_dep_launch();
   x = dep(x); w = dep(w); b = dep(b);
   const float inv_n = 1.f / (float)cols;
-  const int64_t r = (int64_t)blockIdx.x * PER + threadIdx.x / TPR;
-  const bool in = r < rows;                                      // (a warp's other rows still take part in the sums' exchanges)
-  const T* const xr = x + (in ? r : 0) * ldx;
-  Pack<T> v[NU];
+  const int64_t step = (int64_t)gridDim.x * PER;
+  int64_t r = (int64_t)blockIdx.x * PER + threadIdx.x / TPR;
+  // (the weights of unit u are units u WU .. u WU + WU - 1 of theirs, and lie side by side where x's elements do)
+  const auto weights = [&](const W* p, int u, int q) {
+    return VEC && WU > 1 ? load_pack<true>(p, 0, (u * TPR + thread) * WU + q, 1, cols) : load_pack<VEC>(p, u * WU + q, thread, TPR, cols);
+  };
+  Pack<W> wk[KEEP ? NU * WU : 1], bk[KEEP ? NU * WU : 1];
+  if constexpr (KEEP)
 #pragma unroll
-  for (int u = 0; u < NU; ++u) v[u] = load_pack<VEC>(xr, (u * TPR + thread) * V, cols);
-  float s[1] = {0.f};
-#pragma unroll
-  for (int u = 0; u < NU; ++u)
-#pragma unroll
-    for (int e = 0; e < V; ++e) s[0] += v[u].get(e);
-  row_sum<TPR>(s);
-  const float m = s[0] * inv_n;
-  float d[2] = {0.f, 0.f};
-#pragma unroll
-  for (int u = 0; u < NU; ++u)
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float t = v[u].get(e) - m;
-      if ((u * TPR + thread) * V + e < cols) { d[0] += t; d[1] = fmaf(t, t, d[1]); }
+    for (int q = 0; q < NU * WU; ++q) {
+      if (w) wk[q] = weights(w, q / WU, q % WU);
+      if (b) bk[q] = weights(b, q / WU, q % WU);
     }
-  row_sum<TPR>(d);
-  const float off = d[0] * inv_n, rstd = 1.f / sqrtf(d[1] * inv_n - off * off + eps);
+  Pack<T> next[NU];
 #pragma unroll
-  for (int u = 0; u < NU; ++u) {
-    const int c = (u * TPR + thread) * V;
-    if (c >= cols) break;
-    float wv[V], bv[V];
+  for (int u = 0; u < NU; ++u) next[u] = load_pack<VEC>(x + (r < rows ? r : 0) * ldx, u, thread, TPR, cols);
+  // (all threads of a block make the same rounds: those without a row still take part in the sums' exchanges and barriers)
+  for (int64_t r0 = (int64_t)blockIdx.x * PER; r0 < rows; r0 += step, r += step) {
+    const bool in = r < rows;
+    Pack<T> v[NU];
 #pragma unroll
-    for (int q = 0; q < WU; ++q) {
-      constexpr int VW = Pack<W>::V;
-      Pack<W> pw, pb;
-      if (w) pw = load_pack<VEC>(w, c + q * VW, cols);
-      if (b) pb = load_pack<VEC>(b, c + q * VW, cols);
+    for (int u = 0; u < NU; ++u) v[u] = next[u];
+    if (r0 + step < rows)
 #pragma unroll
-      for (int e = 0; e < VW; ++e) { wv[q * VW + e] = w ? pw.get(e) : 1.f; bv[q * VW + e] = b ? pb.get(e) : 0.f; }
+      for (int u = 0; u < NU; ++u) next[u] = load_pack<VEC>(x + (r + step < rows ? r + step : 0) * ldx, u, thread, TPR, cols);
+    // (few instructions an element: at 16 bits the arithmetic alone is half of what memory takes)
+    float t[NU * V], s[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < NU * V; ++k) { t[k] = v[k / V].get(k % V); s[0] += t[k]; }
+    row_sum<TPR>(s, mine);
+    const float m = s[0] * inv_n;
+    float d[2] = {0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      if (pack_col<VEC, T>(u, V - 1, thread, TPR) < cols) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) { t[u * V + e] -= m; d[0] += t[u * V + e]; d[1] = fmaf(t[u * V + e], t[u * V + e], d[1]); }
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (pack_col<VEC, T>(u, e, thread, TPR) < cols) { t[u * V + e] -= m; d[0] += t[u * V + e]; d[1] = fmaf(t[u * V + e], t[u * V + e], d[1]); }
+      }
     }
-    float o[V];
+    row_sum<TPR>(d, mine + (TPR > 32 ? TPR / 32 : 0));
+    const float off = d[0] * inv_n, rstd = 1.f / sqrtf(d[1] * inv_n - off * off + eps), shift = -off * rstd;
 #pragma unroll
-    for (int e = 0; e < V; ++e) o[e] = fmaf((v[u].get(e) - m - off) * rstd, wv[e], bv[e]);
-    Pack<T> p;
-    p.set(o);
-    if (in) store_pack<VEC>(y + r * ldy, p, c, cols);
-  }
-  if (in && thread == 0) {
-    if (mean_out) mean_out[r] = m + off;
-    if (rstd_out) rstd_out[r] = rstd;
+    for (int u = 0; u < NU; ++u) {
+      if (pack_col<VEC, T>(u, 0, thread, TPR) >= cols) break;
+      float o[V];
+#pragma unroll
+      for (int q = 0; q < WU; ++q) {
+        Pack<W> pw, pb;
+        if constexpr (KEEP) { pw = wk[u * WU + q]; pb = bk[u * WU + q]; }
+        else {
+          if (w) pw = weights(w, u, q);
+          if (b) pb = weights(b, u, q);
+        }
+#pragma unroll
+        for (int e = 0; e < VW; ++e) o[q * VW + e] = fmaf(fmaf(t[u * V + q * VW + e], rstd, shift), w ? pw.get(e) : 1.f, b ? pb.get(e) : 0.f);
+      }
+      Pack<T> p;
+      p.set(o);
+      if (in) store_pack<VEC>(y + r * ldy, p, u, thread, TPR, cols);
+    }
+    if (in && thread == 0) {
+      if (mean_out) mean_out[r] = m + off;
+      if (rstd_out) rstd_out[r] = rstd;
+    }
   }
 }
 
@@ -111,15 +133,16 @@ __global__ void __launch_bounds__(TPR > 32 ? TPR : 128) layer_norm_kernel(int64_
 template <class T, class W>
 __global__ void __launch_bounds__(1024) layer_norm_long_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, const W* b, float eps, T* y,
                                                                int64_t ldy, float* mean_out, float* rstd_out) {
+  __shared__ float part[3 * 32];
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const T* xr = x + r * ldx;
     float s[1] = {0.f};
     for (int c = threadIdx.x; c < cols; c += blockDim.x) s[0] += to_f(xr[c]);
-    block_sum(s);
+    row_sum<1024>(s, part);
     const float m = s[0] / cols;
     float d[2] = {0.f, 0.f};
     for (int c = threadIdx.x; c < cols; c += blockDim.x) { const float v = to_f(xr[c]) - m; d[0] += v; d[1] += v * v; }
-    block_sum(d);
+    row_sum<1024>(d, part + 32);
     const float off = d[0] / cols, rstd = 1.f / sqrtf(d[1] / cols - off * off + eps);
     for (int c = threadIdx.x; c < cols; c += blockDim.x) {
       const float v = (to_f(xr[c]) - m - off) * rstd;
@@ -133,8 +156,7 @@ __global__ void __launch_bounds__(1024) layer_norm_long_kernel(int64_t rows, int
 }
 
 // ---- backward ----------------------------------------------------------------------------------
-constexpr int kOwn = 8;              // columns of a thread
-constexpr int kRows = 1;             // rows of a group of threads at a time
+template <class T> constexpr int kOwn = 2 * Pack<T>::V;   // columns of a thread
 
 struct NormGradArgs {
   int64_t rows; int cols;
@@ -146,32 +168,32 @@ struct NormGradArgs {
   int sums;                          // whether the sums over rows are wanted
 };
 
-// The kOwn elements of a row that belong to a thread: units of 16 bytes, `threads` units apart.
-template <class T>
-__device__ __forceinline__ int own_col(int k, int thread, int threads) { return (k / Pack<T>::V * threads + thread) * Pack<T>::V + k % Pack<T>::V; }
+// The kOwn elements of a row that belong to a thread.
+template <bool VEC, class T>
+__device__ __forceinline__ int own_col(int k, int thread, int threads) { return pack_col<VEC, T>(k / Pack<T>::V, k % Pack<T>::V, thread, threads); }
 template <bool VEC, class T>
 struct Own {
-  Pack<T> p[kOwn / Pack<T>::V];
+  Pack<T> p[2];
   __device__ __forceinline__ void load(const T* row, int thread, int threads, int cols) {
 #pragma unroll
-    for (int u = 0; u < kOwn / Pack<T>::V; ++u) p[u] = load_pack<VEC>(row, (u * threads + thread) * Pack<T>::V, cols);
+    for (int u = 0; u < 2; ++u) p[u] = load_pack<VEC>(row, u, thread, threads, cols);
   }
   __device__ __forceinline__ float get(int k) const { return p[k / Pack<T>::V].get(k % Pack<T>::V); }
-  __device__ __forceinline__ void set_store(const float (&o)[kOwn], T* row, int thread, int threads, int cols) {
+  __device__ __forceinline__ void set_store(const float (&o)[kOwn<T>], T* row, int thread, int threads, int cols) {
 #pragma unroll
-    for (int u = 0; u < kOwn / Pack<T>::V; ++u) {
+    for (int u = 0; u < 2; ++u) {
       float q[Pack<T>::V];
 #pragma unroll
       for (int e = 0; e < Pack<T>::V; ++e) q[e] = o[u * Pack<T>::V + e];
       p[u].set(q);
-      store_pack<VEC>(row, p[u], (u * threads + thread) * Pack<T>::V, cols);
+      store_pack<VEC>(row, p[u], u, thread, threads, cols);
     }
   }
 };
 
 // The columns that a thread owns, summed over the block's groups of threads, to the block's row of partial sums.
-template <class T, int TPR, int BLOCK>
-__device__ __forceinline__ void leave_sums(const NormGradArgs& a, float (&sw)[kOwn], float (&sb)[kOwn], float* buf, int64_t block, int first, int cols) {
+template <bool VEC, class T, int TPR, int BLOCK>
+__device__ __forceinline__ void leave_sums(const NormGradArgs& a, float (&sw)[kOwn<T>], float (&sb)[kOwn<T>], float* buf, int64_t block, int first, int cols) {
   constexpr int G = BLOCK / TPR;
   const int thread = threadIdx.x % TPR, group = threadIdx.x / TPR;
   if constexpr (G > 1) {
@@ -179,11 +201,11 @@ __device__ __forceinline__ void leave_sums(const NormGradArgs& a, float (&sw)[kO
     for (int half = 0; half < 2; ++half) {
       __syncthreads();
 #pragma unroll
-      for (int k = 0; k < kOwn; ++k) buf[k * BLOCK + threadIdx.x] = half ? sb[k] : sw[k];
+      for (int k = 0; k < kOwn<T>; ++k) buf[k * BLOCK + threadIdx.x] = half ? sb[k] : sw[k];
       __syncthreads();
       if (group == 0)
 #pragma unroll
-        for (int k = 0; k < kOwn; ++k) {
+        for (int k = 0; k < kOwn<T>; ++k) {
           float t = 0.f;
           for (int q = 0; q < G; ++q) t += buf[k * BLOCK + q * TPR + thread];
           if (half) sb[k] = t; else sw[k] = t;
@@ -192,8 +214,8 @@ __device__ __forceinline__ void leave_sums(const NormGradArgs& a, float (&sw)[kO
   }
   if (group == 0)
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) {
-      const int c = own_col<T>(k, thread, TPR);
+    for (int k = 0; k < kOwn<T>; ++k) {
+      const int c = own_col<VEC, T>(k, thread, TPR);
       if (c < cols) {
         a.part[(block * 2) * a.cols + first + c] = sw[k];
         a.part[(block * 2 + 1) * a.cols + first + c] = sb[k];
@@ -201,12 +223,16 @@ __device__ __forceinline__ void leave_sums(const NormGradArgs& a, float (&sw)[kO
     }
 }
 
+template <int TPR> constexpr int grad_block = TPR > 256 ? TPR : 256;
+// Threads of an SM: what a thread holds of two rows, the weights and the sums takes about 110 registers at 16 bits (16 columns), 80 at 32 (8).
+template <class T> constexpr int grad_threads = sizeof(T) == 2 ? 512 : 768;
+template <class T, int TPR> constexpr int grad_blocks = grad_threads<T> / grad_block<TPR> > 0 ? grad_threads<T> / grad_block<TPR> : 1;
 template <class T, class W, int TPR, bool VEC>
-__global__ void __launch_bounds__(TPR > 256 ? TPR : 256, TPR > 256 ? 1024 / TPR : 4) layer_norm_grad_kernel(const NormGradArgs a) {
-  constexpr int BLOCK = TPR > 256 ? TPR : 256, G = BLOCK / TPR, WARPS = TPR / 32;
-  __shared__ float part[2][G][TPR > 32 ? WARPS : 1][2 * kRows];
-  __shared__ float buf[G > 1 ? kOwn * BLOCK : 1];
-  const int thread = threadIdx.x % TPR, group = threadIdx.x / TPR, lane = threadIdx.x & 31;
+__global__ void __launch_bounds__(grad_block<TPR>, grad_blocks<T, TPR>) layer_norm_grad_kernel(const NormGradArgs a) {
+  constexpr int BLOCK = grad_block<TPR>, G = BLOCK / TPR;
+  __shared__ float part[2][G][TPR > 32 ? 2 * (TPR / 32) : 1];
+  __shared__ float buf[G > 1 ? kOwn<T> * BLOCK : 1];
+  const int thread = threadIdx.x % TPR, group = threadIdx.x / TPR;
   grid_dep_wait();
   grid_dep_launch();
   const T* const dy = (const T*)dep(a.dy);
@@ -217,106 +243,87 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256, TPR > 256 ? 1024 / TPR 
   const float* const rstd = dep(a.rstd);
   const int cols = a.cols;
   const float inv_n = 1.f / (float)cols;
-  float wv[kOwn], sw[kOwn], sb[kOwn];
+  float wv[kOwn<T>], sw[kOwn<T>], sb[kOwn<T>];
 #pragma unroll
-  for (int k = 0; k < kOwn; ++k) {
-    const int c = own_col<T>(k, thread, TPR);
+  for (int k = 0; k < kOwn<T>; ++k) {
+    const int c = own_col<VEC, T>(k, thread, TPR);
     wv[k] = w && c < cols ? to_f(w[c]) : 1.f;
     sw[k] = sb[k] = 0.f;
   }
-  const int64_t step = (int64_t)gridDim.x * G * kRows, rounds = (a.rows + step - 1) / step;
+  const int64_t step = (int64_t)gridDim.x * G;
+  int64_t r = (int64_t)blockIdx.x * G + group;
   int flip = 0;
-  for (int64_t it = 0; it < rounds; ++it, flip ^= 1) {
-    const int64_t r0 = it * step + ((int64_t)blockIdx.x * G + group) * kRows;
-    Own<VEC, T> xo[kRows], go[kRows];
-    float m[kRows], rs[kRows];
+  Own<VEC, T> xn, gn_;
+  float mn = 0.f, rn = 0.f;
+  const auto fetch = [&](int64_t q) {          // (a group without a row reads zeros: rstd 0)
+    const bool in = q < a.rows;
+    mn = in ? mean[q] : 0.f; rn = in ? rstd[q] : 0.f;
+    xn.load(x + (in ? q : 0) * a.ldx, thread, TPR, in ? cols : 0);
+    gn_.load(dy + (in ? q : 0) * a.ld_dy, thread, TPR, in ? cols : 0);
+  };
+  fetch(r);
+  for (int64_t r0 = (int64_t)blockIdx.x * G; r0 < a.rows; r0 += step, r += step, flip ^= 1) {
+    Own<VEC, T> xo = xn, go = gn_, ao;
+    const float m = mn, rs = rn;
+    const bool out = a.dx && r < a.rows;
+    if (out && add) ao.load(add + r * a.ld_add, thread, TPR, cols);
+    if (r0 + step < a.rows) fetch(r + step);
+    float s[2] = {0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const bool in = r0 + i < a.rows;
-      m[i] = in ? mean[r0 + i] : 0.f; rs[i] = in ? rstd[r0 + i] : 0.f;
-      const int n = in ? cols : 0;
-      xo[i].load(x + (in ? r0 + i : 0) * a.ldx, thread, TPR, n);
-      go[i].load(dy + (in ? r0 + i : 0) * a.ld_dy, thread, TPR, n);
+    for (int k = 0; k < kOwn<T>; ++k) {
+      const float g = go.get(k), xh = (xo.get(k) - m) * rs;
+      // (columns past the row's end: dy reads as zero there)
+      s[0] = fmaf(g, wv[k], s[0]);
+      s[1] = fmaf(g * wv[k], xh, s[1]);
+      sw[k] = fmaf(g, xh, sw[k]);
+      sb[k] += g;
     }
-    float s[2 * kRows];
+    row_sum<TPR>(s, part[flip][group]);        // (two sets of words in turn: one barrier a round is enough)
+    if (out) {
+      const float p = -rs * (s[0] * inv_n), q = -rs * (s[1] * inv_n);
+      float o[kOwn<T>];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      s[2 * i] = s[2 * i + 1] = 0.f;
-#pragma unroll
-      for (int k = 0; k < kOwn; ++k) {
-        const float g = go[i].get(k), xh = (xo[i].get(k) - m[i]) * rs[i];
-        // (columns past the row's end: dy reads as zero there)
-        s[2 * i] = fmaf(g, wv[k], s[2 * i]);
-        s[2 * i + 1] = fmaf(g * wv[k], xh, s[2 * i + 1]);
-        sw[k] = fmaf(g, xh, sw[k]);
-        sb[k] += g;
+      for (int k = 0; k < kOwn<T>; ++k) {
+        o[k] = fmaf((xo.get(k) - m) * rs, q, fmaf(go.get(k) * wv[k], rs, p));
+        if (add) o[k] += ao.get(k);
       }
+      go.set_store(o, (T*)a.dx + r * a.ld_dx, thread, TPR, cols);
     }
-#pragma unroll
-    for (int i = 0; i < 2 * kRows; ++i)
-#pragma unroll
-      for (int o = (TPR < 32 ? TPR : 32) / 2; o; o >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
-    if constexpr (TPR > 32) {
-      // (two sets of partial sums in turn: one barrier a round is enough)
-      if (lane == 0)
-#pragma unroll
-        for (int i = 0; i < 2 * kRows; ++i) part[flip][group][thread >> 5][i] = s[i];
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 2 * kRows; ++i) {
-        s[i] = lane < WARPS ? part[flip][group][lane % WARPS][i] : 0.f;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) s[i] += __shfl_xor_sync(0xffffffffu, s[i], o);
-      }
-    }
-    if (a.dx)
-#pragma unroll
-      for (int i = 0; i < kRows; ++i)
-        if (r0 + i < a.rows) {
-          Own<VEC, T> ao;
-          if (add) ao.load(add + (r0 + i) * a.ld_add, thread, TPR, cols);
-          const float p = s[2 * i] * inv_n, q = s[2 * i + 1] * inv_n;
-          float o[kOwn];
-#pragma unroll
-          for (int k = 0; k < kOwn; ++k) {
-            const float xh = (xo[i].get(k) - m[i]) * rs[i];
-            o[k] = rs[i] * (go[i].get(k) * wv[k] - p - xh * q) + (add ? ao.get(k) : 0.f);
-          }
-          go[i].set_store(o, (T*)a.dx + (r0 + i) * a.ld_dx, thread, TPR, cols);
-        }
   }
-  if (a.sums) leave_sums<T, TPR, BLOCK>(a, sw, sb, buf, blockIdx.x, 0, cols);
+  if (a.sums) leave_sums<VEC, T, TPR, BLOCK>(a, sw, sb, buf, blockIdx.x, 0, cols);
 }
 
-// Rows of more than 8192 columns: the two means of a row by a kernel of their own, then column blocks of 2048 that walk a share of the rows.
+// Rows of more than 8192 columns: the two means of a row by a kernel of their own, then blocks of columns that walk a share of the rows.
 template <class T, class W>
 __global__ void __launch_bounds__(1024) layer_norm_stats_kernel(const NormGradArgs a) {
   const T* const dy = (const T*)a.dy;
   const T* const x = (const T*)a.x;
   const W* const w = (const W*)a.w;
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+  __shared__ float part[2][64];
+  int flip = 0;
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x, flip ^= 1) {
     const float m = a.mean[r], rs = a.rstd[r];
     float s[2] = {0.f, 0.f};
     for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
       const float g = to_f(dy[r * a.ld_dy + c]) * (w ? to_f(w[c]) : 1.f);
       s[0] += g; s[1] += g * ((to_f(x[r * a.ldx + c]) - m) * rs);
     }
-    block_sum(s);
+    row_sum<1024>(s, part[flip]);
     if (threadIdx.x == 0) { a.stats[2 * r] = s[0] / a.cols; a.stats[2 * r + 1] = s[1] / a.cols; }
   }
 }
-constexpr int kLongCols = 256 * kOwn;
+template <class T> constexpr int kLongCols = 256 * kOwn<T>;
 template <class T, class W, bool VEC>
 __global__ void __launch_bounds__(256) layer_norm_grad_long_kernel(const NormGradArgs a) {
-  const int first = blockIdx.x * kLongCols, cols = min(kLongCols, a.cols - first), thread = threadIdx.x;
+  const int first = blockIdx.x * kLongCols<T>, cols = min(kLongCols<T>, a.cols - first), thread = threadIdx.x;
   const T* const dy = (const T*)a.dy + first;
   const T* const x = (const T*)a.x + first;
   const T* const add = a.add ? (const T*)a.add + first : nullptr;
   const W* const w = a.w ? (const W*)a.w + first : nullptr;
-  float wv[kOwn], sw[kOwn], sb[kOwn];
+  float wv[kOwn<T>], sw[kOwn<T>], sb[kOwn<T>];
 #pragma unroll
-  for (int k = 0; k < kOwn; ++k) {
-    const int c = own_col<T>(k, thread, 256);
+  for (int k = 0; k < kOwn<T>; ++k) {
+    const int c = own_col<VEC, T>(k, thread, 256);
     wv[k] = w && c < cols ? to_f(w[c]) : 1.f;
     sw[k] = sb[k] = 0.f;
   }
@@ -326,16 +333,16 @@ __global__ void __launch_bounds__(256) layer_norm_grad_long_kernel(const NormGra
     xo.load(x + r * a.ldx, thread, 256, cols);
     go.load(dy + r * a.ld_dy, thread, 256, cols);
     if (add) ao.load(add + r * a.ld_add, thread, 256, cols);
-    float o[kOwn];
+    float o[kOwn<T>];
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) {
+    for (int k = 0; k < kOwn<T>; ++k) {
       const float g = go.get(k), xh = (xo.get(k) - m) * rs;
       sw[k] = fmaf(g, xh, sw[k]); sb[k] += g;
       o[k] = rs * (g * wv[k] - p - xh * q) + (add ? ao.get(k) : 0.f);
     }
     if (a.dx) go.set_store(o, (T*)a.dx + first + r * a.ld_dx, thread, 256, cols);
   }
-  if (a.sums) leave_sums<T, 256, 256>(a, sw, sb, nullptr, blockIdx.y, first, cols);
+  if (a.sums) leave_sums<VEC, T, 256, 256>(a, sw, sb, nullptr, blockIdx.y, first, cols);
 }
 
 // dw, db = sums of the blocks' partial sums, in order of the blocks: 32 columns of either a block, a warp for every 32nd partial row.
@@ -358,22 +365,27 @@ __global__ void __launch_bounds__(1024) layer_norm_sums_kernel(int blocks, int c
   if (lane == 0 && out && blockIdx.x * 32 + warp < cols) out[blockIdx.x * 32 + warp] = from_f<W>(s);
 }
 
-// How a backward pass is cut: threads a row (0: long rows), and the blocks that leave partial sums.  By sizes alone: the workspace
-// and the order of the sums are the same for all types and alignments.
+// How a backward pass is cut: threads a row (0: long rows), and the blocks that leave partial sums.  By the element's size and the matrix' alone.
 struct NormGradPlan { int tpr; int64_t blocks; };
+template <class T>
 NormGradPlan norm_grad_plan(int64_t rows, int cols) {
   NormGradPlan p{0, 0};
-  for (int t = 8; t <= 1024; t *= 2)
-    if (cols <= t * kOwn) { p.tpr = t; break; }
+  for (int t = 8; t <= 8192 / kOwn<T>; t *= 2)
+    if (cols <= t * kOwn<T>) { p.tpr = t; break; }
   if (p.tpr) {
-    const int block = p.tpr > 256 ? p.tpr : 256, per = block / p.tpr * kRows;
-    const int64_t want = (rows + per - 1) / per, most = 148LL * (1024 / block);
+    const int block = p.tpr > 256 ? p.tpr : 256, per = block / p.tpr, resident = grad_threads<T> / block > 0 ? grad_threads<T> / block : 1;
+    const int64_t want = (rows + per - 1) / per, most = 148LL * resident;
     p.blocks = want < most ? want : most;
   } else {
-    const int64_t strips = (cols + kLongCols - 1) / kLongCols, most = (148 * 4 + strips - 1) / strips;
+    const int64_t strips = (cols + kLongCols<T> - 1) / kLongCols<T>, most = (148 * 4 + strips - 1) / strips;
     p.blocks = rows < most ? rows : most;
   }
   return p;
+}
+template <class T>
+int64_t norm_grad_floats(int64_t rows, int cols) {
+  const NormGradPlan p = norm_grad_plan<T>(rows, cols);
+  return p.blocks * 2 * cols + (p.tpr ? 0 : 2 * rows);
 }
 
 struct NormCall {
@@ -387,10 +399,10 @@ struct NormCall {
 
 template <class T, class W, int TPR, int NU>
 cudaError_t norm_as(const NormCall& a, bool vec) {
-  constexpr int PER = TPR > 32 ? 1 : 128 / TPR;
-  const int64_t blocks = (a.rows + PER - 1) / PER;
+  constexpr int BLOCK = norm_block<TPR>, PER = BLOCK / TPR;
+  const int64_t want = (a.rows + PER - 1) / PER, most = 148LL * norm_blocks<TPR>, blocks = want < most ? want : most;
   auto* const k = vec ? layer_norm_kernel<T, W, TPR, NU, true> : layer_norm_kernel<T, W, TPR, NU, false>;
-  return launch_pdl_grid(k, dim3((unsigned)blocks), TPR > 32 ? TPR : 128, 0, a.st, a.rows, a.cols, (const T*)a.x, a.ldx, (const W*)a.w, (const W*)a.b, a.eps,
+  return launch_pdl_grid(k, dim3((unsigned)blocks), BLOCK, 0, a.st, a.rows, a.cols, (const T*)a.x, a.ldx, (const W*)a.w, (const W*)a.b, a.eps,
                          (T*)a.y, a.ldy, a.mean, a.rstd);
 }
 template <class T, class W>
@@ -400,11 +412,11 @@ cudaError_t run_norm(const NormCall& a) {
   if (units <= 8) return norm_as<T, W, 8, 1>(a, vec);
   if (units <= 32) return norm_as<T, W, 32, 1>(a, vec);
   if (units <= 64) return norm_as<T, W, 32, 2>(a, vec);
-  if (units <= 128) return norm_as<T, W, 32, 4>(a, vec);
-  if (units <= 256) return norm_as<T, W, 32, 8>(a, vec);
-  if (units <= 512) return norm_as<T, W, 32, 16>(a, vec);
-  if (units <= 1024) return norm_as<T, W, 256, 4>(a, vec);
-  if (units <= 2048) return norm_as<T, W, 256, 8>(a, vec);
+  if (units <= 128) return norm_as<T, W, 64, 2>(a, vec);
+  if (units <= 256) return norm_as<T, W, 128, 2>(a, vec);
+  if (units <= 512) return norm_as<T, W, 256, 2>(a, vec);
+  if (units <= 1024) return norm_as<T, W, 512, 2>(a, vec);
+  if (units <= 2048) return norm_as<T, W, 1024, 2>(a, vec);
   if (units <= 4096) return norm_as<T, W, 1024, 4>(a, vec);
   const int64_t most = 148 * 2;
   layer_norm_long_kernel<T, W><<<(unsigned)(a.rows < most ? a.rows : most), 1024, 0, a.st>>>(
@@ -414,12 +426,12 @@ cudaError_t run_norm(const NormCall& a) {
 
 template <class T, class W, int TPR>
 cudaError_t norm_grad_as(const NormGradArgs& g, bool vec, int64_t blocks, cudaStream_t st) {
-  return launch_pdl_grid(vec ? layer_norm_grad_kernel<T, W, TPR, true> : layer_norm_grad_kernel<T, W, TPR, false>, dim3((unsigned)blocks),
-                         TPR > 256 ? TPR : 256, 0, st, g);
+  return launch_pdl_grid(vec ? layer_norm_grad_kernel<T, W, TPR, true> : layer_norm_grad_kernel<T, W, TPR, false>, dim3((unsigned)blocks), grad_block<TPR>, 0,
+                         st, g);
 }
 template <class T, class W>
 cudaError_t run_norm_grad(const NormCall& a) {
-  const NormGradPlan plan = norm_grad_plan(a.rows, a.cols);
+  const NormGradPlan plan = norm_grad_plan<T>(a.rows, a.cols);
   NormGradArgs g{a.rows, a.cols, a.dy, a.x, a.w, a.add, a.y, a.ld_dy, a.ldx, a.ld_add, a.ldy, a.mean, a.rstd, (float*)a.ws, nullptr, a.dw || a.db};
   const bool vec = wide_ok(a.dy, a.ld_dy, a.type) && wide_ok(a.x, a.ldx, a.type) && wide_ok(a.add, a.ld_add, a.type) && wide_ok(a.y, a.ldy, a.type);
   cudaError_t e = cudaSuccess;
@@ -432,11 +444,13 @@ cudaError_t run_norm_grad(const NormCall& a) {
       case 128: e = norm_grad_as<T, W, 128>(g, vec, plan.blocks, a.st); break;
       case 256: e = norm_grad_as<T, W, 256>(g, vec, plan.blocks, a.st); break;
       case 512: e = norm_grad_as<T, W, 512>(g, vec, plan.blocks, a.st); break;
-      case 1024: e = norm_grad_as<T, W, 1024>(g, vec, plan.blocks, a.st); break;
+      case 1024:
+        if constexpr (sizeof(T) == 4) e = norm_grad_as<T, W, 1024>(g, vec, plan.blocks, a.st);
+        break;
       default: {
         g.stats = g.part + plan.blocks * 2 * a.cols;
         if (g.dx) layer_norm_stats_kernel<T, W><<<(unsigned)(a.rows < 296 ? a.rows : 296), 1024, 0, a.st>>>(g);
-        const dim3 grid((unsigned)((a.cols + kLongCols - 1) / kLongCols), (unsigned)plan.blocks);
+        const dim3 grid((unsigned)((a.cols + kLongCols<T> - 1) / kLongCols<T>), (unsigned)plan.blocks);
         if (vec) layer_norm_grad_long_kernel<T, W, true><<<grid, 256, 0, a.st>>>(g);
         else layer_norm_grad_long_kernel<T, W, false><<<grid, 256, 0, a.st>>>(g);
         e = cudaGetLastError();
@@ -493,8 +507,8 @@ extern "C" gn_status gn_layer_norm(gn_dtype type, gn_dtype wtype, int64_t rows, 
 
 extern "C" int64_t gn_layer_norm_grad_workspace(int64_t rows, int32_t cols) {
   if (rows < 0 || cols < 1 || cols > kMaxCols) return -1;
-  const NormGradPlan p = norm_grad_plan(rows, cols);
-  return (p.blocks * 2 * cols + (p.tpr ? 0 : 2 * rows)) * 4 + 16;
+  const int64_t a = norm_grad_floats<float>(rows, cols), b = norm_grad_floats<__half>(rows, cols);
+  return (a > b ? a : b) * 4 + 16;
 }
 
 extern "C" gn_status gn_layer_norm_grad(gn_dtype type, gn_dtype wtype, int64_t rows, int32_t cols, const void* d_dy, int64_t ld_dy,

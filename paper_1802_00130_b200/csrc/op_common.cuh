@@ -42,34 +42,47 @@ struct Pack {
     w = make_uint4(o[0], o[1], o[2], o[3]);
   }
 };
-// A thread's V neighbouring elements from column c of a row; those from cols on read as zero and are not written.  VEC: 16-byte accesses
-// can be made to the row.  Where they cannot, the same thread takes the same elements one by one, so that sums keep their order, and results their
-// bits, whatever the alignment; the accesses of a warp to a line follow one another and hit in L1.
+// Column of element e of a thread's unit u of a row that `threads` threads share: neighbours where 16-byte accesses can be made to the rows (VEC), else
+// `threads` apart, so that a warp's accesses to single elements are to consecutive ones.  Elements from cols on read as zero and are not written.
 template <bool VEC, class T>
-__device__ __forceinline__ Pack<T> load_pack(const T* row, int c, int cols) {
+__device__ __forceinline__ int pack_col(int u, int e, int thread, int threads) {
+  return VEC ? (u * threads + thread) * Pack<T>::V + e : (u * Pack<T>::V + e) * threads + thread;
+}
+template <bool VEC, class T>
+__device__ __forceinline__ Pack<T> load_pack(const T* row, int u, int thread, int threads, int cols) {
   Pack<T> p{make_uint4(0u, 0u, 0u, 0u)};
-  if (VEC && c + Pack<T>::V <= cols) { p.w = *reinterpret_cast<const uint4*>(row + c); return p; }
-  if (c >= cols) return p;
+  if constexpr (VEC) {
+    const int c = pack_col<true, T>(u, 0, thread, threads);
+    if (c + Pack<T>::V <= cols) { p.w = *reinterpret_cast<const uint4*>(row + c); return p; }
+    if (c >= cols) return p;
+  }
   uint32_t o[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int e = 0; e < Pack<T>::V; ++e)
-    if (c + e < cols) {
-      if constexpr (sizeof(T) == 4) o[e] = *reinterpret_cast<const uint32_t*>(row + c + e);
-      else o[e >> 1] |= (uint32_t) * reinterpret_cast<const uint16_t*>(row + c + e) << (16 * (e & 1));
+  for (int e = 0; e < Pack<T>::V; ++e) {
+    const int c = pack_col<VEC, T>(u, e, thread, threads);
+    if (c < cols) {
+      if constexpr (sizeof(T) == 4) o[e] = *reinterpret_cast<const uint32_t*>(row + c);
+      else o[e >> 1] |= (uint32_t) * reinterpret_cast<const uint16_t*>(row + c) << (16 * (e & 1));
     }
+  }
   p.w = make_uint4(o[0], o[1], o[2], o[3]);
   return p;
 }
 template <bool VEC, class T>
-__device__ __forceinline__ void store_pack(T* row, const Pack<T>& p, int c, int cols) {
-  if (VEC && c + Pack<T>::V <= cols) { *reinterpret_cast<uint4*>(row + c) = p.w; return; }
-  if (c >= cols) return;
+__device__ __forceinline__ void store_pack(T* row, const Pack<T>& p, int u, int thread, int threads, int cols) {
+  if constexpr (VEC) {
+    const int c = pack_col<true, T>(u, 0, thread, threads);
+    if (c + Pack<T>::V <= cols) { *reinterpret_cast<uint4*>(row + c) = p.w; return; }
+    if (c >= cols) return;
+  }
 #pragma unroll
-  for (int e = 0; e < Pack<T>::V; ++e)
-    if (c + e < cols) {
-      if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(row + c + e) = p.word(e);
-      else *reinterpret_cast<uint16_t*>(row + c + e) = (uint16_t)(p.word(e >> 1) >> (16 * (e & 1)));
+  for (int e = 0; e < Pack<T>::V; ++e) {
+    const int c = pack_col<VEC, T>(u, e, thread, threads);
+    if (c < cols) {
+      if constexpr (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(row + c) = p.word(e);
+      else *reinterpret_cast<uint16_t*>(row + c) = (uint16_t)(p.word(e >> 1) >> (16 * (e & 1)));
     }
+  }
 }
 
 inline gn_status op_fail(gn_status st, const char* why, char* errbuf, int64_t errbuf_len) {

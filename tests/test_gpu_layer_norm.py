@@ -125,6 +125,8 @@ def check_grads(got, dy, x, mean, rstd, w, add, t, wt):
     b_dx = u(t) * ref[0].abs() + tiny(t) + 6 * E * rs * g + rs * rel * (g.mean(1, keepdim=True) + xh * (g * xh).mean(1, keepdim=True)) \
         + rs * (x_err * (g * xh).mean(1, keepdim=True) + xh * (g * x_err).mean(1, keepdim=True)) + 2 * E * (0 if add is None else add.double().abs())
     within(got[0], ref[0], b_dx, "dx")
+    if len(got) == 1:
+        return
     # sums over rows: every addition is off by at most E of a partial sum, in sequence over the rows of a block and then over the blocks
     terms = dy.double().abs() * xh
     acc = 7 * E * max(rows, 1) ** 0.5 + 8 * E
@@ -197,9 +199,6 @@ def test_in_place_and_what_is_left_alone(cols):
     err = C.create_string_buffer(200)
     x, dy, add = rand((rows, cols), torch.float16, 1), rand((rows, cols), torch.float16, 2), rand((rows, cols), torch.float16, 3)
     w = vec(cols, torch.float16, 4)
-    y, mean, rstd = gn.layer_norm(x, w, save=True)
-    want = gn.layer_norm_grad(dy, x, mean, rstd, w, add=add)
-
     def wide(m):
         b = torch.full((rows + 2, ld), 7.0, dtype=torch.float16, device="cuda")
         b[:rows, :cols] = m
@@ -209,19 +208,25 @@ def test_in_place_and_what_is_left_alone(cols):
         assert bool((b[rows:] == 7).all()) and bool((b[:, cols:] == 7).all())
         return b[:rows, :cols]
 
-    bx = wide(x)
-    assert gn.lib().gn_layer_norm(2, 2, rows, cols, bx.data_ptr(), ld, w.data_ptr(), None, 1e-5, bx.data_ptr(), ld, None, None,
-                                  torch.cuda.current_stream().cuda_stream, err, 200) == 0, err.value
-    assert torch.equal(kept(bx), y)
+    bx, by = wide(x), wide(torch.zeros_like(x))
+    _, mean, rstd = gn.layer_norm(bx[:rows, :cols], w, save=True)
+    for out in (by, bx):
+        assert gn.lib().gn_layer_norm(2, 2, rows, cols, bx.data_ptr(), ld, w.data_ptr(), None, 1e-5, out.data_ptr(), ld, None, None,
+                                      torch.cuda.current_stream().cuda_stream, err, 200) == 0, err.value
+    assert torch.equal(kept(bx), kept(by)) and bool(by[:rows, :cols].any())
     n = gn.lib().gn_layer_norm_grad_workspace(rows, cols)
-    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
-    for place in range(2):
-        b = [wide(dy), wide(add)]
-        assert gn.lib().gn_layer_norm_grad(2, 2, rows, cols, b[0].data_ptr(), ld, x.data_ptr(), cols, mean.data_ptr(), rstd.data_ptr(), w.data_ptr(),
+    ws = torch.full((n + 64,), 0x5A, dtype=torch.uint8, device="cuda")
+    got, bx = [], wide(x)
+    for place in (2, 0, 1):
+        b = [wide(dy), wide(add), wide(torch.zeros_like(dy))]
+        assert gn.lib().gn_layer_norm_grad(2, 2, rows, cols, b[0].data_ptr(), ld, bx.data_ptr(), ld, mean.data_ptr(), rstd.data_ptr(), w.data_ptr(),
                                            b[1].data_ptr(), ld, b[place].data_ptr(), ld, None, None, ws.data_ptr(), n,
                                            torch.cuda.current_stream().cuda_stream, err, 200) == 0, err.value
-        assert torch.equal(kept(b[place]), want[0])
-        kept(b[1 - place])
+        got.append(kept(b[place]))
+        assert all(bool((kept(b[k]) == (dy, add)[k]).all()) for k in range(2) if k != place)
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+    check_grads((got[0],), dy, x, mean, rstd, w, add, torch.float16, torch.float16)
+    assert bool((ws[n:] == 0x5A).all())
 
 
 def test_refusals():

@@ -27,4 +27,9 @@ constexpr int kFfnGroup = 4;     // problems of one launch (FFN_STORE)
 // CTA-pair kernel (gemm_pair16.cu).  Returns cudaSuccess, or what the launch or the maps failed with.
 cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, int* err, cudaStream_t st);
 
+// One product with few tokens (gemm_narrow16.cu): M <= kFfnNarrow, A K-major.  early: the kernel before it on the stream is one of these
+// kernels, of the same call, that writes none of the right operands.
+constexpr int kFfnNarrow = 128;
+cudaError_t launch_ffn_narrow(FfnKind kind, bool bf16, int act, const FfnGemm& g, bool early, int* err, cudaStream_t st);
+
 }  // namespace gn

@@ -1,7 +1,7 @@
 // Gated feed-forward block and its backward pass: the calls, their workspaces and the order of their products.
 //
 // 16-bit types: two tensor-core launches forward (both projections with the gate, then the product with Wd), two backward (dh with the
-// gate's gradient, then dx and the three weight gradients as one launch).  TMA reads the operands, so one with a base or a leading
+// gate's gradient, then dx and the three weight gradients as one launch; with few tokens dx is one of its own).  TMA reads the operands, so one with a base or a leading
 // dimension that is no multiple of 16 bytes is copied to the workspace first.
 // FP32: the FP32-accurate products of the rest of the library (gemm_f16x3.cu, gemm_ffma.cu), with the gate as a pass of its own.
 #include <math.h>
@@ -150,6 +150,11 @@ cudaError_t forward_half(const gn_ffn& f, const Half& w, int* err, cudaStream_t 
   b.M = (int)f.rows; b.N = f.cols; b.K[0] = f.inner;
   b.A[0] = in16(w.h); b.B[0] = w.w_down; b.d[0] = out16(f.y);
   cudaError_t e = pack(w, st);
+  if (f.rows <= kFfnNarrow) {
+    if (e == cudaSuccess) e = launch_ffn_narrow(FFN_GATE, bf16, f.act, a, false, err, st);
+    if (e == cudaSuccess) e = launch_ffn_narrow(FFN_STORE, bf16, f.act, b, true, err, st);
+    return e;
+  }
   if (e == cudaSuccess) e = launch_ffn_pair(FFN_GATE, bf16, f.act, &a, 1, err, st);
   if (e == cudaSuccess) e = launch_ffn_pair(FFN_STORE, bf16, f.act, &b, 1, err, st);
   return e;
@@ -180,8 +185,14 @@ cudaError_t backward_half(const gn_ffn& f, const Half& w, int* err, cudaStream_t
   weights(f.cols, f.inner, w.dy, in16(w.h), f.dw_down);
   if (n == 0) return cudaSuccess;
   cudaError_t e = pack(w, st);
-  if (e == cudaSuccess) e = launch_ffn_pair(FFN_GRAD, bf16, f.act, &a, 1, err, st);
-  if (e == cudaSuccess) e = launch_ffn_pair(FFN_STORE, bf16, f.act, list, n, err, st);
+  const bool narrow = R <= kFfnNarrow;
+  if (e == cudaSuccess) e = narrow ? launch_ffn_narrow(FFN_GRAD, bf16, f.act, a, false, err, st) : launch_ffn_pair(FFN_GRAD, bf16, f.act, &a, 1, err, st);
+  int first = 0;
+  if (narrow && f.dx.p) {
+    if (e == cudaSuccess) e = launch_ffn_narrow(FFN_STORE, bf16, f.act, list[0], true, err, st);
+    first = 1;
+  }
+  if (e == cudaSuccess && n > first) e = launch_ffn_pair(FFN_STORE, bf16, f.act, list + first, n - first, err, st);
   return e;
 }
 

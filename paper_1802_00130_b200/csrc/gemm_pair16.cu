@@ -35,6 +35,7 @@ struct PairProblem {
   int M, N, bn, tiles_m, tiles_n, tiles;
   int kb0, kb;                    // k-blocks of the first operand pair, of both
   int a_mn, b_mn, vec;            // vec: every matrix of the epilogue takes 16-byte accesses
+  int a_box3, b_box3;             // an MN-major operand of whole 64-column chunks: one box of several chunks instead of a box each
   Out16 d[3];
   Mat16 gate, up;
 };
@@ -189,6 +190,7 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
       int s = 0;
       uint32_t ph = 0;
       bool ok = true;
+      const uint32_t full_leader = map_to_cta(smem_u32(&full[0]), 0);
       for (int t = pair; ok && t < g.tiles; t += g.pairs) {
         int tm, tn;
         const int k = find_tile(g, t, tm, tn);
@@ -197,29 +199,40 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
         const int m0 = tm * 2 * P_BM + (int)rank * P_BM;
         const int n0 = KIND == FFN_GATE ? tn * hb : tn * p.bn + (int)rank * hb;
         const uint32_t pair_tx = 2u * (P_A_BYTES + (uint32_t)hb * 128u);
-        for (int kb = 0; kb < p.kb; ++kb) {
-          if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, g.err, 1)) { ok = false; break; }
-          if (rank == 0) mbar_expect_tx(&full[s], pair_tx);
-          const uint32_t bar = map_to_cta(smem_u32(&full[s]), 0);
-          const int second = kb >= p.kb0 ? 1 : 0;
-          const int k0 = (second ? kb - p.kb0 : kb) * P_BK;
-          const CUtensorMap* ma = &maps.m[k][2 * second];
-          const CUtensorMap* mb = KIND == FFN_GATE ? &maps.m[k][rank ? 3 : 1] : ma + 1;
-          uint8_t* const sa = smem + s * P_STAGE_BYTES;
-          uint8_t* const sb = sa + P_A_BYTES;
-          if (!p.a_mn) {
-            tma2_load_2d(sa, ma, k0, m0, bar);
-          } else {
-            tma2_load_2d(sa, ma, m0, k0, bar);
-            tma2_load_2d(sa + 8192, ma, m0 + 64, k0, bar);
+        const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0, a3 = p.a_box3 != 0, b3 = p.b_box3 != 0;
+        const int kb_first = p.kb0, kb_all = p.kb;
+        // (one thread issues everything: nothing is in the loop that need not be there)
+#pragma unroll 1
+        for (int part = 0; part < 2 && ok; ++part) {
+          const int end = part ? kb_all - kb_first : kb_first;
+          const CUtensorMap* const ma = &maps.m[k][2 * part];
+          const CUtensorMap* const mb = KIND == FFN_GATE ? &maps.m[k][rank ? 3 : 1] : ma + 1;
+#pragma unroll 1
+          for (int kb = 0; kb < end; ++kb) {
+            if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, g.err, 1)) { ok = false; break; }
+            if (rank == 0) mbar_expect_tx(&full[s], pair_tx);
+            const uint32_t bar = full_leader + (uint32_t)s * 8u;
+            const int k0 = kb * P_BK;
+            uint8_t* const sa = smem + s * P_STAGE_BYTES;
+            uint8_t* const sb = sa + P_A_BYTES;
+            if (!a_mn) {
+              tma2_load_2d(sa, ma, k0, m0, bar);
+            } else if (a3) {
+              tma2_load_3d(sa, ma, 0, k0, m0 >> 6, bar);
+            } else {
+              tma2_load_2d(sa, ma, m0, k0, bar);
+              tma2_load_2d(sa + 8192, ma, m0 + 64, k0, bar);
+            }
+            if (!b_mn) {
+              tma2_load_2d(sb, mb, k0, n0, bar);
+            } else if (b3) {
+              tma2_load_3d(sb, mb, 0, k0, n0 >> 6, bar);
+            } else {
+              tma2_load_2d(sb, mb, n0, k0, bar);
+              if (hb > 64) tma2_load_2d(sb + 8192, mb, n0 + 64, k0, bar);
+            }
+            if (++s == P_STAGES) { s = 0; ph ^= 1u; }
           }
-          if (!p.b_mn) {
-            tma2_load_2d(sb, mb, k0, n0, bar);
-          } else {
-            tma2_load_2d(sb, mb, n0, k0, bar);
-            if (hb > 64) tma2_load_2d(sb + 8192, mb, n0 + 64, k0, bar);
-          }
-          if (++s == P_STAGES) { s = 0; ph ^= 1u; }
         }
       }
     }
@@ -281,16 +294,7 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
           const int nc = n0 + c * 64;
           if (nc >= p.N) break;
           uint32_t w[32];
-          if (KIND == FFN_STORE) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              float v[32];
-              tmem_ld32(tq + (uint32_t)(c * 64 + h * 32), v);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) w[16 * h + i] = pack2<T>(v[2 * i], v[2 * i + 1]);
-            }
-            put_chunk(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
-          } else if (KIND == FFN_GATE) {
+          if (KIND == FFN_GATE) {
             uint32_t gw[32], uw[32];
             with_activation(g.act, [&](auto act) {
 #pragma unroll
@@ -354,6 +358,215 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
   }
 }
 
+// ---- plain products: 256 x 512 tiles ------------------------------------------------------------
+// With 256 x 256 tiles an SM's shared memory takes in 32 KB of operands and gives out 32 KB of them for every 512 cycles of its tensor core: all that
+// it can move, and the tensor core is busy 81 % of the time (8192 x 8192 x 4096).  A tile of 512 columns, two products of 256 on the same rows of
+// A, takes in 48 KB for 1024 cycles.  It fills the tensor memory, so the next tile waits until the epilogue warps have the sums: they take
+// all of theirs to registers first, rounded to the type (128 words each), let the next tile start, and store after that.
+// Tiles left over after the whole rounds of the pairs go as halves of 256 columns where those fit a single round.
+constexpr int W_STAGES = 4, W_STAGE_BYTES = 3 * P_A_BYTES, W_BN = 512;
+constexpr int W_SMEM = W_STAGES * W_STAGE_BYTES + P_EPI_WARPS * P_STG_BYTES + 1024 + 256;
+static_assert(W_SMEM <= 232448, "more shared memory than a block can have");
+
+struct WideProblem {
+  int M, N, tiles_m, tiles_n, tiles;     // tiles of 256 x 512
+  int kb0, kb, a_mn, b_mn, a_box3, b_box3, vec;
+  Out16 d;
+};
+// Work list: items 0 .. whole - 1 are tiles, then halves of the tiles from `whole` on.
+template <int NP> struct WideParams { WideProblem p[NP]; int n, pairs, whole, items; int* err; };
+
+struct WideItem { int k, m0, n0, halves; };
+template <int NP>
+__device__ __forceinline__ WideItem wide_item(const WideParams<NP>& g, int i) {
+  WideItem w;
+  const int rest = i - g.whole;
+  int t = rest < 0 ? i : g.whole + (rest >> 1);
+  w.halves = rest < 0 ? 2 : 1;
+  int k = 0;
+  if (NP > 1)
+    while (k + 1 < g.n && t >= g.p[k].tiles) t -= g.p[k++].tiles;
+  const WideProblem& p = g.p[k];
+  const int strip = t / (P_PANELS * p.tiles_n), in = t - strip * P_PANELS * p.tiles_n;
+  const int high = min(P_PANELS, p.tiles_m - strip * P_PANELS);
+  w.k = k;
+  w.m0 = (strip * P_PANELS + in % high) * 2 * P_BM;
+  w.n0 = in / high * W_BN + (rest < 0 ? 0 : (rest & 1) * P_BN);
+  if (w.n0 + P_BN >= p.N) w.halves = w.n0 < p.N ? 1 : 0;       // (a second half, or a left-over half, without columns)
+  return w;
+}
+
+template <class T, int NP>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
+ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant__ WideParams<NP> g) {
+  constexpr bool BF16 = !__is_same(T, __half);
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  uint8_t* staging = smem + W_STAGES * W_STAGE_BYTES;
+  uint64_t* full = reinterpret_cast<uint64_t*>(staging + P_EPI_WARPS * P_STG_BYTES);
+  uint64_t* empty = full + W_STAGES;
+  uint64_t* acc_full = empty + W_STAGES;
+  uint64_t* acc_empty = acc_full + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < W_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    mbar_init(acc_full, 1);
+    mbar_init(acc_empty, 2 * P_EPI_WARPS);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  grid_dep_wait();
+  grid_dep_launch();
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int s = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      const uint32_t full_leader = map_to_cta(smem_u32(&full[0]), 0);
+      for (int i = pair; ok && i < g.items; i += g.pairs) {
+        const WideItem w = wide_item(g, i);
+        if (w.halves == 0) continue;
+        const WideProblem& p = g.p[w.k];
+        const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0, a3 = p.a_box3 != 0, b3 = p.b_box3 != 0, two = w.halves == 2;
+        const int m0 = w.m0 + (int)rank * P_BM, n0 = w.n0 + (int)rank * P_BM;
+        const uint32_t pair_tx = 2u * P_A_BYTES * (1u + (uint32_t)w.halves);
+#pragma unroll 1
+        for (int part = 0; part < 2 && ok; ++part) {
+          const int end = part ? p.kb - p.kb0 : p.kb0;
+          const CUtensorMap* const ma = &maps.m[w.k][2 * part];
+          const CUtensorMap* const mb = ma + 1;
+#pragma unroll 1
+          for (int kb = 0; kb < end; ++kb) {
+            if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, g.err, 1)) { ok = false; break; }
+            if (rank == 0) mbar_expect_tx(&full[s], pair_tx);
+            const uint32_t bar = full_leader + (uint32_t)s * 8u;
+            const int k0 = kb * P_BK;
+            uint8_t* const sa = smem + s * W_STAGE_BYTES;
+            uint8_t* const sb = sa + P_A_BYTES;
+            if (!a_mn) {
+              tma2_load_2d(sa, ma, k0, m0, bar);
+            } else if (a3) {
+              tma2_load_3d(sa, ma, 0, k0, m0 >> 6, bar);
+            } else {
+              tma2_load_2d(sa, ma, m0, k0, bar);
+              tma2_load_2d(sa + 8192, ma, m0 + 64, k0, bar);
+            }
+            if (!b_mn) {
+              tma2_load_2d(sb, mb, k0, n0, bar);
+              if (two) tma2_load_2d(sb + P_A_BYTES, mb, k0, n0 + P_BN, bar);
+            } else if (b3) {
+              tma2_load_3d(sb, mb, 0, k0, n0 >> 6, bar);
+              if (two) tma2_load_3d(sb + P_A_BYTES, mb, 0, k0, (n0 + P_BN) >> 6, bar);
+            } else {
+              tma2_load_2d(sb, mb, n0, k0, bar);
+              tma2_load_2d(sb + 8192, mb, n0 + 64, k0, bar);
+              if (two) {
+                tma2_load_2d(sb + P_A_BYTES, mb, n0 + P_BN, k0, bar);
+                tma2_load_2d(sb + P_A_BYTES + 8192, mb, n0 + P_BN + 64, k0, bar);
+              }
+            }
+            if (++s == W_STAGES) { s = 0; ph ^= 1u; }
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (rank == 0 && lane == 0) {
+      const uint32_t base = smem_u32(smem);
+      int s = 0, ti = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int i = pair; ok && i < g.items; i += g.pairs) {
+        const WideItem w = wide_item(g, i);
+        if (w.halves == 0) continue;
+        const WideProblem& p = g.p[w.k];
+        const uint32_t idesc = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) |
+                               ((uint32_t)(P_BN >> 3) << 17) | ((uint32_t)((2 * P_BM) >> 4) << 24);
+        const uint64_t a_step = (p.a_mn ? 2048 : 32) >> 4, b_step = (p.b_mn ? 2048 : 32) >> 4;
+        const uint64_t a0 = make_desc(base, p.a_mn ? 8192 : 16, 1024, 2);
+        const uint64_t b0 = make_desc(base + P_A_BYTES, p.b_mn ? 8192 : 16, 1024, 2);
+        if (!wait_or_abort(acc_empty, (ti & 1) ^ 1, abort_flag, g.err, 4)) break;
+        tc_fence_after();
+        uint32_t acc = 0u;
+        const int kbs = p.kb;
+        const bool two = w.halves == 2;
+#pragma unroll 1
+        for (int kb = 0; kb < kbs; ++kb) {
+          if (!wait_or_abort(&full[s], ph, abort_flag, g.err, 2)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t ad = a0 + (uint64_t)(s * (W_STAGE_BYTES >> 4)), bd = b0 + (uint64_t)(s * (W_STAGE_BYTES >> 4));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t on = k ? 1u : acc;
+            pair_mma<BF16>(tmem_base, ad + k * a_step, bd + k * b_step, idesc, on);
+            if (two) pair_mma<BF16>(tmem_base + P_BN, ad + k * a_step, bd + (P_A_BYTES >> 4) + k * b_step, idesc, on);
+          }
+          acc = 1u;
+          mma2_commit_both(&empty[s]);
+          if (++s == W_STAGES) { s = 0; ph ^= 1u; }
+        }
+        if (ok) mma2_commit_both(acc_full);
+        ++ti;
+      }
+    }
+  } else {
+    const int quad = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t stg = smem_u32(staging + (warp - 2) * P_STG_BYTES);
+    const uint32_t acc_leader = map_to_cta(smem_u32(acc_empty), 0);
+    const uint32_t tq = tmem_base + ((uint32_t)(quad * 32) << 16);
+    int ti = 0;
+    for (int i = pair; i < g.items; i += g.pairs) {
+      const WideItem w = wide_item(g, i);
+      if (w.halves == 0) continue;
+      const WideProblem& p = g.p[w.k];
+      const int m0 = w.m0 + (int)rank * P_BM + quad * 32;
+      const int chunks = m0 < p.M ? min(4 * w.halves, (p.N - w.n0 + 63) / 64) : 0;      // of 64 columns; this warp's are half, half + 2, ...
+      int good = 1;
+      if (lane == 0) good = wait_or_abort(acc_full, ti & 1, abort_flag, g.err, 3) ? 1 : 0;
+      good = __shfl_sync(0xffffffffu, good, 0);
+      if (!good) break;
+      ++ti;
+      tc_fence_after();
+      uint32_t x[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (2 * c + half < chunks) {
+          float a[32], b[32];
+          tmem_ld32_pair(tq + (uint32_t)((2 * c + half) * 64), tq + (uint32_t)((2 * c + half) * 64 + 32), a, b);
+#pragma unroll
+          for (int q = 0; q < 16; ++q) { x[c][q] = pack2<T>(a[2 * q], a[2 * q + 1]); x[c][16 + q] = pack2<T>(b[2 * q], b[2 * q + 1]); }
+        }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster_relaxed(acc_leader);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (2 * c + half < chunks) put_chunk(x[c], stg, lane, p.d.p, p.d.ld, m0, p.M, w.n0 + (2 * c + half) * 64, p.N, p.vec);
+    }
+  }
+  tc_fence_before();
+  cluster_sync_all();      // neither CTA leaves (or frees tensor memory) while the other may still use it
+  if (warp == 2) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+  }
+}
+
 // ---- host side ---------------------------------------------------------------------------------
 // 2-D map over a row-major [rows][cols] matrix of 16-bit elements; box = 64 columns x box_r rows.
 bool make_map16(CUtensorMap* m, const Mat16& a, long long rows, long long cols, int box_r, bool bf16) {
@@ -367,7 +580,31 @@ bool make_map16(CUtensorMap* m, const Mat16& a, long long rows, long long cols, 
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// The same of a [K][MN] matrix of whole 64-column chunks: one box holds 64 rows of `chunks` chunks, chunk after chunk.
+bool make_map16_chunks(CUtensorMap* m, const Mat16& a, long long rows, long long cols, int chunks, bool bf16) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(cols / 64)};
+  cuuint64_t strides[2] = {(cuuint64_t)a.ld * 2, 128};
+  cuuint32_t box[3] = {64, 64, (cuuint32_t)chunks};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(a.p), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 template <class P> bool vec16(const P& m) { return !m.p || (((uintptr_t)m.p & 15) == 0 && m.ld % 8 == 0); }
+
+// Maps of one problem's operands: A of rows_a rows of the stored matrix (or of its columns) to a box, B likewise.
+bool encode_problem(CUtensorMap* maps, const FfnGemm& g, bool gate, bool a_box3, bool b_box3, int rows_b, bool bf16) {
+  for (int s = 0; s < 2; ++s) {
+    const int a = g.K[1] > 0 ? s : 0, b = gate ? s : a, K = g.K[a];
+    const auto encode = [&](CUtensorMap* to, const Mat16& mat, bool mn, bool box3, int MN, int rows) {
+      return !mn ? make_map16(to, mat, MN, K, rows, bf16) : box3 ? make_map16_chunks(to, mat, K, MN, rows / 64, bf16) : make_map16(to, mat, K, MN, 64, bf16);
+    };
+    if (!encode(&maps[2 * s], g.A[a], g.a_mn, a_box3, g.M, P_BM) || !encode(&maps[2 * s + 1], g.B[b], g.b_mn, b_box3, g.N, rows_b)) return false;
+  }
+  return true;
+}
 
 template <int KIND, class T, int NP>
 cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStream_t st) {
@@ -402,19 +639,47 @@ cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStrea
     p.tiles = p.tiles_m * p.tiles_n;
     p.kb0 = (g[i].K[0] + P_BK - 1) / P_BK; p.kb = p.kb0 + (g[i].K[1] + P_BK - 1) / P_BK;
     p.a_mn = g[i].a_mn; p.b_mn = g[i].b_mn;
+    p.a_box3 = p.a_mn && p.M % 64 == 0; p.b_box3 = p.b_mn && p.N % 64 == 0;
     for (int k = 0; k < 3; ++k) p.d[k] = g[i].d[k];
     p.gate = g[i].gate; p.up = g[i].up;
     p.vec = vec16(p.d[0]) && vec16(p.d[1]) && vec16(p.d[2]) && vec16(p.gate) && vec16(p.up);
-    for (int s = 0; s < 2; ++s) {
-      const int a = g[i].K[1] > 0 ? s : 0, b = KIND == FFN_GATE ? s : a, K = g[i].K[a];
-      const bool ok = (g[i].a_mn ? make_map16(&maps.m[i][2 * s], g[i].A[a], K, p.M, 64, BF16) : make_map16(&maps.m[i][2 * s], g[i].A[a], p.M, K, P_BM, BF16)) &&
-                      (g[i].b_mn ? make_map16(&maps.m[i][2 * s + 1], g[i].B[b], K, p.N, 64, BF16) : make_map16(&maps.m[i][2 * s + 1], g[i].B[b], p.N, K, bn / 2, BF16));
-      if (!ok) return cudaErrorInvalidValue;
-    }
+    if (!encode_problem(maps.m[i], g[i], KIND == FFN_GATE, p.a_box3, p.b_box3, bn / 2, BF16)) return cudaErrorInvalidValue;
   }
   q.tiles = (int)tiles;
   q.pairs = (int)(tiles < pairs ? tiles : pairs);
   return launch_pdl(kernel, 2 * q.pairs, P_THREADS, P_SMEM, st, maps, q);
+}
+
+template <class T, int NP>
+cudaError_t launch_wide_as(const FfnGemm* g, int n, int* err, cudaStream_t st) {
+  constexpr bool BF16 = !__is_same(T, __half);
+  static std::atomic<signed char> ready[64];
+  auto* const kernel = ffn_wide_kernel<T, NP>;
+  if (!once_per_device(ready, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, W_SMEM) == cudaSuccess; }))
+    return cudaErrorInvalidDevice;
+  PairMaps<NP> maps;
+  WideParams<NP> q = {};
+  q.n = n; q.err = err;
+  long long tiles = 0;
+  for (int i = 0; i < n; ++i) {
+    WideProblem& p = q.p[i];
+    p.M = g[i].M; p.N = g[i].N;
+    p.tiles_m = (p.M + 255) / 256; p.tiles_n = (p.N + W_BN - 1) / W_BN;
+    tiles += (long long)p.tiles_m * p.tiles_n;
+    if (tiles > 0x1fffffff) return cudaErrorInvalidValue;
+    p.tiles = p.tiles_m * p.tiles_n;
+    p.kb0 = (g[i].K[0] + P_BK - 1) / P_BK; p.kb = p.kb0 + (g[i].K[1] + P_BK - 1) / P_BK;
+    p.a_mn = g[i].a_mn; p.b_mn = g[i].b_mn;
+    p.a_box3 = p.a_mn && p.M % 64 == 0; p.b_box3 = p.b_mn && p.N % 64 == 0;
+    p.d = g[i].d[0];
+    p.vec = vec16(p.d);
+    if (!encode_problem(maps.m[i], g[i], false, p.a_box3, p.b_box3, P_BM, BF16)) return cudaErrorInvalidValue;
+  }
+  const int pairs = num_sms() / 2, rem = (int)(tiles % pairs);
+  q.whole = (int)(2 * rem <= pairs ? tiles - rem : tiles);
+  q.items = (int)(q.whole + 2 * (tiles - q.whole));
+  q.pairs = q.items < pairs ? q.items : pairs;
+  return launch_pdl(kernel, 2 * q.pairs, P_THREADS, W_SMEM, st, maps, q);
 }
 
 }  // namespace
@@ -422,7 +687,8 @@ cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStrea
 cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, int* err, cudaStream_t st) {
   if (kind == FFN_GATE) return bf16 ? launch_pair_as<FFN_GATE, __nv_bfloat16, 1>(act, g, n, err, st) : launch_pair_as<FFN_GATE, __half, 1>(act, g, n, err, st);
   if (kind == FFN_GRAD) return bf16 ? launch_pair_as<FFN_GRAD, __nv_bfloat16, 1>(act, g, n, err, st) : launch_pair_as<FFN_GRAD, __half, 1>(act, g, n, err, st);
-  return bf16 ? launch_pair_as<FFN_STORE, __nv_bfloat16, kFfnGroup>(act, g, n, err, st) : launch_pair_as<FFN_STORE, __half, kFfnGroup>(act, g, n, err, st);
+  if (n == 1) return bf16 ? launch_wide_as<__nv_bfloat16, 1>(g, n, err, st) : launch_wide_as<__half, 1>(g, n, err, st);
+  return bf16 ? launch_wide_as<__nv_bfloat16, kFfnGroup>(g, n, err, st) : launch_wide_as<__half, kFfnGroup>(g, n, err, st);
 }
 
 }  // namespace gn

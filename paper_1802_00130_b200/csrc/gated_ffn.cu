@@ -46,7 +46,7 @@ __global__ void gate_kernel(const Gates g) {
 }
 
 // Copies of 16-bit matrices with rows that TMA can address.
-constexpr int kPackMax = 5;
+constexpr int kPackMax = 7;
 struct PackJob { const uint16_t* src; uint16_t* dst; int64_t rows, ld, ld_out; int cols; };
 struct PackList { PackJob j[kPackMax]; };
 __global__ void pack_kernel(const PackList list) {
@@ -106,11 +106,12 @@ char* const kNowhere = reinterpret_cast<char*>(256);
 // ---- 16-bit types ------------------------------------------------------------------------------
 struct Half {
   Mat16 x, w_gate, w_up, w_down, dy;      // as TMA reads them
+  Mat16 gate, up;                         // as the gate's gradient reads them: whole groups of eight columns
   PackList packs; int n_packs; int64_t pack_units;
   Out16 h, dgate, dup;
 };
-Mat16 addressable(const gn_mat& m, int64_t rows, int cols, Workspace& ws, Half& w) {
-  if (((uintptr_t)m.p & 15) == 0 && m.ld % 8 == 0) return {m.p, m.ld};
+Mat16 addressable(const gn_mat& m, int64_t rows, int cols, Workspace& ws, Half& w, int group = 1) {
+  if (((uintptr_t)m.p & 15) == 0 && m.ld % 8 == 0 && cols % group == 0) return {m.p, m.ld};
   const int64_t ld = up8(cols);
   void* const dst = ws.take(rows * ld * 2);
   w.packs.j[w.n_packs++] = {(const uint16_t*)m.p, (uint16_t*)dst, rows, m.ld, ld, cols};
@@ -125,7 +126,11 @@ int64_t lay_out_half(const gn_ffn& f, bool backward, char* base, Half& w) {
   w.w_gate = addressable(f.w_gate, f.inner, f.cols, ws, w);
   w.w_up = addressable(f.w_up, f.inner, f.cols, ws, w);
   w.w_down = addressable(f.w_down, f.cols, f.inner, ws, w);
-  if (backward) w.dy = addressable(f.dy, f.rows, f.cols, ws, w);
+  if (backward) {
+    w.dy = addressable(f.dy, f.rows, f.cols, ws, w);
+    w.gate = addressable(f.gate, f.rows, f.inner, ws, w, 8);
+    w.up = addressable(f.up, f.rows, f.inner, ws, w, 8);
+  }
   for (Out16* o : {&w.h, &w.dgate, &w.dup}) {
     if (o != &w.h && !backward) break;
     *o = {ws.take(f.rows * ld * 2), ld};
@@ -167,7 +172,7 @@ cudaError_t backward_half(const gn_ffn& f, const Half& w, int* err, cudaStream_t
   a.M = R; a.N = f.inner; a.K[0] = f.cols; a.b_mn = true;
   a.A[0] = w.dy; a.B[0] = w.w_down;
   a.d[0] = w.h; a.d[1] = w.dgate; a.d[2] = w.dup;
-  a.gate = {f.gate.p, f.gate.ld}; a.up = {f.up.p, f.up.ld};
+  a.gate = w.gate; a.up = w.up;
   FfnGemm list[kFfnGroup];
   int n = 0;
   if (f.dx.p) {

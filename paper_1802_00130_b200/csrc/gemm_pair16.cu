@@ -4,15 +4,13 @@
 // Persistent: one pair for two SMs, tiles dealt in turn.  Warp roles in each CTA:
 //   warp 0      TMA producer: a ring of STAGES slots, each this CTA's 128 rows of A and its half of the B tile, 64 terms of K
 //   warp 1      MMA issuer (leader CTA only), one thread
-//   warps 2..9  epilogue: two warps per 32-lane quadrant of tensor memory, alternating over the tile's 64-column chunks
-// Two accumulators of 256 tensor-memory columns alternate, so a tile's epilogue runs under the next tile's products.
+//   warps 2..   epilogue, beside the next tile's products where two accumulators fit the tensor memory (256 x 256 tiles)
 //
 // FFN_GATE: the B tile is bn / 2 rows of the gate's weights, staged by the leader, and the same rows of the up projection's, staged by
 // the other CTA: one product gives both sums of bn / 2 hidden units, and a thread finds them in the same tensor-memory lane.
 //
-// A thread of the epilogue holds a row (a tensor-memory lane) of a chunk.  What goes to or comes from global memory passes a
-// staging tile of 32 rows x 128 bytes in shared memory, so that a warp's access covers whole lines: 16-byte units are permuted by the row's
-// low bits, which keeps both directions free of bank conflicts.
+// A thread of the epilogue holds a row (a tensor-memory lane) of a chunk of columns.  What goes to or comes from global memory passes a
+// staging tile in shared memory, so that a warp's access covers whole runs of its rows.
 //
 // Operand layouts are those of gemm_tf32.cu's FP16 copies: K-major rows of 128 bytes, or MN-major chunks of 64 columns x 64 rows, both
 // with the plain 128-byte swizzle.  Every wait is bounded; a role that gives up leaves a code in *err and the CTA drains.
@@ -24,10 +22,15 @@ namespace gn {
 namespace {
 
 constexpr int P_BM = 128, P_BK = 64, P_BN = 256;
-constexpr int P_STAGES = 6, P_EPI_WARPS = 8, P_THREADS = 64 + 32 * P_EPI_WARPS;
+constexpr int P_STAGES = 6;
 constexpr int P_A_BYTES = P_BM * P_BK * 2, P_STAGE_BYTES = 2 * P_A_BYTES;
-constexpr int P_STG_BYTES = 32 * 128;
-constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + P_EPI_WARPS * P_STG_BYTES + 1024 + 256;
+// Epilogue warps, and the 16-byte units of a staging row.  FFN_GRAD's time is latency: with eight warps a tile's epilogue takes longer than the next
+// tile's products (8192 x 8192 x 4096: 757 thousand cycles, 679 with sixteen, whose staging tiles hold 32 columns); FFN_GATE's is instructions (1226 and 1259).
+template <int KIND> constexpr int epi_warps = KIND == FFN_GRAD ? 16 : 8;
+template <int KIND> constexpr int epi_units = KIND == FFN_GRAD ? 4 : 8;
+template <int KIND> constexpr int pair_threads = 64 + 32 * epi_warps<KIND>;
+constexpr int P_STG_ALL = 32 * 1024;
+constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + P_STG_ALL + 1024 + 256;
 static_assert(P_SMEM <= 232448, "more shared memory than a block can have");
 constexpr int P_PANELS = 8;       // tiles are walked in strips of so many row panels: 74 tiles at a time read 8 panels of A and 9 of B
 
@@ -84,7 +87,6 @@ __device__ __forceinline__ int find_tile(const PairParams<NP>& g, int t, int& m,
   return k;
 }
 
-__device__ __forceinline__ uint32_t stg_at(uint32_t stg, int row, int unit) { return stg + (uint32_t)(row * 128 + ((unit ^ (row & 7)) << 4)); }
 __device__ __forceinline__ void sts16(uint32_t a, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -93,71 +95,89 @@ __device__ __forceinline__ uint4 lds16(uint32_t a) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
   return v;
 }
+// A warp's staging tile: 32 rows of U units of 16 bytes (8 or 4: 64 or 32 columns), a row's units permuted by the row's low bits so that neither
+// whole rows nor one unit of many rows meet in a bank.
+template <int U>
+__device__ __forceinline__ uint32_t stg_at(uint32_t stg, int row, int unit) {
+  return stg + (uint32_t)(row * 16 * U + ((unit ^ (U == 8 ? row & 7 : row >> 1 & 3)) << 4));
+}
 
-// This thread's row of a chunk, 64 elements in 32 words, to rows m0.. (of M) and columns n0.. (of N) of a matrix, by way of the staging tile.
-__device__ __forceinline__ void put_chunk(const uint32_t (&w)[32], uint32_t stg, int lane, void* base, int64_t ld, int m0, int M, int n0, int N, int vec) {
+// This thread's row of a chunk, 8 U elements in 4 U words, to rows m0.. (of M) and columns n0.. (of N) of a matrix, by way of the staging tile.
+// vec: 16 bytes an access.  Else a row's words of four bytes, from its first element that is at such a word on, one to a lane.
+template <int U>
+__device__ __forceinline__ void put_chunk(const uint32_t (&w)[4 * U], uint32_t stg, int lane, void* base, int64_t ld, int m0, int M, int n0, int N, int vec) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q) sts16(stg_at(stg, lane, q), make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]));
+  for (int q = 0; q < U; ++q) sts16(stg_at<U>(stg, lane, q), make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]));
   __syncwarp();
-  const int unit = lane & 7, n = n0 + unit * 8;
+  if (vec && n0 + 8 * U <= N) {
+    const int unit = lane % U;
 #pragma unroll
-  for (int it = 0; it < 8; ++it) {
-    const int row = it * 4 + (lane >> 3);
-    const uint4 v = lds16(stg_at(stg, row, unit));
-    if (m0 + row < M && n < N) {
-      uint16_t* const p = reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + row) * ld + n;
-      if (vec && n + 8 <= N) {
-        *reinterpret_cast<uint4*>(p) = v;
-      } else {
-        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (n + e < N) p[e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1)));
+    for (int it = 0; it < U; ++it) {
+      const int row = it * (32 / U) + lane / U;
+      const uint4 v = lds16(stg_at<U>(stg, row, unit));
+      if (m0 + row < M) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + row) * ld + n0 + unit * 8) = v;
+    }
+  } else {
+    const int rows = min(32, M - m0), cols = min(8 * U, N - n0);
+    for (int row = 0; row < rows; ++row) {
+      uint16_t* const p = reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + row) * ld + n0;
+      uint32_t v = 0;
+      if (lane < 4 * U) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(stg_at<U>(stg, row, lane >> 2) + (lane & 3) * 4u) : "memory");
+      const int odd = (int)(reinterpret_cast<uintptr_t>(p) >> 1 & 1);          // (the same for the whole warp)
+      if (odd) {
+        const uint32_t next = __shfl_down_sync(0xffffffffu, v, 1);
+        if (lane == 0) p[0] = (uint16_t)v;
+        v = v >> 16 | next << 16;
       }
+      const int e = 2 * lane + odd;
+      if (e + 1 < cols) *reinterpret_cast<uint32_t*>(p + e) = v;
+      else if (e < cols) p[e] = (uint16_t)v;
     }
   }
   __syncwarp();
 }
-// The other way: eight units of the chunk, four rows apart, as a warp's accesses cover them; then by rows.
-__device__ __forceinline__ void fetch_chunk(uint4 (&v)[8], int lane, const void* base, int64_t ld, int m0, int M, int n0, int N, int vec) {
-  const int unit = lane & 7, n = n0 + unit * 8;
+// The other way, of a matrix whose rows can be read in whole units of eight columns: four units of a chunk of 32 columns, eight rows apart, as a
+// warp's accesses cover them; then by rows.
+__device__ __forceinline__ void fetch_chunk(uint4 (&v)[4], int lane, const void* base, int64_t ld, int m0, int M, int n0, int N) {
+  const int n = n0 + (lane & 3) * 8;
 #pragma unroll
-  for (int it = 0; it < 8; ++it) {
-    const int m = m0 + it * 4 + (lane >> 3);
+  for (int it = 0; it < 4; ++it) {
+    const int m = m0 + it * 8 + (lane >> 2);
     v[it] = make_uint4(0u, 0u, 0u, 0u);
-    if (m < M && n < N) {
-      const uint16_t* const p = reinterpret_cast<const uint16_t*>(base) + (int64_t)m * ld + n;
-      if (vec && n + 8 <= N) {
-        v[it] = __ldg(reinterpret_cast<const uint4*>(p));
-      } else {
-        uint32_t x[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (n + e < N) x[e >> 1] |= (uint32_t)__ldg(p + e) << (16 * (e & 1));
-        v[it] = make_uint4(x[0], x[1], x[2], x[3]);
-      }
-    }
+    if (m < M && n < N) v[it] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(base) + (int64_t)m * ld + n));
   }
 }
-__device__ __forceinline__ void turn_chunk(const uint4 (&v)[8], uint32_t stg, int lane, uint32_t (&w)[32]) {
+__device__ __forceinline__ void turn_chunk(const uint4 (&v)[4], uint32_t stg, int lane, uint32_t (&w)[16]) {
 #pragma unroll
-  for (int it = 0; it < 8; ++it) sts16(stg_at(stg, it * 4 + (lane >> 3), lane & 7), v[it]);
+  for (int it = 0; it < 4; ++it) sts16(stg_at<4>(stg, it * 8 + (lane >> 2), lane & 3), v[it]);
   __syncwarp();
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const uint4 x = lds16(stg_at(stg, lane, q));
+  for (int q = 0; q < 4; ++q) {
+    const uint4 x = lds16(stg_at<4>(stg, lane, q));
     w[4 * q] = x.x; w[4 * q + 1] = x.y; w[4 * q + 2] = x.z; w[4 * q + 3] = x.w;
   }
   __syncwarp();
 }
+// Two times 16 columns of this warp's quadrant (lane = row), waited for in the same statement: nothing may move a value before it is there.
+__device__ __forceinline__ void tmem_ld16_pair(uint32_t a, uint32_t b, float (&x)[16], float (&y)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]), "=f"(x[8]), "=f"(x[9]),
+        "=f"(x[10]), "=f"(x[11]), "=f"(x[12]), "=f"(x[13]), "=f"(x[14]), "=f"(x[15]), "=f"(y[0]), "=f"(y[1]), "=f"(y[2]), "=f"(y[3]),
+        "=f"(y[4]), "=f"(y[5]), "=f"(y[6]), "=f"(y[7]), "=f"(y[8]), "=f"(y[9]), "=f"(y[10]), "=f"(y[11]), "=f"(y[12]), "=f"(y[13]),
+        "=f"(y[14]), "=f"(y[15])
+      : "r"(a), "r"(b) : "memory");
+}
 
 template <int KIND, class T, int NP>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads<KIND>, 1)
 ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant__ PairParams<NP> g) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* staging = smem + P_STAGES * P_STAGE_BYTES;
-  uint64_t* full = reinterpret_cast<uint64_t*>(staging + P_EPI_WARPS * P_STG_BYTES);
+  uint64_t* full = reinterpret_cast<uint64_t*>(staging + P_STG_ALL);
   uint64_t* empty = full + P_STAGES;
   uint64_t* acc_full = empty + P_STAGES;   // [2]
   uint64_t* acc_empty = acc_full + 2;      // [2]
@@ -170,7 +190,7 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < P_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 2 * P_EPI_WARPS); }
+    for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 2 * epi_warps<KIND>); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -274,80 +294,83 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
       }
     }
   } else {
-    const int quad = warp & 3, half = (warp - 2) >> 2;
-    const uint32_t stg = smem_u32(staging + (warp - 2) * P_STG_BYTES);
+    // Epilogue: a quadrant's warps take its chunks of columns in turn.
+    constexpr int U = epi_units<KIND>, COLS = 8 * U, STEP = epi_warps<KIND> / 4;
+    const int quad = warp & 3, first = (warp - 2) >> 2;
+    const uint32_t stg = smem_u32(staging + (warp - 2) * (P_STG_ALL / epi_warps<KIND>));
+    const uint32_t acc_leader = map_to_cta(smem_u32(&acc_empty[0]), 0);
     int ti = 0;
     for (int t = pair; t < g.tiles; t += g.pairs, ++ti) {
       int tm, tn;
       const PairProblem& p = g.p[find_tile(g, t, tm, tn)];
       const int width = KIND == FFN_GATE ? p.bn >> 1 : p.bn;          // columns of the result
       const int m0 = tm * 2 * P_BM + (int)rank * P_BM + quad * 32, n0 = tn * width;
+      const int chunks = m0 < p.M ? min(width / COLS, (p.N - n0 + COLS - 1) / COLS) : 0;
       const int buf = ti & 1;
+      uint4 gx[4], ux[4];                        // FFN_GRAD: the stored gate and up of a chunk, the first one's requested before its sums are there
+      if (KIND == FFN_GRAD && first < chunks) {
+        fetch_chunk(gx, lane, dep(p.gate.p), p.gate.ld, m0, p.M, n0 + first * COLS, p.N);
+        fetch_chunk(ux, lane, dep(p.up.p), p.up.ld, m0, p.M, n0 + first * COLS, p.N);
+      }
       int good = 1;
       if (lane == 0) good = wait_or_abort(&acc_full[buf], (ti >> 1) & 1, abort_flag, g.err, 3) ? 1 : 0;
       good = __shfl_sync(0xffffffffu, good, 0);
       if (!good) break;
       tc_fence_after();
       const uint32_t tq = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * P_BN);
-      if (m0 < p.M) {
-        for (int c = half; c < width / 64; c += 2) {
-          const int nc = n0 + c * 64;
-          if (nc >= p.N) break;
-          uint32_t w[32];
-          if (KIND == FFN_GATE) {
-            uint32_t gw[32], uw[32];
-            with_activation(g.act, [&](auto act) {
+      with_activation(g.act, [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+#pragma unroll 1
+        for (int c = first; c < chunks; c += STEP) {
+          const int nc = n0 + c * COLS;
+          uint32_t w[4 * U], gw[4 * U], uw[4 * U];
+          if constexpr (KIND == FFN_GATE) {
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                float gv[32], uv[32];
-                tmem_ld32_pair(tq + (uint32_t)(c * 64 + h * 32), tq + (uint32_t)(width + c * 64 + h * 32), gv, uv);
+            for (int h = 0; h < COLS / 32; ++h) {
+              float gv[32], uv[32];
+              tmem_ld32_pair(tq + (uint32_t)(c * COLS + h * 32), tq + (uint32_t)(width + c * COLS + h * 32), gv, uv);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  float a0, a1, unused;
-                  activation<decltype(act)::value, true>(gv[2 * i], a0, unused);
-                  activation<decltype(act)::value, true>(gv[2 * i + 1], a1, unused);
-                  w[16 * h + i] = pack2<T>(a0 * uv[2 * i], a1 * uv[2 * i + 1]);
-                  gw[16 * h + i] = pack2<T>(gv[2 * i], gv[2 * i + 1]);
-                  uw[16 * h + i] = pack2<T>(uv[2 * i], uv[2 * i + 1]);
-                }
+              for (int i = 0; i < 16; ++i) {
+                float a0, a1, unused;
+                activation<ACT, true>(gv[2 * i], a0, unused);
+                activation<ACT, true>(gv[2 * i + 1], a1, unused);
+                w[16 * h + i] = pack2<T>(a0 * uv[2 * i], a1 * uv[2 * i + 1]);
+                gw[16 * h + i] = pack2<T>(gv[2 * i], gv[2 * i + 1]);
+                uw[16 * h + i] = pack2<T>(uv[2 * i], uv[2 * i + 1]);
               }
-            });
-            put_chunk(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
-            if (p.d[1].p) put_chunk(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
-            if (p.d[2].p) put_chunk(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
+            }
+            put_chunk<U>(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
+            if (p.d[1].p) put_chunk<U>(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
+            if (p.d[2].p) put_chunk<U>(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
           } else {
-            uint4 gx[8], ux[8];
-            fetch_chunk(gx, lane, dep(p.gate.p), p.gate.ld, m0, p.M, nc, p.N, p.vec);
-            fetch_chunk(ux, lane, dep(p.up.p), p.up.ld, m0, p.M, nc, p.N, p.vec);
-            uint32_t gw[32], uw[32];
             turn_chunk(gx, stg, lane, gw);
             turn_chunk(ux, stg, lane, uw);
-            with_activation(g.act, [&](auto act) {
+            if (c + STEP < chunks) {
+              fetch_chunk(gx, lane, dep(p.gate.p), p.gate.ld, m0, p.M, nc + STEP * COLS, p.N);
+              fetch_chunk(ux, lane, dep(p.up.p), p.up.ld, m0, p.M, nc + STEP * COLS, p.N);
+            }
+            float va[16], vb[16];
+            tmem_ld16_pair(tq + (uint32_t)(c * COLS), tq + (uint32_t)(c * COLS + 16), va, vb);
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                float v[32];
-                tmem_ld32(tq + (uint32_t)(c * 64 + h * 32), v);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                  const float2 gt = unpack2<T>(gw[16 * h + i]), up = unpack2<T>(uw[16 * h + i]);
-                  float a0, a1, s0, s1;
-                  activation<decltype(act)::value, true>(gt.x, a0, s0);
-                  activation<decltype(act)::value, true>(gt.y, a1, s1);
-                  w[16 * h + i] = pack2<T>(a0 * up.x, a1 * up.y);
-                  gw[16 * h + i] = pack2<T>(v[2 * i] * up.x * s0, v[2 * i + 1] * up.y * s1);
-                  uw[16 * h + i] = pack2<T>(v[2 * i] * a0, v[2 * i + 1] * a1);
-                }
-              }
-            });
-            put_chunk(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
-            put_chunk(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
-            put_chunk(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
+            for (int i = 0; i < 16; ++i) {
+              const float d0 = i < 8 ? va[2 * (i & 7)] : vb[2 * (i & 7)], d1 = i < 8 ? va[2 * (i & 7) + 1] : vb[2 * (i & 7) + 1];
+              const float2 gt = unpack2<T>(gw[i]), up = unpack2<T>(uw[i]);
+              float a0, a1, s0, s1;
+              activation<ACT, true>(gt.x, a0, s0);
+              activation<ACT, true>(gt.y, a1, s1);
+              w[i] = pack2<T>(a0 * up.x, a1 * up.y);
+              gw[i] = pack2<T>(d0 * up.x * s0, d1 * up.y * s1);
+              uw[i] = pack2<T>(d0 * a0, d1 * a1);
+            }
+            put_chunk<U>(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
+            put_chunk<U>(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
+            put_chunk<U>(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
           }
         }
-      }
+      });
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&acc_empty[buf]), 0));
+      if (lane == 0) mbar_arrive_cluster_relaxed(acc_leader + (uint32_t)buf * 8u);
     }
   }
   tc_fence_before();
@@ -365,7 +388,8 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
 // all of theirs to registers first, rounded to the type (128 words each), let the next tile start, and store after that.
 // Tiles left over after the whole rounds of the pairs go as halves of 256 columns where those fit a single round.
 constexpr int W_STAGES = 4, W_STAGE_BYTES = 3 * P_A_BYTES, W_BN = 512;
-constexpr int W_SMEM = W_STAGES * W_STAGE_BYTES + P_EPI_WARPS * P_STG_BYTES + 1024 + 256;
+constexpr int W_EPI_WARPS = 8, W_THREADS = 64 + 32 * W_EPI_WARPS, W_STG_BYTES = 32 * 128;
+constexpr int W_SMEM = W_STAGES * W_STAGE_BYTES + W_EPI_WARPS * W_STG_BYTES + 1024 + 256;
 static_assert(W_SMEM <= 232448, "more shared memory than a block can have");
 
 struct WideProblem {
@@ -397,13 +421,13 @@ __device__ __forceinline__ WideItem wide_item(const WideParams<NP>& g, int i) {
 }
 
 template <class T, int NP>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
 ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant__ WideParams<NP> g) {
   constexpr bool BF16 = !__is_same(T, __half);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* staging = smem + W_STAGES * W_STAGE_BYTES;
-  uint64_t* full = reinterpret_cast<uint64_t*>(staging + P_EPI_WARPS * P_STG_BYTES);
+  uint64_t* full = reinterpret_cast<uint64_t*>(staging + W_EPI_WARPS * W_STG_BYTES);
   uint64_t* empty = full + W_STAGES;
   uint64_t* acc_full = empty + W_STAGES;
   uint64_t* acc_empty = acc_full + 1;
@@ -417,7 +441,7 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
   if (threadIdx.x == 0) {
     for (int s = 0; s < W_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     mbar_init(acc_full, 1);
-    mbar_init(acc_empty, 2 * P_EPI_WARPS);
+    mbar_init(acc_empty, 2 * W_EPI_WARPS);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -526,7 +550,7 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
     }
   } else {
     const int quad = warp & 3, half = (warp - 2) >> 2;
-    const uint32_t stg = smem_u32(staging + (warp - 2) * P_STG_BYTES);
+    const uint32_t stg = smem_u32(staging + (warp - 2) * W_STG_BYTES);
     const uint32_t acc_leader = map_to_cta(smem_u32(acc_empty), 0);
     const uint32_t tq = tmem_base + ((uint32_t)(quad * 32) << 16);
     int ti = 0;
@@ -556,7 +580,7 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
       if (lane == 0) mbar_arrive_cluster_relaxed(acc_leader);
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-        if (2 * c + half < chunks) put_chunk(x[c], stg, lane, p.d.p, p.d.ld, m0, p.M, w.n0 + (2 * c + half) * 64, p.N, p.vec);
+        if (2 * c + half < chunks) put_chunk<8>(x[c], stg, lane, p.d.p, p.d.ld, m0, p.M, w.n0 + (2 * c + half) * 64, p.N, p.vec);
     }
   }
   tc_fence_before();
@@ -642,12 +666,12 @@ cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStrea
     p.a_box3 = p.a_mn && p.M % 64 == 0; p.b_box3 = p.b_mn && p.N % 64 == 0;
     for (int k = 0; k < 3; ++k) p.d[k] = g[i].d[k];
     p.gate = g[i].gate; p.up = g[i].up;
-    p.vec = vec16(p.d[0]) && vec16(p.d[1]) && vec16(p.d[2]) && vec16(p.gate) && vec16(p.up);
+    p.vec = vec16(p.d[0]) && vec16(p.d[1]) && vec16(p.d[2]);
     if (!encode_problem(maps.m[i], g[i], KIND == FFN_GATE, p.a_box3, p.b_box3, bn / 2, BF16)) return cudaErrorInvalidValue;
   }
   q.tiles = (int)tiles;
   q.pairs = (int)(tiles < pairs ? tiles : pairs);
-  return launch_pdl(kernel, 2 * q.pairs, P_THREADS, P_SMEM, st, maps, q);
+  return launch_pdl(kernel, 2 * q.pairs, pair_threads<KIND>, P_SMEM, st, maps, q);
 }
 
 template <class T, int NP>
@@ -679,7 +703,7 @@ cudaError_t launch_wide_as(const FfnGemm* g, int n, int* err, cudaStream_t st) {
   q.whole = (int)(2 * rem <= pairs ? tiles - rem : tiles);
   q.items = (int)(q.whole + 2 * (tiles - q.whole));
   q.pairs = q.items < pairs ? q.items : pairs;
-  return launch_pdl(kernel, 2 * q.pairs, P_THREADS, W_SMEM, st, maps, q);
+  return launch_pdl(kernel, 2 * q.pairs, W_THREADS, W_SMEM, st, maps, q);
 }
 
 }  // namespace

@@ -7,9 +7,11 @@
 // another cluster).  Roles: warp 0 TMA producer, warp 1 MMA issuer, warps 2..5 move the sums from tensor memory to shared memory; then every
 // warp takes tokens of the epilogue.
 //
-// The second product of a call reads weights that the first has not written, and that nothing before the first can still be writing (the
-// first has waited for it before it let this one start): its first slots' weights are requested before it waits for the first.
-// Half of an SM's shared memory at most, so that they are in flight while the first product's CTAs finish.
+// The second product of a call reads weights that the first does not write, and that nothing before the first can still be writing (the
+// first has waited for it before it let this one start): its first slots are filled before it waits for the first.
+// Half of an SM's shared memory to a CTA: with a third (more of the next kernel's CTAs find room early) one token took 38.1 us instead of 37.2 (4096 x
+// 8192 bf16), and weights brought to L2 before the wait cost more than they hid (40.7).
+// Bound by the weights' bytes, 5.4 TB/s there, and by 8 us of two dependent launches: 48 tokens, 2048 x 8192 fp16, 28.5 us, of which the stream is 15.
 #include "ffn_act.cuh"
 #include "ffn_kernels.h"
 #include "tc_common.cuh"
@@ -21,11 +23,13 @@ constexpr int N_BM = 128, N_BK = 64, N_WARPS = 6, N_THREADS = 32 * N_WARPS;
 constexpr int N_A_BYTES = N_BM * N_BK * 2;
 constexpr int N_RING_BYTES = 108 * 1024;        // of stages: two CTAs on an SM
 constexpr int N_STAGES_MAX = 8;
+constexpr int N_SLICES = 8;                     // CTAs of a cluster at most
 
 struct NarrowParams {
   int tokens, features;              // of the result: d[0] [tokens][features]
   int n_pad, stages, cols_tmem;
   int kb0, kb;                       // k-blocks of the first operand pair, of both
+  // early: the weights may be loaded before the kernel before this one is done
   int a_mn, act, early, vec;         // vec: every matrix of the epilogue takes accesses to four (FFN_GATE: two) elements
   Out16 d[3];
   Mat16 gate, up;
@@ -110,7 +114,7 @@ __global__ void __launch_bounds__(N_THREADS, 2) ffn_narrow_kernel(const __grid_c
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  if (warp != 0 || !p.early) {
+  if (warp != 0) {
     grid_dep_wait();
     grid_dep_launch();
   }
@@ -139,7 +143,8 @@ __global__ void __launch_bounds__(N_THREADS, 2) ffn_narrow_kernel(const __grid_c
         mbar_expect_tx(&full[i], (uint32_t)stage_bytes);
         weights(kb0 + i, i);
       }
-      if (p.early) grid_dep_wait();
+      grid_dep_wait();
+      grid_dep_launch();
       for (int i = 0; i < head; ++i) tokens(kb0 + i, i);
       int s = head == p.stages ? 0 : head;
       uint32_t ph = head == p.stages ? 1u : 0u;
@@ -193,19 +198,38 @@ __global__ void __launch_bounds__(N_THREADS, 2) ffn_narrow_kernel(const __grid_c
   tc_fence_before();
   cluster_sync_all();                // every CTA's partial sums are in its shared memory
 
-  const uint32_t base = smem_u32(sums);
+  // Tokens rank, rank + slices, ... are this CTA's, dealt to its warps; a token's sums are requested while the one before it is computed.
+  constexpr int EACH = KIND == FFN_GATE ? 2 : 4;                 // columns of a thread
+  const uint32_t mine = smem_u32(sums) + (uint32_t)(EACH * lane) * 4;
+  const int first = (int)rank + (int)slices * warp, step = (int)slices * N_WARPS;
+  float4 v[N_SLICES];                                            // FFN_GATE: two sums of the gate, two of the up projection
+  const auto request = [&](int t) {
+#pragma unroll
+    for (uint32_t q = 0; q < N_SLICES; ++q) {
+      v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (q < slices) {
+        const uint32_t at = map_to_cta(mine + (uint32_t)t * (N_BM * 4), q);
+        if constexpr (KIND == FFN_GATE) {
+          const float2 a = lds_cluster8(at), b = lds_cluster8(at + 256);
+          v[q] = make_float4(a.x, a.y, b.x, b.y);
+        } else {
+          v[q] = lds_cluster16(at);
+        }
+      }
+    }
+  };
+  if (first < p.tokens) request(first);
   with_activation(p.act, [&](auto act) {
     constexpr int ACT = decltype(act)::value;
-    for (int t = (int)rank + (int)slices * warp; t < p.tokens; t += (int)slices * N_WARPS) {
+    for (int t = first; t < p.tokens; t += step) {
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (uint32_t q = 0; q < N_SLICES; ++q) { x[0] += v[q].x; x[1] += v[q].y; x[2] += v[q].z; x[3] += v[q].w; }
+      if (t + step < p.tokens) request(t + step);
+      const int f = f0 + EACH * lane;
+      if (f >= p.features) continue;
       if constexpr (KIND == FFN_GATE) {
-        const int f = f0 + 2 * lane;
-        float g[2] = {0.f, 0.f}, u[2] = {0.f, 0.f}, h[2];
-        for (uint32_t q = 0; q < slices; ++q) {
-          const uint32_t at = map_to_cta(base + (uint32_t)(t * N_BM + 2 * lane) * 4, q);
-          const float2 a = lds_cluster8(at), b = lds_cluster8(at + 256);
-          g[0] += a.x; g[1] += a.y; u[0] += b.x; u[1] += b.y;
-        }
-        if (f >= p.features) continue;
+        float g[2] = {x[0], x[1]}, u[2] = {x[2], x[3]}, h[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           float a, unused;
@@ -215,30 +239,21 @@ __global__ void __launch_bounds__(N_THREADS, 2) ffn_narrow_kernel(const __grid_c
         put<T>(p.d[0], t, f, p.features, p.vec, h);
         if (p.d[1].p) put<T>(p.d[1], t, f, p.features, p.vec, g);
         if (p.d[2].p) put<T>(p.d[2], t, f, p.features, p.vec, u);
+      } else if constexpr (KIND == FFN_STORE) {
+        put<T>(p.d[0], t, f, p.features, p.vec, x);
       } else {
-        const int f = f0 + 4 * lane;
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-        for (uint32_t q = 0; q < slices; ++q) {
-          const float4 a = lds_cluster16(map_to_cta(base + (uint32_t)(t * N_BM + 4 * lane) * 4, q));
-          x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
-        }
-        if (f >= p.features) continue;
-        if constexpr (KIND == FFN_STORE) {
-          put<T>(p.d[0], t, f, p.features, p.vec, x);
-        } else {
-          float g[4], u[4], h[4], dg[4], du[4];
-          get4<T>(p.gate, t, f, p.features, p.vec, g);
-          get4<T>(p.up, t, f, p.features, p.vec, u);
+        float g[4], u[4], h[4], dg[4], du[4];
+        get4<T>(p.gate, t, f, p.features, p.vec, g);
+        get4<T>(p.up, t, f, p.features, p.vec, u);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float a, da;
-            activation<ACT, true>(g[e], a, da);
-            h[e] = a * u[e]; dg[e] = x[e] * u[e] * da; du[e] = x[e] * a;
-          }
-          put<T>(p.d[0], t, f, p.features, p.vec, h);
-          put<T>(p.d[1], t, f, p.features, p.vec, dg);
-          put<T>(p.d[2], t, f, p.features, p.vec, du);
+        for (int e = 0; e < 4; ++e) {
+          float a, da;
+          activation<ACT, true>(g[e], a, da);
+          h[e] = a * u[e]; dg[e] = x[e] * u[e] * da; du[e] = x[e] * a;
         }
+        put<T>(p.d[0], t, f, p.features, p.vec, h);
+        put<T>(p.d[1], t, f, p.features, p.vec, dg);
+        put<T>(p.d[2], t, f, p.features, p.vec, du);
       }
     }
   });
@@ -268,8 +283,7 @@ cudaError_t launch_narrow_as(int act, const FfnGemm& g, bool early, int* err, cu
   constexpr int WIDTH = KIND == FFN_GATE ? 64 : 128, EACH = KIND == FFN_GATE ? 2 : 4;
   static std::atomic<signed char> ready[64];
   auto* const kernel = ffn_narrow_kernel<KIND, T>;
-  constexpr int kSmem = N_RING_BYTES + 1024;
-  if (!once_per_device(ready, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) == cudaSuccess; }))
+  if (!once_per_device(ready, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, N_RING_BYTES + 1024) == cudaSuccess; }))
     return cudaErrorInvalidDevice;
   NarrowMaps maps;
   NarrowParams p = {};
@@ -286,20 +300,20 @@ cudaError_t launch_narrow_as(int act, const FfnGemm& g, bool early, int* err, cu
   const auto wide = [&](const void* q, int64_t ld) { return !q || (((uintptr_t)q & (2 * EACH - 1)) == 0 && ld % EACH == 0); };
   for (const Out16& o : g.d) p.vec &= wide(o.p, o.ld);
   p.vec &= wide(g.gate.p, g.gate.ld) && wide(g.up.p, g.up.ld);
-  for (int s = 0; s < 2; ++s) {
-    const int a = g.K[1] > 0 ? s : 0, w = KIND == FFN_GATE ? s : a, K = g.K[a];
-    if (!(g.b_mn ? make_map16(&maps.m[2 * s], g.B[w], K, g.N, 64, BF16) : make_map16(&maps.m[2 * s], g.B[w], g.N, K, WIDTH, BF16)) ||
-        !make_map16(&maps.m[2 * s + 1], g.A[a], g.M, K, p.n_pad, BF16))
+  for (int s = 0; s < (KIND == FFN_GATE || g.K[1] > 0 ? 2 : 1); ++s) {
+    const int a = KIND == FFN_GATE ? 0 : s, K = g.K[a];
+    if (!(g.b_mn ? make_map16(&maps.m[2 * s], g.B[s], K, g.N, 64, BF16) : make_map16(&maps.m[2 * s], g.B[s], g.N, K, WIDTH, BF16)) ||
+        !(KIND == FFN_GATE && s ? true : make_map16(&maps.m[2 * s + 1], g.A[a], g.M, K, p.n_pad, BF16)))
       return cudaErrorInvalidValue;
   }
   // CTAs to a tile: as many as still find an SM of their own (two of them share one at most), with four k-blocks each at least
   const int tiles = (g.N + WIDTH - 1) / WIDTH;
   int slices = 1;
-  while (slices < 8 && tiles * slices * 2 <= 2 * num_sms() && p.kb >= slices * 2 * 4) slices *= 2;
+  while (slices < N_SLICES && tiles * slices * 2 <= 2 * num_sms() && p.kb >= slices * 2 * 4) slices *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * slices));
   cfg.blockDim = dim3(N_THREADS);
-  cfg.dynamicSmemBytes = kSmem;
+  cfg.dynamicSmemBytes = N_RING_BYTES + 1024;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

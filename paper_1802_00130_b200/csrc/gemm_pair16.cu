@@ -618,14 +618,14 @@ bool make_map16_chunks(CUtensorMap* m, const Mat16& a, long long rows, long long
 }
 template <class P> bool vec16(const P& m) { return !m.p || (((uintptr_t)m.p & 15) == 0 && m.ld % 8 == 0); }
 
-// Maps of one problem's operands: A of rows_a rows of the stored matrix (or of its columns) to a box, B likewise.
+// Maps of one problem's operands, those that it has.
 bool encode_problem(CUtensorMap* maps, const FfnGemm& g, bool gate, bool a_box3, bool b_box3, int rows_b, bool bf16) {
-  for (int s = 0; s < 2; ++s) {
-    const int a = g.K[1] > 0 ? s : 0, b = gate ? s : a, K = g.K[a];
+  for (int s = 0; s < (gate || g.K[1] > 0 ? 2 : 1); ++s) {
+    const int a = gate ? 0 : s, b = s, K = g.K[a];
     const auto encode = [&](CUtensorMap* to, const Mat16& mat, bool mn, bool box3, int MN, int rows) {
       return !mn ? make_map16(to, mat, MN, K, rows, bf16) : box3 ? make_map16_chunks(to, mat, K, MN, rows / 64, bf16) : make_map16(to, mat, K, MN, 64, bf16);
     };
-    if (!encode(&maps[2 * s], g.A[a], g.a_mn, a_box3, g.M, P_BM) || !encode(&maps[2 * s + 1], g.B[b], g.b_mn, b_box3, g.N, rows_b)) return false;
+    if ((gate && s ? false : !encode(&maps[2 * s], g.A[a], g.a_mn, a_box3, g.M, P_BM)) || !encode(&maps[2 * s + 1], g.B[b], g.b_mn, b_box3, g.N, rows_b)) return false;
   }
   return true;
 }

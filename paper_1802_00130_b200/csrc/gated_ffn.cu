@@ -29,20 +29,42 @@ int* error_word() {
   return static_cast<int*>(p);
 }
 
-// h = act(gate) * up, and with dh the two gradients, in FP32.
+// h = act(gate) * up, and with dh the two gradients, in FP32: a thread takes four columns, 64 threads neighbouring ones, a block four rows at a time.
 struct Gates { int64_t rows; int cols, act; const float *gate, *up; int64_t ld_gate, ld_up; const float* dh; float *h, *dgate, *dup; int64_t ld; };
-__global__ void gate_kernel(const Gates g) {
-  const int64_t n = g.rows * g.cols;
+template <bool VEC>
+__global__ void __launch_bounds__(256) gate_kernel(const Gates g) {
+  const int unit = blockIdx.x * 64 + threadIdx.x, units = (g.cols + 3) / 4;
+  if (unit >= units) return;
   with_activation(g.act, [&](auto act) {
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
-      const int64_t r = i / g.cols, c = i % g.cols, o = r * g.ld + c;
-      float a, da;
-      const float u = g.up[r * g.ld_up + c];
-      activation<decltype(act)::value, false>(g.gate[r * g.ld_gate + c], a, da);
-      g.h[o] = a * u;
-      if (g.dh) { g.dup[o] = g.dh[o] * a; g.dgate[o] = g.dh[o] * u * da; }
+    for (int64_t r = (int64_t)blockIdx.y * 4 + threadIdx.y; r < g.rows; r += (int64_t)gridDim.y * 4) {
+      const auto get = [&](const float* p, int64_t ld) { return load_pack<VEC>(p + r * ld, 0, unit, units, g.cols); };
+      const Pack<float> gate = get(g.gate, g.ld_gate), up = get(g.up, g.ld_up);
+      Pack<float> dh = {};
+      if (g.dh) dh = get(g.dh, g.ld);
+      float h[4], dg[4], du[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float a, da;
+        activation<decltype(act)::value, false>(gate.get(e), a, da);
+        h[e] = a * up.get(e); du[e] = dh.get(e) * a; dg[e] = dh.get(e) * up.get(e) * da;
+      }
+      const auto put = [&](const float (&x)[4], float* p) {
+        Pack<float> o;
+        o.set(x);
+        store_pack<VEC>(p + r * g.ld, o, 0, unit, units, g.cols);
+      };
+      put(h, g.h);
+      if (g.dh) { put(dg, g.dgate); put(du, g.dup); }
     }
   });
+}
+cudaError_t launch_gate(const Gates& g, cudaStream_t st) {
+  const int64_t groups = (g.rows + 3) / 4;
+  const unsigned gx = (unsigned)((g.cols + 255) / 256), most = 148 * 8 / gx + 1;
+  const dim3 grid(gx, (unsigned)(groups < most ? groups : most)), block(64, 4);
+  if (wide_ok(g.gate, g.ld_gate, GN_F32) && wide_ok(g.up, g.ld_up, GN_F32)) gate_kernel<true><<<grid, block, 0, st>>>(g);
+  else gate_kernel<false><<<grid, block, 0, st>>>(g);
+  return cudaGetLastError();
 }
 
 // Copies of 16-bit matrices with rows that TMA can address.
@@ -202,7 +224,17 @@ cudaError_t backward_half(const gn_ffn& f, const Half& w, int* err, cudaStream_t
 }
 
 // ---- FP32 --------------------------------------------------------------------------------------
-struct Single { float *gate, *up, *h, *dgate, *dup, *dh; int64_t ld; char* parts; int64_t parts_bytes; float* sums; };
+struct Stored { const float* p; int64_t rows; int cols; int64_t ld; };
+// The two FP16 parts of a call's operands, each split once however many products read it: what the caller gives in one launch at the start (phase
+// 0), what the gate has written in one after it.
+struct Parts {
+  int n;
+  Stored m[8];
+  int phase[8];
+  SplitJob job[8];
+  SplitOperand op[8];
+};
+struct Single { float *gate, *up, *h, *dgate, *dup, *dh; int64_t ld; Parts parts; float* sums; };
 
 // Whether the tensor-core form is the faster way to FP32 accuracy (the rule of the contexts' contractions, see gn_context.cu).
 bool on_tensor_cores(const GemmArgs& g) {
@@ -212,8 +244,8 @@ bool on_tensor_cores(const GemmArgs& g) {
   const double fma_us = 10.0 + (blocks <= 148.0 ? 1.0 : blocks / 148.0) * K * 0.12;
   return gemm_f16x3_estimate_us(g) + 14.0 + (g.M + (double)g.N) * K * 8.0 / 4.0e6 * 0.5 < fma_us;
 }
-struct Stored { const float* p; int64_t rows; int cols; int64_t ld; };
-// The products of a call, one after another: their operands as stored, and what they need of the workspace.
+
+// One product: its operands as stored.
 GemmArgs product(int64_t M, int64_t N, const Stored& A, bool a_k, const Stored& B, bool b_k, float* D, int64_t ldd) {
   GemmArgs g;
   g.M = (int)M; g.N = (int)N;
@@ -222,47 +254,20 @@ GemmArgs product(int64_t M, int64_t N, const Stored& A, bool a_k, const Stored& 
   g.chunk_kb = M > 128 && N >= 128 ? 2 : 1;
   return g;
 }
-Stored stored_a(const GemmArgs& g, int s) {
-  const float* p = s ? g.A2 : g.A1; const int K = s ? g.K2 : g.K1; const int64_t ld = s ? g.lda2 : g.lda1;
-  return g.a_kmajor ? Stored{p, g.M, K, ld} : Stored{p, K, g.M, ld};
-}
-Stored stored_b(const GemmArgs& g, int s) {
-  const float* p = s ? g.B2 : g.B1; const int K = s ? g.K2 : g.K1; const int64_t ld = s ? g.ldb2 : g.ldb1;
+// Operand k of A1, B1, A2, B2.
+Stored stored(const GemmArgs& g, int k) {
+  const int s = k / 2, K = s ? g.K2 : g.K1;
+  if (k % 2 == 0) {
+    const float* p = s ? g.A2 : g.A1; const int64_t ld = s ? g.lda2 : g.lda1;
+    return g.a_kmajor ? Stored{p, g.M, K, ld} : Stored{p, K, g.M, ld};
+  }
+  const float* p = s ? g.B2 : g.B1; const int64_t ld = s ? g.ldb2 : g.ldb1;
   return g.b_kmajor ? Stored{p, g.N, K, ld} : Stored{p, K, g.N, ld};
 }
-// Where the two FP16 parts of a product's operands, and their cells' exponents, go: counted and laid out by the same lines.
-int place_parts(const GemmArgs& g, Workspace& ws, SplitJob (&jobs)[4], SplitOperand (&ops)[4]) {
-  const int n = g.A2 ? 4 : 2;
-  for (int k = 0; k < n; ++k) {
-    const Stored m = k % 2 ? stored_b(g, k / 2) : stored_a(g, k / 2);
-    const int64_t ld = up8(m.cols), cells = (m.rows + 127) / 128 * ((m.cols + 127) / 128);
-    jobs[k] = {m.p, m.rows, m.cols, m.ld, ws.take(m.rows * ld * 2), ws.take(m.rows * ld * 2), ld, (int8_t*)ws.take(cells)};
-    ops[k].hi = jobs[k].hi; ops[k].lo = jobs[k].lo; ops[k].ld = ld; ops[k].cells = jobs[k].cells; ops[k].cells_ld = (m.cols + 127) / 128;
-  }
-  return n;
-}
-// What one product needs for the parts of its operands, and for the sums of K slices.
-void product_needs(const GemmArgs& g, int64_t& parts, int64_t& sums) {
-  Workspace ws{kNowhere};
-  SplitJob jobs[4];
-  SplitOperand ops[4];
-  place_parts(g, ws, jobs, ops);
-  parts = ws.used > parts ? ws.used : parts;
-  const int64_t w = gemm_f16x3_workspace_floats(g) * 4;
-  sums = w > sums ? w : sums;
-}
-cudaError_t run_product(const GemmArgs& g, const Single& w, int* err, cudaStream_t st) {
-  if (g.M < 1 || g.N < 1) return cudaSuccess;
-  if (!on_tensor_cores(g)) { launch_gemm_ffma(g, st); return cudaGetLastError(); }
-  Workspace ws{w.parts};
-  SplitJob jobs[4];
-  SplitOperand ops[4];
-  const int n = place_parts(g, ws, jobs, ops);
-  if (launch_split_f16(jobs, n, st) < 0 || launch_gemm_f16x3(g, ops, w.sums, err, st) < 0) {
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? cudaErrorInvalidValue : e;
-  }
-  return cudaSuccess;
+int find_parts(const Parts& t, const Stored& m) {
+  for (int i = 0; i < t.n; ++i)
+    if (t.m[i].p == m.p && t.m[i].rows == m.rows && t.m[i].cols == m.cols && t.m[i].ld == m.ld) return i;
+  return -1;
 }
 
 struct SingleCall { GemmArgs g[6]; int n, gate_after; };   // products, the gate's pass after the first gate_after of them
@@ -304,24 +309,54 @@ int64_t lay_out_single(const gn_ffn& f, bool backward, char* base, Single& w) {
     w.up = f.up.p ? (float*)f.up.p : (float*)ws.take(hidden);
   }
   const SingleCall c = single_products(f, backward, w);
-  int64_t parts = 0, sums = 0;
-  for (int i = 0; i < c.n; ++i)
-    if (c.g[i].M > 0 && c.g[i].K1 > 0) product_needs(c.g[i], parts, sums);
-  w.parts = (char*)ws.take(parts);
+  int64_t sums = 0;
+  Parts& t = w.parts;
+  for (int i = 0; i < c.n && f.rows > 0; ++i) {
+    const GemmArgs& g = c.g[i];
+    if (!on_tensor_cores(g)) continue;
+    const int64_t b = gemm_f16x3_workspace_floats(g) * 4;
+    sums = b > sums ? b : sums;
+    for (int k = 0; k < (g.A2 ? 4 : 2); ++k) {
+      const Stored m = stored(g, k);
+      if (find_parts(t, m) >= 0) continue;
+      const int64_t ld = up8(m.cols), cells = (m.rows + 127) / 128 * ((m.cols + 127) / 128);
+      t.m[t.n] = m;
+      t.phase[t.n] = m.p == w.h || m.p == w.dgate || m.p == w.dup;
+      t.job[t.n] = {m.p, m.rows, m.cols, m.ld, ws.take(m.rows * ld * 2), ws.take(m.rows * ld * 2), ld, (int8_t*)ws.take(cells)};
+      SplitOperand& o = t.op[t.n];
+      o.hi = t.job[t.n].hi; o.lo = t.job[t.n].lo; o.ld = ld; o.cells = t.job[t.n].cells; o.cells_ld = (m.cols + 127) / 128;
+      ++t.n;
+    }
+  }
   w.sums = (float*)ws.take(sums);
   return ws.used;
+}
+cudaError_t own_error() {             // what a launch of the library's that says -1 has left
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? cudaErrorInvalidValue : e;
+}
+cudaError_t split_phase(const Parts& t, int phase, cudaStream_t st) {
+  SplitJob jobs[8];
+  int n = 0;
+  for (int i = 0; i < t.n; ++i)
+    if (t.phase[i] == phase) jobs[n++] = t.job[i];
+  return n > 0 && launch_split_f16(jobs, n, st) < 0 ? own_error() : cudaSuccess;
+}
+cudaError_t run_product(const GemmArgs& g, const Single& w, int* err, cudaStream_t st) {
+  if (!on_tensor_cores(g)) { launch_gemm_ffma(g, st); return cudaGetLastError(); }
+  SplitOperand ops[4];
+  for (int k = 0; k < (g.A2 ? 4 : 2); ++k) ops[k] = w.parts.op[find_parts(w.parts, stored(g, k))];
+  return launch_gemm_f16x3(g, ops, w.sums, err, st) < 0 ? own_error() : cudaSuccess;
 }
 cudaError_t run_single(const gn_ffn& f, bool backward, const Single& w, int* err, cudaStream_t st) {
   const SingleCall c = single_products(f, backward, w);
   if (backward && c.n == 1) return cudaSuccess;
-  cudaError_t e = cudaSuccess;
+  cudaError_t e = split_phase(w.parts, 0, st);
   for (int i = 0; i < c.n && e == cudaSuccess; ++i) {
     if (i == c.gate_after) {
-      const Gates g = backward ? Gates{f.rows, f.inner, f.act, (const float*)f.gate.p, (const float*)f.up.p, f.gate.ld, f.up.ld, w.dh, w.h, w.dgate, w.dup, w.ld}
-                               : Gates{f.rows, f.inner, f.act, w.gate, w.up, f.gate.p ? f.gate.ld : w.ld, f.up.p ? f.up.ld : w.ld, nullptr, w.h, nullptr, nullptr, w.ld};
-      const int64_t blocks = (f.rows * f.inner + 255) / 256;
-      gate_kernel<<<(unsigned)(blocks < 1184 ? blocks : 1184), 256, 0, st>>>(g);
-      e = cudaGetLastError();
+      e = launch_gate(backward ? Gates{f.rows, f.inner, f.act, (const float*)f.gate.p, (const float*)f.up.p, f.gate.ld, f.up.ld, w.dh, w.h, w.dgate, w.dup, w.ld}
+                               : Gates{f.rows, f.inner, f.act, w.gate, w.up, f.gate.p ? f.gate.ld : w.ld, f.up.p ? f.up.ld : w.ld, nullptr, w.h, nullptr, nullptr, w.ld}, st);
+      if (e == cudaSuccess) e = split_phase(w.parts, 1, st);
     }
     if (e == cudaSuccess) e = run_product(c.g[i], w, err, st);
   }

@@ -102,37 +102,64 @@ __device__ __forceinline__ uint32_t stg_at(uint32_t stg, int row, int unit) {
   return stg + (uint32_t)(row * 16 * U + ((unit ^ (U == 8 ? row & 7 : row >> 1 & 3)) << 4));
 }
 
-// This thread's row of a chunk, 8 U elements in 4 U words, to rows m0.. (of M) and columns n0.. (of N) of a matrix, by way of the staging tile.
-// vec: 16 bytes an access.  Else a row's words of four bytes, from its first element that is at such a word on, one to a lane.
-template <int U>
+// This thread's row of a chunk, 8 U elements in 4 U words, to rows m0.. (of M) and columns n0.. (of N) of a matrix, by way of the staging tile, ROWS rows at
+// a time.  vec: 16 bytes an access.  Else a row's words of four bytes, from its first element that is at such a word on, one to a lane.
+template <int U, int ROWS>
 __device__ __forceinline__ void put_chunk(const uint32_t (&w)[4 * U], uint32_t stg, int lane, void* base, int64_t ld, int m0, int M, int n0, int N, int vec) {
+  const bool whole = vec && n0 + 8 * U <= N;
+  const int cols = min(8 * U, N - n0);
 #pragma unroll
-  for (int q = 0; q < U; ++q) sts16(stg_at<U>(stg, lane, q), make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]));
-  __syncwarp();
-  if (vec && n0 + 8 * U <= N) {
-    const int unit = lane % U;
+  for (int r0 = 0; r0 < 32; r0 += ROWS) {
+    if (ROWS == 32 || lane / ROWS == r0 / ROWS) {
 #pragma unroll
-    for (int it = 0; it < U; ++it) {
-      const int row = it * (32 / U) + lane / U;
-      const uint4 v = lds16(stg_at<U>(stg, row, unit));
-      if (m0 + row < M) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + row) * ld + n0 + unit * 8) = v;
+      for (int q = 0; q < U; ++q) sts16(stg_at<U>(stg, lane % ROWS, q), make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]));
     }
-  } else {
-    const int rows = min(32, M - m0), cols = min(8 * U, N - n0);
-    for (int row = 0; row < rows; ++row) {
-      uint16_t* const p = reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + row) * ld + n0;
-      uint32_t v = 0;
-      if (lane < 4 * U) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(stg_at<U>(stg, row, lane >> 2) + (lane & 3) * 4u) : "memory");
-      const int odd = (int)(reinterpret_cast<uintptr_t>(p) >> 1 & 1);          // (the same for the whole warp)
-      if (odd) {
-        const uint32_t next = __shfl_down_sync(0xffffffffu, v, 1);
-        if (lane == 0) p[0] = (uint16_t)v;
-        v = v >> 16 | next << 16;
+    __syncwarp();
+    if (whole) {
+      const int unit = lane % U;
+#pragma unroll
+      for (int it = 0; it < ROWS * U / 32; ++it) {
+        const int row = it * (32 / U) + lane / U;
+        const uint4 v = lds16(stg_at<U>(stg, row, unit));
+        if (m0 + r0 + row < M) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + r0 + row) * ld + n0 + unit * 8) = v;
       }
-      const int e = 2 * lane + odd;
-      if (e + 1 < cols) *reinterpret_cast<uint32_t*>(p + e) = v;
-      else if (e < cols) p[e] = (uint16_t)v;
+    } else {
+      for (int g = 0; g < ROWS && m0 + r0 + g < M; g += 8) {           // eight rows' words in flight
+        uint32_t v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          v[k] = 0;
+          if (lane < 4 * U) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v[k]) : "r"(stg_at<U>(stg, g + k, lane >> 2) + (lane & 3) * 4u) : "memory");
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (m0 + r0 + g + k >= M) break;
+          uint16_t* const p = reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + r0 + g + k) * ld + n0;
+          const int odd = (int)(reinterpret_cast<uintptr_t>(p) >> 1 & 1);          // (the same for the whole warp)
+          if (odd) {
+            const uint32_t next = __shfl_down_sync(0xffffffffu, v[k], 1);
+            if (lane == 0) p[0] = (uint16_t)v[k];
+            v[k] = v[k] >> 16 | next << 16;
+          }
+          const int e = 2 * lane + odd;
+          if (e + 1 < cols) *reinterpret_cast<uint32_t*>(p + e) = v[k];
+          else if (e < cols) p[e] = (uint16_t)v[k];
+        }
+      }
     }
+    __syncwarp();
+  }
+}
+// A chunk of 32 columns, all of them there and addressable in units of 16 bytes.
+__device__ __forceinline__ void put_whole(const uint32_t* w, uint32_t stg, int lane, void* base, int64_t ld, int m0, int M, int n0) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) sts16(stg_at<4>(stg, lane, q), make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]));
+  __syncwarp();
+#pragma unroll
+  for (int it = 0; it < 4; ++it) {
+    const int row = it * 8 + lane / 4;
+    const uint4 v = lds16(stg_at<4>(stg, row, lane & 3));
+    if (m0 + row < M) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + row) * ld + n0 + (lane & 3) * 8) = v;
   }
   __syncwarp();
 }
@@ -339,9 +366,9 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
                 uw[16 * h + i] = pack2<T>(uv[2 * i], uv[2 * i + 1]);
               }
             }
-            put_chunk<U>(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
-            if (p.d[1].p) put_chunk<U>(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
-            if (p.d[2].p) put_chunk<U>(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
+            put_chunk<U, 32>(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
+            if (p.d[1].p) put_chunk<U, 32>(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
+            if (p.d[2].p) put_chunk<U, 32>(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
           } else {
             turn_chunk(gx, stg, lane, gw);
             turn_chunk(ux, stg, lane, uw);
@@ -362,9 +389,9 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
               gw[i] = pack2<T>(d0 * up.x * s0, d1 * up.y * s1);
               uw[i] = pack2<T>(d0 * a0, d1 * a1);
             }
-            put_chunk<U>(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
-            put_chunk<U>(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
-            put_chunk<U>(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
+            put_chunk<U, 32>(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
+            put_chunk<U, 32>(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
+            put_chunk<U, 32>(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
           }
         }
       });
@@ -388,7 +415,7 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
 // all of theirs to registers first, rounded to the type (128 words each), let the next tile start, and store after that.
 // Tiles left over after the whole rounds of the pairs go as halves of 256 columns where those fit a single round.
 constexpr int W_STAGES = 4, W_STAGE_BYTES = 3 * P_A_BYTES, W_BN = 512;
-constexpr int W_EPI_WARPS = 8, W_THREADS = 64 + 32 * W_EPI_WARPS, W_STG_BYTES = 32 * 128;
+constexpr int W_EPI_WARPS = 16, W_THREADS = 64 + 32 * W_EPI_WARPS, W_STG_BYTES = 32 * 64;
 constexpr int W_SMEM = W_STAGES * W_STAGE_BYTES + W_EPI_WARPS * W_STG_BYTES + 1024 + 256;
 static_assert(W_SMEM <= 232448, "more shared memory than a block can have");
 
@@ -549,7 +576,7 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
       }
     }
   } else {
-    const int quad = warp & 3, half = (warp - 2) >> 2;
+    const int quad = warp & 3, first = (warp - 2) >> 2;
     const uint32_t stg = smem_u32(staging + (warp - 2) * W_STG_BYTES);
     const uint32_t acc_leader = map_to_cta(smem_u32(acc_empty), 0);
     const uint32_t tq = tmem_base + ((uint32_t)(quad * 32) << 16);
@@ -559,28 +586,40 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
       if (w.halves == 0) continue;
       const WideProblem& p = g.p[w.k];
       const int m0 = w.m0 + (int)rank * P_BM + quad * 32;
-      const int chunks = m0 < p.M ? min(4 * w.halves, (p.N - w.n0 + 63) / 64) : 0;      // of 64 columns; this warp's are half, half + 2, ...
+      const int chunks = m0 < p.M ? min(4 * w.halves, (p.N - w.n0 + 63) / 64) : 0;      // of 64 columns; this warp's are first and first + 4
       int good = 1;
       if (lane == 0) good = wait_or_abort(acc_full, ti & 1, abort_flag, g.err, 3) ? 1 : 0;
       good = __shfl_sync(0xffffffffu, good, 0);
       if (!good) break;
       ++ti;
       tc_fence_after();
-      uint32_t x[4][32];
+      uint32_t x[2][32];
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (2 * c + half < chunks) {
-          float a[32], b[32];
-          tmem_ld32_pair(tq + (uint32_t)((2 * c + half) * 64), tq + (uint32_t)((2 * c + half) * 64 + 32), a, b);
+      for (int c = 0; c < 2; ++c)
+        if (4 * c + first < chunks) {
 #pragma unroll
-          for (int q = 0; q < 16; ++q) { x[c][q] = pack2<T>(a[2 * q], a[2 * q + 1]); x[c][16 + q] = pack2<T>(b[2 * q], b[2 * q + 1]); }
+          for (int h = 0; h < 2; ++h) {
+            float a[16], b[16];
+            const uint32_t at = tq + (uint32_t)((4 * c + first) * 64 + 32 * h);
+            tmem_ld16_pair(at, at + 16u, a, b);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) { x[c][16 * h + q] = pack2<T>(a[2 * q], a[2 * q + 1]); x[c][16 * h + 8 + q] = pack2<T>(b[2 * q], b[2 * q + 1]); }
+          }
         }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster_relaxed(acc_leader);
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (2 * c + half < chunks) put_chunk<8>(x[c], stg, lane, p.d.p, p.d.ld, m0, p.M, w.n0 + (2 * c + half) * 64, p.N, p.vec);
+      for (int c = 0; c < 2; ++c)
+        if (4 * c + first < chunks) {
+          const int n = w.n0 + (4 * c + first) * 64;
+          if (p.vec && n + 64 <= p.N) {                  // (rows of 64 bytes are as good as rows of 128 where they are whole, and take fewer steps)
+            put_whole(x[c], stg, lane, p.d.p, p.d.ld, m0, p.M, n);
+            put_whole(x[c] + 16, stg, lane, p.d.p, p.d.ld, m0, p.M, n + 32);
+          } else {
+            put_chunk<8, 16>(x[c], stg, lane, p.d.p, p.d.ld, m0, p.M, n, p.N, 0);
+          }
+        }
     }
   }
   tc_fence_before();

@@ -24,8 +24,10 @@ struct FfnGemm {
 };
 constexpr int kFfnGroup = 4;     // problems of one launch (FFN_STORE)
 
-// CTA-pair kernel (gemm_pair16.cu).  Returns cudaSuccess, or what the launch or the maps failed with.
-cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, int* err, cudaStream_t st);
+// CTA-pair kernels (gemm_pair16.cu).  Returns cudaSuccess, or what the launch or the maps failed with.  ws: ffn_pair_workspace bytes for the same
+// products (FFN_STORE; sizes alone count).
+int64_t ffn_pair_workspace(const FfnGemm* g, int n);
+cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, void* ws, int* err, cudaStream_t st);
 
 // One product with few tokens (gemm_narrow16.cu): M <= kFfnNarrow, A K-major.  early: the kernel before it on the stream is one of these
 // kernels, of the same call, that writes none of the right operands.

@@ -131,6 +131,7 @@ struct Half {
   Mat16 gate, up;                         // as the gate's gradient reads them: whole groups of eight columns
   PackList packs; int n_packs; int64_t pack_units;
   Out16 h, dgate, dup;
+  void* sums;                             // of slices of K
 };
 Mat16 addressable(const gn_mat& m, int64_t rows, int cols, Workspace& ws, Half& w, int group = 1) {
   if (((uintptr_t)m.p & 15) == 0 && m.ld % 8 == 0 && cols % group == 0) return {m.p, m.ld};
@@ -140,6 +141,36 @@ Mat16 addressable(const gn_mat& m, int64_t rows, int cols, Workspace& ws, Half& 
   if (rows * (ld / 8) > w.pack_units) w.pack_units = rows * (ld / 8);
   return {dst, ld};
 }
+inline Mat16 in16(const Out16& m) { return {m.p, m.ld}; }
+inline Out16 out16(const gn_mat& m) { return {m.p, m.ld}; }
+// The plain products of a call, in the order they run: forward the one with Wd, backward dx and the weights' gradients.
+int plain_products(const gn_ffn& f, bool backward, const Half& w, FfnGemm (&list)[kFfnGroup]) {
+  const int R = (int)f.rows;
+  int n = 0;
+  if (!backward) {
+    FfnGemm& q = list[n++];
+    q.M = R; q.N = f.cols; q.K[0] = f.inner;
+    q.A[0] = in16(w.h); q.B[0] = w.w_down; q.d[0] = out16(f.y);
+    return n;
+  }
+  if (f.dx.p) {
+    FfnGemm& q = list[n++];
+    q.M = R; q.N = f.cols; q.K[0] = q.K[1] = f.inner; q.b_mn = true;
+    q.A[0] = in16(w.dgate); q.B[0] = w.w_gate; q.A[1] = in16(w.dup); q.B[1] = w.w_up; q.d[0] = out16(f.dx);
+  }
+  auto weights = [&](int M, int N, const Mat16& A, const Mat16& B, const gn_mat& d) {
+    if (!d.p) return;
+    FfnGemm& q = list[n++];
+    q.M = M; q.N = N; q.K[0] = R; q.a_mn = q.b_mn = true; q.A[0] = A; q.B[0] = B; q.d[0] = out16(d);
+  };
+  weights(f.inner, f.cols, in16(w.dgate), w.x, f.dw_gate);
+  weights(f.inner, f.cols, in16(w.dup), w.x, f.dw_up);
+  weights(f.cols, f.inner, w.dy, in16(w.h), f.dw_down);
+  return n;
+}
+// Of those, the first ones go to the kernel for few tokens, the others to the pairs' as one launch.
+int few_token_products(const gn_ffn& f, bool backward) { return f.rows <= kFfnNarrow && (!backward || f.dx.p) ? 1 : 0; }
+
 int64_t lay_out_half(const gn_ffn& f, bool backward, char* base, Half& w) {
   Workspace ws{base};
   w = Half{};
@@ -157,6 +188,9 @@ int64_t lay_out_half(const gn_ffn& f, bool backward, char* base, Half& w) {
     if (o != &w.h && !backward) break;
     *o = {ws.take(f.rows * ld * 2), ld};
   }
+  FfnGemm list[kFfnGroup];
+  const int n = plain_products(f, backward, w, list), few = few_token_products(f, backward);
+  w.sums = f.rows > 0 && n > few ? ws.take(ffn_pair_workspace(list + few, n - few)) : nullptr;
   return ws.used;
 }
 cudaError_t pack(const Half& w, cudaStream_t st) {
@@ -165,61 +199,26 @@ cudaError_t pack(const Half& w, cudaStream_t st) {
   pack_kernel<<<dim3((unsigned)(blocks < 1184 ? blocks : 1184), (unsigned)w.n_packs), 256, 0, st>>>(w.packs);
   return cudaGetLastError();
 }
-inline Mat16 in16(const Out16& m) { return {m.p, m.ld}; }
-inline Out16 out16(const gn_mat& m) { return {m.p, m.ld}; }
 
-cudaError_t forward_half(const gn_ffn& f, const Half& w, int* err, cudaStream_t st) {
-  const bool bf16 = f.type == GN_BF16;
-  FfnGemm a, b;
-  a.M = (int)f.rows; a.N = f.inner; a.K[0] = f.cols;
-  a.A[0] = w.x; a.B[0] = w.w_gate; a.B[1] = w.w_up;
-  a.d[0] = w.h; a.d[1] = out16(f.gate); a.d[2] = out16(f.up);
-  b.M = (int)f.rows; b.N = f.cols; b.K[0] = f.inner;
-  b.A[0] = in16(w.h); b.B[0] = w.w_down; b.d[0] = out16(f.y);
-  cudaError_t e = pack(w, st);
-  if (f.rows <= kFfnNarrow) {
-    if (e == cudaSuccess) e = launch_ffn_narrow(FFN_GATE, bf16, f.act, a, false, err, st);
-    if (e == cudaSuccess) e = launch_ffn_narrow(FFN_STORE, bf16, f.act, b, true, err, st);
-    return e;
-  }
-  if (e == cudaSuccess) e = launch_ffn_pair(FFN_GATE, bf16, f.act, &a, 1, err, st);
-  if (e == cudaSuccess) e = launch_ffn_pair(FFN_STORE, bf16, f.act, &b, 1, err, st);
-  return e;
-}
-
-cudaError_t backward_half(const gn_ffn& f, const Half& w, int* err, cudaStream_t st) {
-  const bool bf16 = f.type == GN_BF16;
-  const int R = (int)f.rows;
-  FfnGemm a;
-  a.M = R; a.N = f.inner; a.K[0] = f.cols; a.b_mn = true;
-  a.A[0] = w.dy; a.B[0] = w.w_down;
-  a.d[0] = w.h; a.d[1] = w.dgate; a.d[2] = w.dup;
-  a.gate = w.gate; a.up = w.up;
-  FfnGemm list[kFfnGroup];
-  int n = 0;
-  if (f.dx.p) {
-    FfnGemm& q = list[n++];
-    q.M = R; q.N = f.cols; q.K[0] = q.K[1] = f.inner; q.b_mn = true;
-    q.A[0] = in16(w.dgate); q.B[0] = w.w_gate; q.A[1] = in16(w.dup); q.B[1] = w.w_up; q.d[0] = out16(f.dx);
-  }
-  auto weights = [&](int M, int N, const Mat16& A, const Mat16& B, const gn_mat& d) {
-    if (!d.p) return;
-    FfnGemm& q = list[n++];
-    q.M = M; q.N = N; q.K[0] = R; q.a_mn = q.b_mn = true; q.A[0] = A; q.B[0] = B; q.d[0] = out16(d);
-  };
-  weights(f.inner, f.cols, in16(w.dgate), w.x, f.dw_gate);
-  weights(f.inner, f.cols, in16(w.dup), w.x, f.dw_up);
-  weights(f.cols, f.inner, w.dy, in16(w.h), f.dw_down);
+cudaError_t run_half(const gn_ffn& f, bool backward, const Half& w, int* err, cudaStream_t st) {
+  const bool bf16 = f.type == GN_BF16, narrow = f.rows <= kFfnNarrow;
+  FfnGemm list[kFfnGroup], a;
+  const int n = plain_products(f, backward, w, list), few = few_token_products(f, backward);
   if (n == 0) return cudaSuccess;
-  cudaError_t e = pack(w, st);
-  const bool narrow = R <= kFfnNarrow;
-  if (e == cudaSuccess) e = narrow ? launch_ffn_narrow(FFN_GRAD, bf16, f.act, a, false, err, st) : launch_ffn_pair(FFN_GRAD, bf16, f.act, &a, 1, err, st);
-  int first = 0;
-  if (narrow && f.dx.p) {
-    if (e == cudaSuccess) e = launch_ffn_narrow(FFN_STORE, bf16, f.act, list[0], true, err, st);
-    first = 1;
+  a.M = (int)f.rows; a.N = f.inner; a.K[0] = f.cols;
+  a.d[0] = w.h;
+  if (backward) {
+    a.b_mn = true;
+    a.A[0] = w.dy; a.B[0] = w.w_down; a.d[1] = w.dgate; a.d[2] = w.dup;
+    a.gate = w.gate; a.up = w.up;
+  } else {
+    a.A[0] = w.x; a.B[0] = w.w_gate; a.B[1] = w.w_up; a.d[1] = out16(f.gate); a.d[2] = out16(f.up);
   }
-  if (e == cudaSuccess && n > first) e = launch_ffn_pair(FFN_STORE, bf16, f.act, list + first, n - first, err, st);
+  const FfnKind first = backward ? FFN_GRAD : FFN_GATE;
+  cudaError_t e = pack(w, st);
+  if (e == cudaSuccess) e = narrow ? launch_ffn_narrow(first, bf16, f.act, a, false, err, st) : launch_ffn_pair(first, bf16, f.act, &a, 1, nullptr, err, st);
+  if (e == cudaSuccess && few) e = launch_ffn_narrow(FFN_STORE, bf16, f.act, list[0], true, err, st);
+  if (e == cudaSuccess && n > few) e = launch_ffn_pair(FFN_STORE, bf16, f.act, list + few, n - few, w.sums, err, st);
   return e;
 }
 
@@ -393,7 +392,7 @@ gn_status run(const gn_ffn* f, bool back, void* d_ws, int64_t ws_bytes, void* st
   int* const err = error_word();
   if (!err) return op_done(cudaErrorNoDevice, errbuf, errbuf_len);
   if (f->type == GN_F32) e = run_single(*f, back, s, err, st);
-  else e = back ? backward_half(*f, h, err, st) : forward_half(*f, h, err, st);
+  else e = run_half(*f, back, h, err, st);
   return op_done(e, errbuf, errbuf_len);
 }
 

@@ -414,6 +414,8 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
 // A, takes in 48 KB for 1024 cycles.  It fills the tensor memory, so the next tile waits until the epilogue warps have the sums: they take
 // all of theirs to registers first, rounded to the type (128 words each), let the next tile start, and store after that.
 // Tiles left over after the whole rounds of the pairs go as halves of 256 columns where those fit a single round.
+// Fewer tiles than pairs and a long K (a weight gradient of narrow layers, the gradient of a few hundred rows): K is cut into slices whose sums go
+// to the workspace in FP32 and are added, in order of the slices, by ffn_sum_kernel.
 constexpr int W_STAGES = 4, W_STAGE_BYTES = 3 * P_A_BYTES, W_BN = 512;
 constexpr int W_EPI_WARPS = 16, W_THREADS = 64 + 32 * W_EPI_WARPS, W_STG_BYTES = 32 * 64;
 constexpr int W_SMEM = W_STAGES * W_STAGE_BYTES + W_EPI_WARPS * W_STG_BYTES + 1024 + 256;
@@ -422,32 +424,38 @@ static_assert(W_SMEM <= 232448, "more shared memory than a block can have");
 struct WideProblem {
   int M, N, tiles_m, tiles_n, tiles;     // tiles of 256 x 512
   int kb0, kb, a_mn, b_mn, a_box3, b_box3, vec;
+  int slices;                            // of K; of more than one, the sums are those of a slice and go to the workspace
   Out16 d;
 };
-// Work list: items 0 .. whole - 1 are tiles, then halves of the tiles from `whole` on.
-template <int NP> struct WideParams { WideProblem p[NP]; int n, pairs, whole, items; int* err; };
+// Work list: items 0 .. whole - 1 are tiles, then halves of the tiles from `whole` on; or (CUT) slices of tiles, those of a tile side by side.
+template <int NP> struct WideParams { WideProblem p[NP]; int n, pairs, whole, items; float* ws; int* err; };
+constexpr int W_SLOT = 256 * W_BN;       // floats of an item's sums: 32 x 32 pieces, 16 to a row of them, four columns of a piece's 32 rows side by side
 
-struct WideItem { int k, m0, n0, halves; };
-template <int NP>
+struct WideItem { int k, m0, n0, halves, kb0, kb1; };
+template <int NP, bool CUT>
 __device__ __forceinline__ WideItem wide_item(const WideParams<NP>& g, int i) {
   WideItem w;
-  const int rest = i - g.whole;
+  const int rest = CUT ? -1 : i - g.whole;
   int t = rest < 0 ? i : g.whole + (rest >> 1);
   w.halves = rest < 0 ? 2 : 1;
   int k = 0;
   if (NP > 1)
-    while (k + 1 < g.n && t >= g.p[k].tiles) t -= g.p[k++].tiles;
+    while (k + 1 < g.n && t >= g.p[k].tiles * (CUT ? g.p[k].slices : 1)) { t -= g.p[k].tiles * (CUT ? g.p[k].slices : 1); ++k; }
   const WideProblem& p = g.p[k];
+  int slice = 0;
+  if (CUT) { slice = t % p.slices; t /= p.slices; }
   const int strip = t / (P_PANELS * p.tiles_n), in = t - strip * P_PANELS * p.tiles_n;
   const int high = min(P_PANELS, p.tiles_m - strip * P_PANELS);
   w.k = k;
   w.m0 = (strip * P_PANELS + in % high) * 2 * P_BM;
   w.n0 = in / high * W_BN + (rest < 0 ? 0 : (rest & 1) * P_BN);
   if (w.n0 + P_BN >= p.N) w.halves = w.n0 < p.N ? 1 : 0;       // (a second half, or a left-over half, without columns)
+  w.kb0 = CUT ? (int)((long long)p.kb * slice / p.slices) : 0;
+  w.kb1 = CUT ? (int)((long long)p.kb * (slice + 1) / p.slices) : p.kb;
   return w;
 }
 
-template <class T, int NP>
+template <class T, int NP, bool CUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
 ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant__ WideParams<NP> g) {
   constexpr bool BF16 = !__is_same(T, __half);
@@ -490,7 +498,7 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
       bool ok = true;
       const uint32_t full_leader = map_to_cta(smem_u32(&full[0]), 0);
       for (int i = pair; ok && i < g.items; i += g.pairs) {
-        const WideItem w = wide_item(g, i);
+        const WideItem w = wide_item<NP, CUT>(g, i);
         if (w.halves == 0) continue;
         const WideProblem& p = g.p[w.k];
         const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0, a3 = p.a_box3 != 0, b3 = p.b_box3 != 0, two = w.halves == 2;
@@ -498,11 +506,11 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
         const uint32_t pair_tx = 2u * P_A_BYTES * (1u + (uint32_t)w.halves);
 #pragma unroll 1
         for (int part = 0; part < 2 && ok; ++part) {
-          const int end = part ? p.kb - p.kb0 : p.kb0;
+          const int from = part ? p.kb0 : 0, end = min(w.kb1, part ? p.kb : p.kb0) - from;
           const CUtensorMap* const ma = &maps.m[w.k][2 * part];
           const CUtensorMap* const mb = ma + 1;
 #pragma unroll 1
-          for (int kb = 0; kb < end; ++kb) {
+          for (int kb = max(w.kb0 - from, 0); kb < end; ++kb) {
             if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, g.err, 1)) { ok = false; break; }
             if (rank == 0) mbar_expect_tx(&full[s], pair_tx);
             const uint32_t bar = full_leader + (uint32_t)s * 8u;
@@ -543,7 +551,7 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
       uint32_t ph = 0;
       bool ok = true;
       for (int i = pair; ok && i < g.items; i += g.pairs) {
-        const WideItem w = wide_item(g, i);
+        const WideItem w = wide_item<NP, CUT>(g, i);
         if (w.halves == 0) continue;
         const WideProblem& p = g.p[w.k];
         const uint32_t idesc = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) |
@@ -554,7 +562,7 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
         if (!wait_or_abort(acc_empty, (ti & 1) ^ 1, abort_flag, g.err, 4)) break;
         tc_fence_after();
         uint32_t acc = 0u;
-        const int kbs = p.kb;
+        const int kbs = w.kb1 - w.kb0;
         const bool two = w.halves == 2;
 #pragma unroll 1
         for (int kb = 0; kb < kbs; ++kb) {
@@ -582,7 +590,7 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
     const uint32_t tq = tmem_base + ((uint32_t)(quad * 32) << 16);
     int ti = 0;
     for (int i = pair; i < g.items; i += g.pairs) {
-      const WideItem w = wide_item(g, i);
+      const WideItem w = wide_item<NP, CUT>(g, i);
       if (w.halves == 0) continue;
       const WideProblem& p = g.p[w.k];
       const int m0 = w.m0 + (int)rank * P_BM + quad * 32;
@@ -593,6 +601,20 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
       if (!good) break;
       ++ti;
       tc_fence_after();
+      if (CUT && p.slices > 1) {
+        float* const slot = g.ws + (int64_t)i * W_SLOT + ((int)rank * 4 + quad) * 16 * 1024 + lane * 4;
+#pragma unroll 1
+        for (int c = 2 * first; c < 2 * chunks; c += c & 1 ? 7 : 1) {
+          float v[32];
+          tmem_ld32(tq + (uint32_t)(c * 32), v);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) __stcg(reinterpret_cast<float4*>(slot + c * 1024 + q * 128), make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]));
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_relaxed(acc_leader);
+        continue;
+      }
       uint32_t x[2][32];
 #pragma unroll
       for (int c = 0; c < 2; ++c)
@@ -628,6 +650,43 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
   }
+}
+
+// The sums of the slices of a tile, added in their order, to the result: blockIdx.x = 32 columns of a tile, warp = 32 rows.
+template <class T, int NP>
+__global__ void __launch_bounds__(256) ffn_sum_kernel(const __grid_constant__ WideParams<NP> g) {
+  __shared__ __align__(16) uint8_t staging[8][32 * 64];
+  grid_dep_wait();
+  grid_dep_launch();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int t = blockIdx.x / 16, item = 0, k = 0;
+  const int c = blockIdx.x % 16;
+  while (k + 1 < g.n && (g.p[k].slices == 1 || t >= g.p[k].tiles)) {
+    if (g.p[k].slices > 1) t -= g.p[k].tiles;
+    item += g.p[k].tiles * g.p[k].slices;
+    ++k;
+  }
+  const WideProblem& p = g.p[k];
+  item += t * p.slices;
+  const WideItem w = wide_item<NP, true>(g, item);
+  const int m0 = w.m0 + warp * 32, n0 = w.n0 + c * 32;
+  if (m0 >= p.M || n0 >= p.N) return;
+  const float* const from = dep(g.ws) + (int64_t)item * W_SLOT + (warp * 16 + c) * 1024 + lane * 4;
+  float v[32];
+#pragma unroll
+  for (int e = 0; e < 32; ++e) v[e] = 0.f;
+#pragma unroll 2
+  for (int s = 0; s < p.slices; ++s) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(from + (int64_t)s * W_SLOT + q * 128));
+      v[4 * q] += x.x; v[4 * q + 1] += x.y; v[4 * q + 2] += x.z; v[4 * q + 3] += x.w;
+    }
+  }
+  uint32_t o[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) o[e] = pack2<T>(v[2 * e], v[2 * e + 1]);
+  put_chunk<4, 32>(o, smem_u32(staging[warp]), lane, p.d.p, p.d.ld, m0, p.M, n0, p.N, p.vec);
 }
 
 // ---- host side ---------------------------------------------------------------------------------
@@ -713,17 +772,53 @@ cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStrea
   return launch_pdl(kernel, 2 * q.pairs, pair_threads<KIND>, P_SMEM, st, maps, q);
 }
 
-template <class T, int NP>
-cudaError_t launch_wide_as(const FfnGemm* g, int n, int* err, cudaStream_t st) {
+// How a group of products is cut: slices of K for each (all 1: none), and the items that makes.  Estimated times, in us: a k-block of a 256 x 512 tile 0.36
+// (a pair by itself as well: it waits for its loads), an item 4 more; slices a second kernel, 6, and their sums' way out and back at 4 TB/s.
+struct WidePlan { int slices[kFfnGroup]; int items; bool cut; };
+WidePlan plan_wide(const FfnGemm* g, int n) {
+  const int pairs = num_sms() / 2;
+  long long tiles = 0, work = 0;
+  int kb[kFfnGroup], tl[kFfnGroup], longest = 0;
+  WidePlan best{};
+  for (int i = 0; i < n; ++i) {
+    const long long t = (long long)((g[i].M + 255) / 256) * ((g[i].N + W_BN - 1) / W_BN);
+    kb[i] = (g[i].K[0] + P_BK - 1) / P_BK + (g[i].K[1] + P_BK - 1) / P_BK;
+    tl[i] = (int)(t < 0x1fffffff ? t : 0x1fffffff);
+    tiles += t; work += t * kb[i];
+    longest = kb[i] > longest ? kb[i] : longest;
+    best.slices[i] = 1;
+  }
+  if (tiles >= pairs) return best;
+  double best_us = longest * 0.36 + 4.0;
+  for (int len = longest; len >= 4; len = len > 32 ? len * 7 / 8 : len - 1) {
+    WidePlan p{};
+    long long items = 0, cut = 0;
+    int most = 0;
+    for (int i = 0; i < n; ++i) {
+      p.slices[i] = (kb[i] + len - 1) / len;
+      items += (long long)tl[i] * p.slices[i];
+      if (p.slices[i] > 1) cut += (long long)tl[i] * p.slices[i];
+      const int each = (kb[i] + p.slices[i] - 1) / p.slices[i];
+      most = each > most ? each : most;
+    }
+    if (items > 4 * pairs) break;
+    const double us = (items + pairs - 1) / pairs * (most * 0.36 + 4.0) + 6.0 + cut * (W_SLOT * 4.0 * 2.0 / 4e6);
+    if (cut > 0 && us < 0.9 * best_us) { best_us = us; p.items = (int)items; p.cut = true; best = p; }
+  }
+  return best;
+}
+
+template <class T, int NP, bool CUT>
+cudaError_t launch_wide_as(const FfnGemm* g, int n, const WidePlan& plan, void* ws, int* err, cudaStream_t st) {
   constexpr bool BF16 = !__is_same(T, __half);
   static std::atomic<signed char> ready[64];
-  auto* const kernel = ffn_wide_kernel<T, NP>;
+  auto* const kernel = ffn_wide_kernel<T, NP, CUT>;
   if (!once_per_device(ready, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, W_SMEM) == cudaSuccess; }))
     return cudaErrorInvalidDevice;
   PairMaps<NP> maps;
   WideParams<NP> q = {};
-  q.n = n; q.err = err;
-  long long tiles = 0;
+  q.n = n; q.err = err; q.ws = (float*)ws;
+  long long tiles = 0, summed = 0;
   for (int i = 0; i < n; ++i) {
     WideProblem& p = q.p[i];
     p.M = g[i].M; p.N = g[i].N;
@@ -731,6 +826,8 @@ cudaError_t launch_wide_as(const FfnGemm* g, int n, int* err, cudaStream_t st) {
     tiles += (long long)p.tiles_m * p.tiles_n;
     if (tiles > 0x1fffffff) return cudaErrorInvalidValue;
     p.tiles = p.tiles_m * p.tiles_n;
+    p.slices = plan.slices[i];
+    if (p.slices > 1) summed += p.tiles;
     p.kb0 = (g[i].K[0] + P_BK - 1) / P_BK; p.kb = p.kb0 + (g[i].K[1] + P_BK - 1) / P_BK;
     p.a_mn = g[i].a_mn; p.b_mn = g[i].b_mn;
     p.a_box3 = p.a_mn && p.M % 64 == 0; p.b_box3 = p.b_mn && p.N % 64 == 0;
@@ -740,18 +837,31 @@ cudaError_t launch_wide_as(const FfnGemm* g, int n, int* err, cudaStream_t st) {
   }
   const int pairs = num_sms() / 2, rem = (int)(tiles % pairs);
   q.whole = (int)(2 * rem <= pairs ? tiles - rem : tiles);
-  q.items = (int)(q.whole + 2 * (tiles - q.whole));
+  q.items = CUT ? plan.items : (int)(q.whole + 2 * (tiles - q.whole));
   q.pairs = q.items < pairs ? q.items : pairs;
-  return launch_pdl(kernel, 2 * q.pairs, W_THREADS, W_SMEM, st, maps, q);
+  cudaError_t e = launch_pdl(kernel, 2 * q.pairs, W_THREADS, W_SMEM, st, maps, q);
+  if constexpr (CUT)
+    if (e == cudaSuccess) e = launch_pdl(ffn_sum_kernel<T, NP>, (int)summed * 16, 256, 0, st, q);
+  return e;
 }
 
 }  // namespace
 
-cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, int* err, cudaStream_t st) {
+int64_t ffn_pair_workspace(const FfnGemm* g, int n) {
+  const WidePlan p = plan_wide(g, n);
+  return p.cut ? (int64_t)p.items * W_SLOT * 4 : 0;
+}
+
+cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, void* ws, int* err, cudaStream_t st) {
   if (kind == FFN_GATE) return bf16 ? launch_pair_as<FFN_GATE, __nv_bfloat16, 1>(act, g, n, err, st) : launch_pair_as<FFN_GATE, __half, 1>(act, g, n, err, st);
   if (kind == FFN_GRAD) return bf16 ? launch_pair_as<FFN_GRAD, __nv_bfloat16, 1>(act, g, n, err, st) : launch_pair_as<FFN_GRAD, __half, 1>(act, g, n, err, st);
-  if (n == 1) return bf16 ? launch_wide_as<__nv_bfloat16, 1>(g, n, err, st) : launch_wide_as<__half, 1>(g, n, err, st);
-  return bf16 ? launch_wide_as<__nv_bfloat16, kFfnGroup>(g, n, err, st) : launch_wide_as<__half, kFfnGroup>(g, n, err, st);
+  const WidePlan plan = plan_wide(g, n);
+  const auto launch = [&](auto t) {
+    using T = decltype(t);
+    if (n == 1) return plan.cut ? launch_wide_as<T, 1, true>(g, n, plan, ws, err, st) : launch_wide_as<T, 1, false>(g, n, plan, ws, err, st);
+    return plan.cut ? launch_wide_as<T, kFfnGroup, true>(g, n, plan, ws, err, st) : launch_wide_as<T, kFfnGroup, false>(g, n, plan, ws, err, st);
+  };
+  return bf16 ? launch(__nv_bfloat16()) : launch(__half());
 }
 
 }  // namespace gn

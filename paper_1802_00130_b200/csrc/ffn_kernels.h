@@ -34,4 +34,12 @@ cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, 
 constexpr int kFfnNarrow = 128;
 cudaError_t launch_ffn_narrow(FfnKind kind, bool bf16, int act, const FfnGemm& g, bool early, int* err, cudaStream_t st);
 
+// One FP32 product of the forward pass with at most kFfnDot tokens on FMAs (ffn_dot.cu): d[0] = x w[0]^T, or with w[1] act(x w[0]^T) * (x w[1]^T) and
+// the two projections to d[1], d[2] (optional).  Any alignment.
+constexpr int kFfnDot = 8;
+struct FfnMat { const float* p = nullptr; int64_t ld = 0; };
+struct FfnOut { float* p = nullptr; int64_t ld = 0; };
+struct FfnDot { int tokens, features, K, act; FfnMat x, w[2]; FfnOut d[3]; };
+cudaError_t launch_ffn_dot(const FfnDot& g, cudaStream_t st);
+
 }  // namespace gn

@@ -3,6 +3,7 @@
 // 16-bit types: two tensor-core launches forward (both projections with the gate, then the product with Wd), two backward (dh with the
 // gate's gradient, then dx and the three weight gradients as one launch; with few tokens dx is one of its own).  TMA reads the operands, so one with a base or a leading
 // dimension that is no multiple of 16 bytes is copied to the workspace first.
+// Up to eight FP32 tokens: on FMAs, bound by the weights' bytes.
 // FP32: the FP32-accurate products of the rest of the library (gemm_f16x3.cu, gemm_ffma.cu), with the gate as a pass of its own.
 #include <math.h>
 
@@ -367,7 +368,20 @@ cudaError_t clear(const gn_mat& m, int64_t rows, int64_t cols, int type, cudaStr
   return m.p ? cudaMemset2DAsync(m.p, (size_t)m.ld * b, 0, (size_t)cols * b, (size_t)rows, st) : cudaSuccess;
 }
 
+// ---- few FP32 tokens ---------------------------------------------------------------------------
+bool on_fmas(const gn_ffn& f, bool backward) { return !backward && f.rows <= kFfnDot && f.type == GN_F32; }
+cudaError_t run_fmas(const gn_ffn& f, float* h, cudaStream_t st) {
+  const int64_t ld = up8(f.inner);
+  const auto in = [](const gn_mat& m) { return FfnMat{(const float*)m.p, m.ld}; };
+  const auto out = [](const gn_mat& m) { return FfnOut{(float*)m.p, m.ld}; };
+  const FfnDot a{(int)f.rows, f.inner, f.cols, f.act, in(f.x), {in(f.w_gate), in(f.w_up)}, {{h, ld}, out(f.gate), out(f.up)}};
+  const FfnDot b{(int)f.rows, f.cols, f.inner, f.act, {h, ld}, {in(f.w_down), {}}, {out(f.y), {}, {}}};
+  const cudaError_t e = launch_ffn_dot(a, st);
+  return e == cudaSuccess ? launch_ffn_dot(b, st) : e;
+}
+
 int64_t needed(const gn_ffn& f, bool backward, char* base, Half& h, Single& s) {
+  if (on_fmas(f, backward)) return f.rows * up8(f.inner) * 4 + 256;
   return (f.type == GN_F32 ? lay_out_single(f, backward, base, s) : lay_out_half(f, backward, base, h)) + 256;
 }
 
@@ -391,7 +405,8 @@ gn_status run(const gn_ffn* f, bool back, void* d_ws, int64_t ws_bytes, void* st
   }
   int* const err = error_word();
   if (!err) return op_done(cudaErrorNoDevice, errbuf, errbuf_len);
-  if (f->type == GN_F32) e = run_single(*f, back, s, err, st);
+  if (on_fmas(*f, back)) e = run_fmas(*f, (float*)base, st);
+  else if (f->type == GN_F32) e = run_single(*f, back, s, err, st);
   else e = run_half(*f, back, h, err, st);
   return op_done(e, errbuf, errbuf_len);
 }

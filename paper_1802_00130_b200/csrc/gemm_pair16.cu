@@ -773,7 +773,8 @@ cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStrea
 }
 
 // How a group of products is cut: slices of K for each (all 1: none), and the items that makes.  Estimated times, in us: a k-block of a 256 x 512 tile 0.36
-// (a pair by itself as well: it waits for its loads), an item 4 more; slices a second kernel, 6, and their sums' way out and back at 4 TB/s.
+// (a pair by itself as well: it waits for its loads), an item 4 more; a list takes as long as its longest item or its share of all; slices
+// cost a second kernel, 6, and their sums' way out and back at 4 TB/s.
 struct WidePlan { int slices[kFfnGroup]; int items; bool cut; };
 WidePlan plan_wide(const FfnGemm* g, int n) {
   const int pairs = num_sms() / 2;
@@ -788,8 +789,12 @@ WidePlan plan_wide(const FfnGemm* g, int n) {
     longest = kb[i] > longest ? kb[i] : longest;
     best.slices[i] = 1;
   }
-  if (tiles >= pairs) return best;
-  double best_us = longest * 0.36 + 4.0;
+  const auto list_us = [&](int most, long long items) {
+    const double one = most * 0.36 + 4.0, share = (work * 0.36 + items * 4.0) / pairs * (items > pairs ? 1.15 : 1.0);
+    return one > share ? one : share;
+  };
+  if (tiles >= 4 * pairs) return best;
+  double best_us = list_us(longest, tiles);
   for (int len = longest; len >= 4; len = len > 32 ? len * 7 / 8 : len - 1) {
     WidePlan p{};
     long long items = 0, cut = 0;
@@ -801,8 +806,8 @@ WidePlan plan_wide(const FfnGemm* g, int n) {
       const int each = (kb[i] + p.slices[i] - 1) / p.slices[i];
       most = each > most ? each : most;
     }
-    if (items > 4 * pairs) break;
-    const double us = (items + pairs - 1) / pairs * (most * 0.36 + 4.0) + 6.0 + cut * (W_SLOT * 4.0 * 2.0 / 4e6);
+    if (items > 8 * pairs) break;
+    const double us = list_us(most, items) + 6.0 + cut * (W_SLOT * 4.0 * 2.0 / 4e6);
     if (cut > 0 && us < 0.9 * best_us) { best_us = us; p.items = (int)items; p.cut = true; best = p; }
   }
   return best;

@@ -13,7 +13,8 @@ ACTS = ["sigmoid", "silu", "gelu", "gelu_tanh", "relu"]
 # rows, cols, inner: single tokens, odd sizes, tile edges, several tiles and a long inner sum
 SHAPES = [(1, 1, 1), (1, 64, 128), (2, 8, 16), (3, 7, 5), (1, 1000, 3001), (16, 256, 512), (17, 520, 264), (48, 128, 1024), (64, 617, 1201),
           (127, 72, 96), (128, 128, 128), (129, 136, 200), (200, 1024, 384), (255, 520, 1000), (257, 264, 520), (300, 784, 300),
-          (513, 96, 2056), (1003, 617, 1201), (2100, 256, 264), (40, 2048, 8192)]
+          (513, 96, 2056), (1003, 617, 1201), (2100, 256, 264), (40, 2048, 8192),
+          (5000, 40, 72), (2, 1001, 2003), (7, 64, 4001), (8, 136, 40), (300, 64, 5000)]
 # an activation's FP32 value is off by a few steps: exp 2, its quotient 2, the products after it
 ACT = 16 * E
 

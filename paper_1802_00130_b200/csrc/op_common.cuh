@@ -89,10 +89,10 @@ inline gn_status op_fail(gn_status st, const char* why, char* errbuf, int64_t er
   if (errbuf && errbuf_len > 0) snprintf(errbuf, (size_t)errbuf_len, "%s", why);
   return st;
 }
-// The end of a call that has launched: what the runtime says of it.
+// The end of a call that has launched: what the launches said of themselves.
 inline gn_status op_done(cudaError_t e, char* errbuf, int64_t errbuf_len) {
-  if (e == cudaSuccess) e = cudaGetLastError(); else cudaGetLastError();
   if (e == cudaSuccess) { if (errbuf && errbuf_len > 0) errbuf[0] = 0; return GN_OK; }
+  cudaGetLastError();
   return op_fail(e == cudaErrorMemoryAllocation ? GN_ENOMEM : GN_ECUDA, cudaGetErrorString(e), errbuf, errbuf_len);
 }
 inline int type_bytes(int type) { return type == GN_F32 ? 4 : 2; }

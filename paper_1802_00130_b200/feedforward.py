@@ -77,21 +77,18 @@ def _first(t, what):
     return dtype, dev, shape[0], shape[1]
 
 
-def _elsewhere(call, dev, stream):
-    """Runs a call where allocations and launches go to its device and stream, where those are not the current ones."""
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+
+
+def _elsewhere(call, dev, stream, *args):
+    """call(*args) where allocations and launches go to the given device and stream, for calls that are not on the current ones."""
     if stream is None:
         with torch.cuda.device(dev):
-            return call(_raw_stream(dev))
+            return call(*args)
     if stream.device.index != dev:
         raise ValueError(f"the stream is one of {stream.device}, the tensors are on cuda:{dev}")
     with torch.cuda.device(dev), torch.cuda.stream(stream):
-        return call(stream.cuda_stream)
-
-
-def _run(call, dev, stream):
-    if stream is None and dev == torch._C._cuda_getDevice():
-        return call(_raw_stream(dev))
-    return _elsewhere(call, dev, stream)
+        return call(*args)
 
 
 def _checked(status, err):
@@ -105,6 +102,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, stream=None):
     weight, bias: [cols], each optional, both of x's type or both float32.
     """
     dtype, dev, rows, cols = _first(x, "x")
+    if stream is not None or dev != _device():
+        return _elsewhere(layer_norm, dev, stream, x, weight, bias, eps, save)
     px, ldx = _matrix(x, "x", rows, cols, dtype, dev)
     wtype = dtype
     if isinstance(weight, torch.Tensor):
@@ -114,19 +113,16 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, stream=None):
     if wtype is not dtype and wtype is not torch.float32:
         raise TypeError(f"weight and bias: expected {dtype} or float32, got {wtype}")
     pw, pb = _vector(weight, "weight", cols, dev, wtype), _vector(bias, "bias", cols, dev, wtype)
-
-    def call(st):
-        y = x.new_empty((rows, cols))
-        err = _err()
-        if not save:
-            _checked(lib().gn_layer_norm(_TYPES[dtype], _TYPES[wtype], rows, cols, px, ldx, pw, pb, eps, y.data_ptr(), cols, None, None, st, err, 200), err)
-            return y
-        mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
-        _checked(lib().gn_layer_norm(_TYPES[dtype], _TYPES[wtype], rows, cols, px, ldx, pw, pb, eps, y.data_ptr(), cols, mean.data_ptr(),
-                                     rstd.data_ptr(), st, err, 200), err)
-        return y, mean, rstd
-
-    return _run(call, dev, stream)
+    y = x.new_empty(rows, cols)
+    mean = rstd = pm = pr = None
+    if save:
+        mean, rstd = x.new_empty(rows, dtype=torch.float32), x.new_empty(rows, dtype=torch.float32)
+        pm, pr = mean.data_ptr(), rstd.data_ptr()
+    err = _err()
+    status = lib().gn_layer_norm(_TYPES[dtype], _TYPES[wtype], rows, cols, px, ldx, pw, pb, eps, y.data_ptr(), cols, pm, pr, _raw_stream(dev), err, 200)
+    if status:
+        _checked(status, err)
+    return (y, mean, rstd) if save else y
 
 
 def layer_norm_grad(dy, x, mean, rstd, weight=None, add=None, stream=None):
@@ -135,6 +131,8 @@ def layer_norm_grad(dy, x, mean, rstd, weight=None, add=None, stream=None):
     mean, rstd: what layer_norm(..., save=True) has returned.  add: a gradient of x's shape that is added to dx (the residual path).
     """
     dtype, dev, rows, cols = _first(x, "x")
+    if stream is not None or dev != _device():
+        return _elsewhere(layer_norm_grad, dev, stream, dy, x, mean, rstd, weight, add)
     px, ldx = _matrix(x, "x", rows, cols, dtype, dev)
     pdy, ld_dy = _matrix(dy, "dy", rows, cols, dtype, dev)
     pa, ld_add = _matrix(add, "add", rows, cols, dtype, dev) if add is not None else (None, 0)
@@ -143,18 +141,19 @@ def layer_norm_grad(dy, x, mean, rstd, weight=None, add=None, stream=None):
     pm, pr = _vector(mean, "mean", rows, dev, torch.float32), _vector(rstd, "rstd", rows, dev, torch.float32)
     pw = _vector(weight, "weight", cols, dev, dtype, torch.float32)
     wtype = dtype if weight is None else weight.dtype
-
-    def call(st):
-        n = lib().gn_layer_norm_grad_workspace(rows, cols)
-        dx = x.new_empty((rows, cols))
+    handle = lib()
+    n = handle.gn_layer_norm_grad_workspace(rows, cols)
+    dx, ws = x.new_empty(rows, cols), x.new_empty(n, dtype=torch.uint8)
+    if wtype is dtype:
+        dw, db = x.new_empty(cols), x.new_empty(cols)
+    else:
         dw, db = x.new_empty(cols, dtype=wtype), x.new_empty(cols, dtype=wtype)
-        ws = x.new_empty(max(n, 16), dtype=torch.uint8)
-        err = _err()
-        _checked(lib().gn_layer_norm_grad(_TYPES[dtype], _TYPES[wtype], rows, cols, pdy, ld_dy, px, ldx, pm, pr, pw, pa, ld_add, dx.data_ptr(), cols,
-                                          dw.data_ptr(), db.data_ptr(), ws.data_ptr(), n, st, err, 200), err)
-        return dx, dw, db
-
-    return _run(call, dev, stream)
+    err = _err()
+    status = handle.gn_layer_norm_grad(_TYPES[dtype], _TYPES[wtype], rows, cols, pdy, ld_dy, px, ldx, pm, pr, pw, pa, ld_add, dx.data_ptr(), cols,
+                                       dw.data_ptr(), db.data_ptr(), ws.data_ptr(), n, _raw_stream(dev), err, 200)
+    if status:
+        _checked(status, err)
+    return dx, dw, db
 
 
 def dropout(x, p, key, step=0, residual=None, device_step=None, stream=None):
@@ -165,6 +164,8 @@ def dropout(x, p, key, step=0, residual=None, device_step=None, stream=None):
     step when the kernel runs, for steps captured into a graph.
     """
     dtype, dev, rows, cols = _first(x, "x")
+    if stream is not None or dev != _device():
+        return _elsewhere(dropout, dev, stream, x, p, key, step, residual, device_step)
     px, ldx = _matrix(x, "x", rows, cols, dtype, dev)
     pr, ld_res = _matrix(residual, "residual", rows, cols, dtype, dev) if residual is not None else (None, 0)
     ps = None
@@ -174,15 +175,13 @@ def dropout(x, p, key, step=0, residual=None, device_step=None, stream=None):
         if device_step.numel() != 1:
             raise ValueError("device_step: expected one element")
         ps = device_step.data_ptr()
-
-    def call(st):
-        y = x.new_empty((rows, cols))
-        err = _err()
-        _checked(lib().gn_dropout(_TYPES[dtype], rows, cols, px, ldx, pr, ld_res, y.data_ptr(), cols, p, key & 0xFFFFFFFFFFFFFFFF,
-                                  step & 0xFFFFFFFFFFFFFFFF, ps, st, err, 200), err)
-        return y
-
-    return _run(call, dev, stream)
+    y = x.new_empty(rows, cols)
+    err = _err()
+    status = lib().gn_dropout(_TYPES[dtype], rows, cols, px, ldx, pr, ld_res, y.data_ptr(), cols, p, key & 0xFFFFFFFFFFFFFFFF,
+                              step & 0xFFFFFFFFFFFFFFFF, ps, _raw_stream(dev), err, 200)
+    if status:
+        _checked(status, err)
+    return y
 
 
 _Args = C.c_int64 * 27          # gn_ffn: type and act, rows, cols and inner, then pointer and leading dimension of twelve matrices
@@ -202,12 +201,14 @@ def _ffn_inputs(x, w_gate, w_up, w_down, act):
     return dtype, dev, rows, cols, inner, words
 
 
-def _ffn_call(fn, backward, x, words, st):
+def _ffn_call(fn, backward, x, dev, words):
     args = _Args(*words)
     n = lib().gn_gated_ffn_workspace(args, backward)
     ws = x.new_empty(max(n, 16), dtype=torch.uint8)
     err = _err()
-    _checked(fn(args, ws.data_ptr(), n, st, err, 200), err)
+    status = fn(args, ws.data_ptr(), n, _raw_stream(dev), err, 200)
+    if status:
+        _checked(status, err)
 
 
 def gated_ffn(x, w_gate, w_up, w_down, act="silu", save=False, stream=None):
@@ -216,32 +217,30 @@ def gated_ffn(x, w_gate, w_up, w_down, act="silu", save=False, stream=None):
     x [rows][cols], w_gate and w_up [inner][cols], w_down [cols][inner]; act: "sigmoid", "silu", "gelu", "gelu_tanh" or "relu".
     """
     dtype, dev, rows, cols, inner, words = _ffn_inputs(x, w_gate, w_up, w_down, act)
-
-    def call(st):
-        y = x.new_empty((rows, cols))
-        if not save:
-            _ffn_call(lib().gn_gated_ffn, 0, x, words + [y.data_ptr(), cols], st)
-            return y
-        gate, up = x.new_empty((rows, inner)), x.new_empty((rows, inner))
-        _ffn_call(lib().gn_gated_ffn, 0, x, words + [y.data_ptr(), cols, gate.data_ptr(), inner, up.data_ptr(), inner], st)
-        return y, gate, up
-
-    return _run(call, dev, stream)
+    if stream is not None or dev != _device():
+        return _elsewhere(gated_ffn, dev, stream, x, w_gate, w_up, w_down, act, save)
+    y = x.new_empty(rows, cols)
+    words += (y.data_ptr(), cols)
+    if not save:
+        _ffn_call(lib().gn_gated_ffn, 0, x, dev, words)
+        return y
+    gate, up = x.new_empty(rows, inner), x.new_empty(rows, inner)
+    words += (gate.data_ptr(), inner, up.data_ptr(), inner)
+    _ffn_call(lib().gn_gated_ffn, 0, x, dev, words)
+    return y, gate, up
 
 
 def gated_ffn_grad(dy, x, gate, up, w_gate, w_up, w_down, act="silu", stream=None):
     """(dx, dw_gate, dw_up, dw_down) of gated_ffn; gate, up: what gated_ffn(..., save=True) has returned."""
     dtype, dev, rows, cols, inner, words = _ffn_inputs(x, w_gate, w_up, w_down, act)
-    words += [0, 0, *_matrix(gate, "gate", rows, inner, dtype, dev), *_matrix(up, "up", rows, inner, dtype, dev),
-              *_matrix(dy, "dy", rows, cols, dtype, dev)]
-
-    def call(st):
-        dx = x.new_empty((rows, cols))
-        dwg, dwu, dwd = x.new_empty((inner, cols)), x.new_empty((inner, cols)), x.new_empty((cols, inner))
-        _ffn_call(lib().gn_gated_ffn_grad, 1, x, words + [dx.data_ptr(), cols, dwg.data_ptr(), cols, dwu.data_ptr(), cols, dwd.data_ptr(), inner], st)
-        return dx, dwg, dwu, dwd
-
-    return _run(call, dev, stream)
+    if stream is not None or dev != _device():
+        return _elsewhere(gated_ffn_grad, dev, stream, dy, x, gate, up, w_gate, w_up, w_down, act)
+    words += (0, 0, *_matrix(gate, "gate", rows, inner, dtype, dev), *_matrix(up, "up", rows, inner, dtype, dev), *_matrix(dy, "dy", rows, cols, dtype, dev))
+    dx = x.new_empty(rows, cols)
+    dwg, dwu, dwd = x.new_empty(inner, cols), x.new_empty(inner, cols), x.new_empty(cols, inner)
+    words += (dx.data_ptr(), cols, dwg.data_ptr(), cols, dwu.data_ptr(), cols, dwd.data_ptr(), inner)
+    _ffn_call(lib().gn_gated_ffn_grad, 1, x, dev, words)
+    return dx, dwg, dwu, dwd
 
 
 def gated_ffn_status(device=None, stream=None):

@@ -246,3 +246,22 @@ def test_refusals():
                 lambda: gn.gated_ffn_grad(x[:3], x, gate, up, *w), lambda: gn.gated_ffn_grad(x, x, gate[:, :8], up, *w)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_status_after_calls():
+    x, w = inputs(300, 64, 128, torch.bfloat16)
+    gn.gated_ffn(x, *w)
+    gn.gated_ffn_status()
+    gn.gated_ffn_status(stream=torch.cuda.Stream())
+
+
+@pytest.mark.parametrize("rows", [1, 100, 700])
+def test_same_tensor_in_several_places(rows):
+    """One matrix as gate and up projection, and one as x and dy."""
+    for t in (torch.bfloat16, torch.float32):
+        x, w = inputs(rows, 128, 256, t)
+        w[1] = w[0]
+        got = gn.gated_ffn(x, *w, save=True)
+        check_forward(got, x, w, "silu", t)
+        check_backward(gn.gated_ffn_grad(x, x, got[1], got[1], *w), x, x, got[1], got[1], w, "silu", t)
+

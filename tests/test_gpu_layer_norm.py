@@ -192,10 +192,12 @@ def test_no_rows():
     assert dx.shape == (0, 40) and not dw.any() and not db.any()
 
 
-@pytest.mark.parametrize("cols", [12, 600, 4096, 9000, 40000])
-def test_in_place_and_what_is_left_alone(cols):
-    """y in x's place, dx in dy's and in add's; columns past the row's end and rows behind the last keep what they hold."""
-    rows, ld = 9, cols + 5
+@pytest.mark.parametrize("pad", [5, 8])
+@pytest.mark.parametrize("cols", [12, 24, 600, 4096, 9000, 40000])
+def test_in_place_and_what_is_left_alone(cols, pad):
+    """y in x's place, dx in dy's and in add's; columns past the row's end and rows behind the last keep what they hold.  More rows than a
+    launch has blocks, so that blocks walk several."""
+    rows, ld = 9 if cols > 600 else 1500, cols + pad
     err = C.create_string_buffer(200)
     x, dy, add = rand((rows, cols), torch.float16, 1), rand((rows, cols), torch.float16, 2), rand((rows, cols), torch.float16, 3)
     w = vec(cols, torch.float16, 4)

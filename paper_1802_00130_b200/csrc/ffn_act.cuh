@@ -5,12 +5,45 @@
 namespace gn {
 namespace {
 
+__device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float rcp_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float min_nan(float a, float b) { float y; asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
+
 // 1 / (1 + exp(-v)) and 1 / (1 + exp(v)), each to full relative accuracy: one minus the other would lose it where it is small.
-// FAST: the hardware's exponential and reciprocal, off by at most (4 + |v|) 2^-23: for results that are rounded to 16 bits, 2^-12 at best.
+// FAST: the hardware's exponential and reciprocal, off by at most (4 + |v|) 2^-23, for results that are rounded to 16 bits (2^-12 at best), and without
+// a branch on the sign: exp(-v) is kept below 2^126, where its reciprocal is still a normal number and their product one.
 template <bool FAST>
 __device__ __forceinline__ void sigmoids(float v, float& z, float& nz) {
-  const float e = FAST ? __expf(-fabsf(v)) : expf(-fabsf(v)), r = FAST ? __fdividef(1.f, 1.f + e) : 1.f / (1.f + e);
-  z = v < 0.f ? e * r : r; nz = v < 0.f ? r : e * r;
+  if (FAST) {
+    const float e = min_nan(exp2_fast(v * -1.4426950408889634f), 8e37f);
+    z = rcp_fast(1.f + e); nz = e * z;
+  } else {
+    const float e = expf(-fabsf(v)), r = 1.f / (1.f + e);
+    z = v < 0.f ? e * r : r; nz = v < 0.f ? r : e * r;
+  }
+}
+// Phi(v), the normal distribution function, and exp(-v^2 / 2), each to full relative accuracy.  FAST: Phi(-|v|) exp(v^2 / 2) = t P(t) with
+// t = 1 / (1 + 0.35 |v| / sqrt 2); P, of degree 7, was fitted to the smallest largest relative error over t in (0, 1], 8.2e-7 (iterated weighted least
+// squares in 64 bits).  With the exponential's share that is 3e-6 up to |v| = 6 and 7e-6 up to 13.
+template <bool FAST>
+__device__ __forceinline__ void normal(float v, float& cdf, float& e) {
+  if (FAST) {
+    const float t = rcp_fast(fmaf(fabsf(v), 0.24748737341529162f, 1.f));
+    e = exp2_fast(v * v * -0.72134752044448170f);
+    float p = -0.04255257174372673f;
+    p = fmaf(p, t, 0.1006045714020729f);
+    p = fmaf(p, t, -0.007274771109223366f);
+    p = fmaf(p, t, 0.08147183060646057f);
+    p = fmaf(p, t, 0.07733616977930069f);
+    p = fmaf(p, t, 0.09295466542243958f);
+    p = fmaf(p, t, 0.0987265482544899f);
+    p = fmaf(p, t, 0.09873314201831818f);
+    const float q = p * t * e;
+    cdf = v < 0.f ? q : 1.f - q;
+  } else {
+    cdf = 0.5f * erfcf(-0.70710678118654752f * v);
+    e = expf(-0.5f * v * v);
+  }
 }
 // act(v) and its derivative.  A NaN stays one: comparisons with it fall to the branch that computes with it.
 template <int ACT, bool FAST>
@@ -19,16 +52,16 @@ __device__ __forceinline__ void activation(float v, float& a, float& da) {
   if (ACT == GN_ACT_RELU) {
     a = v < 0.f ? 0.f : v; da = v > 0.f ? 1.f : 0.f;
   } else if (ACT == GN_ACT_GELU) {
-    const float cdf = 0.5f * erfcf(-0.70710678118654752f * v);
-    a = v * cdf; da = cdf + v * 0.39894228040143268f * (FAST ? __expf(-0.5f * v * v) : expf(-0.5f * v * v));
-  } else if (ACT == GN_ACT_GELU_TANH) {        // (1 + tanh q) / 2 = 1 / (1 + exp(-2 q))
-    const float k = 1.5957691216057308f;       // 2 sqrt(2 / pi)
-    sigmoids<FAST>(k * (v + 0.044715f * v * v * v), z, nz);
-    a = v * z; da = z + v * z * nz * k * (1.f + 0.134145f * v * v);
+    normal<FAST>(v, z, nz);
+    a = v * z; da = fmaf(v * nz, 0.39894228040143268f, z);
+  } else if (ACT == GN_ACT_GELU_TANH) {        // (1 + tanh q) / 2 = 1 / (1 + exp(-2 q)), q = sqrt(2 / pi) (v + 0.044715 v^3)
+    const float s = v * v;
+    sigmoids<FAST>(v * fmaf(s, 0.071354816272810f, 1.5957691216057308f), z, nz);
+    a = v * z; da = fmaf(a * nz, fmaf(s, 0.214064448818430f, 1.5957691216057308f), z);
   } else if (ACT == GN_ACT_SIGMOID) {
     sigmoids<FAST>(v, z, nz); a = z; da = z * nz;
   } else {
-    sigmoids<FAST>(v, z, nz); a = v * z; da = z + v * z * nz;
+    sigmoids<FAST>(v, z, nz); a = v * z; da = fmaf(a, nz, z);
   }
 }
 // f(integral constant) of the activation that a call names.

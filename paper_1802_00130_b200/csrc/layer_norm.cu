@@ -307,7 +307,7 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int by
 }
 template <class T, class W, int TPR>
 __global__ void __launch_bounds__(grad_block<TPR>, ring_blocks<T, TPR>) layer_norm_grad_ring_kernel(const NormGradArgs a) {
-  constexpr int BLOCK = grad_block<TPR>, G = BLOCK / TPR, AHEAD = kAhead<T, TPR>, STAGES = AHEAD + 1, V = Pack<T>::V;
+  constexpr int BLOCK = grad_block<TPR>, G = BLOCK / TPR, AHEAD = kAhead<T, TPR>, STAGES = AHEAD + 1;
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float part[2][G][TPR > 32 ? 2 * (TPR / 32) : 1];
   const int thread = threadIdx.x % TPR, group = threadIdx.x / TPR;

@@ -43,10 +43,11 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float* part) {
 // TPR threads a row, which hold NU units of 16 bytes each.  A block walks its rows with the next row's loads under way while it works on
 // one; the weights stay in registers where they are few.
 template <int TPR> constexpr int norm_block = TPR > 128 ? TPR : 128;
-// Blocks of an SM.  16384 x 4096 bf16 with two units a thread: 51.3 us at 768 threads an SM (80 registers), 52.6 at 1024, 74 at 1280.
-template <int TPR> constexpr int norm_blocks = TPR > 256 ? 1024 / TPR : 768 / norm_block<TPR>;
+// Blocks of an SM.  16384 x 4096 bf16 with two units a thread: 51.3 us at 768 threads an SM (80 registers), 52.6 at 1024, 74 at 1280; a unit of FP32 has half the
+// elements and needs fewer registers (16384 x 2048: 48.4 and 43.9 us), as do rows of eight threads, one unit each (10^6 x 64 bf16: 63 and 54).
+template <class T, int TPR> constexpr int norm_blocks = (TPR > 256 || sizeof(T) == 4 || TPR == 8 ? 1024 : 768) / norm_block<TPR>;
 template <class T, class W, int TPR, int NU, bool VEC>
-__global__ void __launch_bounds__(norm_block<TPR>, norm_blocks<TPR>)
+__global__ void __launch_bounds__(norm_block<TPR>, norm_blocks<T, TPR>)
 layer_norm_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, const W* b, float eps, T* y, int64_t ldy, float* mean_out, float* rstd_out) {
   constexpr int V = Pack<T>::V, VW = Pack<W>::V, WU = sizeof(W) / sizeof(T);      // WU: units of the weights to a unit of x
   constexpr int PER = norm_block<TPR> / TPR;                     // rows of a block
@@ -509,7 +510,7 @@ struct NormCall {
 template <class T, class W, int TPR, int NU>
 cudaError_t norm_as(const NormCall& a, bool vec) {
   constexpr int BLOCK = norm_block<TPR>, PER = BLOCK / TPR;
-  const int64_t want = (a.rows + PER - 1) / PER, most = 148LL * norm_blocks<TPR>, blocks = want < most ? want : most;
+  const int64_t want = (a.rows + PER - 1) / PER, most = 148LL * norm_blocks<T, TPR>, blocks = want < most ? want : most;
   auto* const k = vec ? layer_norm_kernel<T, W, TPR, NU, true> : layer_norm_kernel<T, W, TPR, NU, false>;
   return launch_pdl_grid(k, dim3((unsigned)blocks), BLOCK, 0, a.st, a.rows, a.cols, (const T*)a.x, a.ldx, (const W*)a.w, (const W*)a.b, a.eps,
                          (T*)a.y, a.ldy, a.mean, a.rstd);

@@ -225,11 +225,12 @@ __device__ __forceinline__ void leave_sums(const NormGradArgs& a, float (&sw)[kO
 }
 
 template <int TPR> constexpr int grad_block = TPR > 256 ? TPR : 256;
-// Threads of an SM: what a thread holds of two rows, the weights and the sums takes about 110 registers at 16 bits (16 columns), 80 at 32 (8).
-template <class T> constexpr int grad_threads = sizeof(T) == 2 ? 512 : 768;
-template <class T, int TPR> constexpr int grad_blocks = grad_threads<T> / grad_block<TPR> > 0 ? grad_threads<T> / grad_block<TPR> : 1;
+// Threads of an SM: what a thread holds of two rows, the weights and the sums takes about 110 registers at 16 bits (16 columns).
+template <class T> constexpr int ring_threads = 512;
+template <class T, int TPR> constexpr int ring_blocks = ring_threads<T> / grad_block<TPR> > 0 ? ring_threads<T> / grad_block<TPR> : 1;
+// 16-bit rows that 16-byte accesses cannot be made to (cp.async has none of two bytes): the next row's elements in registers.
 template <class T, class W, int TPR>
-__global__ void __launch_bounds__(grad_block<TPR>, grad_blocks<T, TPR>) layer_norm_grad_kernel(const NormGradArgs a) {
+__global__ void __launch_bounds__(grad_block<TPR>, ring_blocks<T, TPR>) layer_norm_grad_kernel(const NormGradArgs a) {
   constexpr int BLOCK = grad_block<TPR>, G = BLOCK / TPR;
   constexpr bool VEC = false;
   __shared__ float part[2][G][TPR > 32 ? 2 * (TPR / 32) : 1];
@@ -295,18 +296,19 @@ __global__ void __launch_bounds__(grad_block<TPR>, grad_blocks<T, TPR>) layer_no
   if (a.sums) leave_sums<VEC, T, TPR, BLOCK>(a, sw, sb, buf, blockIdx.x, 0, cols);
 }
 
-// The same where 16-byte accesses can be made: a thread's units of the next rows are on their way to its own places in shared memory (cp.async, which
+// The same where 16-byte accesses can be made, and in FP32 where they cannot (4 bytes each): a thread's elements of the next rows are on their way to its own places in shared memory (cp.async, which
 // nobody else reads: no barrier), so that the loads in flight are not limited by registers.  16384 x 4096 bf16 with `add`: 95 us (117 with one row
 // ahead in registers), 5.7 TB/s of the 6.4 of a copy.  Rows ahead: 2 at 16 bits (3: 96 us), 3 at 32 (16384 x 2048: 84 us, 2: 89).
 template <class T, int TPR> constexpr int kAhead = TPR > 512 ? 1 : sizeof(T) == 2 ? 2 : 3;       // (a block of 1024 threads has 96 KB a row)
-template <class T> constexpr int ring_threads = 512;             // of an SM
-template <class T, int TPR> constexpr int ring_blocks = ring_threads<T> / grad_block<TPR> > 0 ? ring_threads<T> / grad_block<TPR> : 1;
 template <class T, int TPR> constexpr int ring_bytes = (kAhead<T, TPR> + 1) * 3 * 2 * grad_block<TPR> * 16;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {       // (the rest of the 16 reads as zero)
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-template <class T, class W, int TPR>
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+template <class T, class W, int TPR, bool VEC>
 __global__ void __launch_bounds__(grad_block<TPR>, ring_blocks<T, TPR>) layer_norm_grad_ring_kernel(const NormGradArgs a) {
   constexpr int BLOCK = grad_block<TPR>, G = BLOCK / TPR, AHEAD = kAhead<T, TPR>, STAGES = AHEAD + 1;
   extern __shared__ __align__(16) uint8_t ring[];
@@ -326,36 +328,58 @@ __global__ void __launch_bounds__(grad_block<TPR>, ring_blocks<T, TPR>) layer_no
   float wv[kOwn<T>], sw[kOwn<T>], sb[kOwn<T>];
 #pragma unroll
   for (int k = 0; k < kOwn<T>; ++k) {
-    const int c = own_col<true, T>(k, thread, TPR);
+    const int c = own_col<VEC, T>(k, thread, TPR);
     wv[k] = w && c < cols ? to_f(w[c]) : 1.f;
     sw[k] = sb[k] = 0.f;
   }
   int bytes[2], col[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    const int c = pack_col<true, T>(u, 0, thread, TPR), n = (cols - c) * (int)sizeof(T);
+    const int c = pack_col<VEC, T>(u, 0, thread, TPR), n = (cols - c) * (int)sizeof(T);
     bytes[u] = n < 0 ? 0 : n > 16 ? 16 : n;
     col[u] = bytes[u] ? c : 0;
   }
-  const uint32_t own = smem_u32(ring) + threadIdx.x * 16;
+  // (a unit of 16 bytes to a place, or, where an access is to one element, element e of a unit BLOCK words behind element e - 1)
+  const uint32_t own = smem_u32(ring) + threadIdx.x * (VEC ? 16 : 4);
   const auto place = [&](int stage, int matrix, int u) { return own + (uint32_t)(((stage * 3 + matrix) * 2 + u) * BLOCK * 16); };
+  const auto copy = [&](int stage, int matrix, const T* row) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if constexpr (VEC) {
+        cp_async16(place(stage, matrix, u), row + col[u], bytes[u]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < Pack<T>::V; ++e) {
+          const int c = pack_col<false, T>(u, e, thread, TPR);
+          cp_async4(place(stage, matrix, u) + (uint32_t)(e * BLOCK * 4), row + (c < cols ? c : 0), c < cols ? 4 : 0);
+        }
+      }
+    }
+  };
   const int64_t step = (int64_t)gridDim.x * G;
   int64_t r = (int64_t)blockIdx.x * G + group;
   const auto request = [&](int64_t q, int stage) {
     if (q < a.rows) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        cp_async16(place(stage, 0, u), x + q * a.ldx + col[u], bytes[u]);
-        cp_async16(place(stage, 1, u), dy + q * a.ld_dy + col[u], bytes[u]);
-        if (adds) cp_async16(place(stage, 2, u), add + q * a.ld_add + col[u], bytes[u]);
-      }
+      copy(stage, 0, x + q * a.ldx);
+      copy(stage, 1, dy + q * a.ld_dy);
+      if (adds) copy(stage, 2, add + q * a.ld_add);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  const auto take = [&](int stage, int matrix, Own<true, T>& o) {
+  const auto take = [&](int stage, int matrix, Own<VEC, T>& o) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(o.p[u].w.x), "=r"(o.p[u].w.y), "=r"(o.p[u].w.z), "=r"(o.p[u].w.w) : "r"(place(stage, matrix, u)) : "memory");
+    for (int u = 0; u < 2; ++u) {
+      uint4& w4 = o.p[u].w;
+      if constexpr (VEC) {
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w4.x), "=r"(w4.y), "=r"(w4.z), "=r"(w4.w) : "r"(place(stage, matrix, u)) : "memory");
+      } else {
+        const uint32_t at = place(stage, matrix, u);
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w4.x) : "r"(at) : "memory");
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w4.y) : "r"(at + BLOCK * 4u) : "memory");
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w4.z) : "r"(at + BLOCK * 8u) : "memory");
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w4.w) : "r"(at + BLOCK * 12u) : "memory");
+      }
+    }
   };
 #pragma unroll
   for (int k = 0; k < AHEAD; ++k) request(r + k * step, k);
@@ -366,7 +390,7 @@ __global__ void __launch_bounds__(grad_block<TPR>, ring_blocks<T, TPR>) layer_no
     const float m = mn, rs = rn;
     request(r + AHEAD * step, stage == 0 ? STAGES - 1 : stage - 1);
     asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
-    Own<true, T> xo, go, ao;
+    Own<VEC, T> xo, go, ao;
     if (in) {
       take(stage, 0, xo); take(stage, 1, go);
       if (adds) take(stage, 2, ao);
@@ -399,7 +423,7 @@ __global__ void __launch_bounds__(grad_block<TPR>, ring_blocks<T, TPR>) layer_no
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   __syncthreads();
-  if (a.sums) leave_sums<true, T, TPR, BLOCK>(a, sw, sb, (float*)ring, blockIdx.x, 0, cols);
+  if (a.sums) leave_sums<VEC, T, TPR, BLOCK>(a, sw, sb, (float*)ring, blockIdx.x, 0, cols);
 }
 
 // Rows of more than 8192 columns: the two means of a row by a kernel of their own, then blocks of columns that walk a share of the rows.
@@ -477,12 +501,12 @@ __global__ void __launch_bounds__(1024) layer_norm_sums_kernel(int blocks, int c
 // How a backward pass is cut: threads a row (0: long rows), and the blocks that leave partial sums.
 struct NormGradPlan { int tpr; int64_t blocks; };
 template <class T>
-NormGradPlan norm_grad_plan(int64_t rows, int cols, bool vec) {
+NormGradPlan norm_grad_plan(int64_t rows, int cols) {
   NormGradPlan p{0, 0};
   for (int t = 8; t <= 8192 / kOwn<T>; t *= 2)
     if (cols <= t * kOwn<T>) { p.tpr = t; break; }
   if (p.tpr) {
-    const int block = p.tpr > 256 ? p.tpr : 256, per = block / p.tpr, threads = vec ? ring_threads<T> : grad_threads<T>;
+    const int block = p.tpr > 256 ? p.tpr : 256, per = block / p.tpr, threads = ring_threads<T>;
     const int resident = threads / block > 0 ? threads / block : 1;
     const int64_t want = (rows + per - 1) / per, most = 148LL * resident;
     p.blocks = want < most ? want : most;
@@ -494,8 +518,8 @@ NormGradPlan norm_grad_plan(int64_t rows, int cols, bool vec) {
 }
 template <class T>
 int64_t norm_grad_floats(int64_t rows, int cols) {
-  const NormGradPlan p = norm_grad_plan<T>(rows, cols, false), q = norm_grad_plan<T>(rows, cols, true);
-  return (p.blocks > q.blocks ? p.blocks : q.blocks) * 2 * cols + (p.tpr ? 0 : 2 * rows);
+  const NormGradPlan p = norm_grad_plan<T>(rows, cols);
+  return p.blocks * 2 * cols + (p.tpr ? 0 : 2 * rows);
 }
 
 struct NormCall {
@@ -536,19 +560,18 @@ cudaError_t run_norm(const NormCall& a) {
 
 template <class T, class W, int TPR>
 cudaError_t norm_grad_as(const NormGradArgs& g, bool vec, int64_t blocks, cudaStream_t st) {
-  if (vec) {
-    static std::atomic<signed char> ready[64];
-    auto* const k = layer_norm_grad_ring_kernel<T, W, TPR>;
-    if (!once_per_device(ready, [&] { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes<T, TPR>) == cudaSuccess; })) return cudaErrorInvalidDevice;
-    return launch_pdl_grid(k, dim3((unsigned)blocks), grad_block<TPR>, ring_bytes<T, TPR>, st, g);
-  }
-  return launch_pdl_grid(layer_norm_grad_kernel<T, W, TPR>, dim3((unsigned)blocks), grad_block<TPR>, 0, st, g);
+  if constexpr (sizeof(T) == 2)
+    if (!vec) return launch_pdl_grid(layer_norm_grad_kernel<T, W, TPR>, dim3((unsigned)blocks), grad_block<TPR>, 0, st, g);
+  auto* const k = vec ? layer_norm_grad_ring_kernel<T, W, TPR, true> : layer_norm_grad_ring_kernel<T, W, TPR, sizeof(T) == 2>;
+  static std::atomic<signed char> ready[2][64];
+  if (!once_per_device(ready[vec], [&] { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes<T, TPR>) == cudaSuccess; })) return cudaErrorInvalidDevice;
+  return launch_pdl_grid(k, dim3((unsigned)blocks), grad_block<TPR>, ring_bytes<T, TPR>, st, g);
 }
 template <class T, class W>
 cudaError_t run_norm_grad(const NormCall& a) {
   NormGradArgs g{a.rows, a.cols, a.dy, a.x, a.w, a.add, a.y, a.ld_dy, a.ldx, a.ld_add, a.ldy, a.mean, a.rstd, (float*)a.ws, nullptr, a.dw || a.db};
   const bool vec = wide_ok(a.dy, a.ld_dy, a.type) && wide_ok(a.x, a.ldx, a.type) && wide_ok(a.add, a.ld_add, a.type) && wide_ok(a.y, a.ldy, a.type);
-  const NormGradPlan plan = norm_grad_plan<T>(a.rows, a.cols, vec);
+  const NormGradPlan plan = norm_grad_plan<T>(a.rows, a.cols);
   cudaError_t e = cudaSuccess;
   if (a.rows > 0 && (g.sums || g.dx)) {
     switch (plan.tpr) {

@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes as C
 import threading
+from array import array
 
 import torch
 
@@ -143,7 +144,7 @@ def layer_norm_grad(dy, x, mean, rstd, weight=None, add=None, stream=None):
     wtype = dtype if weight is None else weight.dtype
     handle = lib()
     n = handle.gn_layer_norm_grad_workspace(rows, cols)
-    dx, ws = x.new_empty(rows, cols), x.new_empty(n, dtype=torch.uint8)
+    dx, ws = x.new_empty(rows, cols), x.new_empty(n // x.element_size())
     if wtype is dtype:
         dw, db = x.new_empty(cols), x.new_empty(cols)
     else:
@@ -184,7 +185,7 @@ def dropout(x, p, key, step=0, residual=None, device_step=None, stream=None):
     return y
 
 
-_Args = C.c_int64 * 27          # gn_ffn: type and act, rows, cols and inner, then pointer and leading dimension of twelve matrices
+_REST = [(0,) * (24 - 2 * k) for k in range(13)]       # gn_ffn: the members behind the k-th of its twelve matrices
 
 
 def _ffn_inputs(x, w_gate, w_up, w_down, act):
@@ -201,12 +202,15 @@ def _ffn_inputs(x, w_gate, w_up, w_down, act):
     return dtype, dev, rows, cols, inner, words
 
 
-def _ffn_call(fn, backward, x, dev, words):
-    args = _Args(*words)
-    n = lib().gn_gated_ffn_workspace(args, backward)
-    ws = x.new_empty(max(n, 16), dtype=torch.uint8)
+def _ffn_call(fn, backward, x, dev, words, mats):
+    """gn_ffn as 27 words: type and act, rows, cols and inner, then pointer and leading dimension of twelve matrices."""
+    words.extend(_REST[mats])
+    args = array("q", words)
+    at = args.buffer_info()[0]
+    n = lib().gn_gated_ffn_workspace(at, backward)
+    ws = x.new_empty(max(n, 16) // x.element_size())
     err = _err()
-    status = fn(args, ws.data_ptr(), n, _raw_stream(dev), err, 200)
+    status = fn(at, ws.data_ptr(), n, _raw_stream(dev), err, 200)
     if status:
         _checked(status, err)
 
@@ -222,11 +226,11 @@ def gated_ffn(x, w_gate, w_up, w_down, act="silu", save=False, stream=None):
     y = x.new_empty(rows, cols)
     words += (y.data_ptr(), cols)
     if not save:
-        _ffn_call(lib().gn_gated_ffn, 0, x, dev, words)
+        _ffn_call(lib().gn_gated_ffn, 0, x, dev, words, 5)
         return y
     gate, up = x.new_empty(rows, inner), x.new_empty(rows, inner)
     words += (gate.data_ptr(), inner, up.data_ptr(), inner)
-    _ffn_call(lib().gn_gated_ffn, 0, x, dev, words)
+    _ffn_call(lib().gn_gated_ffn, 0, x, dev, words, 7)
     return y, gate, up
 
 
@@ -239,7 +243,7 @@ def gated_ffn_grad(dy, x, gate, up, w_gate, w_up, w_down, act="silu", stream=Non
     dx = x.new_empty(rows, cols)
     dwg, dwu, dwd = x.new_empty(inner, cols), x.new_empty(inner, cols), x.new_empty(cols, inner)
     words += (dx.data_ptr(), cols, dwg.data_ptr(), cols, dwu.data_ptr(), cols, dwd.data_ptr(), inner)
-    _ffn_call(lib().gn_gated_ffn_grad, 1, x, dev, words)
+    _ffn_call(lib().gn_gated_ffn_grad, 1, x, dev, words, 12)
     return dx, dwg, dwu, dwd
 
 

@@ -29,10 +29,14 @@ constexpr int kFfnGroup = 4;     // problems of one launch (FFN_STORE)
 int64_t ffn_pair_workspace(const FfnGemm* g, int n);
 cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, void* ws, int* err, cudaStream_t st);
 
-// One product with few tokens (gemm_narrow16.cu): M <= kFfnNarrow, A K-major.  early: the kernel before it on the stream is one of these
+// One product with few tokens (gemm_narrow16.cu): A K-major.  early: the kernel before it on the stream is one of these
 // kernels, of the same call, that writes none of the right operands.
-constexpr int kFfnNarrow = 128;
 cudaError_t launch_ffn_narrow(FfnKind kind, bool bf16, int act, const FfnGemm& g, bool early, int* err, cudaStream_t st);
+// Estimated times, to choose between the two: of a product of M = tokens and N = features (K terms, of both operand pairs), and of a list of FFN_STORE products.
+constexpr int kFfnNarrow = 128;          // tokens up to which the choice is the narrow form without a look
+double ffn_narrow_us(FfnKind kind, int tokens, int features, int K);
+double ffn_pair_us(FfnKind kind, int M, int N, int K);
+double ffn_pair_list_us(const FfnGemm* g, int n);
 
 // One FP32 product of the forward pass with at most kFfnDot tokens on FMAs (ffn_dot.cu): d[0] = x w[0]^T, or with w[1] act(x w[0]^T) * (x w[1]^T) and
 // the two projections to d[1], d[2] (optional).  Any alignment.

@@ -169,8 +169,19 @@ int plain_products(const gn_ffn& f, bool backward, const Half& w, FfnGemm (&list
   weights(f.cols, f.inner, w.dy, in16(w.h), f.dw_down);
   return n;
 }
-// Of those, the first ones go to the kernel for few tokens, the others to the pairs' as one launch.
-int few_token_products(const gn_ffn& f, bool backward) { return f.rows <= kFfnNarrow && (!backward || f.dx.p) ? 1 : 0; }
+// Which products go to the kernel for few tokens: the call's first one, and the first of the list above (y, or dx).  By sizes alone.
+struct Few { bool first; int listed; };
+Few few_tokens(const gn_ffn& f, bool backward, const FfnGemm* list, int n) {
+  const FfnKind kind = backward ? FFN_GRAD : FFN_GATE;
+  const bool candidate = !backward || f.dx.p;              // (a weight's gradient has a long K and many rows: never)
+  if (f.rows <= kFfnNarrow) return {true, candidate ? 1 : 0};
+  if (f.rows > 4096) return {false, 0};
+  const int R = (int)f.rows;
+  Few c{ffn_narrow_us(kind, R, f.inner, f.cols) < ffn_pair_us(kind, R, f.inner, f.cols), 0};
+  if (candidate && n > 0)
+    c.listed = ffn_narrow_us(FFN_STORE, R, f.cols, list[0].K[0] + list[0].K[1]) + ffn_pair_list_us(list + 1, n - 1) < ffn_pair_list_us(list, n) ? 1 : 0;
+  return c;
+}
 
 int64_t lay_out_half(const gn_ffn& f, bool backward, char* base, Half& w) {
   Workspace ws{base};
@@ -190,7 +201,7 @@ int64_t lay_out_half(const gn_ffn& f, bool backward, char* base, Half& w) {
     *o = {ws.take(f.rows * ld * 2), ld};
   }
   FfnGemm list[kFfnGroup];
-  const int n = plain_products(f, backward, w, list), few = few_token_products(f, backward);
+  const int n = plain_products(f, backward, w, list), few = f.rows > 0 ? few_tokens(f, backward, list, n).listed : 0;
   w.sums = f.rows > 0 && n > few ? ws.take(ffn_pair_workspace(list + few, n - few)) : nullptr;
   return ws.used;
 }
@@ -202,9 +213,9 @@ cudaError_t pack(const Half& w, cudaStream_t st) {
 }
 
 cudaError_t run_half(const gn_ffn& f, bool backward, const Half& w, int* err, cudaStream_t st) {
-  const bool bf16 = f.type == GN_BF16, narrow = f.rows <= kFfnNarrow;
+  const bool bf16 = f.type == GN_BF16;
   FfnGemm list[kFfnGroup], a;
-  const int n = plain_products(f, backward, w, list), few = few_token_products(f, backward);
+  const int n = plain_products(f, backward, w, list);
   if (n == 0) return cudaSuccess;
   a.M = (int)f.rows; a.N = f.inner; a.K[0] = f.cols;
   a.d[0] = w.h;
@@ -216,6 +227,9 @@ cudaError_t run_half(const gn_ffn& f, bool backward, const Half& w, int* err, cu
     a.A[0] = w.x; a.B[0] = w.w_gate; a.B[1] = w.w_up; a.d[1] = out16(f.gate); a.d[2] = out16(f.up);
   }
   const FfnKind first = backward ? FFN_GRAD : FFN_GATE;
+  const Few choice = few_tokens(f, backward, list, n);
+  const bool narrow = choice.first;
+  const int few = choice.listed;
   cudaError_t e = pack(w, st);
   if (e == cudaSuccess) e = narrow ? launch_ffn_narrow(first, bf16, f.act, a, false, err, st) : launch_ffn_pair(first, bf16, f.act, &a, 1, nullptr, err, st);
   if (e == cudaSuccess && few) e = launch_ffn_narrow(FFN_STORE, bf16, f.act, list[0], true, err, st);

@@ -1,5 +1,6 @@
-// Products of 16-bit matrices for the gated feed-forward block with few tokens (up to 128, one and upwards): bound by reading the weights,
-// so the weights are the rows of the tensor core's tile, 128 of them to a CTA, and the tokens its 16 to 128 columns.
+// Products of 16-bit matrices for the gated feed-forward block with few tokens (one and upwards): bound by reading the weights, so the weights are
+// the rows of the tensor core's tile, 128 of them to a CTA, and the tokens its 16 to 128 columns.  Some hundred tokens take several columns of tiles,
+// where the pairs' 256 x 256 tiles would be too few to fill the GPU.
 //
 // FFN_GATE takes 64 rows of the gate's weights and the same 64 of the up projection's, so that both sums of a hidden unit are in one CTA.
 // Where the tiles are fewer than the SMs, a cluster of up to eight CTAs shares a tile, each with a part of K: the partial sums stay in
@@ -11,7 +12,10 @@
 // first has waited for it before it let this one start): its first slots are filled before it waits for the first.
 // Half of an SM's shared memory to a CTA: with a third (more of the next kernel's CTAs find room early) one token took 38.1 us instead of 37.2 (4096 x
 // 8192 bf16), and weights brought to L2 before the wait cost more than they hid (40.7).
-// Bound by the weights' bytes, 5.4 TB/s there, and by 8 us of two dependent launches: 48 tokens, 2048 x 8192 fp16, 28.5 us, of which the stream is 15.
+// Bound by the weights' bytes, 5.4 TB/s there, and by 8 us of two dependent launches: 48 tokens, 2048 x 8192 fp16, 27.6 us, of which the stream is 15.
+// Tiles of tokens: 256 tokens, 768 x 2048, 14.7 us (29.7 on the pairs' kernel), 256 x 4096 x 8192 60 (76).
+#include <math.h>
+
 #include "ffn_act.cuh"
 #include "ffn_kernels.h"
 #include "tc_common.cuh"
@@ -24,6 +28,7 @@ constexpr int N_A_BYTES = N_BM * N_BK * 2;
 constexpr int N_RING_BYTES = 108 * 1024;        // of stages: two CTAs on an SM
 constexpr int N_STAGES_MAX = 8;
 constexpr int N_SLICES = 8;                     // CTAs of a cluster at most
+constexpr int N_TOKENS = 128;                   // tokens of a tile at most
 
 struct NarrowParams {
   int tokens, features;              // of the result: d[0] [tokens][features]
@@ -45,13 +50,22 @@ __device__ __forceinline__ void narrow_mma(uint32_t d, uint64_t a, uint64_t b, u
       "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
       ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accum) : "memory");
 }
-__device__ __forceinline__ float4 lds_cluster16(uint32_t addr) {
+// (local: the address is one of this CTA's)
+__device__ __forceinline__ float4 lds_cluster16(uint32_t addr, bool local) {
   float4 v;
+  if (local) {
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+  }
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ float2 lds_cluster8(uint32_t addr) {
+__device__ __forceinline__ float2 lds_cluster8(uint32_t addr, bool local) {
   float2 v;
+  if (local) {
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+  }
   asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
   return v;
 }
@@ -96,7 +110,8 @@ __global__ void __launch_bounds__(N_THREADS, 2) ffn_narrow_kernel(const __grid_c
   uint32_t slices, rank;
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(slices));
   asm volatile("mov.u32 %0, %%cluster_ctaid.x;" : "=r"(rank));
-  const int tile = blockIdx.x / slices, f0 = tile * WIDTH;
+  const int f0 = (int)(blockIdx.x / slices) * WIDTH, t0 = (int)blockIdx.y * N_TOKENS;
+  const int tokens_here = min(N_TOKENS, p.tokens - t0);
   const int kb0 = (int)((long long)p.kb * rank / slices), kb1 = (int)((long long)p.kb * (rank + 1) / slices);
   const int stage_bytes = N_A_BYTES + p.n_pad * 128;
 
@@ -136,7 +151,7 @@ __global__ void __launch_bounds__(N_THREADS, 2) ffn_narrow_kernel(const __grid_c
       };
       const auto tokens = [&](int kb, int s) {
         const int second = kb >= p.kb0 ? 1 : 0, k0 = (second ? kb - p.kb0 : kb) * N_BK;
-        tma_load_2d(smem + s * stage_bytes + N_A_BYTES, &maps.m[KIND == FFN_GATE ? 1 : 2 * second + 1], k0, 0, &full[s]);
+        tma_load_2d(smem + s * stage_bytes + N_A_BYTES, &maps.m[KIND == FFN_GATE ? 1 : 2 * second + 1], k0, t0, &full[s]);
       };
       const int head = p.early ? min(p.stages, kb1 - kb0) : 0;   // slots whose weights do not wait for the kernel before
       for (int i = 0; i < head; ++i) {
@@ -202,30 +217,27 @@ __global__ void __launch_bounds__(N_THREADS, 2) ffn_narrow_kernel(const __grid_c
   constexpr int EACH = KIND == FFN_GATE ? 2 : 4;                 // columns of a thread
   const uint32_t mine = smem_u32(sums) + (uint32_t)(EACH * lane) * 4;
   const int first = (int)rank + (int)slices * warp, step = (int)slices * N_WARPS;
-  float4 v[N_SLICES];                                            // FFN_GATE: two sums of the gate, two of the up projection
-  const auto request = [&](int t) {
+  const auto finish = [&](auto n_slices, auto act) {
+    constexpr int S = decltype(n_slices)::value, ACT = decltype(act)::value;
+    float4 v[S];                                                 // FFN_GATE: two sums of the gate, two of the up projection
+    const auto request = [&](int t) {
 #pragma unroll
-    for (uint32_t q = 0; q < N_SLICES; ++q) {
-      v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (q < slices) {
-        const uint32_t at = map_to_cta(mine + (uint32_t)t * (N_BM * 4), q);
+      for (int q = 0; q < S; ++q) {
+        const uint32_t here = mine + (uint32_t)t * (N_BM * 4), at = S == 1 ? here : map_to_cta(here, (uint32_t)q);
         if constexpr (KIND == FFN_GATE) {
-          const float2 a = lds_cluster8(at), b = lds_cluster8(at + 256);
+          const float2 a = lds_cluster8(at, S == 1), b = lds_cluster8(at + 256, S == 1);
           v[q] = make_float4(a.x, a.y, b.x, b.y);
         } else {
-          v[q] = lds_cluster16(at);
+          v[q] = lds_cluster16(at, S == 1);
         }
       }
-    }
-  };
-  if (first < p.tokens) request(first);
-  with_activation(p.act, [&](auto act) {
-    constexpr int ACT = decltype(act)::value;
-    for (int t = first; t < p.tokens; t += step) {
-      float x[4] = {0.f, 0.f, 0.f, 0.f};
+    };
+    if (first < tokens_here) request(first);
+    for (int t = first; t < tokens_here; t += step) {
+      float x[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
 #pragma unroll
-      for (uint32_t q = 0; q < N_SLICES; ++q) { x[0] += v[q].x; x[1] += v[q].y; x[2] += v[q].z; x[3] += v[q].w; }
-      if (t + step < p.tokens) request(t + step);
+      for (int q = 1; q < S; ++q) { x[0] += v[q].x; x[1] += v[q].y; x[2] += v[q].z; x[3] += v[q].w; }
+      if (t + step < tokens_here) request(t + step);
       const int f = f0 + EACH * lane;
       if (f >= p.features) continue;
       if constexpr (KIND == FFN_GATE) {
@@ -236,27 +248,37 @@ __global__ void __launch_bounds__(N_THREADS, 2) ffn_narrow_kernel(const __grid_c
           activation<ACT, true>(g[e], a, unused);
           h[e] = a * u[e];
         }
-        put<T>(p.d[0], t, f, p.features, p.vec, h);
-        if (p.d[1].p) put<T>(p.d[1], t, f, p.features, p.vec, g);
-        if (p.d[2].p) put<T>(p.d[2], t, f, p.features, p.vec, u);
+        put<T>(p.d[0], t0 + t, f, p.features, p.vec, h);
+        if (p.d[1].p) put<T>(p.d[1], t0 + t, f, p.features, p.vec, g);
+        if (p.d[2].p) put<T>(p.d[2], t0 + t, f, p.features, p.vec, u);
       } else if constexpr (KIND == FFN_STORE) {
-        put<T>(p.d[0], t, f, p.features, p.vec, x);
+        put<T>(p.d[0], t0 + t, f, p.features, p.vec, x);
       } else {
         float g[4], u[4], h[4], dg[4], du[4];
-        get4<T>(p.gate, t, f, p.features, p.vec, g);
-        get4<T>(p.up, t, f, p.features, p.vec, u);
+        get4<T>(p.gate, t0 + t, f, p.features, p.vec, g);
+        get4<T>(p.up, t0 + t, f, p.features, p.vec, u);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float a, da;
           activation<ACT, true>(g[e], a, da);
           h[e] = a * u[e]; dg[e] = x[e] * u[e] * da; du[e] = x[e] * a;
         }
-        put<T>(p.d[0], t, f, p.features, p.vec, h);
-        put<T>(p.d[1], t, f, p.features, p.vec, dg);
-        put<T>(p.d[2], t, f, p.features, p.vec, du);
+        put<T>(p.d[0], t0 + t, f, p.features, p.vec, h);
+        put<T>(p.d[1], t0 + t, f, p.features, p.vec, dg);
+        put<T>(p.d[2], t0 + t, f, p.features, p.vec, du);
       }
     }
-  });
+  };
+  const auto by_slices = [&](auto act) {
+    switch (slices) {
+      case 1: finish(ActIs<1>{}, act); break;
+      case 2: finish(ActIs<2>{}, act); break;
+      case 4: finish(ActIs<4>{}, act); break;
+      default: finish(ActIs<N_SLICES>{}, act);
+    }
+  };
+  if constexpr (KIND == FFN_STORE) by_slices(ActIs<GN_ACT_RELU>{});
+  else with_activation(p.act, by_slices);
   cluster_sync_all();                // nobody leaves while others read its sums
   if (warp == 2) {
     tc_fence_after();
@@ -277,6 +299,15 @@ bool make_map16(CUtensorMap* m, const Mat16& a, long long rows, long long cols, 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tiles of features and of tokens, and CTAs to a tile: as many as still find an SM of their own (two of them share one at most), with four k-blocks each at least.
+struct NarrowPlan { int tiles, columns, slices; };
+NarrowPlan plan_narrow(int kind, int tokens, int features, int kb) {
+  const int width = kind == FFN_GATE ? 64 : 128;
+  NarrowPlan p{(features + width - 1) / width, (tokens + N_TOKENS - 1) / N_TOKENS, 1};
+  while (p.slices < N_SLICES && (long long)p.tiles * p.columns * p.slices * 2 <= 2 * num_sms() && kb >= p.slices * 2 * 4) p.slices *= 2;
+  return p;
+}
+
 template <int KIND, class T>
 cudaError_t launch_narrow_as(int act, const FfnGemm& g, bool early, int* err, cudaStream_t st) {
   constexpr bool BF16 = !__is_same(T, __half);
@@ -288,7 +319,7 @@ cudaError_t launch_narrow_as(int act, const FfnGemm& g, bool early, int* err, cu
   NarrowMaps maps;
   NarrowParams p = {};
   p.tokens = g.M; p.features = g.N;
-  p.n_pad = (g.M + 15) / 16 * 16;
+  p.n_pad = g.M < N_TOKENS ? (g.M + 15) / 16 * 16 : N_TOKENS;
   p.cols_tmem = p.n_pad <= 32 ? 32 : p.n_pad <= 64 ? 64 : 128;
   const int stage = N_A_BYTES + p.n_pad * 128;
   p.stages = N_RING_BYTES / stage < N_STAGES_MAX ? N_RING_BYTES / stage : N_STAGES_MAX;
@@ -306,12 +337,9 @@ cudaError_t launch_narrow_as(int act, const FfnGemm& g, bool early, int* err, cu
         !(KIND == FFN_GATE && s ? true : make_map16(&maps.m[2 * s + 1], g.A[a], g.M, K, p.n_pad, BF16)))
       return cudaErrorInvalidValue;
   }
-  // CTAs to a tile: as many as still find an SM of their own (two of them share one at most), with four k-blocks each at least
-  const int tiles = (g.N + WIDTH - 1) / WIDTH;
-  int slices = 1;
-  while (slices < N_SLICES && tiles * slices * 2 <= 2 * num_sms() && p.kb >= slices * 2 * 4) slices *= 2;
+  const NarrowPlan plan = plan_narrow(KIND, p.tokens, p.features, p.kb);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(tiles * slices));
+  cfg.gridDim = dim3((unsigned)(plan.tiles * plan.slices), (unsigned)plan.columns);
   cfg.blockDim = dim3(N_THREADS);
   cfg.dynamicSmemBytes = N_RING_BYTES + 1024;
   cfg.stream = st;
@@ -319,13 +347,22 @@ cudaError_t launch_narrow_as(int act, const FfnGemm& g, bool early, int* err, cu
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)slices; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  attr[1].val.clusterDim.x = (unsigned)plan.slices; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, maps, p);
 }
 
 }  // namespace
+
+// 5 us for a launch, 3 for the ends of a round of CTAs (two on an SM) and 6 for another round's, and the k-blocks of an SM, or of a CTA where it has the SM for
+// itself, 0.33 each: measured at 64 to 2048 tokens, 256 to 4096 columns and 256 to 8192 hidden units, within a fifth.
+double ffn_narrow_us(FfnKind kind, int tokens, int features, int K) {
+  const int kb = (K + N_BK - 1) / N_BK, sms = num_sms();
+  const NarrowPlan p = plan_narrow(kind, tokens, features, kb);
+  const double ctas = (double)p.tiles * p.columns * p.slices, share = (double)p.tiles * p.columns * kb / sms, own = (double)kb / p.slices;
+  return 2.0 + 6.0 * ceil(ctas / (2 * sms)) + 0.33 * (share > own ? share : own);
+}
 
 cudaError_t launch_ffn_narrow(FfnKind kind, bool bf16, int act, const FfnGemm& g, bool early, int* err, cudaStream_t st) {
   if (kind == FFN_GATE) return bf16 ? launch_narrow_as<FFN_GATE, __nv_bfloat16>(act, g, early, err, st) : launch_narrow_as<FFN_GATE, __half>(act, g, early, err, st);

@@ -728,6 +728,13 @@ bool encode_problem(CUtensorMap* maps, const FfnGemm& g, bool gate, bool a_box3,
   return true;
 }
 
+// Width of the tiles: that of the fewer rounds, a round of narrow ones taking a little over half the time of one of wide ones.
+long long pair_rounds(int kind, int M, int N, int bn) {
+  const int width = kind == FFN_GATE ? bn / 2 : bn, pairs = num_sms() / 2;
+  return ((long long)((M + 255) / 256) * ((N + width - 1) / width) + pairs - 1) / pairs;
+}
+int pair_width(int kind, int M, int N) { return pair_rounds(kind, M, N, 128) * 5 < pair_rounds(kind, M, N, 256) * 8 ? 128 : 256; }
+
 template <int KIND, class T, int NP>
 cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStream_t st) {
   constexpr bool BF16 = !__is_same(T, __half);
@@ -739,17 +746,7 @@ cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStrea
   PairParams<NP> q = {};
   q.n = n; q.act = act; q.err = err;
   const int pairs = num_sms() / 2;
-  // width of the tiles: that of the fewer waves, a wave of narrow ones taking a little over half the time of one of wide ones
-  long long cost[2] = {0, 0};
-  for (int w = 0; w < 2; ++w) {
-    long long tiles = 0;
-    for (int i = 0; i < n; ++i) {
-      const int width = (w ? 128 : 256) / (KIND == FFN_GATE ? 2 : 1);
-      tiles += (long long)((g[i].M + 255) / 256) * ((g[i].N + width - 1) / width);
-    }
-    cost[w] = (tiles + pairs - 1) / pairs * (w ? 5 : 8);
-  }
-  const int bn = cost[1] < cost[0] ? 128 : 256;
+  const int bn = pair_width(KIND, g[0].M, g[0].N);
   long long tiles = 0;
   for (int i = 0; i < n; ++i) {
     PairProblem& p = q.p[i];
@@ -773,12 +770,13 @@ cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStrea
 }
 
 // How a group of products is cut: slices of K for each (all 1: none), and the items that makes.  Estimated times, in us: a k-block of a 256 x 512 tile 0.36
-// (a pair by itself as well: it waits for its loads), an item 4 more; a list takes as long as its longest item or its share of all; slices
-// cost a second kernel, 6, and their sums' way out and back at 4 TB/s.
-struct WidePlan { int slices[kFfnGroup]; int items; bool cut; };
+// (a pair by itself as well: it waits for its loads), an item 4 more; a list takes as long as its longest item, its share of all, or its
+// bytes at 5 TB/s; slices cost a second kernel, 6, and their sums' way out and back at 4 TB/s.
+struct WidePlan { int slices[kFfnGroup]; int items; bool cut; double us; };
 WidePlan plan_wide(const FfnGemm* g, int n) {
   const int pairs = num_sms() / 2;
   long long tiles = 0, work = 0;
+  double bytes_us = 0.0;
   int kb[kFfnGroup], tl[kFfnGroup], longest = 0;
   WidePlan best{};
   for (int i = 0; i < n; ++i) {
@@ -787,14 +785,17 @@ WidePlan plan_wide(const FfnGemm* g, int n) {
     tl[i] = (int)(t < 0x1fffffff ? t : 0x1fffffff);
     tiles += t; work += t * kb[i];
     longest = kb[i] > longest ? kb[i] : longest;
+    bytes_us += (((double)g[i].M + g[i].N) * ((double)g[i].K[0] + g[i].K[1]) + (double)g[i].M * g[i].N) * 2.0 / 5e6;
     best.slices[i] = 1;
   }
   const auto list_us = [&](int most, long long items) {
     const double one = most * 0.36 + 4.0, share = (work * 0.36 + items * 4.0) / pairs * (items > pairs ? 1.15 : 1.0);
-    return one > share ? one : share;
+    const double list = one > share ? one : share;
+    return list > bytes_us ? list : bytes_us;
   };
-  if (tiles >= 4 * pairs) return best;
   double best_us = list_us(longest, tiles);
+  best.us = best_us;
+  if (tiles >= 4 * pairs) return best;
   for (int len = longest; len >= 4; len = len > 32 ? len * 7 / 8 : len - 1) {
     WidePlan p{};
     long long items = 0, cut = 0;
@@ -808,7 +809,7 @@ WidePlan plan_wide(const FfnGemm* g, int n) {
     }
     if (items > 8 * pairs) break;
     const double us = list_us(most, items) + 6.0 + cut * (W_SLOT * 4.0 * 2.0 / 4e6);
-    if (cut > 0 && us < 0.9 * best_us) { best_us = us; p.items = (int)items; p.cut = true; best = p; }
+    if (cut > 0 && us < 0.9 * best_us) { best_us = us; p.items = (int)items; p.cut = true; p.us = us; best = p; }
   }
   return best;
 }
@@ -851,6 +852,14 @@ cudaError_t launch_wide_as(const FfnGemm* g, int n, const WidePlan& plan, void* 
 }
 
 }  // namespace
+
+// 8 us for a launch and the last round's epilogue; a k-block 0.40 of a wide tile and 0.28 of a narrow one; an epilogue 7, beside the next round's products.
+double ffn_pair_us(FfnKind kind, int M, int N, int K) {
+  const int bn = pair_width(kind, M, N), kb = (K + P_BK - 1) / P_BK;
+  const double round = kb * (bn == 256 ? 0.40 : 0.28);
+  return 8.0 + round + (pair_rounds(kind, M, N, bn) - 1) * (round > 7.0 ? round : 7.0);
+}
+double ffn_pair_list_us(const FfnGemm* g, int n) { return n > 0 ? plan_wide(g, n).us : 0.0; }
 
 int64_t ffn_pair_workspace(const FfnGemm* g, int n) {
   const WidePlan p = plan_wide(g, n);

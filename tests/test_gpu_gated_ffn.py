@@ -14,7 +14,9 @@ ACTS = ["sigmoid", "silu", "gelu", "gelu_tanh", "relu"]
 SHAPES = [(1, 1, 1), (1, 64, 128), (2, 8, 16), (3, 7, 5), (1, 1000, 3001), (16, 256, 512), (17, 520, 264), (48, 128, 1024), (64, 617, 1201),
           (127, 72, 96), (128, 128, 128), (129, 136, 200), (200, 1024, 384), (255, 520, 1000), (257, 264, 520), (300, 784, 300),
           (513, 96, 2056), (1003, 617, 1201), (2100, 256, 264), (40, 2048, 8192),
-          (5000, 40, 72), (2, 1001, 2003), (7, 64, 4001), (8, 136, 40), (300, 64, 5000)]
+          (5000, 40, 72), (2, 1001, 2003), (7, 64, 4001), (8, 136, 40), (300, 64, 5000),
+          # several tiles of tokens: all of them full, one token in the last, odd rows in all three matrices, and the sizes around a tile's
+          (256, 768, 2048), (385, 512, 1024), (1500, 200, 1000), (130, 1537, 773), (4096, 72, 136), (4097, 136, 72)]
 # an activation's FP32 value is off by a few steps: exp 2, its quotient 2, the products after it
 ACT = 16 * E
 

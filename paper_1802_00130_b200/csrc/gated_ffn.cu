@@ -12,6 +12,7 @@
 #include "ffn_act.cuh"
 #include "ffn_kernels.h"
 #include "gn_kernels.h"
+#include "tc_common.cuh"
 
 namespace gn {
 namespace {
@@ -68,23 +69,32 @@ cudaError_t launch_gate(const Gates& g, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-// Copies of 16-bit matrices with rows that TMA can address.
+// Copies of 16-bit matrices with rows that TMA can address: a warp per 256 columns of a row.
 constexpr int kPackMax = 7;
 struct PackJob { const uint16_t* src; uint16_t* dst; int64_t rows, ld, ld_out; int cols; };
 struct PackList { PackJob j[kPackMax]; };
-__global__ void pack_kernel(const PackList list) {
+__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackList list) {
+  grid_dep_wait();
+  grid_dep_launch();
   const PackJob& j = list.j[blockIdx.y];
-  const int units = (j.cols + 7) / 8;
-  const int64_t n = j.rows * units;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
-    const int64_t r = i / units;
-    const int c = (int)(i - r * units) * 8;
-    const uint16_t* const s = j.src + r * j.ld + c;
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
+  const uint16_t* const src = dep(j.src);
+  const int64_t per_row = (j.cols + 255) / 256, n = j.rows * per_row, step = (int64_t)gridDim.x * 8;
+  int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), r = i / per_row;
+  int part = (int)(i - r * per_row);
+  const int64_t step_r = step / per_row;
+  const int step_part = (int)(step - step_r * per_row);
+  for (; i < n; i += step) {
+    const int c = part * 256 + (threadIdx.x & 31) * 8, left = j.cols - c;
+    if (left > 0) {
+      const uint16_t* const s = src + r * j.ld + c;
+      uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (c + e < j.cols) w[e >> 1] |= (uint32_t)s[e] << (16 * (e & 1));
-    *reinterpret_cast<uint4*>(j.dst + r * j.ld_out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int e = 0; e < 8; ++e)
+        if (e < left) w[e >> 1] |= (uint32_t)__ldg(s + e) << (16 * (e & 1));
+      *reinterpret_cast<uint4*>(j.dst + r * j.ld_out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    r += step_r; part += step_part;
+    if (part >= per_row) { part -= (int)per_row; ++r; }
   }
 }
 
@@ -128,18 +138,18 @@ char* const kNowhere = reinterpret_cast<char*>(256);
 
 // ---- 16-bit types ------------------------------------------------------------------------------
 struct Half {
-  Mat16 x, w_gate, w_up, w_down, dy;      // as TMA reads them
-  Mat16 gate, up;                         // as the gate's gradient reads them: whole groups of eight columns
-  PackList packs; int n_packs; int64_t pack_units;
+  Mat16 x, w_gate, w_up, w_down, dy, gate, up;      // with rows of 16-byte units, as TMA and the gate's gradient read them
+  PackList packs; int n_packs; int64_t pack_warps;
   Out16 h, dgate, dup;
   void* sums;                             // of slices of K
 };
-Mat16 addressable(const gn_mat& m, int64_t rows, int cols, Workspace& ws, Half& w, int group = 1) {
-  if (((uintptr_t)m.p & 15) == 0 && m.ld % 8 == 0 && cols % group == 0) return {m.p, m.ld};
+Mat16 addressable(const gn_mat& m, int64_t rows, int cols, Workspace& ws, Half& w) {
+  if (((uintptr_t)m.p & 15) == 0 && m.ld % 8 == 0) return {m.p, m.ld};
   const int64_t ld = up8(cols);
   void* const dst = ws.take(rows * ld * 2);
   w.packs.j[w.n_packs++] = {(const uint16_t*)m.p, (uint16_t*)dst, rows, m.ld, ld, cols};
-  if (rows * (ld / 8) > w.pack_units) w.pack_units = rows * (ld / 8);
+  const int64_t warps = rows * ((cols + 255) / 256);
+  if (warps > w.pack_warps) w.pack_warps = warps;
   return {dst, ld};
 }
 inline Mat16 in16(const Out16& m) { return {m.p, m.ld}; }
@@ -193,8 +203,8 @@ int64_t lay_out_half(const gn_ffn& f, bool backward, char* base, Half& w) {
   w.w_down = addressable(f.w_down, f.cols, f.inner, ws, w);
   if (backward) {
     w.dy = addressable(f.dy, f.rows, f.cols, ws, w);
-    w.gate = addressable(f.gate, f.rows, f.inner, ws, w, 8);
-    w.up = addressable(f.up, f.rows, f.inner, ws, w, 8);
+    w.gate = addressable(f.gate, f.rows, f.inner, ws, w);
+    w.up = addressable(f.up, f.rows, f.inner, ws, w);
   }
   for (Out16* o : {&w.h, &w.dgate, &w.dup}) {
     if (o != &w.h && !backward) break;
@@ -207,9 +217,8 @@ int64_t lay_out_half(const gn_ffn& f, bool backward, char* base, Half& w) {
 }
 cudaError_t pack(const Half& w, cudaStream_t st) {
   if (w.n_packs == 0) return cudaSuccess;
-  const int64_t blocks = (w.pack_units + 255) / 256;
-  pack_kernel<<<dim3((unsigned)(blocks < 1184 ? blocks : 1184), (unsigned)w.n_packs), 256, 0, st>>>(w.packs);
-  return cudaGetLastError();
+  const int64_t blocks = (w.pack_warps + 7) / 8;
+  return launch_pdl_grid(pack_kernel, dim3((unsigned)(blocks < 1184 ? blocks : 1184), (unsigned)w.n_packs), 256, 0, st, w.packs);
 }
 
 cudaError_t run_half(const gn_ffn& f, bool backward, const Half& w, int* err, cudaStream_t st) {

@@ -37,7 +37,7 @@ constexpr int P_PANELS = 8;       // tiles are walked in strips of so many row p
 struct PairProblem {
   int M, N, bn, tiles_m, tiles_n, tiles;
   int kb0, kb;                    // k-blocks of the first operand pair, of both
-  int a_mn, b_mn, vec;            // vec: every matrix of the epilogue takes 16-byte accesses
+  int a_mn, b_mn, vec;            // vec: bit k: 16-byte accesses for d[k]
   int a_box3, b_box3;             // an MN-major operand of whole 64-column chunks: one box of several chunks instead of a box each
   Out16 d[3];
   Mat16 gate, up;
@@ -102,12 +102,18 @@ __device__ __forceinline__ uint32_t stg_at(uint32_t stg, int row, int unit) {
   return stg + (uint32_t)(row * 16 * U + ((unit ^ (U == 8 ? row & 7 : row >> 1 & 3)) << 4));
 }
 
+__device__ __forceinline__ uint16_t lds2(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
+  return v;
+}
 // This thread's row of a chunk, 8 U elements in 4 U words, to rows m0.. (of M) and columns n0.. (of N) of a matrix, by way of the staging tile, ROWS rows at
-// a time.  vec: 16 bytes an access.  Else a row's words of four bytes, from its first element that is at such a word on, one to a lane.
+// a time, in stores of 16 bytes.  vec: the rows' chunks start where such a store may.  Else a store's 16 bytes are put together from two units of the
+// staging tile, and the up to seven elements before a row's first such place, and those after its last, go one by one.
+// 8000 tokens, 1001 columns, 3001 hidden units forward: 172 us where no matrix is aligned (228 in words of four bytes, a row at a time), 143 where all are.
 template <int U, int ROWS>
-__device__ __forceinline__ void put_chunk(const uint32_t (&w)[4 * U], uint32_t stg, int lane, void* base, int64_t ld, int m0, int M, int n0, int N, int vec) {
-  const bool whole = vec && n0 + 8 * U <= N;
-  const int cols = min(8 * U, N - n0);
+__device__ __forceinline__ void put_chunk(const uint32_t (&w)[4 * U], uint32_t stg, int lane, void* base, int64_t ld, int m0, int M, int n0, int N, bool vec) {
+  const int cols = min(8 * U, N - n0), unit = lane % U;
 #pragma unroll
   for (int r0 = 0; r0 < 32; r0 += ROWS) {
     if (ROWS == 32 || lane / ROWS == r0 / ROWS) {
@@ -115,35 +121,37 @@ __device__ __forceinline__ void put_chunk(const uint32_t (&w)[4 * U], uint32_t s
       for (int q = 0; q < U; ++q) sts16(stg_at<U>(stg, lane % ROWS, q), make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]));
     }
     __syncwarp();
-    if (whole) {
-      const int unit = lane % U;
+    uint16_t* const at = reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + r0) * ld + n0;
+    if (vec) {
+      if (unit * 8 + 8 <= cols) {
 #pragma unroll
+        for (int it = 0; it < ROWS * U / 32; ++it) {
+          const int row = it * (32 / U) + lane / U;
+          const uint4 v = lds16(stg_at<U>(stg, row, unit));
+          if (m0 + r0 + row < M) *reinterpret_cast<uint4*>(at + (int64_t)row * ld + unit * 8) = v;
+        }
+      }
+      if (lane < ROWS && m0 + r0 + lane < M)
+        for (int e = cols & ~7; e < cols; ++e) at[(int64_t)lane * ld + e] = lds2(stg_at<U>(stg, lane, e >> 3) + (e & 7) * 2u);
+    } else {
+#pragma unroll 2
       for (int it = 0; it < ROWS * U / 32; ++it) {
         const int row = it * (32 / U) + lane / U;
-        const uint4 v = lds16(stg_at<U>(stg, row, unit));
-        if (m0 + r0 + row < M) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + r0 + row) * ld + n0 + unit * 8) = v;
-      }
-    } else {
-      for (int g = 0; g < ROWS && m0 + r0 + g < M; g += 8) {           // eight rows' words in flight
-        uint32_t v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          v[k] = 0;
-          if (lane < 4 * U) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v[k]) : "r"(stg_at<U>(stg, g + k, lane >> 2) + (lane & 3) * 4u) : "memory");
+        if (m0 + r0 + row >= M) break;
+        uint16_t* const p = at + (int64_t)row * ld;
+        const int head = min(cols, (int)(-(reinterpret_cast<uintptr_t>(p) >> 1) & 7)), wholes = (cols - head) >> 3;
+        if (unit < wholes) {
+          const uint4 x = lds16(stg_at<U>(stg, row, unit)), y = lds16(stg_at<U>(stg, row, unit + (head > 0)));
+          const bool two = head & 4, one = head & 2;
+          const uint32_t a0 = two ? x.z : x.x, a1 = two ? x.w : x.y, a2 = two ? y.x : x.z, a3 = two ? y.y : x.w, a4 = two ? y.z : y.x, a5 = two ? y.w : y.y;
+          const uint32_t b0 = one ? a1 : a0, b1 = one ? a2 : a1, b2 = one ? a3 : a2, b3 = one ? a4 : a3, b4 = one ? a5 : a4;
+          const uint32_t by = (head & 1) * 16;
+          *reinterpret_cast<uint4*>(p + head + unit * 8) =
+              make_uint4(__funnelshift_r(b0, b1, by), __funnelshift_r(b1, b2, by), __funnelshift_r(b2, b3, by), __funnelshift_r(b3, b4, by));
         }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          if (m0 + r0 + g + k >= M) break;
-          uint16_t* const p = reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + r0 + g + k) * ld + n0;
-          const int odd = (int)(reinterpret_cast<uintptr_t>(p) >> 1 & 1);          // (the same for the whole warp)
-          if (odd) {
-            const uint32_t next = __shfl_down_sync(0xffffffffu, v[k], 1);
-            if (lane == 0) p[0] = (uint16_t)v[k];
-            v[k] = v[k] >> 16 | next << 16;
-          }
-          const int e = 2 * lane + odd;
-          if (e + 1 < cols) *reinterpret_cast<uint32_t*>(p + e) = v[k];
-          else if (e < cols) p[e] = (uint16_t)v[k];
+        for (int i = unit; i < cols - 8 * wholes; i += U) {
+          const int e = i < head ? i : 8 * wholes + i;
+          p[e] = lds2(stg_at<U>(stg, row, e >> 3) + (e & 7) * 2u);
         }
       }
     }
@@ -163,7 +171,7 @@ __device__ __forceinline__ void put_whole(const uint32_t* w, uint32_t stg, int l
   }
   __syncwarp();
 }
-// The other way, of a matrix whose rows can be read in whole units of eight columns: four units of a chunk of 32 columns, eight rows apart, as a
+// The other way, of a matrix whose rows start where an access of 16 bytes may: four units of a chunk of 32 columns, eight rows apart, as a
 // warp's accesses cover them; then by rows.
 __device__ __forceinline__ void fetch_chunk(uint4 (&v)[4], int lane, const void* base, int64_t ld, int m0, int M, int n0, int N) {
   const int n = n0 + (lane & 3) * 8;
@@ -171,7 +179,19 @@ __device__ __forceinline__ void fetch_chunk(uint4 (&v)[4], int lane, const void*
   for (int it = 0; it < 4; ++it) {
     const int m = m0 + it * 8 + (lane >> 2);
     v[it] = make_uint4(0u, 0u, 0u, 0u);
-    if (m < M && n < N) v[it] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(base) + (int64_t)m * ld + n));
+    if (m >= M || n >= N) continue;
+    const uint16_t* const p = reinterpret_cast<const uint16_t*>(base) + (int64_t)m * ld + n;
+    if (n + 8 <= N) {
+      v[it] = __ldg(reinterpret_cast<const uint4*>(p));
+    } else {
+      unsigned long long half[2] = {0, 0};
+#pragma unroll 1
+      for (int e = N - n - 1; e >= 0; --e) {               // (the last one read is the lowest)
+        half[1] = half[1] << 16 | half[0] >> 48;
+        half[0] = half[0] << 16 | __ldg(p + e);
+      }
+      v[it] = make_uint4((uint32_t)half[0], (uint32_t)(half[0] >> 32), (uint32_t)half[1], (uint32_t)(half[1] >> 32));
+    }
   }
 }
 __device__ __forceinline__ void turn_chunk(const uint4 (&v)[4], uint32_t stg, int lane, uint32_t (&w)[16]) {
@@ -366,9 +386,9 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
                 uw[16 * h + i] = pack2<T>(uv[2 * i], uv[2 * i + 1]);
               }
             }
-            put_chunk<U, 32>(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
-            if (p.d[1].p) put_chunk<U, 32>(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
-            if (p.d[2].p) put_chunk<U, 32>(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
+            put_chunk<U, 32>(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec & 1);
+            if (p.d[1].p) put_chunk<U, 32>(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec & 2);
+            if (p.d[2].p) put_chunk<U, 32>(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec & 4);
           } else {
             turn_chunk(gx, stg, lane, gw);
             turn_chunk(ux, stg, lane, uw);
@@ -389,9 +409,9 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
               gw[i] = pack2<T>(d0 * up.x * s0, d1 * up.y * s1);
               uw[i] = pack2<T>(d0 * a0, d1 * a1);
             }
-            put_chunk<U, 32>(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec);
-            put_chunk<U, 32>(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec);
-            put_chunk<U, 32>(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec);
+            put_chunk<U, 32>(w, stg, lane, p.d[0].p, p.d[0].ld, m0, p.M, nc, p.N, p.vec & 1);
+            put_chunk<U, 32>(gw, stg, lane, p.d[1].p, p.d[1].ld, m0, p.M, nc, p.N, p.vec & 2);
+            put_chunk<U, 32>(uw, stg, lane, p.d[2].p, p.d[2].ld, m0, p.M, nc, p.N, p.vec & 4);
           }
         }
       });
@@ -639,7 +659,7 @@ ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
             put_whole(x[c], stg, lane, p.d.p, p.d.ld, m0, p.M, n);
             put_whole(x[c] + 16, stg, lane, p.d.p, p.d.ld, m0, p.M, n + 32);
           } else {
-            put_chunk<8, 16>(x[c], stg, lane, p.d.p, p.d.ld, m0, p.M, n, p.N, 0);
+            put_chunk<8, 16>(x[c], stg, lane, p.d.p, p.d.ld, m0, p.M, n, p.N, p.vec);
           }
         }
     }
@@ -761,7 +781,7 @@ cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStrea
     p.a_box3 = p.a_mn && p.M % 64 == 0; p.b_box3 = p.b_mn && p.N % 64 == 0;
     for (int k = 0; k < 3; ++k) p.d[k] = g[i].d[k];
     p.gate = g[i].gate; p.up = g[i].up;
-    p.vec = vec16(p.d[0]) && vec16(p.d[1]) && vec16(p.d[2]);
+    p.vec = vec16(p.d[0]) | vec16(p.d[1]) << 1 | vec16(p.d[2]) << 2;
     if (!encode_problem(maps.m[i], g[i], KIND == FFN_GATE, p.a_box3, p.b_box3, bn / 2, BF16)) return cudaErrorInvalidValue;
   }
   q.tiles = (int)tiles;

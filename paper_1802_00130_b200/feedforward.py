@@ -219,6 +219,7 @@ def gated_ffn(x, w_gate, w_up, w_down, act="silu", save=False, stream=None):
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T; with `save` (y, gate, up), the two projections for the backward pass.
 
     x [rows][cols], w_gate and w_up [inner][cols], w_down [cols][inner]; act: "sigmoid", "silu", "gelu", "gelu_tanh" or "relu".
+    gate and up are views of wider buffers where their 16-bit rows would not start on 16 bytes otherwise.
     """
     dtype, dev, rows, cols, inner, words = _ffn_inputs(x, w_gate, w_up, w_down, act)
     if stream is not None or dev != _device():
@@ -228,8 +229,12 @@ def gated_ffn(x, w_gate, w_up, w_down, act="silu", save=False, stream=None):
     if not save:
         _ffn_call(lib().gn_gated_ffn, 0, x, dev, words, 5)
         return y
-    gate, up = x.new_empty(rows, inner), x.new_empty(rows, inner)
-    words += (gate.data_ptr(), inner, up.data_ptr(), inner)
+    if dtype is not torch.float32 and inner % 8:     # rows that start on 16 bytes: the backward pass reads them without a copy
+        ld = (inner + 7) // 8 * 8
+        gate, up = x.new_empty(rows, ld)[:, :inner], x.new_empty(rows, ld)[:, :inner]
+    else:
+        ld, gate, up = inner, x.new_empty(rows, inner), x.new_empty(rows, inner)
+    words += (gate.data_ptr(), ld, up.data_ptr(), ld)
     _ffn_call(lib().gn_gated_ffn, 0, x, dev, words, 7)
     return y, gate, up
 

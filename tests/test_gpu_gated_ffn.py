@@ -236,6 +236,27 @@ def test_what_is_left_alone_and_outputs_not_wanted(t, rows, cols, inner, pad):
         compare(out)
 
 
+@pytest.mark.parametrize("pad", [0, 1, 3])
+@pytest.mark.parametrize("rows,cols,inner", [(4200, 130, 203), (700, 1001, 1300)])
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+def test_large_tiles_of_unaligned_rows(t, rows, cols, inner, pad):
+    """Rows of outputs that start at every even byte of 16, in whole and in cut chunks of columns, and what lies around them."""
+    kind, t = {"bf16": 1, "f16": 2}[t], TYPES[t]
+    x, w = inputs(rows, cols, inner, t)
+    dy = rand((rows, cols), t, 9)
+    shapes = dict(y=(rows, cols), gate=(rows, inner), up=(rows, inner), dx=(rows, cols), dw_gate=(inner, cols), dw_up=(inner, cols), dw_down=(cols, inner))
+    ins = dict(x=x, w_gate=w[0], w_up=w[1], w_down=w[2])
+    whole = {n: torch.full(((s[0] + 2) * (s[1] + pad) + 1,), 7.0, dtype=t, device="cuda") for n, s in shapes.items()}
+    out = {n: b[1:].view(shapes[n][0] + 2, shapes[n][1] + pad) for n, b in whole.items()}        # (bases off by one element)
+    got = {n: b[:shapes[n][0], :shapes[n][1]] for n, b in out.items()}
+    raw(0, kind, 2, rows, cols, inner, dict(ins, **{n: out[n] for n in ("y", "gate", "up")}))
+    check_forward([got[n] for n in ("y", "gate", "up")], x, w, "gelu", t)
+    raw(1, kind, 2, rows, cols, inner, dict(ins, dy=dy, **{n: out[n] for n in shapes if n != "y"}))
+    check_backward([got[n] for n in ("dx", "dw_gate", "dw_up", "dw_down")], dy, x, got["gate"], got["up"], w, "gelu", t)
+    for n, (r, c) in shapes.items():
+        assert whole[n][0] == 7 and bool((out[n][r:] == 7).all()) and bool((out[n][:, c:] == 7).all()), n
+
+
 def test_refusals():
     x, w = inputs(4, 16, 24, torch.bfloat16)
     _, gate, up = gn.gated_ffn(x, *w, save=True)
@@ -248,6 +269,14 @@ def test_refusals():
                 lambda: gn.gated_ffn_grad(x[:3], x, gate, up, *w), lambda: gn.gated_ffn_grad(x, x, gate[:, :8], up, *w)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_saved_rows_start_on_16_bytes():
+    for t in (torch.bfloat16, torch.float32):
+        x, w = inputs(5, 16, 27, t)
+        _, gate, up = gn.gated_ffn(x, *w, save=True)
+        for m in (gate, up):
+            assert m.shape == (5, 27) and m.stride(1) == 1 and m.stride(0) == (27 if t is torch.float32 else 32)
 
 
 def test_status_after_calls():

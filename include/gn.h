@@ -473,7 +473,8 @@ gn_status gn_thin_m_gemm_noalloc(int M, int N, int64_t rows, const float* dA, in
  * Inputs and outputs do not overlap unless a call says so.  Rows behind the last, and what lies between a row's end and the next row, is
  * neither read into a result nor written.  rows == 0 is a call without rows: sums over rows are zero.
  * ERRORS.  Arguments are checked before anything is launched; a failure's reason goes to errbuf (optional, errbuf_len bytes).
- * Results are the same bits from one call to the next on the same operands.
+ * Results are the same bits from one call to the next with the same arguments (the order of a sum depends on sizes, types, alignment and on
+ * which outputs are wanted, never on the data or on timing).
  * ====================================================================================================== */
 
 typedef enum { GN_F32 = 0, GN_BF16 = 1, GN_F16 = 2 } gn_dtype;

@@ -1,6 +1,7 @@
-// Products of the gated feed-forward block's forward pass in FP32 with at most eight tokens, on FMAs.
+// Products of the gated feed-forward block's forward pass in FP32 with few tokens, on FMAs.
 //
-// Bound by reading the weights once (two FP16 parts of them would be written and read again): a warp takes R rows of them at a time and walks K with 16
+// Up to eight tokens bound by reading the weights once (two FP16 parts of them would be written and read again), with more of them, eight to a block, by the loads
+// and by the sums at the end; what it saves there is launches.  A warp takes R rows of the weights at a time and walks K with 16
 // bytes a lane from each (single elements, as many to a step, where rows are not 16-byte aligned), the tokens' values from L1, all of a step's loads
 // before its first product.  Each lane's sums are added across the warp at the end.
 #include "ffn_act.cuh"
@@ -25,7 +26,8 @@ __global__ void __launch_bounds__(32 * D_WARPS) ffn_dot_kernel(const __grid_cons
   grid_dep_wait();
   grid_dep_launch();
   if (f0 >= p.features) return;
-  const float* const x = (const float*)dep(p.x);
+  const int t0 = blockIdx.y * TOK, tokens = min(TOK, p.tokens - t0);
+  const float* const x = (const float*)dep(p.x) + t0 * p.ldx;
   const float* row[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -46,7 +48,7 @@ __global__ void __launch_bounds__(32 * D_WARPS) ffn_dot_kernel(const __grid_cons
 #pragma unroll
     for (int r = 0; r < R; ++r) w[r] = load_pack<VEC>(row[r] + at, 0, lane, 32, left);
 #pragma unroll
-    for (int t = 0; t < TOK; ++t) v[t] = load_pack<VEC>(x + min(t, p.tokens - 1) * p.ldx + at, 0, lane, 32, left);
+    for (int t = 0; t < TOK; ++t) v[t] = load_pack<VEC>(x + min(t, tokens - 1) * p.ldx + at, 0, lane, 32, left);
 #pragma unroll
     for (int t = 0; t < TOK; ++t)
 #pragma unroll
@@ -68,8 +70,8 @@ __global__ void __launch_bounds__(32 * D_WARPS) ffn_dot_kernel(const __grid_cons
 #pragma unroll
       for (int t = 0; t < TOK; ++t)
         if (lane == t) { a = s[GATE ? 2 * f : f][t]; b = GATE ? s[2 * f + (GATE ? 1 : 0)][t] : 0.f; }
-      if (lane >= p.tokens || f0 + f >= p.features) continue;
-      const auto put = [&](int k, float v) { ((float*)p.d[k])[lane * p.ldd[k] + f0 + f] = v; };
+      if (lane >= tokens || f0 + f >= p.features) continue;
+      const auto put = [&](int k, float v) { ((float*)p.d[k])[(t0 + lane) * p.ldd[k] + f0 + f] = v; };
       if (GATE) {
         float h, unused;
         activation<decltype(act)::value, false>(a, h, unused);
@@ -86,14 +88,15 @@ __global__ void __launch_bounds__(32 * D_WARPS) ffn_dot_kernel(const __grid_cons
 template <bool GATE, int R, int TOK>
 cudaError_t launch_dot_as(const DotParams& p, bool vec, cudaStream_t st) {
   const int each = D_WARPS * (GATE ? R / 2 : R);
-  return launch_pdl(vec ? ffn_dot_kernel<GATE, R, TOK, true> : ffn_dot_kernel<GATE, R, TOK, false>, (p.features + each - 1) / each, 32 * D_WARPS, 0, st, p);
+  return launch_pdl_grid(vec ? ffn_dot_kernel<GATE, R, TOK, true> : ffn_dot_kernel<GATE, R, TOK, false>,
+                         dim3((unsigned)((p.features + each - 1) / each), (unsigned)((p.tokens + TOK - 1) / TOK)), 32 * D_WARPS, 0, st, p);
 }
 template <bool GATE>
 cudaError_t launch_dot(const DotParams& p, cudaStream_t st) {
   const bool vec = wide_ok(p.x, p.ldx, GN_F32) && wide_ok(p.w[0], p.ldw[0], GN_F32) && (!GATE || wide_ok(p.w[1], p.ldw[1], GN_F32));
   // (four rows of the weights a warp share the tokens' loads, where that leaves every SM eight warps)
   constexpr int FEW = GATE ? 2 : 1;
-  const bool few = (int64_t)p.features * FEW < 4LL * 8 * num_sms();
+  const bool few = (int64_t)p.features * FEW * ((p.tokens + 7) / 8) < 4LL * 8 * num_sms();
   const auto launch = [&](auto tok) {
     constexpr int TOK = decltype(tok)::value;
     return few ? launch_dot_as<GATE, FEW, TOK>(p, vec, st) : launch_dot_as<GATE, 4, TOK>(p, vec, st);

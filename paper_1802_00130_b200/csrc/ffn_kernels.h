@@ -38,7 +38,7 @@ double ffn_narrow_us(FfnKind kind, int tokens, int features, int K);
 double ffn_pair_us(FfnKind kind, int M, int N, int K);
 double ffn_pair_list_us(const FfnGemm* g, int n);
 
-// One FP32 product of the forward pass with at most kFfnDot tokens on FMAs (ffn_dot.cu): d[0] = x w[0]^T, or with w[1] act(x w[0]^T) * (x w[1]^T) and
+// One FP32 product of the forward pass on FMAs, for few tokens (always up to kFfnDot of them; ffn_dot.cu): d[0] = x w[0]^T, or with w[1] act(x w[0]^T) * (x w[1]^T) and
 // the two projections to d[1], d[2] (optional).  Any alignment.
 constexpr int kFfnDot = 8;
 struct FfnMat { const float* p = nullptr; int64_t ld = 0; };

@@ -3,7 +3,7 @@
 // 16-bit types: two tensor-core launches forward (both projections with the gate, then the product with Wd), two backward (dh with the
 // gate's gradient, then dx and the three weight gradients as one launch; with few tokens dx is one of its own).  TMA reads the operands, so one with a base or a leading
 // dimension that is no multiple of 16 bytes is copied to the workspace first.
-// Up to eight FP32 tokens: on FMAs, bound by the weights' bytes.
+// Few FP32 tokens: on FMAs.
 // FP32: the FP32-accurate products of the rest of the library (gemm_f16x3.cu, gemm_ffma.cu), with the gate as a pass of its own.
 #include <math.h>
 
@@ -392,7 +392,17 @@ cudaError_t clear(const gn_mat& m, int64_t rows, int64_t cols, int type, cudaStr
 }
 
 // ---- few FP32 tokens ---------------------------------------------------------------------------
-bool on_fmas(const gn_ffn& f, bool backward) { return !backward && f.rows <= kFfnDot && f.type == GN_F32; }
+// Forward by ffn_dot.cu where its estimated time, in us, is the smaller one: its sums end in shuffles (0.085 a thousand of them), its FMAs run at 33 TFLOP/s;
+// the three products at FP32 accuracy take six launches, their k-blocks and the weights' parts.  Measured, here and there: 9 x 64 x 128 5.3 and 33,
+// 64 x 256 x 512 14 and 31, 64 x 617 x 1201 46 and 56, 128 x 617 x 1201 75 and 57, 16 x 2048 x 4096 102 and 137, 64 x 2048 x 4096 263 and 139.
+bool on_fmas(const gn_ffn& f, bool backward) {
+  if (backward || f.type != GN_F32) return false;
+  if (f.rows <= kFfnDot) return true;
+  const double R = (double)((f.rows + 7) / 8 * 8), C = f.cols, F = f.inner, C128 = (f.cols + 127) / 128 * 128.0, F128 = (f.inner + 127) / 128 * 128.0;
+  const double fmas = 5.0 + 85e-6 * R * (2 * F + C) + 60e-9 * R * (2 * F * C128 + C * F128) * 2;
+  const double products = 27.0 + 0.011 * (C + F) + 5.5e-6 * C * F + R * C * F * 18 / 1.2e9;
+  return fmas < products;
+}
 cudaError_t run_fmas(const gn_ffn& f, float* h, cudaStream_t st) {
   const int64_t ld = up8(f.inner);
   const auto in = [](const gn_mat& m) { return FfnMat{(const float*)m.p, m.ld}; };

@@ -120,7 +120,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save=False, stream=None):
         mean, rstd = x.new_empty(rows, dtype=torch.float32), x.new_empty(rows, dtype=torch.float32)
         pm, pr = mean.data_ptr(), rstd.data_ptr()
     err = _err()
-    status = lib().gn_layer_norm(_TYPES[dtype], _TYPES[wtype], rows, cols, px, ldx, pw, pb, eps, y.data_ptr(), cols, pm, pr, _raw_stream(dev), err, 200)
+    status = lib().gn_layer_norm(_TYPES[dtype], _TYPES[wtype], rows, cols, px, ldx, pw, pb, float(eps), y.data_ptr(), cols, pm, pr, _raw_stream(dev), err, 200)
     if status:
         _checked(status, err)
     return (y, mean, rstd) if save else y
@@ -178,7 +178,7 @@ def dropout(x, p, key, step=0, residual=None, device_step=None, stream=None):
         ps = device_step.data_ptr()
     y = x.new_empty(rows, cols)
     err = _err()
-    status = lib().gn_dropout(_TYPES[dtype], rows, cols, px, ldx, pr, ld_res, y.data_ptr(), cols, p, key & 0xFFFFFFFFFFFFFFFF,
+    status = lib().gn_dropout(_TYPES[dtype], rows, cols, px, ldx, pr, ld_res, y.data_ptr(), cols, float(p), key & 0xFFFFFFFFFFFFFFFF,
                               step & 0xFFFFFFFFFFFFFFFF, ps, _raw_stream(dev), err, 200)
     if status:
         _checked(status, err)

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgn_b200.so")
 SOURCES = ["gn_context.cu", "gemm_ffma.cu", "gemm_tf32.cu", "gemm_f16x3.cu", "gemm_thin.cu", "half_copy.cu", "small_net.cu", "vector_ops.cu",
            "layer_norm.cu", "dropout.cu", "gated_ffn.cu",
-           "gemm_pair16.cu", "gemm_narrow16.cu", "ffn_dot.cu"]
+           "gemm_pair16.cu", "gemm_narrow16.cu", "ffn_dot.cu", "ffn_small.cu"]
 FLAGS = ["-shared", "-Xcompiler", "-fPIC", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
          "-O3", "-std=c++17"]
 

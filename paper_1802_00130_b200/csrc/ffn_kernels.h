@@ -46,4 +46,11 @@ struct FfnOut { float* p = nullptr; int64_t ld = 0; };
 struct FfnDot { int tokens, features, K, act; FfnMat x, w[2]; FfnOut d[3]; };
 cudaError_t launch_ffn_dot(const FfnDot& g, cudaStream_t st);
 
+// FP32 products of a small backward pass on FMAs, n of them as one launch (ffn_small.cu): d [M][N] = sum over s of A_s B_s, B stored [K][N], A [M][K] or
+// (a_mn) [K][M].  With `grad` the one product is dh, and what is written is h, dgate and dup.  Any alignment.  ffn_small_us: an estimate.
+struct FfnSmall { int M = 0, N = 0, K[2] = {0, 0}; bool a_mn = false; FfnMat A[2], B[2]; FfnOut d; };
+struct FfnSmallGrad { int act; FfnMat gate, up; FfnOut out[3]; };
+double ffn_small_us(const FfnSmall* g, int n);
+cudaError_t launch_ffn_small(const FfnSmall* g, int n, const FfnSmallGrad* grad, cudaStream_t st);
+
 }  // namespace gn

@@ -3,7 +3,7 @@
 // 16-bit types: two tensor-core launches forward (both projections with the gate, then the product with Wd), two backward (dh with the
 // gate's gradient, then dx and the three weight gradients as one launch; with few tokens dx is one of its own).  TMA reads the operands, so one with a base or a leading
 // dimension that is no multiple of 16 bytes is copied to the workspace first.
-// Few FP32 tokens: on FMAs.
+// FP32, few tokens forward or a small backward pass: on FMAs (ffn_dot.cu, ffn_small.cu).
 // FP32: the FP32-accurate products of the rest of the library (gemm_f16x3.cu, gemm_ffma.cu), with the gate as a pass of its own.
 #include <math.h>
 
@@ -413,7 +413,53 @@ cudaError_t run_fmas(const gn_ffn& f, float* h, cudaStream_t st) {
   return e == cudaSuccess ? launch_ffn_dot(b, st) : e;
 }
 
+// ---- a small FP32 backward pass ----------------------------------------------------------------
+struct Small { FfnSmall dh, list[kFfnGroup]; int n; FfnSmallGrad grad; int64_t bytes; };
+Small lay_out_small(const gn_ffn& f, char* base) {
+  const auto in = [](const gn_mat& m) { return FfnMat{(const float*)m.p, m.ld}; };
+  const auto out = [](const gn_mat& m) { return FfnOut{(float*)m.p, m.ld}; };
+  Workspace ws{base};
+  Small w{};
+  const int R = (int)f.rows, C = f.cols, F = f.inner;
+  FfnMat part[3];
+  for (int k = 0; k < 3; ++k) {
+    w.grad.out[k] = {(float*)ws.take(f.rows * up8(F) * 4), up8(F)};
+    part[k] = {w.grad.out[k].p, w.grad.out[k].ld};
+  }
+  w.grad.act = f.act; w.grad.gate = in(f.gate); w.grad.up = in(f.up);
+  w.dh.M = R; w.dh.N = F; w.dh.K[0] = C; w.dh.A[0] = in(f.dy); w.dh.B[0] = in(f.w_down);
+  if (f.dx.p) {
+    FfnSmall& q = w.list[w.n++];
+    q.M = R; q.N = C; q.K[0] = q.K[1] = F; q.A[0] = part[1]; q.B[0] = in(f.w_gate); q.A[1] = part[2]; q.B[1] = in(f.w_up); q.d = out(f.dx);
+  }
+  const auto weights = [&](int M, int N, const FfnMat& A, const FfnMat& B, const gn_mat& d) {
+    if (!d.p) return;
+    FfnSmall& q = w.list[w.n++];
+    q.M = M; q.N = N; q.K[0] = R; q.a_mn = true; q.A[0] = A; q.B[0] = B; q.d = out(d);
+  };
+  weights(F, C, part[1], in(f.x), f.dw_gate);
+  weights(F, C, part[2], in(f.x), f.dw_up);
+  weights(C, F, in(f.dy), part[0], f.dw_down);
+  w.bytes = ws.used;
+  return w;
+}
+// Where its estimated time, in us, is the smaller one; the products at FP32 accuracy and what goes with them take 40 to 60 whatever the size, of which the wanted ones
+// their share.  Measured, here and there: 32 x 64 x 128 9.3 and 50, 1000 x 64 x 512 41 and 68, 32 x 617 x 1201 55 and 77, 300 x 300 x 784 64 and 56.
+bool is_small(const gn_ffn& f, bool backward) {
+  if (!backward || f.type != GN_F32 || f.rows > (1 << 20)) return false;
+  const Small w = lay_out_small(f, kNowhere);
+  const double R = (double)f.rows, C = f.cols, F = f.inner;
+  const double products = (40.0 + 0.011 * (C + F) + 8e-6 * C * F + 0.005 * R + R * C * F * 36 / 1.2e9) * (1 + w.n) / 5.0;
+  return ffn_small_us(&w.dh, 1) + ffn_small_us(w.list, w.n) < products;
+}
+cudaError_t run_small(const Small& w, cudaStream_t st) {
+  if (w.n == 0) return cudaSuccess;
+  const cudaError_t e = launch_ffn_small(&w.dh, 1, &w.grad, st);
+  return e == cudaSuccess ? launch_ffn_small(w.list, w.n, nullptr, st) : e;
+}
+
 int64_t needed(const gn_ffn& f, bool backward, char* base, Half& h, Single& s) {
+  if (is_small(f, backward)) return lay_out_small(f, base).bytes + 256;
   if (on_fmas(f, backward)) return f.rows * up8(f.inner) * 4 + 256;
   return (f.type == GN_F32 ? lay_out_single(f, backward, base, s) : lay_out_half(f, backward, base, h)) + 256;
 }
@@ -439,6 +485,7 @@ gn_status run(const gn_ffn* f, bool back, void* d_ws, int64_t ws_bytes, void* st
   int* const err = error_word();
   if (!err) return op_done(cudaErrorNoDevice, errbuf, errbuf_len);
   if (on_fmas(*f, back)) e = run_fmas(*f, (float*)base, st);
+  else if (is_small(*f, back)) e = run_small(lay_out_small(*f, base), st);
   else if (f->type == GN_F32) e = run_single(*f, back, s, err, st);
   else e = run_half(*f, back, h, err, st);
   return op_done(e, errbuf, errbuf_len);

@@ -16,7 +16,8 @@ SHAPES = [(1, 1, 1), (1, 64, 128), (2, 8, 16), (3, 7, 5), (1, 1000, 3001), (16, 
           (513, 96, 2056), (1003, 617, 1201), (2100, 256, 264), (40, 2048, 8192),
           (5000, 40, 72), (2, 1001, 2003), (7, 64, 4001), (8, 136, 40), (300, 64, 5000),
           # several tiles of tokens: all of them full, one token in the last, odd rows in all three matrices, and the sizes around a tile's
-          (256, 768, 2048), (385, 512, 1024), (1500, 200, 1000), (130, 1537, 773), (4096, 72, 136), (4097, 136, 72)]
+          (256, 768, 2048), (385, 512, 1024), (1500, 200, 1000), (130, 1537, 773), (4096, 72, 136), (4097, 136, 72),
+          (33, 31, 65), (96, 64, 32), (9, 129, 33), (700, 33, 31)]
 # an activation's FP32 value is off by a few steps: exp 2, its quotient 2, the products after it
 ACT = 16 * E
 

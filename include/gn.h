@@ -546,7 +546,7 @@ typedef struct { void* p; int64_t ld; } gn_mat;
  *   dy [rows][cols], x, gate, up, and the three weights are inputs; dx, dw_gate, dw_up, dw_down are outputs of the shapes of x and the
  *   weights, each with p == NULL where it is not wanted.
  * GN_BF16 and GN_F16: operands go to the tensor cores as they are; h, dup and dgate are rounded to the type on their way into the next
- * product.  GN_F32: every product at FP32 accuracy (see gn_set_accurate_method).
+ * product (h not where 128 tokens or fewer meet few weights: it goes in two parts there).  GN_F32: every product at FP32 accuracy (see gn_set_accurate_method).
  * Workspace: gn_gated_ffn_workspace(args, backward) bytes for the same args; it depends on sizes, types, leading dimensions
  * and on the alignment of the pointers, and is negative for bad arguments.
  * 1 <= cols, inner <= 2^24 with cols * inner < 2^31; rows < 2^30.

@@ -11,7 +11,8 @@ struct Out16 { void* p = nullptr; int64_t ld = 0; };
 
 // What becomes of the sums acc(m, n) = sum_k A(m, k) B(k, n) (+ the same of a second operand pair):
 //   FFN_STORE  d[0] = acc
-//   FFN_GATE   two right operands, B[0] and B[1], one sum each: gate and up.  d[0] = act(gate) * up; d[1], d[2] = gate, up (optional)
+//   FFN_GATE   two right operands, B[0] and B[1], one sum each: gate and up.  d[0] = h = act(gate) * up; d[1], d[2] = gate, up (optional);
+//              low = what the rounding of h has left (optional, the kernel for few tokens only)
 //   FFN_GRAD   acc = dh: d[0] = act(gate) * up, d[1] = dh up act'(gate), d[2] = dh act(gate), from the stored gate and up
 enum FfnKind { FFN_STORE = 0, FFN_GATE = 1, FFN_GRAD = 2 };
 struct FfnGemm {
@@ -19,7 +20,7 @@ struct FfnGemm {
   int K[2] = {0, 0};             // K[1] > 0: a second operand pair (FFN_STORE)
   bool a_mn = false, b_mn = false;   // stored [K][M], [K][N] instead of [M][K], [N][K]
   Mat16 A[2], B[2];
-  Out16 d[3];
+  Out16 d[3], low;
   Mat16 gate, up;
 };
 constexpr int kFfnGroup = 4;     // problems of one launch (FFN_STORE)

@@ -140,7 +140,7 @@ char* const kNowhere = reinterpret_cast<char*>(256);
 struct Half {
   Mat16 x, w_gate, w_up, w_down, dy, gate, up;      // with rows of 16-byte units, as TMA and the gate's gradient read them
   PackList packs; int n_packs; int64_t pack_warps;
-  Out16 h, dgate, dup;
+  Out16 h, low, dgate, dup;               // low: see two_parts
   void* sums;                             // of slices of K
 };
 Mat16 addressable(const gn_mat& m, int64_t rows, int cols, Workspace& ws, Half& w) {
@@ -154,6 +154,12 @@ Mat16 addressable(const gn_mat& m, int64_t rows, int cols, Workspace& ws, Half& 
 }
 inline Mat16 in16(const Out16& m) { return {m.p, m.ld}; }
 inline Out16 out16(const gn_mat& m) { return {m.p, m.ld}; }
+// Whether h goes to the product with Wd in two parts, rounded and what that has left.  Its rounding makes y's error sqrt 2 times that of y's own, and more where
+// few values make it up (1.6, one token and 25 hidden units).  The second pass over Wd, 2 MB of it at most, takes 0.2 to 0.9 us (1 x 64 x 128 6.0 and 6.9, 128 x 1024 x
+// 1024 13.0 and 13.7); with more hidden units, whose roundings average, it would take more (1 x 512 x 2048 8.4 and 10.0, 128 x 128 x 8192 19 and 26).
+bool two_parts(const gn_ffn& f, bool backward) {
+  return !backward && f.rows <= kFfnNarrow && f.inner <= 1024 && (int64_t)f.cols * f.inner <= (1 << 20);
+}
 // The plain products of a call, in the order they run: forward the one with Wd, backward dx and the weights' gradients.
 int plain_products(const gn_ffn& f, bool backward, const Half& w, FfnGemm (&list)[kFfnGroup]) {
   const int R = (int)f.rows;
@@ -162,6 +168,7 @@ int plain_products(const gn_ffn& f, bool backward, const Half& w, FfnGemm (&list
     FfnGemm& q = list[n++];
     q.M = R; q.N = f.cols; q.K[0] = f.inner;
     q.A[0] = in16(w.h); q.B[0] = w.w_down; q.d[0] = out16(f.y);
+    if (two_parts(f, backward)) { q.K[1] = f.inner; q.A[1] = in16(w.low); q.B[1] = w.w_down; }
     return n;
   }
   if (f.dx.p) {
@@ -206,8 +213,8 @@ int64_t lay_out_half(const gn_ffn& f, bool backward, char* base, Half& w) {
     w.gate = addressable(f.gate, f.rows, f.inner, ws, w);
     w.up = addressable(f.up, f.rows, f.inner, ws, w);
   }
-  for (Out16* o : {&w.h, &w.dgate, &w.dup}) {
-    if (o != &w.h && !backward) break;
+  for (Out16* o : {&w.h, &w.low, &w.dgate, &w.dup}) {
+    if (o == &w.low ? !two_parts(f, backward) : o != &w.h && !backward) continue;
     *o = {ws.take(f.rows * ld * 2), ld};
   }
   FfnGemm list[kFfnGroup];
@@ -227,7 +234,7 @@ cudaError_t run_half(const gn_ffn& f, bool backward, const Half& w, int* err, cu
   const int n = plain_products(f, backward, w, list);
   if (n == 0) return cudaSuccess;
   a.M = (int)f.rows; a.N = f.inner; a.K[0] = f.cols;
-  a.d[0] = w.h;
+  a.d[0] = w.h; a.low = w.low;
   if (backward) {
     a.b_mn = true;
     a.A[0] = w.dy; a.B[0] = w.w_down; a.d[1] = w.dgate; a.d[2] = w.dup;

@@ -36,7 +36,7 @@ struct NarrowParams {
   int kb0, kb;                       // k-blocks of the first operand pair, of both
   // early: the weights may be loaded before the kernel before this one is done
   int a_mn, act, early, vec;         // vec: every matrix of the epilogue takes accesses to four (FFN_GATE: two) elements
-  Out16 d[3];
+  Out16 d[3], low;
   Mat16 gate, up;
   int* err;
 };
@@ -249,6 +249,15 @@ __global__ void __launch_bounds__(N_THREADS, 2) ffn_narrow_kernel(const __grid_c
           h[e] = a * u[e];
         }
         put<T>(p.d[0], t0 + t, f, p.features, p.vec, h);
+        if (p.low.p) {               // (nothing is left of infinities and NaN, the rounding's own among them)
+          float low[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float high = to_f(from_f<T>(h[e]));
+            low[e] = fabsf(high) < __int_as_float(0x7f800000) ? h[e] - high : 0.f;
+          }
+          put<T>(p.low, t0 + t, f, p.features, p.vec, low);
+        }
         if (p.d[1].p) put<T>(p.d[1], t0 + t, f, p.features, p.vec, g);
         if (p.d[2].p) put<T>(p.d[2], t0 + t, f, p.features, p.vec, u);
       } else if constexpr (KIND == FFN_STORE) {
@@ -327,9 +336,11 @@ cudaError_t launch_narrow_as(int act, const FfnGemm& g, bool early, int* err, cu
   p.a_mn = g.b_mn; p.act = act; p.early = early; p.err = err;
   p.vec = 1;
   for (int k = 0; k < 3; ++k) p.d[k] = g.d[k];
+  p.low = g.low;
   p.gate = g.gate; p.up = g.up;
   const auto wide = [&](const void* q, int64_t ld) { return !q || (((uintptr_t)q & (2 * EACH - 1)) == 0 && ld % EACH == 0); };
   for (const Out16& o : g.d) p.vec &= wide(o.p, o.ld);
+  p.vec &= wide(g.low.p, g.low.ld);
   p.vec &= wide(g.gate.p, g.gate.ld) && wide(g.up.p, g.up.ld);
   for (int s = 0; s < (KIND == FFN_GATE || g.K[1] > 0 ? 2 : 1); ++s) {
     const int a = KIND == FFN_GATE ? 0 : s, K = g.K[a];

@@ -29,7 +29,7 @@ def inputs(rows, cols, inner, t, pad=0, seed=0):
     return x, w
 
 
-def check_forward(got, x, w, act, t):
+def check_forward(got, x, w, act, t, h_round=1.0):
     x64, wg, wu, wd = x.double(), *(m.double() for m in w)
     gate, gate_err = product(x64, wg, 0, 0)
     up, up_err = product(x64, wu, 0, 0)
@@ -37,7 +37,7 @@ def check_forward(got, x, w, act, t):
     h = a * up
     # |act''| <= 1.2 for all of them but relu, whose kink costs at most gate_err itself
     h_err = up.abs() * (da.abs() + 1) * gate_err + a.abs() * up_err + (ACT * (a.abs() + gate.abs() * ACT) * up.abs()) + E * h.abs()
-    y, y_err = product(h, wd, h_err + u(t) * h.abs() + tiny(t), 0)
+    y, y_err = product(h, wd, h_err + h_round * u(t) * h.abs() + tiny(t), 0)
     within(got[0], y, y_err + u(t) * y.abs() + tiny(t), "y")
     if len(got) > 1:
         within(got[1], gate, gate_err + u(t) * gate.abs() + tiny(t), "gate")
@@ -70,6 +70,29 @@ def test_forward(t, shape):
     alone = gn.gated_ffn(x, *w, act=act)
     check_forward((alone,), x, w, act, t)
     assert torch.equal(alone, gn.gated_ffn(x, *w, act=act))
+
+
+@pytest.mark.parametrize("shape", [(1, 30, 37), (1, 1728, 25), (3, 64, 128), (17, 617, 1001), (128, 1024, 1024)])
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+def test_few_tokens_and_weights_keep_h(t, shape):
+    """h in two parts: what is left of its rounding is half a step of a half step."""
+    t = TYPES[t]
+    for act in ACTS:
+        x, w = inputs(*shape, t)
+        check_forward(gn.gated_ffn(x, *w, act=act, save=True), x, w, act, t, h_round=u(t))
+
+
+def test_h_beyond_the_type():
+    """An h that FP16 cannot hold is infinite, with the sign that it has, and not NaN."""
+    x, w = inputs(2, 16, 24, torch.float16)
+    w[0].fill_(0); w[1].fill_(0); w[2].fill_(1)
+    x[:, :2] = 256
+    w[0][3, 0], w[1][3, 1] = 64, 64
+    y, gate, up = gn.gated_ffn(x, *w, act="relu", save=True)
+    assert bool((gate[:, 3] == 16384).all()) and bool((up[:, 3] == 16384).all())
+    assert bool((y == float("inf")).all())
+    w[1][3, 1] = -64
+    assert bool((gn.gated_ffn(x, *w, act="relu") == -float("inf")).all())
 
 
 @pytest.mark.parametrize("shape", SHAPES)

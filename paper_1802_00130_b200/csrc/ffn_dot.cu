@@ -1,7 +1,9 @@
 // Products of the gated feed-forward block's forward pass in FP32 with few tokens, on FMAs.
 //
-// Up to eight tokens bound by reading the weights once (two FP16 parts of them would be written and read again), with more of them, eight to a block, by the loads
-// and by the sums at the end; what it saves there is launches.  A warp takes R rows of the weights at a time and walks K with 16
+// One token is bound by reading the weights once (two FP16 parts of them would be written and read again): 3584 x 15232 133 us, 4.9 TB/s, 2048 x 4096 33; up to four
+// 188 and 38.  With five to eight the loads of the tokens' values from L1, twice the weights' bytes at four rows a warp, take longer (370 and 56; the
+// weights ahead in shared memory did not help: 377 and 60).  More tokens go eight to a block; what it saves there is launches.
+// A warp takes R rows of the weights at a time and walks K with 16
 // bytes a lane from each (single elements, as many to a step, where rows are not 16-byte aligned), the tokens' values from L1, all of a step's loads
 // before its first product.  Each lane's sums are added across the warp at the end.
 #include "ffn_act.cuh"

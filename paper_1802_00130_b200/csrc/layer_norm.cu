@@ -3,7 +3,8 @@
 //
 // Forward: 8 or 32 threads a row up to 4096 columns of 16 bits (no barrier, a row's loads all in flight), a block a row above it.  The sums
 // of a row are taken twice from the registers, of x for the mean m and then of x - m and its square: the first of these two
-// is what m's rounding has left, which corrects the mean and the variance, so a mean far above the spread costs no accuracy.
+// is what m's rounding has left, which corrects the mean and the variance, so a mean far above the spread costs no accuracy (see about and variance for
+// a spread of nothing or of a few steps).
 //
 // Backward: two units a thread.  With mean and rstd at hand a row needs one reduction, of g and g xhat; the sums
 // over rows of dy xhat and dy stay with the thread that owns the column, and each block leaves one row of partial sums, which a
@@ -40,6 +41,19 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float* part) {
   }
 }
 
+// Where a row's sums are taken about: its mean, or its first element where that is as near to the mean as the mean's rounding `near` (relative) lets one
+// tell.  Elements that are all equal then leave nothing at all, whatever their sum has been rounded to, or overflowed to.
+constexpr float kNear = 0x1p-18f;              // 32 terms a thread, ten steps of a tree, the quotient: 44 times 2^-24 at most
+// With variance() it costs FP32 rows up to 5 % (19794 x 599 24.5 us instead of 23.4, 16384 x 2048 46.2 and 45.8).
+// (16-bit elements up to 8192 columns need neither: the sum of equal ones is exact, its quotient is made so, and any spread is 2^-11 of a value or more.)
+__device__ __forceinline__ float about(float mean, float first, float near) { return fabsf(first - mean) <= near * fabsf(mean) ? first : mean; }
+// sum t^2 / n - (sum t / n)^2 of n elements t, from their sums s, s2 and off = s / n rounded.  s^2 / n = s off + off (s - off n) but for terms of second order, and
+// neither product is rounded before it is taken from s2, so where the two are almost equal little is lost (few steps of FP32 between the elements
+// make their sums exact).  Never below zero; NaN stays.
+__device__ __forceinline__ float variance(float s, float s2, float off, float n, float inv_n) {
+  return __fmul_rn(max_nan(fmaf(-off, fmaf(-off, n, s), fmaf(-s, off, s2)), 0.f), inv_n);
+}
+
 // TPR threads a row, which hold NU units of 16 bytes each.  A block walks its rows with the next row's loads under way while it works on
 // one; the weights stay in registers where they are few.
 template <int TPR> constexpr int norm_block = TPR > 128 ? TPR : 128;
@@ -52,13 +66,14 @@ layer_norm_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, c
   constexpr int V = Pack<T>::V, VW = Pack<W>::V, WU = sizeof(W) / sizeof(T);      // WU: units of the weights to a unit of x
   constexpr int PER = norm_block<TPR> / TPR;                     // rows of a block
   constexpr bool KEEP = NU * WU <= 2;
-  __shared__ float part[TPR > 32 ? PER : 1][3 * (TPR > 32 ? TPR / 32 : 1)];
+  constexpr bool NEAR = sizeof(T) == 4 || TPR * NU * V > 8192;     // see about
+  __shared__ float part[TPR > 32 ? PER : 1][3 * (TPR > 32 ? TPR / 32 : 1) + 1];    // (the last word: the row's first element)
   const int thread = threadIdx.x % TPR;
   float* const mine = part[TPR > 32 ? threadIdx.x / TPR : 0];
   grid_dep_wait();
   grid_dep_launch();
   x = dep(x); w = dep(w); b = dep(b);
-  const float inv_n = 1.f / (float)cols;
+  const float n = (float)cols, inv_n = 1.f / n;
   const int64_t step = (int64_t)gridDim.x * PER;
   int64_t r = (int64_t)blockIdx.x * PER + threadIdx.x / TPR;
   // (the weights of unit u are units u WU .. u WU + WU - 1 of theirs, and lie side by side where x's elements do)
@@ -88,8 +103,16 @@ layer_norm_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, c
     float t[NU * V], s[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < NU * V; ++k) { t[k] = v[k / V].get(k % V); s[0] += t[k]; }
+    float first = t[0];
+    if (NEAR && TPR > 32 && thread == 0) mine[3 * TPR / 32] = first;
     row_sum<TPR>(s, mine);
-    const float m = s[0] * inv_n;
+    float m = s[0] * inv_n;
+    if constexpr (NEAR) {
+      first = TPR > 32 ? mine[3 * TPR / 32] : __shfl_sync(0xffffffffu, first, 0, TPR > 32 ? 32 : TPR);
+      m = about(m, first, kNear);
+    } else {
+      m = fmaf(fmaf(-m, n, s[0]), inv_n, m);
+    }
     float d[2] = {0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
@@ -103,7 +126,8 @@ layer_norm_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, c
       }
     }
     row_sum<TPR>(d, mine + (TPR > 32 ? TPR / 32 : 0));
-    const float off = d[0] * inv_n, rstd = 1.f / sqrtf(d[1] * inv_n - off * off + eps), shift = -off * rstd;
+    const float off = d[0] * inv_n, var = NEAR ? variance(d[0], d[1], off, n, inv_n) : d[1] * inv_n - off * off;
+    const float rstd = 1.f / sqrtf(var + eps), shift = -off * rstd;
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       if (pack_col<VEC, T>(u, 0, thread, TPR) >= cols) break;
@@ -135,16 +159,17 @@ template <class T, class W>
 __global__ void __launch_bounds__(1024) layer_norm_long_kernel(int64_t rows, int cols, const T* x, int64_t ldx, const W* w, const W* b, float eps, T* y,
                                                                int64_t ldy, float* mean_out, float* rstd_out) {
   __shared__ float part[3 * 32];
+  const float near = kNear + 0x1p-24f * (cols / 1024);     // (as many terms a thread)
   for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
     const T* xr = x + r * ldx;
     float s[1] = {0.f};
     for (int c = threadIdx.x; c < cols; c += blockDim.x) s[0] += to_f(xr[c]);
     row_sum<1024>(s, part);
-    const float m = s[0] / cols;
+    const float m = about(s[0] / cols, to_f(xr[0]), near);
     float d[2] = {0.f, 0.f};
     for (int c = threadIdx.x; c < cols; c += blockDim.x) { const float v = to_f(xr[c]) - m; d[0] += v; d[1] += v * v; }
     row_sum<1024>(d, part + 32);
-    const float off = d[0] / cols, rstd = 1.f / sqrtf(d[1] / cols - off * off + eps);
+    const float off = d[0] / cols, rstd = 1.f / sqrtf(variance(d[0], d[1], off, (float)cols, 1.f / cols) + eps);
     for (int c = threadIdx.x; c < cols; c += blockDim.x) {
       const float v = (to_f(xr[c]) - m - off) * rstd;
       y[r * ldy + c] = from_f<T>(v * (w ? to_f(w[c]) : 1.f) + (b ? to_f(b[c]) : 0.f));

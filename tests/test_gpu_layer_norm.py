@@ -1,5 +1,6 @@
 """Layer norm and its backward pass against a plain form in 64 bits."""
 import ctypes as C
+import math
 
 import pytest
 import torch
@@ -105,6 +106,54 @@ def test_forward_rows_of_equal_elements_and_bad_rows(cols):
     assert torch.equal(y[[0, 2, 5]], good[[0, 2, 5]])
     assert bool((y[1] == 0).all()) and float(mean[1]) == 3.25 and abs(float(rstd[1]) - 1e-5 ** -0.5) < 1e-3
     assert bool(y[3].isnan().all()) and bool(y[4].isnan().any())
+
+
+@pytest.mark.parametrize("eps", [1e-5, 1e-12])
+@pytest.mark.parametrize("cols", [5, 33, 100, 500, 617, 1001, 1201, 4097, 9001, 20001, 300000, 1 << 20])
+def test_forward_of_equal_elements_whose_sum_is_not_exact(cols, eps):
+    """A row of n times v has the mean v, no variance and the bias, whatever the sum of n v is rounded to.
+
+    The sums are taken about the row's first element, so they are zero: y is b and the mean v.  rstd: eps in FP32, the root, the quotient."""
+    values = [v * s for v in (1e3, 1.7e4, 1e5, 1e6, 1.9e7, 122624096.0, 1.2345e9, 2.9e9, 1e25, 0.1) for s in (1, -1.0001)] + [3e38]
+    x = torch.tensor(values, dtype=torch.float64, device="cuda").float()[:, None].repeat(1, cols)
+    w, b = vec(cols, torch.float32, 1, 0.2, 1.0), vec(cols, torch.float32, 2, 0.3)
+    y, mean, rstd = gn.layer_norm(x, w, b, eps, save=True)
+    within(rstd, torch.full((len(values),), eps ** -0.5, dtype=torch.float64, device="cuda"), 4 * E * torch.full((1,), eps ** -0.5, device="cuda"), "rstd")
+    assert torch.equal(mean, x[:, 0]) and bool((y == b).all())
+
+
+@pytest.mark.parametrize("eps", [1e-5, 1e-12])
+@pytest.mark.parametrize("cols", [5, 33, 100, 500, 617, 1001, 1201, 4097, 8191, 9001, 20001, 40001])
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+def test_forward_of_equal_elements_in_16_bits(t, cols, eps):
+    """The same, over every mantissa of BF16 and an eighth of FP16's, at two ends of the exponents."""
+    t = TYPES[t]
+    top = torch.arange(1024, 2048, 8, device="cuda").double() / 2048
+    x = torch.cat([top * (65504.0 if t == torch.float16 else 2.0 ** 40), top * -0.125]).to(t)[:, None].repeat(1, cols)
+    b = vec(cols, torch.float32, 2, 0.3)
+    y, mean, rstd = gn.layer_norm(x, None, b, eps, save=True)
+    within(rstd, torch.full((256,), eps ** -0.5, dtype=torch.float64, device="cuda"), 4 * E * torch.full((1,), eps ** -0.5, device="cuda"), "rstd")
+    assert torch.equal(mean, x[:, 0].float()) and bool((y == b.to(t)).all())
+
+
+@pytest.mark.parametrize("cols", [7, 64, 250, 1001, 3001, 9001, 20001])
+@pytest.mark.parametrize("v", [1e4, 1e6, 1.2345e9])
+def test_forward_of_a_spread_of_a_few_steps(cols, v):
+    """Elements within three steps of FP32 of one another beside rows of equal ones: x - m and its sums are exact, (sum)^2 / n but for E^2 of it, so the
+    bounds are those of the values x - mean."""
+    x = torch.full((12, cols), v, dtype=torch.float32, device="cuda")
+    step = 2.0 ** (math.floor(math.log2(v)) - 23)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(cols)
+    x[::2] += torch.randint(-1, 3, (6, cols), generator=g, device="cuda") * step
+    x[4], x[4, cols // 2] = v, v + step
+    eps = (step * 1e-3) ** 2
+    y, mean, rstd = gn.layer_norm(x, eps=eps, save=True)
+    ry, rm, rr = norm64(x, None, None, eps)
+    rel = E * (cols / 32 + 40)
+    within(rstd, rr, rel * rr, "rstd")
+    within(mean, rm, 2 * E * rm.abs(), "mean")
+    within(y, ry, rel * (ry.abs() + 1), "y")
 
 
 def grads64(dy, x, mean, rstd, w, add):

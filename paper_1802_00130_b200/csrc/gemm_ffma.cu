@@ -23,6 +23,7 @@ struct FfmaParams {
   float alpha;
   const float* cin; long long ld_cin; float beta;
   int vec_epi;
+  int tiles_n;                       // tiles in one dimension of the grid, row by row: the others end at 65535
 };
 
 // Four consecutive elements along the contiguous dimension `c` of a matrix whose other index is `r`.
@@ -51,7 +52,7 @@ __global__ void __launch_bounds__(NT, 2) gemm_ffma_kernel(const FfmaParams p) {
 
   const int tid = threadIdx.x;
   const int tx = tid & 15, ty = tid >> 4;
-  const int m0 = blockIdx.y * BM, n0 = blockIdx.x * BN;
+  const int tile_m = (int)(blockIdx.x / (unsigned)p.tiles_n), m0 = tile_m * BM, n0 = ((int)blockIdx.x - tile_m * p.tiles_n) * BN;
 
   const int nk0 = (p.K[0] + BK - 1) / BK;
   const int nk1 = p.A[1] ? (p.K[1] + BK - 1) / BK : 0;
@@ -198,11 +199,12 @@ int launch_gemm_ffma(const GemmArgs& g, cudaStream_t st) {
   p.vec_epi = aligned16(g.D) && (g.ldd % 4 == 0) && (!g.bias || aligned16(g.bias)) &&
               (!g.dsig || (aligned16(g.dsig) && g.ld_dsig % 4 == 0)) &&
               (!g.cin || (aligned16(g.cin) && g.ld_cin % 4 == 0));
-  dim3 grid((g.N + BN - 1) / BN, (g.M + BM - 1) / BM);
-  if (g.a_kmajor && g.b_kmajor)        launch_pdl_grid(gemm_ffma_kernel<true, true>, dim3(grid), NT, 0, st, p);
-  else if (g.a_kmajor && !g.b_kmajor)  launch_pdl_grid(gemm_ffma_kernel<true, false>, dim3(grid), NT, 0, st, p);
-  else if (!g.a_kmajor && g.b_kmajor)  launch_pdl_grid(gemm_ffma_kernel<false, true>, dim3(grid), NT, 0, st, p);
-  else                                 launch_pdl_grid(gemm_ffma_kernel<false, false>, dim3(grid), NT, 0, st, p);
+  p.tiles_n = (g.N + BN - 1) / BN;
+  const dim3 grid((unsigned)((long long)((g.M + BM - 1) / BM) * p.tiles_n));
+  if (g.a_kmajor && g.b_kmajor)        launch_pdl_grid(gemm_ffma_kernel<true, true>, grid, NT, 0, st, p);
+  else if (g.a_kmajor && !g.b_kmajor)  launch_pdl_grid(gemm_ffma_kernel<true, false>, grid, NT, 0, st, p);
+  else if (!g.a_kmajor && g.b_kmajor)  launch_pdl_grid(gemm_ffma_kernel<false, true>, grid, NT, 0, st, p);
+  else                                 launch_pdl_grid(gemm_ffma_kernel<false, false>, grid, NT, 0, st, p);
   return 1;
 }
 

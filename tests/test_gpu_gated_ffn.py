@@ -108,6 +108,17 @@ def test_backward(t, shape):
     assert all(torch.equal(p, q) for p, q in zip(got, again))
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_more_rows_than_a_grid_has_tiles_in_its_second_dimension(t):
+    """65535 tiles of 128 rows and one row."""
+    t = TYPES[t]
+    x, w = inputs(65535 * 128 + 1, 3, 5, t)
+    dy = rand(x.shape, t, 9, 0.5)
+    got = gn.gated_ffn(x, *w, save=True)
+    check_forward(got, x, w, "silu", t)
+    check_backward(gn.gated_ffn_grad(dy, x, got[1], got[2], *w), dy, x, got[1], got[2], w, "silu", t)
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("rows", [5, 140])
 @pytest.mark.parametrize("t", TYPES)

@@ -12,6 +12,7 @@ namespace gn {
 namespace {
 
 constexpr int BM = 128, BN = 128, BK = 16, NT = 256, PAD = 4;
+constexpr int GRID_Y = 65535;      // a grid's second dimension ends there: more rows of tiles go to the third (the last of them may find no rows)
 
 struct FfmaParams {
   int M, N;
@@ -23,7 +24,6 @@ struct FfmaParams {
   float alpha;
   const float* cin; long long ld_cin; float beta;
   int vec_epi;
-  int tiles_n;                       // tiles in one dimension of the grid, row by row: the others end at 65535
 };
 
 // Four consecutive elements along the contiguous dimension `c` of a matrix whose other index is `r`.
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(NT, 2) gemm_ffma_kernel(const FfmaParams p) {
 
   const int tid = threadIdx.x;
   const int tx = tid & 15, ty = tid >> 4;
-  const int tile_m = (int)(blockIdx.x / (unsigned)p.tiles_n), m0 = tile_m * BM, n0 = ((int)blockIdx.x - tile_m * p.tiles_n) * BN;
+  const int m0 = (int)(blockIdx.z * GRID_Y + blockIdx.y) * BM, n0 = blockIdx.x * BN;
 
   const int nk0 = (p.K[0] + BK - 1) / BK;
   const int nk1 = p.A[1] ? (p.K[1] + BK - 1) / BK : 0;
@@ -199,8 +199,8 @@ int launch_gemm_ffma(const GemmArgs& g, cudaStream_t st) {
   p.vec_epi = aligned16(g.D) && (g.ldd % 4 == 0) && (!g.bias || aligned16(g.bias)) &&
               (!g.dsig || (aligned16(g.dsig) && g.ld_dsig % 4 == 0)) &&
               (!g.cin || (aligned16(g.cin) && g.ld_cin % 4 == 0));
-  p.tiles_n = (g.N + BN - 1) / BN;
-  const dim3 grid((unsigned)((long long)((g.M + BM - 1) / BM) * p.tiles_n));
+  const int tiles_m = (g.M + BM - 1) / BM;
+  const dim3 grid((g.N + BN - 1) / BN, tiles_m < GRID_Y ? tiles_m : GRID_Y, (tiles_m + GRID_Y - 1) / GRID_Y);
   if (g.a_kmajor && g.b_kmajor)        launch_pdl_grid(gemm_ffma_kernel<true, true>, grid, NT, 0, st, p);
   else if (g.a_kmajor && !g.b_kmajor)  launch_pdl_grid(gemm_ffma_kernel<true, false>, grid, NT, 0, st, p);
   else if (!g.a_kmajor && g.b_kmajor)  launch_pdl_grid(gemm_ffma_kernel<false, true>, grid, NT, 0, st, p);

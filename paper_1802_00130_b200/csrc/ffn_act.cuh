@@ -7,15 +7,15 @@ namespace {
 
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rcp_fast(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-__device__ __forceinline__ float min_nan(float a, float b) { float y; asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b)); return y; }
 
 // 1 / (1 + exp(-v)) and 1 / (1 + exp(v)), each to full relative accuracy: one minus the other would lose it where it is small.
 // FAST: the hardware's exponential and reciprocal, off by at most (4 + |v|) 2^-23, for results that are rounded to 16 bits (2^-12 at best), and without
-// a branch on the sign: exp(-v) is kept below 2^126, where its reciprocal is still a normal number and their product one.
+// a branch on the sign.  It takes v from kSigmoidLow on: exp(-v) is below 2^126 there, where its reciprocal is still a normal number and their product one.
+constexpr float kSigmoidLow = -87.3f;
 template <bool FAST>
 __device__ __forceinline__ void sigmoids(float v, float& z, float& nz) {
   if (FAST) {
-    const float e = min_nan(exp2_fast(v * -1.4426950408889634f), 8e37f);
+    const float e = exp2_fast(v * -1.4426950408889634f);
     z = rcp_fast(1.f + e); nz = e * z;
   } else {
     const float e = expf(-fabsf(v)), r = 1.f / (1.f + e);
@@ -46,9 +46,12 @@ __device__ __forceinline__ void normal(float v, float& cdf, float& e) {
   }
 }
 // act(v) and its derivative.  A NaN stays one: comparisons with it fall to the branch that computes with it.
+// FAST: what is so far below that sigmoids takes it no more is as the last value that it takes, v itself in v z too (they are less than 2e-36 there).
 template <int ACT, bool FAST>
 __device__ __forceinline__ void activation(float v, float& a, float& da) {
   float z, nz;
+  if (FAST && (ACT == GN_ACT_SIGMOID || ACT == GN_ACT_SILU)) v = max_nan(v, kSigmoidLow);
+  if (FAST && ACT == GN_ACT_GELU_TANH) v = max_nan(v, -9.99f);       // (2 q = -87.1)
   if (ACT == GN_ACT_RELU) {
     a = v < 0.f ? 0.f : v; da = v > 0.f ? 1.f : 0.f;
   } else if (ACT == GN_ACT_GELU) {

@@ -146,6 +146,34 @@ def test_gates_far_out_stay_finite(t, rows, act):
     check_backward(gn.gated_ffn_grad(x, x, got[1], got[2], *w, act=act), x, x, got[1], got[2], w, act, t)
 
 
+FAR = [60.0, 88.0, 100.0, 300.0, 1e3, 1e5, 1e9, 1e12, 1e15, 1e18, 1.8e19, 2e19, 1e20, 1e25, 1e30, 1e37]
+
+
+def far_gates(rows, t, act, gates):
+    """(y, dw_gate, dw_up) of gates of any size, with up = 1, weights and dy of ones: h = act(gate), dh = cols."""
+    cols, inner = 8, len(gates)
+    x = torch.zeros(rows, cols, dtype=t, device="cuda")
+    x[:, 0] = 1
+    one = lambda *shape: torch.ones(*shape, dtype=t, device="cuda")
+    wg, wu = torch.zeros(inner, cols, dtype=t, device="cuda"), one(inner, cols)
+    wg[:, 0] = torch.tensor(gates, dtype=torch.float64, device="cuda").to(t)
+    y, gate, up = gn.gated_ffn(x, wg, wu, one(cols, inner), act=act, save=True)
+    assert torch.equal(gate, wg[:, 0].expand(rows, inner)) and bool((up == 1).all())
+    dx, dwg, dwu, dwd = gn.gated_ffn_grad(one(rows, cols), x, gate, up, wg, wu, one(cols, inner), act=act)
+    return y.double(), dwg[:, 0].double(), dwu[:, 0].double()
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("rows", [3, 200, 5000])
+def test_gates_far_below_leave_nothing(rows, act):
+    """act and its derivative are zero, or below 1e-24, from -60 down to the type's last value.
+
+    A sum of 16 such values, times cols = 8 and up to 5000 rows, and of their roundings: below 1e-18."""
+    y, dwg, dwu = far_gates(rows, torch.bfloat16, act, [-v for v in FAR] + [-3e38])
+    for m, name in ((y, "y"), (dwg, "dw_gate"), (dwu, "dw_up")):
+        assert float(m.abs().max()) < 1e-18, (name, m.abs().max())
+
+
 @pytest.mark.parametrize("pad", [1, 4, 8])
 @pytest.mark.parametrize("rows", [2, 33, 300])
 @pytest.mark.parametrize("t", TYPES)

@@ -60,7 +60,8 @@ __device__ __forceinline__ void activation(float v, float& a, float& da) {
   } else if (ACT == GN_ACT_GELU_TANH) {        // (1 + tanh q) / 2 = 1 / (1 + exp(-2 q)), q = sqrt(2 / pi) (v + 0.044715 v^3)
     const float s = v * v;
     sigmoids<FAST>(v * fmaf(s, 0.071354816272810f, 1.5957691216057308f), z, nz);
-    a = v * z; da = fmaf(a * nz, fmaf(s, 0.214064448818430f, 1.5957691216057308f), z);
+    // (beyond |v| = 100, where z nz is zero, v^2 is bounded: it would overflow, and zero times infinity is not zero)
+    a = v * z; da = fmaf(a * nz, fmaf(fminf(s, 1e4f), 0.214064448818430f, 1.5957691216057308f), z);
   } else if (ACT == GN_ACT_SIGMOID) {
     sigmoids<FAST>(v, z, nz); a = z; da = z * nz;
   } else {

@@ -19,6 +19,7 @@ import torch
 from .binding import GnError, lib
 
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_WIDE = 1 << 31                          # widths are 32-bit words of the library's calls, and what does not fit would be cut off on the way
 ACTIVATIONS = {"sigmoid": 0, "silu": 1, "gelu": 2, "gelu_tanh": 3, "relu": 4}
 
 # A small call is bound by what the host does for it, so the ordinary case (contiguous tensors on the current device and stream) takes few steps:
@@ -75,6 +76,8 @@ def _first(t, what):
     shape = t.shape
     if len(shape) != 2 or shape[1] < 1:
         raise ValueError(f"{what}: expected a matrix with at least one column, got shape {tuple(shape)}")
+    if shape[1] >= _WIDE:
+        raise ValueError(f"{what}: expected fewer than 2^31 columns, got shape {tuple(shape)}")
     return dtype, dev, shape[0], shape[1]
 
 
@@ -196,6 +199,8 @@ def _ffn_inputs(x, w_gate, w_up, w_down, act):
     if not isinstance(w_gate, torch.Tensor) or w_gate.dim() != 2 or w_gate.shape[0] < 1:
         raise (ValueError if isinstance(w_gate, torch.Tensor) else TypeError)("w_gate: expected a matrix with at least one row")
     inner = w_gate.shape[0]
+    if inner >= _WIDE:
+        raise ValueError(f"w_gate: expected fewer than 2^31 rows, got shape {tuple(w_gate.shape)}")
     words = [_TYPES[dtype] | a << 32, rows, cols | inner << 32, *_matrix(x, "x", rows, cols, dtype, dev),
              *_matrix(w_gate, "w_gate", inner, cols, dtype, dev), *_matrix(w_up, "w_up", inner, cols, dtype, dev),
              *_matrix(w_down, "w_down", cols, inner, dtype, dev)]

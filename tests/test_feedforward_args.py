@@ -114,3 +114,25 @@ def test_the_binding_refuses_tensors_that_are_not_on_a_device():
                  lambda: gn.gated_ffn(x, x, x, x), lambda: gn.gated_ffn_grad(x, x, x, x, x, x, x)):
         with pytest.raises(TypeError, match="CUDA"):
             call()
+
+
+class OnDevice(torch.Tensor):
+    """A tensor without memory that says it is on device 0."""
+
+    def get_device(self):
+        return 0
+
+
+@pytest.mark.parametrize("cols", [1 << 31, 1 << 32, (1 << 32) + 8])
+def test_the_binding_refuses_widths_beyond_the_library(cols):
+    """Cut to 32 bits, 2^32 + 8 columns would be 8."""
+    x = torch.empty(1, cols, dtype=torch.bfloat16, device="meta").as_subclass(OnDevice)
+    w = torch.empty(4, cols, dtype=torch.bfloat16, device="meta").as_subclass(OnDevice)
+    v = torch.empty(1, device="meta").as_subclass(OnDevice)
+    for call in (lambda: gn.layer_norm(x), lambda: gn.layer_norm_grad(x, x, v, v), lambda: gn.dropout(x, 0.1, 1),
+                 lambda: gn.gated_ffn(x, w, w, w), lambda: gn.gated_ffn_grad(x, x, w, w, w, w, w)):
+        with pytest.raises(ValueError, match="fewer than 2\\^31 columns"):
+            call()
+    narrow, tall = (torch.empty(*s, dtype=torch.bfloat16, device="meta").as_subclass(OnDevice) for s in ((1, 8), (cols, 8)))
+    with pytest.raises(ValueError, match="fewer than 2\\^31 rows"):
+        gn.gated_ffn(narrow, tall, tall, narrow)

@@ -146,8 +146,8 @@ def layer_norm_grad(dy, x, mean, rstd, weight=None, add=None, stream=None):
     pw = _vector(weight, "weight", cols, dev, dtype, torch.float32)
     wtype = dtype if weight is None else weight.dtype
     handle = lib()
-    n = handle.gn_layer_norm_grad_workspace(rows, cols)
-    dx, ws = x.new_empty(rows, cols), x.new_empty(n // x.element_size())
+    n = handle.gn_layer_norm_grad_workspace(rows, cols)              # (negative for sizes that the call is to refuse)
+    dx, ws = x.new_empty(rows, cols), x.new_empty(max(n, 16) // x.element_size())
     if wtype is dtype:
         dw, db = x.new_empty(cols), x.new_empty(cols)
     else:

@@ -296,3 +296,11 @@ def test_refusals():
             bad()
     with pytest.raises(gn.GnError, match="eps"):
         gn.layer_norm(x, eps=-1.0)
+
+
+def test_rows_too_long_are_refused_by_the_library():
+    x = torch.zeros(1, (1 << 20) + 1, dtype=torch.bfloat16, device="cuda")
+    one = torch.ones(1, device="cuda")
+    for call in (lambda: gn.layer_norm(x), lambda: gn.layer_norm_grad(x, x, one, one)):
+        with pytest.raises(gn.GnError, match="cols must be in"):
+            call()

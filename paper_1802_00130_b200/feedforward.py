@@ -5,7 +5,8 @@
 Matrices are 2-D CUDA tensors of float32, bfloat16 or float16 with unit stride inside a row (rows may be apart, as in a view
 of a wider matrix); all tensors of a call are on one device and, where not said otherwise, of one type.  A call enqueues on `stream`
 (default: the current stream of that device), never synchronises, and returns new tensors that belong to that stream; it can be
-captured into a CUDA graph once a call of its kind has run on the device.  Nothing here takes part in autograd: the backward
+captured into a CUDA graph once a call of its kind has run on the device.  A given `stream` does not wait for the current one, which the
+caller sees to (Stream.wait_stream), but the arguments' memory is kept until it is done with them, whether or not the caller drops them.  Nothing here takes part in autograd: the backward
 passes are calls of their own.  Bad arguments raise TypeError or ValueError, the library's own refusals GnError.
 """
 from __future__ import annotations
@@ -89,10 +90,16 @@ def _elsewhere(call, dev, stream, *args):
     if stream is None:
         with torch.cuda.device(dev):
             return call(*args)
+    if not isinstance(stream, torch.cuda.Stream):
+        raise TypeError(f"stream: expected a torch.cuda.Stream, got {type(stream).__name__}")
     if stream.device.index != dev:
         raise ValueError(f"the stream is one of {stream.device}, the tensors are on cuda:{dev}")
     with torch.cuda.device(dev), torch.cuda.stream(stream):
-        return call(*args)
+        out = call(*args)
+    for t in args:                       # (memory of another stream's may be dropped, and handed out again, before this one has read it)
+        if isinstance(t, torch.Tensor):
+            t.record_stream(stream)
+    return out
 
 
 def _checked(status, err):

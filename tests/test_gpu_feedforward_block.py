@@ -120,3 +120,41 @@ def test_single_tokens_agree_with_a_batch():
         some = gn.gated_ffn(gn.layer_norm(x[:n], q["w"], q["b"]), q["gate"], q["up"], q["down"])
         # h and y rounded once in each form: four half steps at most, independent
         assert float((some.double() - batch[:n].double()).norm() / batch[:n].double().norm()) < 4 * torch.finfo(t).eps / 2
+
+
+@pytest.mark.parametrize("rows", [3, 300])
+def test_arguments_dropped_after_a_call_on_another_stream(rows):
+    """Their memory is not handed out again before that stream has read it: the calls wait behind a pause of some 50 ms, while the current
+    stream allocates tensors of the same sizes and fills them."""
+    t = torch.bfloat16
+    q, side = parameters(256, 520, t), torch.cuda.Stream()
+    x, dout = rand((rows, 256), t, 1), rand((rows, 256), t, 2)
+    step = torch.tensor([1], dtype=torch.int64, device="cuda")
+    h, mean, rstd = gn.layer_norm(x, q["w"], q["b"], save=True)
+    y, gate, up = gn.gated_ffn(h, q["gate"], q["up"], q["down"], save=True)
+    W = (q["gate"], q["up"], q["down"])
+    calls = [(gn.layer_norm, (x, q["w"], q["b"])), (gn.layer_norm_grad, (dout, x, mean, rstd, q["w"], dout)), (gn.dropout, (x, P, KEY, STEP, dout, step)),
+             (gn.gated_ffn, (h, *W)), (gn.gated_ffn_grad, (dout, h, gate, up, *W))]
+    for call, args in calls:
+        want = call(*args)
+        mine = [a.clone() if torch.is_tensor(a) else a for a in args]
+        places = {a.data_ptr(): a.shape for a in mine if torch.is_tensor(a)}
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+        got = call(*mine, stream=side)
+        del mine
+        over = []
+        for shape in [shape for shape in places.values() for _ in range(4)]:
+            over.append(torch.full(shape, 1 if tuple(shape) == (1,) else 7, dtype=torch.int64 if tuple(shape) == (1,) else t, device="cuda"))
+            assert over[-1].data_ptr() not in places or side.query()          # (an allocation that waits for the device may outlast the pause)
+        torch.cuda.synchronize()
+        one = lambda r: r if isinstance(r, tuple) else (r,)
+        assert all(torch.equal(a, b) for a, b in zip(one(got), one(want)))
+
+
+def test_a_stream_is_a_stream_of_the_tensors_device():
+    x = rand((4, 16), torch.bfloat16, 1)
+    for bad in (0, "side", torch.device("cuda")):
+        with pytest.raises(TypeError, match="torch.cuda.Stream"):
+            gn.layer_norm(x, stream=bad)

@@ -5,6 +5,7 @@ import concurrent.futures
 import os
 import subprocess
 import sys
+import time
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -32,36 +33,52 @@ def is_stale():
 
 def build(force=False, verbose=False):
     """Compile libgn_b200.so next to this file; returns its path.  Each source becomes an object in _build/, several at a time; one whose
-    source and headers are older than its object is taken over unless `force`."""
+    source and headers are older than its object is taken over, if it was compiled by the same command, unless `force`."""
     if not force and not is_stale():
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
     # GN_NVTX=1: named ranges around the phases of the path for timeline tools (header-only NVTX, off by default)
     extra = ["-DGN_NVTX"] if os.environ.get("GN_NVTX") == "1" else []
+    compiler = [nvcc] + [f for f in FLAGS if f != "-shared"] + extra
     out_dir = os.path.join(HERE, "_build")
     os.makedirs(out_dir, exist_ok=True)
+    objects = [os.path.join(out_dir, s + ".o") for s in SOURCES]
+    command = os.path.join(out_dir, "command")           # that the objects were compiled by
+    if not os.path.exists(command) or open(command).read() != "\n".join(compiler):
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
+        with open(command, "w") as f:
+            f.write("\n".join(compiler))
     newest = max(os.path.getmtime(p) for p in _deps() if not p.endswith(".cu"))
 
-    def compile_one(source):
-        src, obj = os.path.join(CSRC, source), os.path.join(out_dir, source + ".o")
-        if not force and not extra and os.path.exists(obj) and os.path.getmtime(obj) > max(newest, os.path.getmtime(src)):
-            return obj
-        cmd = [nvcc] + [f for f in FLAGS if f != "-shared"] + extra + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-o", obj, source]
-        _run(cmd, verbose)
-        return obj
+    def compile_one(source, obj):
+        if not force and os.path.exists(obj) and os.path.getmtime(obj) > max(newest, os.path.getmtime(os.path.join(CSRC, source))):
+            return
+        _make(compiler + (["-Xptxas", "-v"] if verbose else []), ["-c", source], obj, verbose)
 
+    begin = time.time()
     with concurrent.futures.ThreadPoolExecutor(os.cpu_count() or 1) as pool:
-        objects = list(pool.map(compile_one, SOURCES))
-    _run([nvcc] + FLAGS + ["-o", LIB] + objects, verbose)
+        list(pool.map(compile_one, SOURCES, objects))
+    _make([nvcc] + FLAGS, objects, LIB, verbose, begin)
     return LIB
 
 
-def _run(cmd, verbose):
-    res = subprocess.run(cmd, cwd=CSRC, capture_output=True, text=True)
-    if verbose:
-        sys.stderr.write(res.stderr)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+def _make(command, args, out, verbose, begin=None):
+    """Run `command -o out args`.  `out` is there whole or not at all, and as old as what was read for it may be: an edit made meanwhile is newer."""
+    begin = begin or time.time()
+    part = f"{out}.{os.getpid()}.part"
+    try:
+        res = subprocess.run(command + ["-o", part] + args, cwd=CSRC, capture_output=True, text=True)
+        if verbose:
+            sys.stderr.write(res.stderr)
+        if res.returncode != 0:
+            raise RuntimeError("nvcc failed:\n" + res.stdout + res.stderr)
+        os.utime(part, (begin, begin))
+        os.replace(part, out)
+    finally:
+        if os.path.exists(part):
+            os.remove(part)
 
 
 if __name__ == "__main__":

@@ -26,7 +26,7 @@ struct FfnGemm {
 constexpr int kFfnGroup = 4;     // problems of one launch (FFN_STORE)
 
 // CTA-pair kernels (gemm_pair16.cu).  Returns cudaSuccess, or what the launch or the maps failed with.  ws: ffn_pair_workspace bytes for the same
-// products (FFN_STORE; sizes alone count).
+// products (FFN_STORE; sizes alone count).  Of FFN_GATE (operands K-major) and FFN_GRAD (B [K][N]) one product with one pair of operands.
 int64_t ffn_pair_workspace(const FfnGemm* g, int n);
 cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, void* ws, int* err, cudaStream_t st);
 

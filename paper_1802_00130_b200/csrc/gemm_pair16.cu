@@ -1,7 +1,7 @@
-// Products of 16-bit matrices for the gated feed-forward block: a CTA pair per 256 x bn tile (tcgen05.mma.cta_group::2, operands by
-// TMA, accumulators in tensor memory), with the gate, its gradient or a plain rounding as the epilogue.
+// Products of 16-bit matrices for the gated feed-forward block: a CTA pair per tile (tcgen05.mma.cta_group::2, operands by TMA, accumulators in
+// tensor memory).  ffn_pair_kernel has 256 x bn tiles, with the gate or its gradient as the epilogue; ffn_wide_kernel, below, plain products.
 //
-// Persistent: one pair for two SMs, tiles dealt in turn.  Warp roles in each CTA:
+// Persistent: one pair for two SMs, tiles dealt in turn.  Warp roles in each CTA of ffn_pair_kernel:
 //   warp 0      TMA producer: a ring of STAGES slots, each this CTA's 128 rows of A and its half of the B tile, 64 terms of K
 //   warp 1      MMA issuer (leader CTA only), one thread
 //   warps 2..   epilogue, beside the next tile's products where two accumulators fit the tensor memory (256 x 256 tiles)
@@ -34,16 +34,17 @@ constexpr int P_SMEM = P_STAGES * P_STAGE_BYTES + P_STG_ALL + 1024 + 256;
 static_assert(P_SMEM <= 232448, "more shared memory than a block can have");
 constexpr int P_PANELS = 8;       // tiles are walked in strips of so many row panels: 74 tiles at a time read 8 panels of A and 9 of B
 
-struct PairProblem {
-  int M, N, bn, tiles_m, tiles_n, tiles;
-  int kb0, kb;                    // k-blocks of the first operand pair, of both
-  int a_mn, b_mn, vec;            // vec: bit k: 16-byte accesses for d[k]
-  int a_box3, b_box3;             // an MN-major operand of whole 64-column chunks: one box of several chunks instead of a box each
+struct PairParams {
+  int M, N, bn, tiles_m, tiles_n, tiles, pairs;
+  int kb;                         // k-blocks
+  int vec, act;                   // vec: bit k: 16-byte accesses for d[k]
+  int b_box3;                     // an MN-major B of whole 64-column chunks: one box of several chunks instead of a box each
   Out16 d[3];
   Mat16 gate, up;
+  int* err;
 };
-template <int NP> struct PairParams { PairProblem p[NP]; int n, act, pairs, tiles; int* err; };
-template <int NP> struct PairMaps { CUtensorMap m[NP][4]; };   // A0, B0, A1, B1 (FFN_GATE: A, gate weights, -, up weights)
+struct PairMaps { CUtensorMap m[3]; };           // A, B (FFN_GATE: gate weights, up weights)
+template <int NP> struct WideMaps { CUtensorMap m[NP][4]; };   // A0, B0, A1, B1
 
 template <bool BF16>
 __device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accum) {
@@ -74,17 +75,11 @@ __device__ __forceinline__ void tmem_ld32_pair(uint32_t a, uint32_t b, float (&x
       : "r"(a), "r"(b) : "memory");
 }
 
-// Problem and tile of the t-th piece of work.
-template <int NP>
-__device__ __forceinline__ int find_tile(const PairParams<NP>& g, int t, int& m, int& n) {
-  int k = 0;
-  if (NP > 1)
-    while (k + 1 < g.n && t >= g.p[k].tiles) t -= g.p[k++].tiles;
-  const PairProblem& p = g.p[k];
+// Place of the t-th tile.
+__device__ __forceinline__ void find_tile(const PairParams& p, int t, int& m, int& n) {
   const int strip = t / (P_PANELS * p.tiles_n), rest = t - strip * P_PANELS * p.tiles_n;
   const int high = min(P_PANELS, p.tiles_m - strip * P_PANELS);
   m = strip * P_PANELS + rest % high; n = rest / high;
-  return k;
 }
 
 __device__ __forceinline__ void sts16(uint32_t a, uint4 v) {
@@ -218,9 +213,11 @@ __device__ __forceinline__ void tmem_ld16_pair(uint32_t a, uint32_t b, float (&x
       : "r"(a), "r"(b) : "memory");
 }
 
-template <int KIND, class T, int NP>
+template <int KIND, class T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads<KIND>, 1)
-ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant__ PairParams<NP> g) {
+ffn_pair_kernel(const __grid_constant__ PairMaps maps, const __grid_constant__ PairParams p) {
+  static_assert(KIND == FFN_GATE || KIND == FFN_GRAD, "plain products: ffn_wide_kernel");
+  constexpr bool B_MN = KIND == FFN_GRAD;          // (dy is K-major, Wd [cols][inner] is not; the forward pass' operands are)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* staging = smem + P_STAGES * P_STAGE_BYTES;
@@ -258,75 +255,58 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
       uint32_t ph = 0;
       bool ok = true;
       const uint32_t full_leader = map_to_cta(smem_u32(&full[0]), 0);
-      for (int t = pair; ok && t < g.tiles; t += g.pairs) {
+      const int hb = p.bn >> 1;                            // B rows staged by each CTA
+      const uint32_t pair_tx = 2u * (P_A_BYTES + (uint32_t)hb * 128u);
+      const CUtensorMap* const ma = &maps.m[0];
+      const CUtensorMap* const mb = &maps.m[KIND == FFN_GATE && rank ? 2 : 1];
+      const bool b3 = p.b_box3 != 0;
+      for (int t = pair; ok && t < p.tiles; t += p.pairs) {
         int tm, tn;
-        const int k = find_tile(g, t, tm, tn);
-        const PairProblem& p = g.p[k];
-        const int hb = p.bn >> 1;                          // B rows staged by each CTA
+        find_tile(p, t, tm, tn);
         const int m0 = tm * 2 * P_BM + (int)rank * P_BM;
         const int n0 = KIND == FFN_GATE ? tn * hb : tn * p.bn + (int)rank * hb;
-        const uint32_t pair_tx = 2u * (P_A_BYTES + (uint32_t)hb * 128u);
-        const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0, a3 = p.a_box3 != 0, b3 = p.b_box3 != 0;
-        const int kb_first = p.kb0, kb_all = p.kb;
         // (one thread issues everything: nothing is in the loop that need not be there)
 #pragma unroll 1
-        for (int part = 0; part < 2 && ok; ++part) {
-          const int end = part ? kb_all - kb_first : kb_first;
-          const CUtensorMap* const ma = &maps.m[k][2 * part];
-          const CUtensorMap* const mb = KIND == FFN_GATE ? &maps.m[k][rank ? 3 : 1] : ma + 1;
-#pragma unroll 1
-          for (int kb = 0; kb < end; ++kb) {
-            if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, g.err, 1)) { ok = false; break; }
-            if (rank == 0) mbar_expect_tx(&full[s], pair_tx);
-            const uint32_t bar = full_leader + (uint32_t)s * 8u;
-            const int k0 = kb * P_BK;
-            uint8_t* const sa = smem + s * P_STAGE_BYTES;
-            uint8_t* const sb = sa + P_A_BYTES;
-            if (!a_mn) {
-              tma2_load_2d(sa, ma, k0, m0, bar);
-            } else if (a3) {
-              tma2_load_3d(sa, ma, 0, k0, m0 >> 6, bar);
-            } else {
-              tma2_load_2d(sa, ma, m0, k0, bar);
-              tma2_load_2d(sa + 8192, ma, m0 + 64, k0, bar);
-            }
-            if (!b_mn) {
-              tma2_load_2d(sb, mb, k0, n0, bar);
-            } else if (b3) {
-              tma2_load_3d(sb, mb, 0, k0, n0 >> 6, bar);
-            } else {
-              tma2_load_2d(sb, mb, n0, k0, bar);
-              if (hb > 64) tma2_load_2d(sb + 8192, mb, n0 + 64, k0, bar);
-            }
-            if (++s == P_STAGES) { s = 0; ph ^= 1u; }
+        for (int kb = 0; kb < p.kb; ++kb) {
+          if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, p.err, 1)) { ok = false; break; }
+          if (rank == 0) mbar_expect_tx(&full[s], pair_tx);
+          const uint32_t bar = full_leader + (uint32_t)s * 8u;
+          const int k0 = kb * P_BK;
+          uint8_t* const sa = smem + s * P_STAGE_BYTES;
+          uint8_t* const sb = sa + P_A_BYTES;
+          tma2_load_2d(sa, ma, k0, m0, bar);
+          if (!B_MN) {
+            tma2_load_2d(sb, mb, k0, n0, bar);
+          } else if (b3) {
+            tma2_load_3d(sb, mb, 0, k0, n0 >> 6, bar);
+          } else {
+            tma2_load_2d(sb, mb, n0, k0, bar);
+            if (hb > 64) tma2_load_2d(sb + 8192, mb, n0 + 64, k0, bar);
           }
+          if (++s == P_STAGES) { s = 0; ph ^= 1u; }
         }
       }
     }
   } else if (warp == 1) {
     if (rank == 0 && lane == 0) {
-      constexpr bool BF16 = sizeof(T) == 2 && !__is_same(T, __half);
+      constexpr bool BF16 = !__is_same(T, __half);
       const uint32_t base = smem_u32(smem);
+      const uint32_t idesc = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)((2 * P_BM) >> 4) << 24);
+      constexpr uint64_t a_step = 32 >> 4, b_step = (B_MN ? 2048 : 32) >> 4;
+      const uint64_t a0 = make_desc(base, 16, 1024, 2);
+      const uint64_t b0 = make_desc(base + P_A_BYTES, B_MN ? 8192 : 16, 1024, 2);
       int s = 0, ti = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int t = pair; ok && t < g.tiles; t += g.pairs, ++ti) {
-        int tm, tn;
-        const PairProblem& p = g.p[find_tile(g, t, tm, tn)];
+      for (int t = pair; ok && t < p.tiles; t += p.pairs, ++ti) {
         const int buf = ti & 1;
-        if (!wait_or_abort(&acc_empty[buf], ((ti >> 1) & 1) ^ 1, abort_flag, g.err, 4)) break;
+        if (!wait_or_abort(&acc_empty[buf], ((ti >> 1) & 1) ^ 1, abort_flag, p.err, 4)) break;
         tc_fence_after();
         const uint32_t tmem_d = tmem_base + (uint32_t)(buf * P_BN);
-        const uint32_t idesc = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)p.a_mn << 15) | ((uint32_t)p.b_mn << 16) |
-                               ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)((2 * P_BM) >> 4) << 24);
-        const uint64_t a_step = (p.a_mn ? 2048 : 32) >> 4, b_step = (p.b_mn ? 2048 : 32) >> 4;
-        const uint64_t a0 = make_desc(base, p.a_mn ? 8192 : 16, 1024, 2);
-        const uint64_t b0 = make_desc(base + P_A_BYTES, p.b_mn ? 8192 : 16, 1024, 2);
         uint32_t acc = 0u;
-        const int kbs = p.kb;
 #pragma unroll 1
-        for (int kb = 0; kb < kbs; ++kb) {
-          if (!wait_or_abort(&full[s], ph, abort_flag, g.err, 2)) { ok = false; break; }
+        for (int kb = 0; kb < p.kb; ++kb) {
+          if (!wait_or_abort(&full[s], ph, abort_flag, p.err, 2)) { ok = false; break; }
           tc_fence_after();
           const uint64_t ad = a0 + (uint64_t)(s * (P_STAGE_BYTES >> 4)), bd = b0 + (uint64_t)(s * (P_STAGE_BYTES >> 4));
           pair_mma<BF16>(tmem_d, ad, bd, idesc, acc);
@@ -347,9 +327,9 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
     const uint32_t stg = smem_u32(staging + (warp - 2) * (P_STG_ALL / epi_warps<KIND>));
     const uint32_t acc_leader = map_to_cta(smem_u32(&acc_empty[0]), 0);
     int ti = 0;
-    for (int t = pair; t < g.tiles; t += g.pairs, ++ti) {
+    for (int t = pair; t < p.tiles; t += p.pairs, ++ti) {
       int tm, tn;
-      const PairProblem& p = g.p[find_tile(g, t, tm, tn)];
+      find_tile(p, t, tm, tn);
       const int width = KIND == FFN_GATE ? p.bn >> 1 : p.bn;          // columns of the result
       const int m0 = tm * 2 * P_BM + (int)rank * P_BM + quad * 32, n0 = tn * width;
       const int chunks = m0 < p.M ? min(width / COLS, (p.N - n0 + COLS - 1) / COLS) : 0;
@@ -360,12 +340,12 @@ ffn_pair_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant
         fetch_chunk(ux, lane, dep(p.up.p), p.up.ld, m0, p.M, n0 + first * COLS, p.N);
       }
       int good = 1;
-      if (lane == 0) good = wait_or_abort(&acc_full[buf], (ti >> 1) & 1, abort_flag, g.err, 3) ? 1 : 0;
+      if (lane == 0) good = wait_or_abort(&acc_full[buf], (ti >> 1) & 1, abort_flag, p.err, 3) ? 1 : 0;
       good = __shfl_sync(0xffffffffu, good, 0);
       if (!good) break;
       tc_fence_after();
       const uint32_t tq = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(buf * P_BN);
-      with_activation(g.act, [&](auto act) {
+      with_activation(p.act, [&](auto act) {
         constexpr int ACT = decltype(act)::value;
 #pragma unroll 1
         for (int c = first; c < chunks; c += STEP) {
@@ -477,7 +457,7 @@ __device__ __forceinline__ WideItem wide_item(const WideParams<NP>& g, int i) {
 
 template <class T, int NP, bool CUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(W_THREADS, 1)
-ffn_wide_kernel(const __grid_constant__ PairMaps<NP> maps, const __grid_constant__ WideParams<NP> g) {
+ffn_wide_kernel(const __grid_constant__ WideMaps<NP> maps, const __grid_constant__ WideParams<NP> g) {
   constexpr bool BF16 = !__is_same(T, __half);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -736,14 +716,14 @@ bool make_map16_chunks(CUtensorMap* m, const Mat16& a, long long rows, long long
 }
 template <class P> bool vec16(const P& m) { return !m.p || (((uintptr_t)m.p & 15) == 0 && m.ld % 8 == 0); }
 
-// Maps of one problem's operands, those that it has.
-bool encode_problem(CUtensorMap* maps, const FfnGemm& g, bool gate, bool a_box3, bool b_box3, int rows_b, bool bf16) {
-  for (int s = 0; s < (gate || g.K[1] > 0 ? 2 : 1); ++s) {
-    const int a = gate ? 0 : s, b = s, K = g.K[a];
-    const auto encode = [&](CUtensorMap* to, const Mat16& mat, bool mn, bool box3, int MN, int rows) {
-      return !mn ? make_map16(to, mat, MN, K, rows, bf16) : box3 ? make_map16_chunks(to, mat, K, MN, rows / 64, bf16) : make_map16(to, mat, K, MN, 64, bf16);
+// Maps of a plain product's operands, those that it has.
+bool encode_problem(CUtensorMap* maps, const FfnGemm& g, bool a_box3, bool b_box3, bool bf16) {
+  for (int s = 0; s < (g.K[1] > 0 ? 2 : 1); ++s) {
+    const int K = g.K[s];
+    const auto encode = [&](CUtensorMap* to, const Mat16& mat, bool mn, bool box3, int MN) {
+      return !mn ? make_map16(to, mat, MN, K, P_BM, bf16) : box3 ? make_map16_chunks(to, mat, K, MN, P_BM / 64, bf16) : make_map16(to, mat, K, MN, 64, bf16);
     };
-    if ((gate && s ? false : !encode(&maps[2 * s], g.A[a], g.a_mn, a_box3, g.M, P_BM)) || !encode(&maps[2 * s + 1], g.B[b], g.b_mn, b_box3, g.N, rows_b)) return false;
+    if (!encode(&maps[2 * s], g.A[s], g.a_mn, a_box3, g.M) || !encode(&maps[2 * s + 1], g.B[s], g.b_mn, b_box3, g.N)) return false;
   }
   return true;
 }
@@ -755,38 +735,34 @@ long long pair_rounds(int kind, int M, int N, int bn) {
 }
 int pair_width(int kind, int M, int N) { return pair_rounds(kind, M, N, 128) * 5 < pair_rounds(kind, M, N, 256) * 8 ? 128 : 256; }
 
-template <int KIND, class T, int NP>
-cudaError_t launch_pair_as(int act, const FfnGemm* g, int n, int* err, cudaStream_t st) {
+template <int KIND, class T>
+cudaError_t launch_pair_as(int act, const FfnGemm& g, int* err, cudaStream_t st) {
   constexpr bool BF16 = !__is_same(T, __half);
   static std::atomic<signed char> ready[64];
-  auto* const kernel = ffn_pair_kernel<KIND, T, NP>;
+  auto* const kernel = ffn_pair_kernel<KIND, T>;
   if (!once_per_device(ready, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, P_SMEM) == cudaSuccess; }))
     return cudaErrorInvalidDevice;
-  PairMaps<NP> maps;
-  PairParams<NP> q = {};
-  q.n = n; q.act = act; q.err = err;
-  const int pairs = num_sms() / 2;
-  const int bn = pair_width(KIND, g[0].M, g[0].N);
-  long long tiles = 0;
-  for (int i = 0; i < n; ++i) {
-    PairProblem& p = q.p[i];
-    const int width = KIND == FFN_GATE ? bn / 2 : bn;
-    p.M = g[i].M; p.N = g[i].N; p.bn = bn;
-    p.tiles_m = (p.M + 255) / 256; p.tiles_n = (p.N + width - 1) / width;
-    tiles += (long long)p.tiles_m * p.tiles_n;
-    if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
-    p.tiles = p.tiles_m * p.tiles_n;
-    p.kb0 = (g[i].K[0] + P_BK - 1) / P_BK; p.kb = p.kb0 + (g[i].K[1] + P_BK - 1) / P_BK;
-    p.a_mn = g[i].a_mn; p.b_mn = g[i].b_mn;
-    p.a_box3 = p.a_mn && p.M % 64 == 0; p.b_box3 = p.b_mn && p.N % 64 == 0;
-    for (int k = 0; k < 3; ++k) p.d[k] = g[i].d[k];
-    p.gate = g[i].gate; p.up = g[i].up;
-    p.vec = vec16(p.d[0]) | vec16(p.d[1]) << 1 | vec16(p.d[2]) << 2;
-    if (!encode_problem(maps.m[i], g[i], KIND == FFN_GATE, p.a_box3, p.b_box3, bn / 2, BF16)) return cudaErrorInvalidValue;
-  }
-  q.tiles = (int)tiles;
-  q.pairs = (int)(tiles < pairs ? tiles : pairs);
-  return launch_pdl(kernel, 2 * q.pairs, pair_threads<KIND>, P_SMEM, st, maps, q);
+  PairMaps maps;
+  PairParams p = {};
+  const int pairs = num_sms() / 2, bn = pair_width(KIND, g.M, g.N), width = KIND == FFN_GATE ? bn / 2 : bn;
+  p.M = g.M; p.N = g.N; p.bn = bn;
+  p.tiles_m = (p.M + 255) / 256; p.tiles_n = (p.N + width - 1) / width;
+  const long long tiles = (long long)p.tiles_m * p.tiles_n;
+  if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
+  p.tiles = (int)tiles;
+  p.pairs = p.tiles < pairs ? p.tiles : pairs;
+  p.kb = (g.K[0] + P_BK - 1) / P_BK;
+  p.b_box3 = KIND == FFN_GRAD && p.N % 64 == 0;
+  for (int k = 0; k < 3; ++k) p.d[k] = g.d[k];
+  p.gate = g.gate; p.up = g.up;
+  p.vec = vec16(p.d[0]) | vec16(p.d[1]) << 1 | vec16(p.d[2]) << 2;
+  p.act = act; p.err = err;
+  const auto rows_of_b = [&](CUtensorMap* m, const Mat16& b) { return make_map16(m, b, g.N, g.K[0], bn / 2, BF16); };
+  bool ok = make_map16(&maps.m[0], g.A[0], g.M, g.K[0], P_BM, BF16);
+  if constexpr (KIND == FFN_GATE) ok = ok && rows_of_b(&maps.m[1], g.B[0]) && rows_of_b(&maps.m[2], g.B[1]);
+  else ok = ok && (p.b_box3 ? make_map16_chunks(&maps.m[1], g.B[0], g.K[0], g.N, bn / 128, BF16) : make_map16(&maps.m[1], g.B[0], g.K[0], g.N, 64, BF16));
+  if (!ok) return cudaErrorInvalidValue;
+  return launch_pdl(kernel, 2 * p.pairs, pair_threads<KIND>, P_SMEM, st, maps, p);
 }
 
 // How a group of products is cut: slices of K for each (all 1: none), and the items that makes.  Estimated times, in us: a k-block of a 256 x 512 tile 0.36
@@ -841,7 +817,7 @@ cudaError_t launch_wide_as(const FfnGemm* g, int n, const WidePlan& plan, void* 
   auto* const kernel = ffn_wide_kernel<T, NP, CUT>;
   if (!once_per_device(ready, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, W_SMEM) == cudaSuccess; }))
     return cudaErrorInvalidDevice;
-  PairMaps<NP> maps;
+  WideMaps<NP> maps;
   WideParams<NP> q = {};
   q.n = n; q.err = err; q.ws = (float*)ws;
   long long tiles = 0, summed = 0;
@@ -859,7 +835,7 @@ cudaError_t launch_wide_as(const FfnGemm* g, int n, const WidePlan& plan, void* 
     p.a_box3 = p.a_mn && p.M % 64 == 0; p.b_box3 = p.b_mn && p.N % 64 == 0;
     p.d = g[i].d[0];
     p.vec = vec16(p.d);
-    if (!encode_problem(maps.m[i], g[i], false, p.a_box3, p.b_box3, P_BM, BF16)) return cudaErrorInvalidValue;
+    if (!encode_problem(maps.m[i], g[i], p.a_box3, p.b_box3, BF16)) return cudaErrorInvalidValue;
   }
   const int pairs = num_sms() / 2, rem = (int)(tiles % pairs);
   q.whole = (int)(2 * rem <= pairs ? tiles - rem : tiles);
@@ -887,8 +863,8 @@ int64_t ffn_pair_workspace(const FfnGemm* g, int n) {
 }
 
 cudaError_t launch_ffn_pair(FfnKind kind, bool bf16, int act, const FfnGemm* g, int n, void* ws, int* err, cudaStream_t st) {
-  if (kind == FFN_GATE) return bf16 ? launch_pair_as<FFN_GATE, __nv_bfloat16, 1>(act, g, n, err, st) : launch_pair_as<FFN_GATE, __half, 1>(act, g, n, err, st);
-  if (kind == FFN_GRAD) return bf16 ? launch_pair_as<FFN_GRAD, __nv_bfloat16, 1>(act, g, n, err, st) : launch_pair_as<FFN_GRAD, __half, 1>(act, g, n, err, st);
+  if (kind == FFN_GATE) return bf16 ? launch_pair_as<FFN_GATE, __nv_bfloat16>(act, *g, err, st) : launch_pair_as<FFN_GATE, __half>(act, *g, err, st);
+  if (kind == FFN_GRAD) return bf16 ? launch_pair_as<FFN_GRAD, __nv_bfloat16>(act, *g, err, st) : launch_pair_as<FFN_GRAD, __half>(act, *g, err, st);
   const WidePlan plan = plan_wide(g, n);
   const auto launch = [&](auto t) {
     using T = decltype(t);

@@ -41,8 +41,11 @@ __device__ __forceinline__ void normal(float v, float& cdf, float& e) {
     const float q = p * t * e;
     cdf = v < 0.f ? q : 1.f - q;
   } else {
-    cdf = 0.5f * erfcf(-0.70710678118654752f * v);
-    e = expf(-0.5f * v * v);
+    // (the roundings of v / sqrt 2 and of v^2 come with a factor of v^2 in the tails, 45 steps at |v| = 6: taken back to first order, where e is not zero)
+    const float c = -0.70710678118654752f, q = copysignf(fminf(fabsf(v), 30.f), v), s = q * q, x = c * q;
+    e = expf(-0.5f * s);
+    e = fmaf(-0.5f * fmaf(q, q, -s), e, e);
+    cdf = fmaf(-0.56418958354775629f * e, fmaf(c, q, -x) + q * -1.2101617e-8f, 0.5f * erfcf(c * v));       // 1 / sqrt pi; what c's rounding has left
   }
 }
 // act(v) and its derivative.  A NaN stays one: comparisons with it fall to the branch that computes with it.

@@ -1,5 +1,6 @@
 """Gated feed-forward block and its backward pass against a plain form in 64 bits."""
 import ctypes as C
+import math
 
 import pytest
 import torch
@@ -172,6 +173,34 @@ def test_gates_far_below_leave_nothing(rows, act):
     y, dwg, dwu = far_gates(rows, torch.bfloat16, act, [-v for v in FAR] + [-3e38])
     for m, name in ((y, "y"), (dwg, "dw_gate"), (dwu, "dw_up")):
         assert float(m.abs().max()) < 1e-18, (name, m.abs().max())
+
+
+@pytest.mark.parametrize("act", ["sigmoid", "silu", "gelu"])
+def test_tails_in_fp32(act):
+    """One token, one column in use, the unit matrix behind it: y is the activation of each gate, and dw_gate its derivative.
+
+    Relative to its terms each is off by the functions' own errors, at most 4 ulp of erfc and 2 of exp (8 E and 4 E), and five roundings; in
+    both terms of a derivative."""
+    n = 256
+    v = torch.linspace(-12.5, 6.0, n, device="cuda")
+    x = torch.zeros(1, n, device="cuda")
+    x[0, 0] = 1
+    wg, wu, wd = (torch.zeros(n, n, device="cuda") for _ in range(3))
+    wg[:, 0], wu[:, 0] = v, 1
+    wd.fill_diagonal_(1)
+    y, gate, up = gn.gated_ffn(x, wg, wu, wd, act=act, save=True)
+    assert torch.equal(gate[0], v) and bool((up == 1).all())
+    dx, dwg, dwu, dwd = gn.gated_ffn_grad(torch.ones(1, n, device="cuda"), x, gate, up, wg, wu, wd, act=act)
+    v = v.double()
+    a, da = act64(act, v)
+    if act == "gelu":                    # (Phi by erfc: torch's ndtr is 1 + erf in 64 bits too, and zero below -8.3)
+        cdf, bell = 0.5 * torch.special.erfc(-v / math.sqrt(2)), v * torch.exp(-v * v / 2) / math.sqrt(2 * math.pi)
+        a, da, terms = v * cdf, cdf + bell, cdf + bell.abs()
+    else:
+        terms = (torch.special.expit(v) + v.abs() * torch.special.expit(v) * torch.special.expit(-v)) if act == "silu" else da
+    within(y[0], a, 13 * E * a.abs() + tiny(torch.float32), "y")
+    within(dwu[:, 0], a, 13 * E * a.abs() + tiny(torch.float32), "dw_up")
+    within(dwg[:, 0], da, 13 * E * terms + tiny(torch.float32), "dw_gate")
 
 
 @pytest.mark.parametrize("act", ACTS)

@@ -34,7 +34,7 @@ int* error_word() {
 // h = act(gate) * up, and with dh the two gradients, in FP32: a thread takes four columns, 64 threads neighbouring ones, a block four rows at a time.
 struct Gates { int64_t rows; int cols, act; const float *gate, *up; int64_t ld_gate, ld_up; const float* dh; float *h, *dgate, *dup; int64_t ld; };
 template <bool VEC>
-__global__ void __launch_bounds__(256) gate_kernel(const Gates g) {
+__global__ void __launch_bounds__(256, VEC ? 5 : 4) gate_kernel(const Gates g) {
   const int unit = blockIdx.x * 64 + threadIdx.x, units = (g.cols + 3) / 4;
   if (unit >= units) return;
   with_activation(g.act, [&](auto act) {

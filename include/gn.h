@@ -484,7 +484,7 @@ typedef enum { GN_F32 = 0, GN_BF16 = 1, GN_F16 = 2 } gn_dtype;
  * var = sum (x - mean)^2 / cols.
  *   wtype            type of d_weight and d_bias: `type` or GN_F32.
  *   d_weight, d_bias [cols], each may be NULL (1 and 0).
- *   eps              >= 0.  (0 and a row of equal elements give NaN.)
+ *   eps              >= 0.  (0 and a row of equal elements give NaN; any other gives such a row b, if FP32 holds its sum.)
  *   d_y              [rows][ldy]; may be d_x (with ldy == ldx).
  *   d_mean, d_rstd   [rows] floats for the backward pass, each may be NULL.
  * 1 <= cols <= 2^20.
@@ -546,12 +546,14 @@ typedef struct { void* p; int64_t ld; } gn_mat;
  *   dy [rows][cols], x, gate, up, and the three weights are inputs; dx, dw_gate, dw_up, dw_down are outputs of the shapes of x and the
  *   weights, each with p == NULL where it is not wanted.
  * GN_BF16 and GN_F16: operands go to the tensor cores as they are; h, dup and dgate are rounded to the type on their way into the next
- * product (h not where 128 tokens or fewer meet few weights: it goes in two parts there).  GN_F32: every product at FP32 accuracy (see gn_set_accurate_method).
+ * product (h not where 128 tokens or fewer meet few weights: it goes in two parts there).  So in GN_F16 an h above 65504 is infinite, and y with it, and what of dup and
+ * dgate is below 3e-8 is lost: scale the loss, or take GN_BF16.  GN_F32: every product at FP32 accuracy (see gn_set_accurate_method).
+ * A gate may be any finite number: far out, where its exponential overflows, act and act' are their limits.
  * Workspace: gn_gated_ffn_workspace(args, backward) bytes for the same args; it depends on sizes, types, leading dimensions
  * and on the alignment of the pointers, and is negative for bad arguments.
  * 1 <= cols, inner <= 2^24 with cols * inner < 2^31; rows < 2^30.
  * gn_gated_ffn_status - synchronises the stream and returns GN_ETIMEOUT if a bounded wait of one of these calls' tensor-core kernels has
- * run out on the current device since the last look (results are invalid then), else GN_OK.
+ * run out on the current device since the last look (results are invalid then), else GN_OK.  The other calls do not look: they never synchronise.
  */
 typedef struct {
   int32_t type, act;          /* gn_dtype, gn_act */

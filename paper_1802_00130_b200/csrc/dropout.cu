@@ -2,7 +2,7 @@
 //
 // Bound by memory and, close behind, by the generator: ten rounds of two 32 x 32 -> 64 bit products and two three-way exclusive ors for four
 // elements, 10 of the some 17 issue slots of an element, and the wide products have a pipe of their own busy for 46 us at 16384 x 4096 elements.  There, in bf16:
-// 68 us with a residual (5.9 TB/s, 62 us at the rate of a copy), 65 us without (4.1 TB/s: the generator's bound).
+// 75 us with a residual (5.4 TB/s; an addition of the two alone takes 62), 66 us without (4.1 TB/s: the generator's bound).
 // A thread asks for the next unit of 16 bytes (and the residual's) before it draws the numbers of one.
 // Matrices without gaps are one long row, whatever their width; others go by units of a row where no unit straddles one, else by the
 // generator's blocks of four elements.
@@ -38,7 +38,7 @@ __device__ __forceinline__ uint64_t step_of(const DropParams& p) {
 }
 
 // Units of 16 bytes; cols a multiple of their elements, or one row, whose last elements the first thread takes by themselves.  I: what numbers the units.
-constexpr int kDropBlocks = 8;            // of an SM: 68 us where 6 take 69 and 4 96 (16384 x 4096 bf16 with a residual)
+constexpr int kDropBlocks = 8;            // of an SM: 75 us where 6 take 76 and 4 80 (16384 x 4096 bf16 with a residual)
 template <class T, bool ONE_ROW, class I>
 __global__ void __launch_bounds__(256, kDropBlocks) dropout_units_kernel(const __grid_constant__ DropParams p) {
   constexpr int V = Pack<T>::V;

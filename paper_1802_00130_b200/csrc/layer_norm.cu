@@ -1,12 +1,13 @@
 // Layer norm and its backward pass, each in one pass over the data: memory bound, so a row is read once, kept in registers as it is
 // stored, and written once.
 //
-// Forward: 8 or 32 threads a row up to 4096 columns of 16 bits (no barrier, a row's loads all in flight), a block a row above it.  The sums
+// Forward: a thread has one or two units of 16 bytes, four of the longest rows: 8 or 32 threads a row up to 512 columns of 16 bits (no barrier), 64 to 1024 threads
+// and a barrier for each sum up to 32768, a row's loads all in flight; longer rows are read three times.  The sums
 // of a row are taken twice from the registers, of x for the mean m and then of x - m and its square: the first of these two
 // is what m's rounding has left, which corrects the mean and the variance, so a mean far above the spread costs no accuracy (see about and variance for
 // a spread of nothing or of a few steps).
 //
-// Backward: two units a thread.  With mean and rstd at hand a row needs one reduction, of g and g xhat; the sums
+// Backward, up to 8192 columns (longer rows: two kernels that read them once each): two units a thread.  With mean and rstd at hand a row needs one reduction, of g and g xhat; the sums
 // over rows of dy xhat and dy stay with the thread that owns the column, and each block leaves one row of partial sums, which a
 // second kernel adds in a fixed order.
 #include <math.h>

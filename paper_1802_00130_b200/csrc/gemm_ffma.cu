@@ -12,7 +12,6 @@ namespace gn {
 namespace {
 
 constexpr int BM = 128, BN = 128, BK = 16, NT = 256, PAD = 4;
-constexpr int GRID_Y = 65535;      // a grid's second dimension ends there: more rows of tiles go to the third (the last of them may find no rows)
 
 struct FfmaParams {
   int M, N;
@@ -52,7 +51,7 @@ __global__ void __launch_bounds__(NT, 2) gemm_ffma_kernel(const FfmaParams p) {
 
   const int tid = threadIdx.x;
   const int tx = tid & 15, ty = tid >> 4;
-  const int m0 = (int)(blockIdx.z * GRID_Y + blockIdx.y) * BM, n0 = blockIdx.x * BN;
+  const int m0 = (int)(blockIdx.z * gridDim.y + blockIdx.y) * BM, n0 = blockIdx.x * BN;
 
   const int nk0 = (p.K[0] + BK - 1) / BK;
   const int nk1 = p.A[1] ? (p.K[1] + BK - 1) / BK : 0;
@@ -199,8 +198,10 @@ int launch_gemm_ffma(const GemmArgs& g, cudaStream_t st) {
   p.vec_epi = aligned16(g.D) && (g.ldd % 4 == 0) && (!g.bias || aligned16(g.bias)) &&
               (!g.dsig || (aligned16(g.dsig) && g.ld_dsig % 4 == 0)) &&
               (!g.cin || (aligned16(g.cin) && g.ld_cin % 4 == 0));
-  const int tiles_m = (g.M + BM - 1) / BM;
-  const dim3 grid((g.N + BN - 1) / BN, tiles_m < GRID_Y ? tiles_m : GRID_Y, (tiles_m + GRID_Y - 1) / GRID_Y);
+  // A grid's second dimension ends at 65535: more rows of tiles go to the third as well, fewer than `layers` of them without rows.  (What would bring those past 32 bits
+  // stays in two dimensions, and is refused.)
+  const unsigned tiles_m = ((unsigned)g.M + BM - 1) / BM, layers = g.M < 0x7fff0000 ? (tiles_m + 65534) / 65535 : 1;
+  const dim3 grid((g.N + BN - 1) / BN, (tiles_m + layers - 1) / layers, layers);
   if (g.a_kmajor && g.b_kmajor)        launch_pdl_grid(gemm_ffma_kernel<true, true>, grid, NT, 0, st, p);
   else if (g.a_kmajor && !g.b_kmajor)  launch_pdl_grid(gemm_ffma_kernel<true, false>, grid, NT, 0, st, p);
   else if (!g.a_kmajor && g.b_kmajor)  launch_pdl_grid(gemm_ffma_kernel<false, true>, grid, NT, 0, st, p);

@@ -90,9 +90,9 @@ def _elsewhere(call, dev, stream, *args):
     if stream is None:
         with torch.cuda.device(dev):
             return call(*args)
-    if not isinstance(stream, torch.cuda.Stream):
+    if not isinstance(stream, torch.Stream):             # (torch.cuda.Stream is one)
         raise TypeError(f"stream: expected a torch.cuda.Stream, got {type(stream).__name__}")
-    if stream.device.index != dev:
+    if stream.device.type != "cuda" or stream.device.index != dev:
         raise ValueError(f"the stream is one of {stream.device}, the tensors are on cuda:{dev}")
     with torch.cuda.device(dev), torch.cuda.stream(stream):
         out = call(*args)

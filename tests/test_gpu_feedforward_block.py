@@ -153,8 +153,31 @@ def test_arguments_dropped_after_a_call_on_another_stream(rows):
         assert all(torch.equal(a, b) for a, b in zip(one(got), one(want)))
 
 
+def test_captured_on_a_given_stream():
+    """The block's calls on the stream that captures, given by name, with arguments that are dropped meanwhile."""
+    t = torch.bfloat16
+    q, x, dout, side = parameters(256, 520, t), rand((300, 256), t, 1), rand((300, 256), t, 2), torch.cuda.Stream()
+    out, kept = forward(x, q)
+    want = [out] + backward(dout, x, q, kept)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out, kept = forward(x, q, stream=side)
+        got = [out] + backward(dout, x, q, kept, stream=side)
+        del kept
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_a_stream_is_a_stream_of_the_tensors_device():
     x = rand((4, 16), torch.bfloat16, 1)
+    side, want = torch.Stream(device="cuda"), gn.layer_norm(x)
+    torch.cuda.synchronize()
+    got = gn.layer_norm(x, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
     for bad in (0, "side", torch.device("cuda")):
         with pytest.raises(TypeError, match="torch.cuda.Stream"):
             gn.layer_norm(x, stream=bad)

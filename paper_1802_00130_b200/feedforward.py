@@ -6,8 +6,9 @@ Matrices are 2-D CUDA tensors of float32, bfloat16 or float16 with unit stride i
 of a wider matrix); all tensors of a call are on one device and, where not said otherwise, of one type.  A call enqueues on `stream`
 (default: the current stream of that device), never synchronises, and returns new tensors that belong to that stream; it can be
 captured into a CUDA graph once a call of its kind has run on the device.  A given `stream` does not wait for the current one, which the
-caller sees to (Stream.wait_stream), but the arguments' memory is kept until it is done with them, whether or not the caller drops them.  Nothing here takes part in autograd: the backward
-passes are calls of their own.  Bad arguments raise TypeError or ValueError, the library's own refusals GnError.
+caller sees to (Stream.wait_stream), but the arguments' memory is kept until it is done with them, whether or not the caller drops
+them.  Nothing here takes part in autograd: the backward passes are calls of their own.  Bad arguments raise TypeError or ValueError,
+the library's own refusals GnError.
 """
 from __future__ import annotations
 

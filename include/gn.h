@@ -567,6 +567,46 @@ gn_status gn_gated_ffn(const gn_ffn* args, void* d_ws, int64_t ws_bytes, void* c
 gn_status gn_gated_ffn_grad(const gn_ffn* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 gn_status gn_gated_ffn_status(void* cuda_stream, char* errbuf, int64_t errbuf_len);
 
+/* ======================================================================================================
+ * A MIXTURE OF EXPERTS: routing, the experts' gated feed-forward layers, 4-bit weights
+ *
+ * Several gated feed-forward layers ("experts") in the place of one, of which each token takes k:
+ *     y_t = sum_j w_tj ffn_e(x_t),   e = index_tj,   (index_t, w_t) = route(logits_t).
+ * What is said above of matrices, streams, workspaces, overlap, errors and the order of sums holds here.  Indices are 32-bit words.
+ * ====================================================================================================== */
+
+typedef enum { GN_SOFTMAX = 0, GN_SIGMOID = 1 } gn_score;
+
+/*
+ * gn_route - the experts of each token and their weights.  With s = softmax(logits) or sigmoid(logits) of a row of `experts` logits:
+ *   - the value of expert e is s_e + bias_e; without a bias experts are compared by their logits;
+ *   - of `groups` groups of neighbouring experts those top_groups remain that have the largest sum of their group_best (1 or 2, or all they have) largest values;
+ *   - index [tokens][k]: the k experts of the largest values, the largest first;
+ *   - weight [tokens][k]: scale s_e, with `renormalise` divided by the sum of the chosen experts' s_e.  (The bias takes part in the choice alone.)
+ * Equal values go by the lower number (experts and groups).  The order is that of the exact values: no rounding of FP32 decides it.  -inf is the
+ * logit of an expert that cannot be taken: it has the score 0, and comes last without a bias (with one, a bias of -inf keeps it out); a row of
+ * nothing else has weights of 0.  NaN comes behind every number; with softmax a NaN or +inf in a row makes its weights NaN.
+ *   d_bias           [experts] floats or NULL.
+ * 1 <= k <= 32; k <= experts <= 1024; groups <= 32 divides experts; k <= experts / groups * top_groups; tokens < 2^31.
+ */
+gn_status gn_route(gn_dtype type, gn_score score, int64_t tokens, int32_t experts, int32_t k, const void* d_logits, int64_t ld,
+                   const float* d_bias, int32_t groups, int32_t top_groups, int32_t group_best, int32_t renormalise, double scale,
+                   int32_t* d_index, float* d_weight, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+
+/*
+ * gn_route_grad - the gradient of the weights to that of the logits (the choice itself has none).  With u_j = scale dweight_j, s_j the chosen experts' scores:
+ *     softmax                  dlogits_e = s_e (sum_{j: e_j = e} u_j - sum_j u_j s_j)
+ *     sigmoid                  dlogits_e = s_e (1 - s_e) sum_{j: e_j = e} u_j
+ *   and with `renormalise`, p_j = s_j / sum s:
+ *     softmax                  dlogits_e = sum_{j: e_j = e} p_j (u_j - sum_i u_i p_i)
+ *     sigmoid                  the same times 1 - s_e.
+ * d_logits: those of the forward call.  d_index [tokens][k]: what it has written; entries outside [0, experts) take no part.
+ * d_dlogits [tokens][ld_d] is written whole.
+ */
+gn_status gn_route_grad(gn_dtype type, gn_score score, int64_t tokens, int32_t experts, int32_t k, const float* d_dweight,
+                        const void* d_logits, int64_t ld, const int32_t* d_index, int32_t renormalise, double scale, void* d_dlogits,
+                        int64_t ld_d, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+
 #ifdef __cplusplus
 }
 #endif

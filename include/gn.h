@@ -607,6 +607,41 @@ gn_status gn_route_grad(gn_dtype type, gn_score score, int64_t tokens, int32_t e
                         const void* d_logits, int64_t ld, const int32_t* d_index, int32_t renormalise, double scale, void* d_dlogits,
                         int64_t ld_d, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 
+typedef struct { void* p; int64_t ld, stride; } gn_stack;   /* a matrix of every expert, `stride` elements apart */
+
+/*
+ * gn_experts - y_t = sum_j weight_tj (act(x_t Wg_e^T) * (x_t Wu_e^T)) Wd_e^T with e = index_tj.
+ *   type, act, tokens, cols, inner, experts, k   x, y [tokens][cols]; w_gate, w_up [experts][inner][cols]; w_down [experts][cols][inner]
+ *   index, weight                  [tokens][k]; an index outside [0, experts) is no expert and adds nothing (a token that has none has y = 0);
+ *                                  the same expert twice adds both
+ *   gate, up                       [tokens k][inner], row t k + j, each with p == NULL or an output for the backward pass (rows of no expert are left as they were)
+ * gn_experts_grad - its backward pass.  With h = act(gate) * up and q = dy_t Wd_e of the pair (t, j):
+ *     dweight_tj = q . h,   dup = weight q act(gate),   dgate = weight q up act'(gate),   dx_t = sum_j (dgate Wg_e + dup Wu_e),
+ *     dWg_e = sum dgate x_t^T,   dWu_e = sum dup x_t^T,   dWd_e = sum weight dy_t h^T   over the pairs of expert e (zero without any).
+ *   dy, x, index, weight, gate, up and the weights are inputs; dx, dweight [tokens][k] (0 where there is no expert), dw_gate, dw_up, dw_down are outputs, each NULL where
+ *   it is not wanted.
+ * GN_BF16, GN_F16: h, weight h, dup, dgate and each pair's row of y and dx are rounded to the type on their way into the next product or sum, dweight is FP32
+ * throughout; what is said of GN_F16's range at gn_gated_ffn holds here.  GN_F32: sums of FP32 products.
+ * A bounded wait that ran out shows in gn_gated_ffn_status.
+ * Workspace: gn_experts_workspace(args, backward) bytes for the same args; it depends on sizes, types, leading dimensions, strides and on the alignment of
+ * the pointers, and is negative for bad arguments.
+ * experts <= 1024; k <= 32; 1 <= cols, inner <= 2^20 with cols * inner < 2^31; tokens * k < 2^28; the matrices of the experts do not overlap.
+ */
+typedef struct {
+  int32_t type, act;          /* gn_dtype, gn_act */
+  int64_t tokens;
+  int32_t cols, inner, experts, k;
+  const int32_t* index;
+  const float* weight;
+  float* dweight;
+  gn_mat x, y, gate, up, dy, dx;
+  gn_stack w_gate, w_up, w_down, dw_gate, dw_up, dw_down;
+} gn_mixture;
+
+int64_t gn_experts_workspace(const gn_mixture* args, int32_t backward);
+gn_status gn_experts(const gn_mixture* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+gn_status gn_experts_grad(const gn_mixture* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+
 #ifdef __cplusplus
 }
 #endif

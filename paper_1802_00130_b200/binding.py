@@ -64,6 +64,9 @@ _SIGNATURES = {
     "gn_gated_ffn": (_i32, [_vp, _vp, _i64, _vp, C.c_char_p, _i64]),
     "gn_gated_ffn_grad": (_i32, [_vp, _vp, _i64, _vp, C.c_char_p, _i64]),
     "gn_gated_ffn_status": (_i32, [_vp, C.c_char_p, _i64]),
+    "gn_experts_workspace": (_i64, [_vp, _i32]),
+    "gn_experts": (_i32, [_vp, _vp, _i64, _vp, C.c_char_p, _i64]),
+    "gn_experts_grad": (_i32, [_vp, _vp, _i64, _vp, C.c_char_p, _i64]),
     "gn_route": (_i32, [_i32, _i32, _i64, _i32, _i32, _vp, _i64, _vp, _i32, _i32, _i32, _i32, _dbl, _vp, _vp, _vp, C.c_char_p, _i64]),
     "gn_route_grad": (_i32, [_i32, _i32, _i64, _i32, _i32, _vp, _vp, _i64, _vp, _i32, _dbl, _vp, _i64, _vp, C.c_char_p, _i64]),
 }

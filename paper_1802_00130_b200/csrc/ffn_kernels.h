@@ -25,6 +25,9 @@ struct FfnGemm {
 };
 constexpr int kFfnGroup = 4;     // problems of one launch (FFN_STORE)
 
+// The current device's word for the code of a bounded wait that ran out (nullptr: there is none); gn_gated_ffn_status looks at it, and clears it.
+int* ffn_error_word();
+
 // CTA-pair kernels (gemm_pair16.cu).  Returns cudaSuccess, or what the launch or the maps failed with.  ws: ffn_pair_workspace bytes for the same
 // products (FFN_STORE; sizes alone count).  Of FFN_GATE (operands K-major) and FFN_GRAD (B [K][N]) one product with one pair of operands.
 int64_t ffn_pair_workspace(const FfnGemm* g, int n);

@@ -16,10 +16,10 @@
 
 namespace gn {
 namespace {
+__device__ int ffn_error;        // code of a bounded wait that ran out
+}
 
-__device__ int ffn_error;        // code of a bounded wait that ran out; looked at, and cleared, by gn_gated_ffn_status
-
-int* error_word() {
+int* ffn_error_word() {
   static std::atomic<void*> at[64];
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
@@ -30,6 +30,8 @@ int* error_word() {
   }
   return static_cast<int*>(p);
 }
+
+namespace {
 
 // h = act(gate) * up, and with dh the two gradients, in FP32: a thread takes four columns, 64 threads neighbouring ones, a block four rows at a time.
 struct Gates { int64_t rows; int cols, act; const float *gate, *up; int64_t ld_gate, ld_up; const float* dh; float *h, *dgate, *dup; int64_t ld; };
@@ -489,7 +491,7 @@ gn_status run(const gn_ffn* f, bool back, void* d_ws, int64_t ws_bytes, void* st
     }
     return op_done(e, errbuf, errbuf_len);
   }
-  int* const err = error_word();
+  int* const err = ffn_error_word();
   if (!err) return op_done(cudaErrorNoDevice, errbuf, errbuf_len);
   if (on_fmas(*f, back)) e = run_fmas(*f, (float*)base, st);
   else if (is_small(*f, back)) e = run_small(lay_out_small(*f, base), st);
@@ -515,7 +517,7 @@ extern "C" gn_status gn_gated_ffn_grad(const gn_ffn* args, void* d_ws, int64_t w
   return run(args, true, d_ws, ws_bytes, cuda_stream, errbuf, errbuf_len);
 }
 extern "C" gn_status gn_gated_ffn_status(void* cuda_stream, char* errbuf, int64_t errbuf_len) {
-  int* const err = error_word();
+  int* const err = ffn_error_word();
   if (!err) return op_done(cudaErrorNoDevice, errbuf, errbuf_len);
   cudaStream_t st = (cudaStream_t)cuda_stream;
   int code = 0;

@@ -8,10 +8,12 @@ float32, bfloat16 or float16 with unit stride inside a row, results are new tens
 """
 from __future__ import annotations
 
+from array import array
+
 import torch
 
 from .binding import lib
-from .feedforward import _TYPES, _checked, _device, _elsewhere, _err, _first, _matrix, _raw_stream, _vector
+from .feedforward import _TYPES, ACTIVATIONS, _checked, _device, _elsewhere, _err, _first, _matrix, _raw_stream, _vector
 
 SCORES = {"softmax": 0, "sigmoid": 1}
 
@@ -90,3 +92,98 @@ def route_grad(dweight, logits, index, score="softmax", renormalise=False, scale
     if status:
         _checked(status, err)
     return dlogits
+
+
+def _stack(t, what, experts, rows, cols, dtype, dev):
+    """(pointer, leading dimension, stride) of a matrix of every expert."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what}: expected a CUDA tensor")
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise TypeError(f"{what}: expected a {dtype} tensor on cuda:{dev}, got {t.dtype} on {t.device}")
+    if t.shape != (experts, rows, cols):
+        raise ValueError(f"{what}: expected shape ({experts}, {rows}, {cols}), got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), cols, rows * cols
+    stride, ld, inner = t.stride()
+    if cols > 1 and inner != 1:
+        raise ValueError(f"{what}: expected unit stride inside a row")
+    if rows == 1:
+        ld = max(ld, cols)
+    if ld < cols:
+        raise ValueError(f"{what}: its rows overlap")
+    if experts == 1:
+        stride = max(stride, rows * ld)
+    if stride < (rows - 1) * ld + cols:
+        raise ValueError(f"{what}: its experts overlap")
+    return t.data_ptr(), ld, stride
+
+
+_NONE2, _NONE3 = (0, 0), (0, 0, 0)
+
+
+def _mixture(x, index, weight, w_gate, w_up, w_down, act):
+    """(type, device, sizes, first words of a gn_mixture, the three weights' words)."""
+    dtype, dev, tokens, cols = _first(x, "x")
+    a = ACTIVATIONS.get(act)
+    if a is None:
+        raise ValueError(f"act: expected one of {', '.join(ACTIVATIONS)}, got {act!r}")
+    if not isinstance(w_gate, torch.Tensor):
+        raise TypeError("w_gate: expected a CUDA tensor")
+    if w_gate.dim() != 3 or w_gate.shape[0] < 1 or w_gate.shape[1] < 1:
+        raise ValueError(f"w_gate: expected shape (experts, inner, {cols}), got {tuple(w_gate.shape)}")
+    experts, inner = w_gate.shape[0], w_gate.shape[1]
+    k = _choices(index, tokens)
+    if max(cols, inner, experts, k) >= 1 << 31:
+        raise ValueError("x, w_gate and index: expected sizes below 2^31")
+    head = [_TYPES[dtype] | a << 32, tokens, cols | inner << 32, experts | k << 32, _table(index, "index", tokens, k, torch.int32, dev),
+            _table(weight, "weight", tokens, k, torch.float32, dev)]
+    stacks = (*_stack(w_gate, "w_gate", experts, inner, cols, dtype, dev), *_stack(w_up, "w_up", experts, inner, cols, dtype, dev),
+              *_stack(w_down, "w_down", experts, cols, inner, dtype, dev))
+    return dtype, dev, tokens, cols, inner, experts, k, head, stacks
+
+
+def _mixture_call(fn, backward, x, dev, words):
+    args = array("q", words)
+    at = args.buffer_info()[0]
+    n = lib().gn_experts_workspace(at, backward)
+    ws = x.new_empty(max(n, 16) // x.element_size())
+    err = _err()
+    status = fn(at, ws.data_ptr(), n, _raw_stream(dev), err, 200)
+    if status:
+        _checked(status, err)
+
+
+def experts(x, index, weight, w_gate, w_up, w_down, act="silu", save=False, stream=None):
+    """y = sum over a token's k experts of weight * (act(x w_gate^T) * (x w_up^T)) w_down^T; with `save` (y, gate, up), the projections for the backward pass.
+
+    x [tokens][cols]; index (int32) and weight (float32) [tokens][k] as route gives them, an index that is no expert adds nothing; w_gate, w_up
+    [experts][inner][cols], w_down [experts][cols][inner]; act as in gated_ffn.  gate and up: [tokens k][inner], row t k + j that of the token's j-th choice (not written
+    where that is no expert); views of wider buffers where their 16-bit rows would not start on 16 bytes otherwise.
+    """
+    dtype, dev, tokens, cols, inner, n, k, head, stacks = _mixture(x, index, weight, w_gate, w_up, w_down, act)
+    if stream is not None or dev != _device():
+        return _elsewhere(experts, dev, stream, x, index, weight, w_gate, w_up, w_down, act, save)
+    px = _matrix(x, "x", tokens, cols, dtype, dev)
+    y = x.new_empty(tokens, cols)
+    gate = up = None
+    if save:
+        ld = inner if dtype is torch.float32 else (inner + 7) // 8 * 8
+        gate, up = (x.new_empty(tokens * k, ld)[:, :inner] for _ in range(2))
+    saved = (gate.data_ptr(), ld, up.data_ptr(), ld) if save else (0, 0, 0, 0)
+    _mixture_call(lib().gn_experts, 0, x, dev, (*head, 0, *px, y.data_ptr(), cols, *saved, *_NONE2, *_NONE2, *stacks, *_NONE3, *_NONE3, *_NONE3))
+    return (y, gate, up) if save else y
+
+
+def experts_grad(dy, x, index, weight, gate, up, w_gate, w_up, w_down, act="silu", stream=None):
+    """(dx, dweight, dw_gate, dw_up, dw_down) of experts; gate, up: what experts(..., save=True) has returned.  dweight (float32): 0 where there is no expert."""
+    dtype, dev, tokens, cols, inner, n, k, head, stacks = _mixture(x, index, weight, w_gate, w_up, w_down, act)
+    if stream is not None or dev != _device():
+        return _elsewhere(experts_grad, dev, stream, dy, x, index, weight, gate, up, w_gate, w_up, w_down, act)
+    mats = (*_matrix(x, "x", tokens, cols, dtype, dev), *_NONE2, *_matrix(gate, "gate", tokens * k, inner, dtype, dev),
+            *_matrix(up, "up", tokens * k, inner, dtype, dev), *_matrix(dy, "dy", tokens, cols, dtype, dev))
+    dx, dweight = x.new_empty(tokens, cols), x.new_empty(tokens, k, dtype=torch.float32)
+    dwg, dwu, dwd = x.new_empty(n, inner, cols), x.new_empty(n, inner, cols), x.new_empty(n, cols, inner)
+    each = inner * cols
+    _mixture_call(lib().gn_experts_grad, 1, x, dev, (*head, dweight.data_ptr(), *mats, dx.data_ptr(), cols, *stacks, dwg.data_ptr(), cols, each, dwu.data_ptr(), cols,
+                                                     each, dwd.data_ptr(), inner, each))
+    return dx, dweight, dwg, dwu, dwd

@@ -52,3 +52,56 @@ def test_the_binding_refuses_tensors_that_are_not_on_a_device():
     for call in (lambda: gn.route(x, 2), lambda: gn.route_grad(x, x, x)):
         with pytest.raises(TypeError, match="CUDA"):
             call()
+
+
+def mixture(**change):
+    """gn_mixture as 39 words."""
+    mats, stacks = ["x", "y", "gate", "up", "dy", "dx"], ["w_gate", "w_up", "w_down", "dw_gate", "dw_up", "dw_down"]
+    a = dict(type=1, act=1, tokens=4, cols=8, inner=16, experts=3, k=2, index=1 << 20, weight=1 << 20, dweight=1 << 20)
+    a.update({n: (1 << (21 + i), 16) for i, n in enumerate(mats)})
+    a.update({n: (1 << (30 + i), 16, 256) for i, n in enumerate(stacks)})
+    a.update(change)
+    words = [a["type"] | a["act"] << 32, a["tokens"], a["cols"] | a["inner"] << 32, a["experts"] | a["k"] << 32, a["index"], a["weight"], a["dweight"]]
+    words += [v for n in mats for v in a[n]] + [v for n in stacks for v in a[n]]
+    return (C.c_int64 * 37)(*words)
+
+
+BOTH = [(dict(type=5), "type"), (dict(act=5), "act"), (dict(tokens=-1), "tokens"), (dict(tokens=1 << 27), "tokens"), (dict(cols=0), "cols"), (dict(inner=0), "cols"),
+        (dict(cols=(1 << 20) + 1), "cols"), (dict(cols=1 << 16, inner=1 << 15), "product"), (dict(experts=0), "experts"), (dict(experts=1025), "experts"), (dict(k=0), "k must"),
+        (dict(k=33), "k must"), (dict(index=0), "index"), (dict(index=2), "index"), (dict(weight=0), "weight"), (dict(weight=6), "weight"), (dict(x=(0, 16)), "x:"),
+        (dict(x=(1 << 20, 7)), "x:"), (dict(w_gate=(0, 8, 256)), "w_gate"), (dict(w_up=(1 << 20, 7, 256)), "w_up"), (dict(w_down=(1 << 20, 15, 256)), "w_down"),
+        (dict(w_gate=(1 << 20, 8, 127)), "w_gate"), (dict(w_down=(1 << 20, 16, 127)), "w_down"), (dict(gate=(1 << 20, 15)), "gate"), (dict(up=(3, 16)), "up")]
+
+
+@pytest.mark.parametrize("change,word", BOTH + [(dict(y=(0, 8)), "y:"), (dict(y=(1 << 20, 7)), "y:")])
+def test_experts_refuse(change, word):
+    args = mixture(**change)
+    assert word in refused(gn.lib().gn_experts, args, P, 1 << 40, None)
+    assert gn.lib().gn_experts_workspace(args, 0) < 0
+
+
+@pytest.mark.parametrize("change,word", BOTH + [
+    (dict(gate=(0, 16)), "gate"), (dict(up=(0, 16)), "up"), (dict(dy=(0, 8)), "dy"), (dict(dx=(1 << 20, 7)), "dx"), (dict(dweight=6), "dweight"),
+    (dict(dw_gate=(1 << 20, 7, 256)), "dw_gate"), (dict(dw_up=(1, 16, 256)), "dw_up"), (dict(dw_down=(1 << 20, 15, 256)), "dw_down"), (dict(dw_down=(1 << 20, 16, 100)), "dw_down")])
+def test_experts_grad_refuses(change, word):
+    args = mixture(**change)
+    assert word in refused(gn.lib().gn_experts_grad, args, P, 1 << 40, None)
+    assert gn.lib().gn_experts_workspace(args, 1) < 0
+
+
+@pytest.mark.parametrize("fn", ["gn_experts", "gn_experts_grad"])
+@pytest.mark.parametrize("type", [0, 1, 2])
+def test_experts_refuse_a_bad_workspace(fn, type):
+    args = mixture(type=type)
+    need = gn.lib().gn_experts_workspace(args, fn.endswith("grad"))
+    assert need > 0
+    for ws, n in ((None, need), (C.c_void_p((1 << 20) + 8), need), (P, need - 1)):
+        assert "workspace" in refused(getattr(gn.lib(), fn), args, ws, n, None)
+    assert "no arguments" in refused(getattr(gn.lib(), fn), None, P, need, None)
+
+
+def test_experts_without_a_device():
+    x, i, w = torch.zeros(4, 8), torch.zeros(4, 2, dtype=torch.int32), torch.zeros(3, 16, 8)
+    for call in (lambda: gn.experts(x, i, x[:, :2], w, w, w), lambda: gn.experts_grad(x, x, i, x[:, :2], x, x, w, w, w)):
+        with pytest.raises(TypeError, match="CUDA"):
+            call()

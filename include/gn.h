@@ -642,6 +642,55 @@ int64_t gn_experts_workspace(const gn_mixture* args, int32_t backward);
 gn_status gn_experts(const gn_mixture* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 gn_status gn_experts_grad(const gn_mixture* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 
+/*
+ * 4-BIT WEIGHTS for serving, where a few tokens read all of a layer's weights.  A weight is s (q - 8) with q of 0..15 and a scale s for each `group` (32, 64 or
+ * 128) of neighbouring columns of a row (the last group may be shorter).  They are laid out once, for the products' kernel, as two arrays:
+ *   q      gn_weight4_bytes(experts, rows, cols) bytes.  Expert after expert; 16 rows after 16 rows; 128 columns after 128 columns: a record of 1024 bytes.  In it
+ *          column c (of 128) of row r (of 16) is a nibble of 32-bit word (r / 8) 128 + (r mod 8) 16 + (c / 8 mod 4) 4 + c / 32, the nibble
+ *          from bit 4 (c mod 8) / 2 on where c is even, 16 further where it is odd.  Rows and columns beyond the matrix have q = 8.
+ *   scale  gn_weight4_scales(experts, rows, cols, group) numbers of the call's type, in the same order: [experts][rows / 16][columns / 128][16][128 / group], zero beyond
+ *          the matrix.
+ * Both 16-byte aligned.  The *_bytes and *_scales calls are negative for bad sizes.
+ * gn_pack4      from d_from [experts][rows][ld] bytes (experts `stride` apart), a weight's q in the low four bits of each, and d_scales [experts][rows][groups].
+ * gn_quantize4  from weights [experts][rows][ld]: s = (largest magnitude of the group) / 7 rounded to the type, q - 8 = w / s rounded to nearest even, kept within -8..7;
+ *               a group of zeros (or one whose scale the type cannot hold) has q = 8.  A group with a NaN or an infinity becomes NaN.
+ * gn_unpack4    what they stand for, rounded to the type.
+ * experts <= 1024; 1 <= rows, cols <= 2^20 with rows * cols < 2^31.
+ */
+int64_t gn_weight4_bytes(int32_t experts, int64_t rows, int64_t cols);
+int64_t gn_weight4_scales(int32_t experts, int64_t rows, int64_t cols, int32_t group);
+gn_status gn_pack4(gn_dtype type, int32_t experts, int64_t rows, int64_t cols, int32_t group, const uint8_t* d_from, int64_t ld, int64_t stride,
+                   const void* d_scales, void* d_q, void* d_scale, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+gn_status gn_quantize4(gn_dtype type, int32_t experts, int64_t rows, int64_t cols, int32_t group, const void* d_w, int64_t ld, int64_t stride,
+                       void* d_q, void* d_scale, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+gn_status gn_unpack4(gn_dtype type, int32_t experts, int64_t rows, int64_t cols, int32_t group, const void* d_q, const void* d_scale, void* d_w,
+                     int64_t ld, int64_t stride, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+
+/*
+ * gn_matvec4 - y [tokens][rows] = x [tokens][cols] W^T of packed weights W [rows][cols].  Meant for a few tokens; any number below 2^20 is taken, 32 at a time.
+ * Products of the type's numbers and whole q - 8, summed in FP32 group by group, times the scale; FP32 tokens lose nothing.
+ */
+gn_status gn_matvec4(gn_dtype type, int64_t tokens, int64_t rows, int64_t cols, int32_t group, const void* d_x, int64_t ldx, const void* d_q,
+                     const void* d_scale, void* d_y, int64_t ldy, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+
+/*
+ * gn_gated_ffn4 - gn_gated_ffn, or with an index gn_experts, on packed weights: q_gate, q_up [experts][inner][cols] and q_down [experts][cols][inner] with their scales.
+ *   index, weight   [tokens][k] as in gn_experts, or both NULL with experts == 1 and k == 1: y = ffn(x).
+ * The hidden units go to the second product as 17 bits of FP32 (24 in GN_F32) whatever the type; y is rounded once.  tokens * k < 2^20.
+ */
+typedef struct {
+  int32_t type, act;          /* gn_dtype, gn_act */
+  int64_t tokens;
+  int32_t cols, inner, experts, k, group, reserved;
+  const int32_t* index;
+  const float* weight;
+  gn_mat x, y;
+  const void *q_gate, *s_gate, *q_up, *s_up, *q_down, *s_down;
+} gn_ffn4;
+
+int64_t gn_gated_ffn4_workspace(const gn_ffn4* args);
+gn_status gn_gated_ffn4(const gn_ffn4* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+
 #ifdef __cplusplus
 }
 #endif

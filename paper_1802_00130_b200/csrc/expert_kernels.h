@@ -28,7 +28,7 @@ inline int64_t plan_slots(int64_t pairs, int experts) { return (pairs + (kSlots 
 inline int64_t plan_tiles(int64_t pairs, int experts, int height) { return pairs / height + (pairs < experts ? pairs : (int64_t)experts); }
 int64_t plan_ints(int64_t pairs, int experts, int height);                          // words of a plan's memory
 ExpertPlan plan_at(int* mem, int64_t pairs, int experts, int height);               // the plan's parts in it (16-byte aligned)
-// The plan of an index table, with tiles of `height` slots (a multiple of kSlots).
+// The plan of an index table, with tiles of `height` slots (where `padded` is looked at, a multiple of kSlots).
 cudaError_t launch_plan(const int* index, const ExpertPlan& plan, int height, cudaStream_t st);
 
 // Rows of tokens to their pairs' slots: dst[slot of (t, j)] = src[t], empty slots zero.  `bytes` of an element (2 or 4); rows of dst are 16-byte aligned.

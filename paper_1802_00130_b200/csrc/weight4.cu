@@ -1,0 +1,232 @@
+// 4-bit weights: their layout, from and to what they stand for, and the calls on them.  The products' kernel is in weight4_product.cuh.
+#include <math.h>
+
+#include "op_common.cuh"
+#include "tc_common.cuh"
+#include "weight4_kernels.h"
+
+namespace gn {
+namespace {
+
+// The word of eight columns from c0 on of a row: its place in an expert's q.
+__device__ __forceinline__ int64_t word_at(int64_t r, int64_t c0, int64_t kblocks) {
+  const int in = (int)(r & 15), lane = (in & 7) * 4 + (int)(c0 >> 3 & 3);
+  return (((r >> 4) * kblocks + (c0 >> 7)) * 2 + (in >> 3)) * 128 + lane * 4 + (c0 >> 5 & 3);
+}
+__device__ __forceinline__ int64_t scale_at(int64_t r, int64_t c0, int64_t kblocks, int group) {
+  return (((r >> 4) * kblocks + (c0 >> 7)) * 16 + (r & 15)) * (128 / group) + (c0 & 127) / group;
+}
+__device__ __forceinline__ uint32_t nibble(uint32_t q, int e) { return q << (4 * ((e & 1) * 4 + (e >> 1))); }
+
+// A thread has a group of a row, those that fill up the last record and the last rows of a tile included (q = 8, which stands for 0, and a scale of 0).
+struct Layout4 {
+  int64_t rows, cols, tiles, kblocks; int experts, group;
+  const void* from; int64_t ld, stride;          // weights, or their q in bytes
+  const void* scales;                            // [experts][rows][groups]
+  uint32_t* q; void* scale;
+  void* to;                                      // unpacked
+};
+template <class T, bool QUANTIZE>
+__global__ void __launch_bounds__(256) pack4_kernel(const __grid_constant__ Layout4 p) {
+  grid_dep_wait();
+  grid_dep_launch();
+  const int64_t groups = p.kblocks * (128 / p.group), rows = p.tiles * 16, work = p.experts * rows * groups;
+  const int64_t real = (p.cols + p.group - 1) / p.group;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < work; i += (int64_t)gridDim.x * 256) {
+    const int64_t e = i / (rows * groups), r = i / groups % rows, g = i % groups, c0 = g * p.group;
+    const int n = r < p.rows && c0 < p.cols ? (int)min((int64_t)p.group, p.cols - c0) : 0;
+    uint32_t* const q = p.q + e * p.tiles * p.kblocks * 256;
+    T* const scale = (T*)p.scale + e * rows * groups;
+    T s = from_f<T>(0.f);
+    if constexpr (QUANTIZE) {
+      const T* const w = (const T*)dep(p.from) + e * p.stride + r * p.ld + c0;
+      float most = 0.f;
+      for (int k = 0; k < n; ++k) most = max_nan(most, fabsf(to_f(w[k])));
+      s = from_f<T>(most / 7.f);
+      const float by = to_f(s);
+      for (int k = 0; k < p.group; k += 8) {
+        uint32_t word = 0;
+        for (int j = 0; j < 8; ++j) {
+          int v = 0;
+          if (k + j < n && by != 0.f) v = max(-8, min(7, __float2int_rn(__fdiv_rn(to_f(w[k + j]), by))));      // (NaN: 0)
+          word |= nibble((uint32_t)(v + 8), j);
+        }
+        q[word_at(r, c0 + k, p.kblocks)] = word;
+      }
+    } else {
+      const uint8_t* const w = (const uint8_t*)dep(p.from) + e * p.stride + r * p.ld + c0;
+      if (n > 0) s = ((const T*)dep(p.scales))[(e * p.rows + r) * real + g];
+      for (int k = 0; k < p.group; k += 8) {
+        uint32_t word = 0;
+        for (int j = 0; j < 8; ++j) word |= nibble(k + j < n ? w[k + j] & 15u : 8u, j);
+        q[word_at(r, c0 + k, p.kblocks)] = word;
+      }
+    }
+    scale[scale_at(r, c0, p.kblocks, p.group)] = s;
+  }
+}
+template <class T>
+__global__ void __launch_bounds__(256) unpack4_kernel(const __grid_constant__ Layout4 p) {
+  grid_dep_wait();
+  grid_dep_launch();
+  const int64_t eights = (p.cols + 7) / 8, work = p.experts * p.rows * eights;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < work; i += (int64_t)gridDim.x * 256) {
+    const int64_t e = i / (p.rows * eights), r = i / eights % p.rows, c0 = i % eights * 8;
+    const uint32_t word = p.q[e * p.tiles * p.kblocks * 256 + word_at(r, c0, p.kblocks)];
+    const float s = to_f(((const T*)p.scale)[e * p.tiles * 16 * p.kblocks * (128 / p.group) + scale_at(r, c0, p.kblocks, p.group)]);
+    T* const to = (T*)p.to + e * p.stride + r * p.ld + c0;
+    for (int j = 0; j < 8; ++j)
+      if (c0 + j < p.cols) to[j] = from_f<T>((float)((int)(word >> (4 * ((j & 1) * 4 + (j >> 1))) & 15) - 8) * s);
+  }
+}
+template <class T>
+cudaError_t run_layout(const Layout4& p, int what, cudaStream_t st) {
+  const int64_t work = what == 2 ? p.experts * p.rows * ((p.cols + 7) / 8) : p.experts * p.tiles * 16 * p.kblocks * (128 / p.group);
+  const int64_t want = (work + 255) / 256, most = (int64_t)num_sms() * 8;
+  const int grid = (int)(want < most ? want : most);
+  if (what == 2) return launch_pdl(unpack4_kernel<T>, grid, 256, 0, st, p);
+  return launch_pdl(what ? pack4_kernel<T, true> : pack4_kernel<T, false>, grid, 256, 0, st, p);
+}
+
+const char* sizes4(int type, int64_t experts, int64_t rows, int64_t cols, int group) {
+  if (!type_ok(type)) return "type is not a gn_dtype";
+  if (experts < 1 || experts > kMostExperts) return "experts must be in [1, 1024]";
+  if (rows < 1 || cols < 1 || rows > (1 << 20) || cols > (1 << 20) || rows * cols >= (int64_t(1) << 31)) return "rows and cols must be in [1, 2^20] with a product below 2^31";
+  if (group != 32 && group != 64 && group != 128) return "group must be 32, 64 or 128";
+  return nullptr;
+}
+bool packed_ok(const void* q, const void* scale) { return q && scale && ((uintptr_t)q & 15) == 0 && ((uintptr_t)scale & 15) == 0; }
+const char* const kPackedWhy = "q or scale of packed weights: null or not 16-byte aligned";
+
+gn_status layout4(int what, gn_dtype type, int32_t experts, int64_t rows, int64_t cols, int32_t group, const void* from, int64_t ld, int64_t stride, const void* scales,
+                  void* d_q, void* d_scale, void* to, void* stream, char* errbuf, int64_t errbuf_len) {
+  const char* why = sizes4(type, experts, rows, cols, group);
+  const void* const flat = what == 2 ? to : from;
+  if (!why) {
+    if (!packed_ok(d_q, d_scale)) why = kPackedWhy;
+    else if (!flat || (what && (uintptr_t)flat % (uintptr_t)type_bytes(type)) || ld < cols || ld >= (int64_t(1) << 40) ||
+             (experts > 1 && (stride < (rows - 1) * ld + cols || stride >= (int64_t(1) << 40))))
+      why = "weights: null, misaligned, or a leading dimension or stride too small";
+    else if (what == 0 && (!scales || (uintptr_t)scales % (uintptr_t)type_bytes(type))) why = "scales: null or misaligned";
+  }
+  if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
+  const Layout4 p{rows, cols, w4_tiles(rows), w4_blocks(cols), experts, group, from, ld, experts == 1 ? 0 : stride, scales, (uint32_t*)d_q, d_scale, to};
+  cudaStream_t st = (cudaStream_t)stream;
+  return op_done(type == GN_F32 ? run_layout<float>(p, what, st) : type == GN_BF16 ? run_layout<__nv_bfloat16>(p, what, st) : run_layout<__half>(p, what, st), errbuf, errbuf_len);
+}
+
+cudaError_t launch_product4(int type, const Product4& p, cudaStream_t st) {
+  return type == GN_F32 ? launch_product4_f32(p, st) : type == GN_BF16 ? launch_product4_bf16(p, st) : launch_product4_f16(p, st);
+}
+
+// ---- the gated layer ----------------------------------------------------------------------------
+struct Workspace {               // hands out 256-byte aligned pieces (of no memory at all where a call is only measured)
+  char* p; int64_t used = 0;
+  void* take(int64_t bytes) { void* r = p + used; used += (bytes + 255) / 256 * 256; return r; }
+};
+char* const kNowhere = reinterpret_cast<char*>(256);
+
+const char* ffn4_args(const gn_ffn4* f) {
+  if (!f) return "no arguments";
+  if (f->act < GN_ACT_SIGMOID || f->act > GN_ACT_RELU) return "act is not a gn_act";
+  const char* why = sizes4(f->type, f->experts, f->inner, f->cols, f->group);
+  if (why) return why;
+  if (f->k < 1 || f->k > 32) return "k must be in [1, 32]";
+  if (f->tokens < 0 || f->tokens >= (1 << 20) / f->k) return "tokens times k must be in [0, 2^20)";
+  if (f->tokens > 0 && !f->index && (f->experts != 1 || f->k != 1)) return "without an index there is one expert, and one choice";
+  if (!packed_ok(f->q_gate, f->s_gate) || !packed_ok(f->q_up, f->s_up) || !packed_ok(f->q_down, f->s_down)) return kPackedWhy;
+  if (f->tokens == 0) return nullptr;
+  if (!mat_ok(f->x.p, f->x.ld, f->cols, f->type)) return "x: null, misaligned, or a leading dimension below cols";
+  if (!mat_ok(f->y.p, f->y.ld, f->cols, f->type)) return "y: null, misaligned, or a leading dimension below cols";
+  if ((uintptr_t)f->index & 3) return "index: misaligned";
+  if (f->index && (!f->weight || ((uintptr_t)f->weight & 3))) return "weight: null or misaligned";
+  return nullptr;
+}
+struct Few4 { ExpertPlan plan; float *h, *out; int64_t ld_h, ld_out; int columns; };
+// Columns of a tile: eight where that is what a tile has, on average over the experts that can have one.
+int columns4(int64_t pairs, int experts) { return pairs <= 8 * (pairs < experts ? pairs : (int64_t)experts) ? 8 : 32; }
+int64_t lay_out(const gn_ffn4& f, char* base, Few4& w) {
+  Workspace ws{base};
+  const int64_t pairs = f.tokens * f.k;
+  w = Few4{};
+  w.columns = columns4(pairs, f.experts);
+  w.ld_h = (f.inner + 3) / 4 * 4; w.ld_out = (f.cols + 7) / 8 * 8;
+  w.h = (float*)ws.take(pairs * w.ld_h * 4);
+  if (f.index) {
+    w.plan = plan_at((int*)ws.take(plan_ints(pairs, f.experts, w.columns) * 4), pairs, f.experts, w.columns);
+    w.out = (float*)ws.take(pairs * w.ld_out * 4);
+  }
+  return ws.used + 256;
+}
+cudaError_t run_ffn4(const gn_ffn4& f, const Few4& w, cudaStream_t st) {
+  cudaError_t e = f.index ? launch_plan(f.index, w.plan, w.columns, st) : cudaSuccess;
+  Product4 a, b;
+  a.rows = f.inner; a.cols = f.cols; a.group = b.group = f.group; a.act = f.act; a.tokens = b.tokens = f.tokens; a.k = b.k = f.k; a.columns = b.columns = w.columns;
+  a.gate = true; a.x = f.x.p; a.ldx = f.x.ld; a.token_rows = true;
+  a.w[0] = {(const uint8_t*)f.q_gate, f.s_gate}; a.w[1] = {(const uint8_t*)f.q_up, f.s_up};
+  a.d = w.h; a.ldd = w.ld_h; a.d32 = true;
+  b.rows = f.cols; b.cols = f.inner; b.x = w.h; b.ldx = w.ld_h; b.x32 = true; b.early = true;
+  b.w[0] = {(const uint8_t*)f.q_down, f.s_down};
+  if (f.index) { a.plan = b.plan = &w.plan; b.d = w.out; b.ldd = w.ld_out; b.d32 = true; }
+  else { b.d = f.y.p; b.ldd = f.y.ld; }
+  if (e == cudaSuccess) e = launch_product4(f.type, a, st);
+  if (e == cudaSuccess) e = launch_product4(f.type, b, st);
+  if (!f.index || e != cudaSuccess) return e;
+  Combine c = {};
+  c.tokens = f.tokens; c.k = f.k; c.cols = f.cols; c.experts = f.experts; c.index = f.index; c.weight = f.weight; c.src = w.out; c.ld = w.ld_out; c.d = f.y.p; c.ld_d = f.y.ld;
+  return launch_combine(f.type, GN_F32, c, st);
+}
+
+}  // namespace
+}  // namespace gn
+
+using namespace gn;
+
+extern "C" int64_t gn_weight4_bytes(int32_t experts, int64_t rows, int64_t cols) {
+  return sizes4(GN_F32, experts, rows, cols, 128) ? -1 : experts * w4_bytes(rows, cols);
+}
+extern "C" int64_t gn_weight4_scales(int32_t experts, int64_t rows, int64_t cols, int32_t group) {
+  return sizes4(GN_F32, experts, rows, cols, group) ? -1 : experts * w4_scales(rows, cols, group);
+}
+extern "C" gn_status gn_pack4(gn_dtype type, int32_t experts, int64_t rows, int64_t cols, int32_t group, const uint8_t* d_from, int64_t ld, int64_t stride, const void* d_scales,
+                              void* d_q, void* d_scale, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
+  return layout4(0, type, experts, rows, cols, group, d_from, ld, stride, d_scales, d_q, d_scale, nullptr, cuda_stream, errbuf, errbuf_len);
+}
+extern "C" gn_status gn_quantize4(gn_dtype type, int32_t experts, int64_t rows, int64_t cols, int32_t group, const void* d_w, int64_t ld, int64_t stride, void* d_q, void* d_scale,
+                                  void* cuda_stream, char* errbuf, int64_t errbuf_len) {
+  return layout4(1, type, experts, rows, cols, group, d_w, ld, stride, nullptr, d_q, d_scale, nullptr, cuda_stream, errbuf, errbuf_len);
+}
+extern "C" gn_status gn_unpack4(gn_dtype type, int32_t experts, int64_t rows, int64_t cols, int32_t group, const void* d_q, const void* d_scale, void* d_w, int64_t ld, int64_t stride,
+                                void* cuda_stream, char* errbuf, int64_t errbuf_len) {
+  return layout4(2, type, experts, rows, cols, group, nullptr, ld, stride, nullptr, const_cast<void*>(d_q), const_cast<void*>(d_scale), d_w, cuda_stream, errbuf, errbuf_len);
+}
+extern "C" gn_status gn_matvec4(gn_dtype type, int64_t tokens, int64_t rows, int64_t cols, int32_t group, const void* d_x, int64_t ldx, const void* d_q, const void* d_scale,
+                                void* d_y, int64_t ldy, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
+  const char* why = sizes4(type, 1, rows, cols, group);
+  if (!why) {
+    if (tokens < 0 || tokens >= (1 << 20)) why = "tokens must be in [0, 2^20)";
+    else if (!packed_ok(d_q, d_scale)) why = kPackedWhy;
+    else if (tokens > 0 && !mat_ok(d_x, ldx, cols, type)) why = "x: null, misaligned, or a leading dimension below cols";
+    else if (tokens > 0 && !mat_ok(d_y, ldy, rows, type)) why = "y: null, misaligned, or a leading dimension below rows";
+  }
+  if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
+  if (tokens == 0) return op_done(cudaSuccess, errbuf, errbuf_len);
+  Product4 p;
+  p.rows = (int)rows; p.cols = (int)cols; p.group = group; p.tokens = tokens; p.x = d_x; p.ldx = ldx; p.w[0] = {(const uint8_t*)d_q, d_scale}; p.d = d_y; p.ldd = ldy;
+  p.columns = columns4(tokens, 1);
+  return op_done(launch_product4(type, p, (cudaStream_t)cuda_stream), errbuf, errbuf_len);
+}
+extern "C" int64_t gn_gated_ffn4_workspace(const gn_ffn4* args) {
+  Few4 w;
+  return ffn4_args(args) ? -1 : lay_out(*args, kNowhere, w);
+}
+extern "C" gn_status gn_gated_ffn4(const gn_ffn4* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
+  const char* why = ffn4_args(args);
+  if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
+  Few4 w;
+  char* const base = (char*)(((uintptr_t)d_ws + 255) & ~(uintptr_t)255);
+  if (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < lay_out(*args, base, w))
+    return op_fail(GN_EINVAL, "workspace: null, not 16-byte aligned or too small", errbuf, errbuf_len);
+  if (args->tokens == 0) return op_done(cudaSuccess, errbuf, errbuf_len);
+  return op_done(run_ffn4(*args, w, (cudaStream_t)cuda_stream), errbuf, errbuf_len);
+}

@@ -1,0 +1,10 @@
+// Products with 4-bit weights: the kernels of one type.
+#include "weight4_product.cuh"
+
+namespace gn {
+
+cudaError_t launch_product4_f16(const Product4& p, cudaStream_t st) {
+  return p.x32 ? launch_product4_x<__half, float, 2>(p, st) : launch_product4_x<__half, __half, 1>(p, st);
+}
+
+}  // namespace gn

@@ -105,3 +105,74 @@ def test_experts_without_a_device():
     for call in (lambda: gn.experts(x, i, x[:, :2], w, w, w), lambda: gn.experts_grad(x, x, i, x[:, :2], x, x, w, w, w)):
         with pytest.raises(TypeError, match="CUDA"):
             call()
+
+
+def layout(fn, **change):
+    a = dict(type=1, experts=2, rows=20, cols=40, group=32, w=P, ld=40, stride=800, scales=P, q=P, scale=P, st=None)
+    a.update(change)
+    if fn == "gn_quantize4":
+        del a["scales"]
+    if fn == "gn_unpack4":
+        a = dict(type=a["type"], experts=a["experts"], rows=a["rows"], cols=a["cols"], group=a["group"], q=a["q"], scale=a["scale"], w=a["w"], ld=a["ld"], stride=a["stride"], st=None)
+    return refused(getattr(gn.lib(), fn), *a.values())
+
+
+SIZES4 = [(dict(type=3), "type"), (dict(experts=0), "experts"), (dict(experts=1025), "experts"), (dict(rows=0), "rows"), (dict(cols=0), "rows"), (dict(rows=1 << 16, cols=1 << 15), "rows"),
+          (dict(cols=(1 << 20) + 1), "rows"), (dict(group=16), "group"), (dict(group=256), "group")]
+
+
+@pytest.mark.parametrize("fn", ["gn_pack4", "gn_quantize4", "gn_unpack4"])
+@pytest.mark.parametrize("change,word", SIZES4 + [(dict(w=None), "weights"), (dict(ld=39), "weights"), (dict(stride=799), "weights"), (dict(q=None), "packed"), (dict(scale=C.c_void_p(8)), "packed")])
+def test_layouts_refuse(fn, change, word):
+    assert word in layout(fn, **change)
+
+
+def test_layouts_refuse_misaligned_elements():
+    assert "scales" in layout("gn_pack4", scales=C.c_void_p(3)) and "scales" in layout("gn_pack4", scales=None)
+    assert "weights" in layout("gn_quantize4", w=C.c_void_p(3)) and "weights" in layout("gn_unpack4", w=C.c_void_p(3))
+    lib = gn.lib()
+    assert lib.gn_weight4_bytes(0, 16, 16) < 0 and lib.gn_weight4_scales(1, 16, 16, 48) < 0 and lib.gn_weight4_bytes(1, 1 << 20, 1 << 11) < 0
+    assert lib.gn_weight4_bytes(2, 17, 129) == 2 * 2 * 2 * 1024 and lib.gn_weight4_scales(2, 17, 129, 32) == 2 * 2 * 2 * 64
+
+
+@pytest.mark.parametrize("change,word", [c for c in SIZES4 if "experts" not in c[0]] + [
+    (dict(tokens=-1), "tokens"), (dict(tokens=1 << 20), "tokens"), (dict(x=None), "x:"), (dict(ldx=39), "x:"), (dict(q=C.c_void_p(8)), "packed"), (dict(y=None), "y:"), (dict(ldy=19), "y:")])
+def test_matvec4_refuses(change, word):
+    a = dict(type=1, tokens=3, rows=20, cols=40, group=32, x=P, ldx=40, q=P, scale=P, y=P, ldy=20, st=None)
+    a.update(change)
+    assert word in refused(gn.lib().gn_matvec4, *a.values())
+
+
+def ffn4(**change):
+    """gn_ffn4 as 17 words."""
+    a = dict(type=1, act=1, tokens=4, cols=8, inner=16, experts=3, k=2, group=32, index=1 << 20, weight=1 << 20, x=(1 << 21, 8), y=(1 << 22, 8))
+    a.update({n: 1 << 23 for n in ("q_gate", "s_gate", "q_up", "s_up", "q_down", "s_down")})
+    a.update(change)
+    words = [a["type"] | a["act"] << 32, a["tokens"], a["cols"] | a["inner"] << 32, a["experts"] | a["k"] << 32, a["group"], a["index"], a["weight"], *a["x"], *a["y"]]
+    return (C.c_int64 * 17)(*words, *(a[n] for n in ("q_gate", "s_gate", "q_up", "s_up", "q_down", "s_down")))
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(type=4), "type"), (dict(act=7), "act"), (dict(tokens=-1), "tokens"), (dict(tokens=1 << 19), "tokens"), (dict(cols=0), "rows"), (dict(inner=0), "rows"), (dict(experts=0), "experts"),
+    (dict(k=0), "k must"), (dict(k=33), "k must"), (dict(group=1), "group"), (dict(index=0), "index"), (dict(index=0, experts=1), "index"), (dict(index=2), "index"), (dict(weight=0), "weight"),
+    (dict(x=(0, 8)), "x:"), (dict(x=(1 << 21, 7)), "x:"), (dict(y=(0, 8)), "y:"), (dict(y=(1 << 21, 7)), "y:"), (dict(q_gate=0), "packed"), (dict(s_up=8), "packed"), (dict(q_down=4), "packed")])
+def test_gated_ffn4_refuses(change, word):
+    args = ffn4(**change)
+    assert word in refused(gn.lib().gn_gated_ffn4, args, P, 1 << 40, None)
+    assert gn.lib().gn_gated_ffn4_workspace(args) < 0
+
+
+def test_gated_ffn4_refuses_a_bad_workspace():
+    args = ffn4()
+    need = gn.lib().gn_gated_ffn4_workspace(args)
+    assert need > 0
+    for ws, n in ((None, need), (C.c_void_p((1 << 20) + 8), need), (P, need - 1)):
+        assert "workspace" in refused(gn.lib().gn_gated_ffn4, args, ws, n, None)
+    assert "no arguments" in refused(gn.lib().gn_gated_ffn4, None, P, need, None)
+
+
+def test_4_bit_weights_without_a_device():
+    q = torch.zeros(4, 8, dtype=torch.uint8)
+    for call in (lambda: gn.pack4(q, q.float()), lambda: gn.quantize4(q.float())):
+        with pytest.raises(TypeError, match="CUDA"):
+            call()

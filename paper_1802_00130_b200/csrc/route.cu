@@ -7,7 +7,8 @@
 //
 // The order of two experts has to be that of their values, whatever FP32 makes of them.  Without a bias it is the order of the logits, which are at hand.
 // With one, and for sums of a group's two best, the values are computed in FP32 with a bound on what they may be off; where two neighbours in the
-// order are nearer than that (and not the same logit with the same bias, which are equal in any arithmetic), the row is done again in FP64.
+// order are nearer than that (and not the same logit with the same bias, which are equal in any arithmetic), the row is done again in FP64, from shared memory, in a
+// function of its own that leaves the usual case its registers.
 //
 // The backward pass reads a whole row only where the scores are shares of all experts; else the chosen logits alone.
 #include <math.h>
@@ -20,7 +21,7 @@ namespace {
 
 constexpr int kRouteWarps = 8, kRouteExperts = 1024, kRouteChoices = 32;
 struct RouteParams {
-  int64_t tokens; int experts, k, softmax, renormalise, groups, each, top, best, vec;
+  int64_t tokens; int experts, k, softmax, renormalise, groups, each, top, best, vec, lanes;
   float scale;
   const void* logits; int64_t ld;
   const float* bias;
@@ -53,9 +54,6 @@ __device__ __forceinline__ double warp_sum(double x) {
   for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
 }
-__device__ __forceinline__ float exp_of(float x) { return expf(x); }
-__device__ __forceinline__ double exp_of(double x) { return exp(x); }
-
 // This lane's V logits of a row; -inf where there is no expert.
 template <int V, class T>
 __device__ __forceinline__ void load_row(const T* row, int lane, int experts, bool vec, float (&l)[V]) {
@@ -95,113 +93,185 @@ __device__ __forceinline__ void load_row(const T* row, int lane, int experts, bo
   for (int v = 0; v < V; ++v) l[v] = e0 + v < experts ? to_f(row[e0 + v]) : -__int_as_float(0x7f800000);
 }
 
-// What lane j < k has of the j-th chosen expert.
-struct Chosen { int index; float logit; };
-
-// Scores of this lane's experts.  A row of -inf alone has zeros.
-template <int V, class F>
-__device__ __forceinline__ void scores_of(const float (&l)[V], bool softmax, int lane, int experts, F (&s)[V]) {
-  if (softmax) {
-    float top = l[0];
+__device__ __forceinline__ float value_of(uint32_t key) { return key == 1u ? __int_as_float(0x7fffffff) : __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
+__device__ __forceinline__ float warp_max_nan(float x) {
 #pragma unroll
-    for (int v = 1; v < V; ++v) top = max_nan(top, l[v]);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (top == -__int_as_float(0x7f800000)) top = 0.f;
-    F sum = 0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) { s[v] = exp_of((F)l[v] - (F)top); sum += s[v]; }
-    sum = warp_sum(sum);
-    if (sum == (F)0) sum = 1;
-#pragma unroll
-    for (int v = 0; v < V; ++v) s[v] /= sum;
-  } else {
-#pragma unroll
-    for (int v = 0; v < V; ++v) s[v] = (F)1 / ((F)1 + exp_of(-(F)l[v]));
-  }
+  for (int o = 16; o; o >>= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
 }
+__device__ __forceinline__ float exp_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f)); return y; }
 
-// The choice in arithmetic F.  ORDERED: by the logits, without groups.  Returns whether it is certain (always in FP64).
-template <class F, int V, bool ORDERED>
-__device__ __forceinline__ bool choose(const RouteParams& p, const float (&l)[V], const float* bias, F* stage, int lane, Chosen& c) {
-  using Key = decltype(key_of(F()));
-  constexpr bool EXACT = sizeof(F) == 8;
-  constexpr float E = 5.9604645e-8f;                       // 2^-24
-  F s[V];
-  float b[V];
-  Key key[V];
-  if constexpr (!ORDERED) {
-    scores_of<V, F>(l, p.softmax, lane, p.experts, s);
-#pragma unroll
-    for (int v = 0; v < V; ++v) b[v] = bias && lane * V + v < p.experts ? bias[lane * V + v] : 0.f;
+// The k experts of a row in FP64, by a warp, from and to shared memory (an element for each expert): lane j < k returns the j-th.  Rare: few registers, no speed.
+template <class T>
+__device__ __noinline__ int choose_exactly(const RouteParams& p, const T* row, const float* bias, double* order, int lane) {
+  const double LOW = -(double)__int_as_float(0x7f800000);
+  float top = (float)LOW;
+  double sum = 0.0;
+  if (p.softmax) {
+    for (int e = lane; e < p.experts; e += 32) top = max_nan(top, to_f(row[e]));
+    top = warp_max_nan(top);
+    if (top == (float)LOW) top = 0.f;
+    for (int e = lane; e < p.experts; e += 32) sum += exp((double)to_f(row[e]) - (double)top);
+    sum = warp_sum(sum);
+    if (sum == 0.0) sum = 1.0;
   }
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    if constexpr (ORDERED) key[v] = key_of((F)l[v]);
-    else key[v] = bias ? key_of(s[v] + (F)b[v]) : key_of((F)l[v]);
-    if (lane * V + v >= p.experts) key[v] = 0;
-  }
-  bool certain = true;
-  if (!ORDERED && p.groups > 1) {
-    // Values of the groups, a lane each; rows of the stage are an odd number of elements apart.
-    const int pitch = p.each | 1;
-    const bool by_logit = p.best == 1 && !bias;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int x = lane * V + v;
-      if (x < p.experts) stage[x / p.each * pitch + x % p.each] = by_logit ? (F)l[v] : s[v] + (F)b[v];
-    }
-    __syncwarp();
-    // (NaN, as a group's best, is below every number: it loses against the -inf that a sum starts from)
-    const F low = -(F)__int_as_float(0x7f800000);
-    F first = low, second = low;
-    int i1 = 0, i2 = 0;
+  const auto score = [&](int e) {
+    const double l = (double)to_f(row[e]);
+    return p.softmax ? exp(l - (double)top) / sum : 1.0 / (1.0 + exp(-l));
+  };
+  for (int e = lane; e < p.experts; e += 32) order[e] = bias ? score(e) + (double)bias[e] : (double)to_f(row[e]);
+  __syncwarp();
+  uint32_t kept = 0xffffffffu;
+  if (p.groups > 1) {
+    double first = LOW, second = LOW;
+    int i1 = -1, i2 = -1;
     bool any = false;                // an element that is no NaN
     if (lane < p.groups)
-      for (int i = 0; i < p.each; ++i) {
-        const F x = stage[lane * pitch + i];
-        if (x > first) { second = first; first = x; i2 = i1; i1 = i; } else if (x > second) { second = x; i2 = i; }
+      for (int e = lane * p.each; e < (lane + 1) * p.each; ++e) {
+        const double x = order[e];
+        if (x > first || (i1 < 0 && x == x)) { second = first; i2 = i1; first = x; i1 = e; } else if (x > second || (i2 < 0 && x == x)) { second = x; i2 = e; }
         any |= x == x;
       }
-    __syncwarp();
-    F value = p.best == 2 && p.each > 1 ? first + second : first;
-    if (EXACT && p.best == 2 && p.each > 1) {
-      // Scores and biases by themselves: two groups that have the same ones in other pairs are equal, which roundings of four different values might not show.
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int x = lane * V + v;
-        if (x < p.experts) stage[x / p.each * pitch + x % p.each] = s[v];
-      }
-      __syncwarp();
-      if (lane < p.groups && first > low && second > low) {
-        const int e0 = lane * p.each;
-        value = (stage[lane * pitch + i1] + stage[lane * pitch + i2]) + (bias ? (F)bias[e0 + i1] + (F)bias[e0 + i2] : (F)0);
-      }
-      __syncwarp();
-    }
-    Key g = lane < p.groups ? (any ? key_of(value) : (Key)1) : (Key)0;
-    uint32_t kept = 0;
-    F last = 0;
-    for (int j = 0; j <= p.top && j < p.groups; ++j) {
-      const Key m = warp_max(g);
+    double value = first;
+    // Scores and biases by themselves: two groups that have the same ones in other pairs are equal, which roundings of four different values might not show.
+    if (p.best == 2 && p.each > 1) value = i2 < 0 ? LOW : (score(i1) + score(i2)) + (bias ? (double)bias[i1] + (double)bias[i2] : 0.0);
+    uint64_t g = lane < p.groups ? (any ? key_of(value) : 1u) : 0u;
+    kept = 0;
+    for (int j = 0; j < p.top; ++j) {
+      const uint64_t m = warp_max(g);
       const int from = __ffs(__ballot_sync(0xffffffffu, g == m)) - 1;
-      const F mine = __shfl_sync(0xffffffffu, value, from);
-      if (j == p.top) {
-        // two sums of two scores, each score off by 150 steps of itself at most (see below), and the biases' roundings
-        const float gap = (float)(last - mine), bound = E * (300.f * 2.f + 4.f * (fabsf((float)last) + fabsf((float)mine)));
-        if (!EXACT && !by_logit && gap <= bound) certain = false;
-      } else {
-        kept |= 1u << from;
-        last = mine;
-        if (lane == from) g = 0;
-      }
+      kept |= 1u << from;
+      if (lane == from) g = 0;
     }
+  }
+  uint64_t best;
+  int at, mine = -1;
+  const auto look = [&] {
+    best = 0; at = -1;
+#pragma unroll 1
+    for (int e = lane; e < p.experts; e += 32) {
+      if (p.groups > 1 && !(kept >> (e / p.each) & 1)) continue;
+      const uint64_t k = key_of(order[e]);
+      if (k > best && !(__double_as_longlong(order[e]) == 0x7fffffffffffffffll)) { best = k; at = e; }
+    }
+  };
+  look();
+#pragma unroll 1
+  for (int j = 0; j < p.k; ++j) {
+    const uint64_t m = warp_max(best);
+    const int e = (int)__reduce_min_sync(0xffffffffu, best == m ? (unsigned)at : 0xffffffffu);
+    if (lane == j) mine = e;
+    if (best == m && at == e) { order[e] = __longlong_as_double(0x7fffffffffffffffll); look(); }      // (a NaN of its own: taken)
+  }
+  __syncwarp();
+  return mine;
+}
+
+// The same in FP32.  ORDERED: by the logits, without groups.  Whether the order is certain goes to `certain`.
+template <int V, bool ORDERED, class T>
+__device__ __forceinline__ int choose(const RouteParams& p, const T* row, const float (&l)[V], const float (&b)[V], const float* bias, float* stage, int lane, bool& certain) {
+  constexpr float E = 5.9604645e-8f;                       // 2^-24
+  const float LOW = -__int_as_float(0x7f800000);
+  uint32_t key[V];
+  // What a score may be off, in 2^-24.  Sigmoid: the exponential's argument (|l| s (1 - s) is below 0.23), the exponential 2, the sum and the reciprocal 1 each.
+  // Softmax, of the largest score: the two roundings of the argument (|x| exp(x) is below 0.37), the exponential 2, the sum of up to 1024 of them 5 + 32, 2 more.
+  float off = 8.f;
+  if constexpr (!ORDERED) {
+    float s[V];
+    if (p.softmax) {
+      float top = l[0], sum = 0.f;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (!(kept >> (min(lane * V + v, p.experts - 1) / p.each) & 1)) key[v] = 0;
+      for (int v = 1; v < V; ++v) top = max_nan(top, l[v]);
+      top = warp_max_nan(top);
+      if (top == LOW) top = 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) { s[v] = exp_fast(l[v] - top); sum += s[v]; }
+      sum = warp_sum(sum);
+      sum = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int v = 0; v < V; ++v) s[v] *= sum;
+      off = 48.f * sum;
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) s[v] = sigmoid_from(exp_fast(-l[v]));
+    }
+    const bool by_logit = !bias;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      s[v] += b[v];                                        // (from here on the values)
+      key[v] = key_of(by_logit ? l[v] : s[v]);
+      if (lane * V + v >= p.experts) key[v] = 0;
+    }
+    if (p.groups > 1) {
+      const bool one = p.best == 1 || p.each == 1, plain = one && by_logit;
+      float first = LOW, second = LOW;
+      bool any = false;              // an element that is no NaN
+      const auto take = [&](float x) { second = fmaxf(second, fminf(first, x)); first = fmaxf(first, x); any |= x == x; };
+      uint32_t g, kept = 0;
+      int lanes = 1;                 // to a group
+      if (p.lanes) {                 // a power of two of whole lanes
+        lanes = p.lanes;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const float x = plain ? l[v] : s[v];
+          if (x == x) take(x);
+        }
+        any = false;
+#pragma unroll
+        for (int v = 0; v < V; ++v) any |= (plain ? l[v] : s[v]) == (plain ? l[v] : s[v]);
+        for (int o = 1; o < lanes; o <<= 1) {
+          const float f = __shfl_xor_sync(0xffffffffu, first, o), q = __shfl_xor_sync(0xffffffffu, second, o);
+          second = fmaxf(fminf(first, f), fmaxf(second, q));
+          first = fmaxf(first, f);
+          any |= __shfl_xor_sync(0xffffffffu, (int)any, o) != 0;
+        }
+        g = lane * V < p.experts ? 2u : 0u;
+      } else {                       // a lane each; rows of the stage are an odd number of elements apart
+        const int pitch = p.each | 1;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int x = lane * V + v;
+          if (x < p.experts) stage[x / p.each * pitch + x % p.each] = plain ? l[v] : s[v];
+        }
+        __syncwarp();
+        if (lane < p.groups)
+          for (int i = 0; i < p.each; ++i) {
+            const float x = stage[lane * pitch + i];
+            if (x == x) take(x);
+          }
+        __syncwarp();
+        g = lane < p.groups ? 2u : 0u;
+      }
+      const float value = one ? first : first + second;
+      if (g) g = any ? key_of(value) : 1u;
+      float last = 0.f;
+      const uint32_t span = lanes == 32 ? 0xffffffffu : (1u << lanes) - 1;
+      for (int j = 0; j <= p.top && j < p.groups; ++j) {
+        const uint32_t m = warp_max(g);
+        const int from = __ffs(__ballot_sync(0xffffffffu, g == m)) - 1;
+        const float v = value_of(m);
+        if (j == p.top) {
+          // two sums of two values, each a score and a bias, and their roundings
+          if (!plain && last - v <= E * (4.f * off + 4.f * (fabsf(last) + fabsf(v)))) certain = false;
+        } else {
+          kept |= span << from;
+          last = v;
+          if (kept >> lane & 1) g = 0;
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (!(kept >> (p.lanes ? lane : min(lane * V + v, p.experts - 1) / p.each) & 1)) key[v] = 0;
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      key[v] = key_of(l[v]);
+      if (lane * V + v >= p.experts) key[v] = 0;
+    }
   }
 
-  Key best;
+  uint32_t best;
   int at;
   const auto look = [&] {
     best = key[0]; at = 0;
@@ -210,35 +280,26 @@ __device__ __forceinline__ bool choose(const RouteParams& p, const float (&l)[V]
       if (key[v] > best) { best = key[v]; at = v; }
   };
   look();
-  c = Chosen{-1, 0.f};
   // ORDERED, and without a bias, the keys are the values; else the first one behind the last that is not its equal is looked at too.
-  const bool sure = ORDERED || EXACT || !bias;
-  float last_l = 0.f, last_s = 0.f, last_b = 0.f;
+  const bool sure = ORDERED || !bias;
+  int mine = -1, last_index = 0;
+  float last = __int_as_float(0x7fffffff);
   for (int j = 0; j < p.k || !sure; ++j) {
-    const Key m = warp_max(best);
+    const uint32_t m = warp_max(best);
     if (m == 0) break;                                     // (nobody is left)
     const int from = __ffs(__ballot_sync(0xffffffffu, best == m)) - 1;
-    float mine_l = l[0], mine_s = 0.f, mine_b = 0.f;
-    if constexpr (!ORDERED) { mine_s = (float)s[0]; mine_b = b[0]; }
-#pragma unroll
-    for (int v = 1; v < V; ++v)
-      if (at == v) {
-        mine_l = l[v];
-        if constexpr (!ORDERED) { mine_s = (float)s[v]; mine_b = b[v]; }
-      }
     const int index = __shfl_sync(0xffffffffu, lane * V + at, from);
-    const float logit = __shfl_sync(0xffffffffu, mine_l, from);
     if (!sure) {
-      const float score = __shfl_sync(0xffffffffu, mine_s, from), by = __shfl_sync(0xffffffffu, mine_b, from);
-      const bool same = logit == last_l && by == last_b;
-      // A score is off by at most 150 steps of itself: the sum of up to 1024 exponentials by 5 + 32 + 2 of them, an exponential by 2 and, with its argument's
-      // rounding, as many as the argument is large, 103 before it is zero; the division by 1.  A value by its own rounding besides.
-      const float value = score + by, last = last_s + last_b;
-      if (j > 0 && !same && last - value <= E * (150.f * (last_s + score) + fabsf(last) + fabsf(value))) { certain = false; break; }
+      const float value = value_of(m);
+      bool same = false;
+      if (last - value <= E * (2.f * off + fabsf(last) + fabsf(value))) {
+        same = to_f(row[index]) == to_f(row[last_index]) && bias[index] == bias[last_index];
+        if (!same) { certain = false; break; }
+      }
       if (j >= p.k && !same) break;
-      last_l = logit; last_s = score; last_b = by;
+      last = value; last_index = index;
     }
-    if (lane == j && j < p.k) { c.index = index; c.logit = logit; }
+    if (lane == j && j < p.k) mine = index;
     if (lane == from) {
 #pragma unroll
       for (int v = 0; v < V; ++v)
@@ -246,48 +307,38 @@ __device__ __forceinline__ bool choose(const RouteParams& p, const float (&l)[V]
       look();
     }
   }
-  return certain;
-}
-
-// (by itself, so that the usual case keeps its registers)
-template <int V>
-__device__ __noinline__ Chosen choose_exactly(const RouteParams& p, const float (&l)[V], const float* bias, double* stage, int lane) {
-  Chosen c;
-  choose<double, V, false>(p, l, bias, stage, lane, c);
-  return c;
+  return mine;
 }
 
 template <class T, int V, bool ORDERED>
 __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const __grid_constant__ RouteParams p) {
-  extern __shared__ double stages[];                       // (groups: an element for each expert and for each group)
+  extern __shared__ double stages[];                       // (an element for each expert and for each group)
   grid_dep_wait();
   grid_dep_launch();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   double* const stage = stages + warp * (p.experts + p.groups);
   const T* const logits = (const T*)dep(p.logits);
   const float* const bias = dep(p.bias);
-  for (int64_t t = (int64_t)blockIdx.x * kRouteWarps + warp; t < p.tokens; t += (int64_t)gridDim.x * kRouteWarps) {
-    float l[V];
-    load_row<V, T>(logits + t * p.ld, lane, p.experts, p.vec, l);
-    Chosen c;
-    if (!choose<float, V, ORDERED>(p, l, bias, reinterpret_cast<float*>(stage), lane, c)) {
-      if constexpr (!ORDERED) {
-        float copy[V];               // (of which the call takes an address)
+  float b[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) copy[v] = l[v];
-        c = choose_exactly<V>(p, copy, bias, stage, lane);
-      }
-    }
-    float w;
+  for (int v = 0; v < V; ++v) b[v] = !ORDERED && bias && lane * V + v < p.experts ? bias[lane * V + v] : 0.f;
+  for (int64_t t = (int64_t)blockIdx.x * kRouteWarps + warp; t < p.tokens; t += (int64_t)gridDim.x * kRouteWarps) {
+    const T* const row = logits + t * p.ld;
+    float l[V];
+    load_row<V, T>(row, lane, p.experts, p.vec, l);
+    bool certain = true;
+    int index = choose<V, ORDERED, T>(p, row, l, b, bias, reinterpret_cast<float*>(stage), lane, certain);
+    if (!ORDERED && !certain) index = choose_exactly<T>(p, row, bias, stage, lane);
     const bool mine = lane < p.k;
+    const float z = mine ? to_f(row[index]) : 0.f;
+    float w;
     if (p.softmax) {
       float top = l[0], sum = 0.f;
 #pragma unroll
       for (int v = 1; v < V; ++v) top = max_nan(top, l[v]);
-#pragma unroll
-      for (int o = 16; o; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+      top = warp_max_nan(top);
       if (top == -__int_as_float(0x7f800000)) top = 0.f;
-      w = mine ? expf(c.logit - top) : 0.f;
+      w = mine ? expf(z - top) : 0.f;
       if (p.renormalise) {
         sum = w;
       } else {
@@ -297,14 +348,14 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const __grid_co
       sum = warp_sum(sum);
       w = sum == 0.f ? 0.f : w / sum;
     } else {
-      w = mine ? 1.f / (1.f + expf(-c.logit)) : 0.f;
+      w = mine ? 1.f / (1.f + expf(-z)) : 0.f;
       if (p.renormalise) {
         const float sum = warp_sum(w);
         w = sum == 0.f ? 0.f : w / sum;
       }
     }
     if (mine) {
-      p.index[t * p.k + lane] = c.index;
+      p.index[t * p.k + lane] = index;
       p.weight[t * p.k + lane] = w * p.scale;
     }
   }
@@ -413,7 +464,7 @@ cudaError_t launch_route(const RouteParams& p, bool grad, cudaStream_t st) {
   const int grid = (int)(want < most ? want : most);
   if (grad) return launch_pdl(p.softmax && !p.renormalise ? route_grad_kernel<T, V, true> : route_grad_kernel<T, V, false>, grid, 32 * kRouteWarps, 0, st, p);
   if (!p.bias && p.groups == 1) return launch_pdl(route_kernel<T, V, true>, grid, 32 * kRouteWarps, 0, st, p);
-  const int smem = p.groups > 1 ? kRouteWarps * (p.experts + p.groups) * 8 : 0;
+  const int smem = kRouteWarps * (p.experts + p.groups) * 8;
   auto* const kernel = route_kernel<T, V, false>;
   static std::atomic<signed char> ready[64];
   if (!once_per_device(ready, [&] {
@@ -433,6 +484,8 @@ cudaError_t run_route(RouteParams p, bool grad, cudaStream_t st) {
     return ((uintptr_t)q % (uintptr_t)piece) == 0 && ld * (int)sizeof(T) % piece == 0;
   };
   p.vec = p.experts % v == 0 && whole(p.logits, p.ld) && (!grad || whole(p.dlogits, p.ld_d));
+  // lanes of a group where they are whole and a power of two
+  p.lanes = p.groups > 1 && p.each % v == 0 && (p.each / v & (p.each / v - 1)) == 0 ? p.each / v : 0;
   switch (v) {
     case 1: return launch_route<T, 1>(p, grad, st);
     case 2: return launch_route<T, 2>(p, grad, st);

@@ -125,6 +125,7 @@ struct Workspace {               // hands out 256-byte aligned pieces (of no mem
   void* take(int64_t bytes) { void* r = p + used; used += (bytes + 255) / 256 * 256; return r; }
 };
 char* const kNowhere = reinterpret_cast<char*>(256);
+inline int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 
 const char* ffn4_args(const gn_ffn4* f) {
   if (!f) return "no arguments";
@@ -142,30 +143,40 @@ const char* ffn4_args(const gn_ffn4* f) {
   if (f->index && (!f->weight || ((uintptr_t)f->weight & 3))) return "weight: null or misaligned";
   return nullptr;
 }
-struct Few4 { ExpertPlan plan; float *h, *out; int64_t ld_h, ld_out; int columns; };
-// Columns of a tile: eight where that is what a tile has, on average over the experts that can have one.
-int columns4(int64_t pairs, int experts) { return pairs <= 8 * (pairs < experts ? pairs : (int64_t)experts) ? 8 : 32; }
+struct Few4 { ExpertPlan plan; void *x, *h; float* out; int64_t ld_x, ld_h, ld_out; int tile; };
+// Tokens of a plan's tile: eight (five in FP32, whose operands are three rows each) where that is what the experts that can have one have on average, else twice as many.
+int tile_tokens(int64_t pairs, int experts, bool f32) {
+  const bool few = pairs <= 4 * (pairs < experts ? pairs : (int64_t)experts);
+  return f32 ? (few ? 5 : 10) : few ? 8 : 16;
+}
 int64_t lay_out(const gn_ffn4& f, char* base, Few4& w) {
   Workspace ws{base};
   const int64_t pairs = f.tokens * f.k;
+  const bool f32 = f.type == GN_F32;
   w = Few4{};
-  w.columns = columns4(pairs, f.experts);
-  w.ld_h = (f.inner + 3) / 4 * 4; w.ld_out = (f.cols + 7) / 8 * 8;
-  w.h = (float*)ws.take(pairs * w.ld_h * 4);
+  w.tile = tile_tokens(pairs, f.experts, f32);
+  w.ld_x = up8(f.cols); w.ld_h = up8(f.inner); w.ld_out = up8(f.cols);
+  if (f32) w.x = ws.take(3 * f.tokens * w.ld_x * 2);
+  w.h = ws.take((f32 ? 3 : 2) * pairs * w.ld_h * 2);
   if (f.index) {
-    w.plan = plan_at((int*)ws.take(plan_ints(pairs, f.experts, w.columns) * 4), pairs, f.experts, w.columns);
+    w.plan = plan_at((int*)ws.take(plan_ints(pairs, f.experts, w.tile) * 4), pairs, f.experts, w.tile);
     w.out = (float*)ws.take(pairs * w.ld_out * 4);
   }
   return ws.used + 256;
 }
 cudaError_t run_ffn4(const gn_ffn4& f, const Few4& w, cudaStream_t st) {
-  cudaError_t e = f.index ? launch_plan(f.index, w.plan, w.columns, st) : cudaSuccess;
+  const int64_t pairs = f.tokens * f.k;
+  cudaError_t e = f.index ? launch_plan(f.index, w.plan, w.tile, st) : cudaSuccess;
   Product4 a, b;
-  a.rows = f.inner; a.cols = f.cols; a.group = b.group = f.group; a.act = f.act; a.tokens = b.tokens = f.tokens; a.k = b.k = f.k; a.columns = b.columns = w.columns;
+  a.rows = f.inner; a.cols = f.cols; a.group = b.group = f.group; a.act = f.act; a.tokens = b.tokens = f.tokens; a.k = b.k = f.k; a.tile_tokens = b.tile_tokens = w.tile;
   a.gate = true; a.x = f.x.p; a.ldx = f.x.ld; a.token_rows = true;
+  if (w.x) {
+    if (e == cudaSuccess) e = launch_parts((const float*)f.x.p, f.x.ld, f.tokens, f.cols, w.x, w.ld_x, st);
+    a.x = w.x; a.ldx = w.ld_x; a.part_stride = f.tokens * w.ld_x;
+  }
   a.w[0] = {(const uint8_t*)f.q_gate, f.s_gate}; a.w[1] = {(const uint8_t*)f.q_up, f.s_up};
-  a.d = w.h; a.ldd = w.ld_h; a.d32 = true;
-  b.rows = f.cols; b.cols = f.inner; b.x = w.h; b.ldx = w.ld_h; b.x32 = true; b.early = true;
+  a.d = w.h; a.ldd = w.ld_h; a.part_stride_d = pairs * w.ld_h;
+  b.rows = f.cols; b.cols = f.inner; b.x = w.h; b.ldx = w.ld_h; b.part_stride = a.part_stride_d; b.in_parts = true; b.early = true;
   b.w[0] = {(const uint8_t*)f.q_down, f.s_down};
   if (f.index) { a.plan = b.plan = &w.plan; b.d = w.out; b.ldd = w.ld_out; b.d32 = true; }
   else { b.d = f.y.p; b.ldd = f.y.ld; }
@@ -200,21 +211,32 @@ extern "C" gn_status gn_unpack4(gn_dtype type, int32_t experts, int64_t rows, in
                                 void* cuda_stream, char* errbuf, int64_t errbuf_len) {
   return layout4(2, type, experts, rows, cols, group, nullptr, ld, stride, nullptr, const_cast<void*>(d_q), const_cast<void*>(d_scale), d_w, cuda_stream, errbuf, errbuf_len);
 }
+extern "C" int64_t gn_matvec4_workspace(gn_dtype type, int64_t tokens, int64_t cols) {
+  if (!type_ok(type) || tokens < 0 || tokens >= (1 << 20) || cols < 1 || cols > (1 << 20)) return -1;
+  return type == GN_F32 ? 3 * tokens * up8(cols) * 2 : 0;
+}
 extern "C" gn_status gn_matvec4(gn_dtype type, int64_t tokens, int64_t rows, int64_t cols, int32_t group, const void* d_x, int64_t ldx, const void* d_q, const void* d_scale,
-                                void* d_y, int64_t ldy, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
+                                void* d_y, int64_t ldy, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
   const char* why = sizes4(type, 1, rows, cols, group);
   if (!why) {
-    if (tokens < 0 || tokens >= (1 << 20)) why = "tokens must be in [0, 2^20)";
+    const int64_t need = gn_matvec4_workspace(type, tokens, cols);
+    if (need < 0) why = "tokens must be in [0, 2^20)";
     else if (!packed_ok(d_q, d_scale)) why = kPackedWhy;
     else if (tokens > 0 && !mat_ok(d_x, ldx, cols, type)) why = "x: null, misaligned, or a leading dimension below cols";
     else if (tokens > 0 && !mat_ok(d_y, ldy, rows, type)) why = "y: null, misaligned, or a leading dimension below rows";
+    else if (need > 0 && (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < need)) why = "workspace: null, not 16-byte aligned or too small";
   }
   if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
   if (tokens == 0) return op_done(cudaSuccess, errbuf, errbuf_len);
+  cudaStream_t st = (cudaStream_t)cuda_stream;
   Product4 p;
   p.rows = (int)rows; p.cols = (int)cols; p.group = group; p.tokens = tokens; p.x = d_x; p.ldx = ldx; p.w[0] = {(const uint8_t*)d_q, d_scale}; p.d = d_y; p.ldd = ldy;
-  p.columns = columns4(tokens, 1);
-  return op_done(launch_product4(type, p, (cudaStream_t)cuda_stream), errbuf, errbuf_len);
+  cudaError_t e = cudaSuccess;
+  if (type == GN_F32) {
+    e = launch_parts((const float*)d_x, ldx, tokens, (int)cols, d_ws, up8(cols), st);
+    p.x = d_ws; p.ldx = up8(cols); p.part_stride = tokens * up8(cols);
+  }
+  return op_done(e == cudaSuccess ? launch_product4(type, p, st) : e, errbuf, errbuf_len);
 }
 extern "C" int64_t gn_gated_ffn4_workspace(const gn_ffn4* args) {
   Few4 w;

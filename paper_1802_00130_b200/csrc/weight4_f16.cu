@@ -4,7 +4,8 @@
 namespace gn {
 
 cudaError_t launch_product4_f16(const Product4& p, cudaStream_t st) {
-  return p.x32 ? launch_product4_x<__half, float, 2>(p, st) : launch_product4_x<__half, __half, 1>(p, st);
+  if (p.gate) return launch_product4_of<__half, __half, 1, 2>(p, st);
+  return p.in_parts ? launch_product4_of<__half, __nv_bfloat16, 2, 1>(p, st) : launch_product4_of<__half, __half, 1, 1>(p, st);
 }
 
 }  // namespace gn

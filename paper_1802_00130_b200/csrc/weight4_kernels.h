@@ -14,22 +14,24 @@ inline int64_t w4_blocks(int64_t cols) { return (cols + 127) / 128; }
 inline int64_t w4_bytes(int64_t rows, int64_t cols) { return w4_tiles(rows) * w4_blocks(cols) * 1024; }                                   // of an expert's q
 inline int64_t w4_scales(int64_t rows, int64_t cols, int group) { return w4_tiles(rows) * w4_blocks(cols) * 16 * (128 / group); }          // of an expert
 
-// d [columns][rows] = x w^T, columns being tokens (or pairs of a plan: a tile of up to 8 or 32 of an expert's).  gate: w[0] and w[1], d = act(.) * (.) in FP32.
-//   x        of the type, or (x32) FP32: what the gate has written
-//   d        of the type, or (d32) FP32
+// d [tokens][rows] = x w^T.  gate: w[0] and w[1], d = act(.) * (.).
+//   x        16-bit operands: tokens of the type; or `parts` BF16 rows that add up to each token, part_stride apart
+//   d        of the type, or (d32) FP32; gate: BF16 parts that add up to it, two or (FP32) three, part_stride_d apart
 struct Product4 {
   int rows = 0, cols = 0, group = 128, act = 0;
   int64_t tokens = 0;
-  bool gate = false, x32 = false, d32 = false, early = false;        // early: the weights may be loaded before the kernel before this one is done
-  const void* x = nullptr; int64_t ldx = 0;
+  bool gate = false, in_parts = false, d32 = false, early = false;       // early: weights and plan may be read before the kernel before this one is done
+  const void* x = nullptr; int64_t ldx = 0, part_stride = 0;
   Weight4 w[2];
-  void* d = nullptr; int64_t ldd = 0;
-  const ExpertPlan* plan = nullptr;  // its tiles have 8 or 32 columns
+  void* d = nullptr; int64_t ldd = 0, part_stride_d = 0;
+  const ExpertPlan* plan = nullptr; int tile_tokens = 0;         // the tokens are pairs of a plan with tiles of so many, of at most 32 operand rows
   int k = 1; bool token_rows = false;            // of a plan: rows of x are the tokens', else the pairs'
-  int columns = 8;                   // of a tile
 };
+inline int w4_parts(bool f32, bool in_parts) { return f32 ? 3 : in_parts ? 2 : 1; }
 cudaError_t launch_product4_f32(const Product4& p, cudaStream_t st);
 cudaError_t launch_product4_bf16(const Product4& p, cudaStream_t st);
 cudaError_t launch_product4_f16(const Product4& p, cudaStream_t st);
+// FP32 rows as three BF16 ones: to [3][rows][ld_out], ld_out a multiple of 8.
+cudaError_t launch_parts(const float* x, int64_t ldx, int64_t rows, int cols, void* to, int64_t ld_out, cudaStream_t st);
 
 }  // namespace gn

@@ -2,14 +2,16 @@
 //
 // The weights are laid out for the kernel: a record of 1 KB has 16 rows by 128 columns, 16 bytes for each lane of a warp from rows 0..7 and 16 from rows 8..15, so
 // that a warp's load is 512 bytes in a row and a tile's records follow one another.  A lane's word has eight neighbouring columns, the even ones in its low
-// halves' nibbles: a mask and an exclusive or make two of them a pair of 16-bit numbers, 128 + q or 1024 + q, from which 136 or 1032 is
-// taken: q - 8 exactly.  The tensor core's m16n8k16 takes them against eight tokens; its 32-bit sums of a group of columns get the group's scale.  (A tile of
-// tcgen05 would need the operands in shared memory, as many bytes again as sixteen-bit weights.)
+// halves' nibbles: a mask and an or make two of them a pair of 16-bit numbers, 128 + q say, from which 136 is taken: q - 8 exactly.  The tensor core's m16n8k16 takes
+// them against eight tokens; its 32-bit sums of a group of columns get the group's scale.  (A tile of tcgen05 would need the operands in shared memory, as many bytes
+// again as 16-bit weights.  A second product, of the tokens with 136, in the place of the operands' subtractions took longer: 31 against 25 us for a token
+// through 4096 x 8192.)
 //
-// FP32 tokens go in three 16-bit parts of eight bits each, exact; the hidden units of a gated layer, FP32 as the first kernel leaves them, in two (17 bits) where the result is
-// rounded to 16 bits.
-// Eight warps share a block: W of them a tile of 16 rows (of both matrices, gate), each with every W-th record; their sums are added in order in shared memory.  A
-// warp has the loads of the next records under way while it computes.
+// FP32 tokens are columns of three BF16 parts of eight bits each, exact; the hidden units of a gated layer of two (17 bits) where the result is rounded to 16
+// bits, as the first kernel has written them.
+// Four or eight warps share a block: W of them a tile of 16 rows (of both matrices, gate), each with every W-th record; their sums are added in order in shared memory.  W is
+// what it takes to give every SM its warps: a warp with many records streams them, through a ring of its own in shared memory that asynchronous copies fill
+// several records ahead (a lane reads back what it has asked for itself, and the scales what its warp has).
 #pragma once
 #include "ffn_act.cuh"
 #include "tc_common.cuh"
@@ -18,279 +20,314 @@
 namespace gn {
 namespace {
 
-constexpr int Q_WARPS = 8, Q_THREADS = 32 * Q_WARPS;
+constexpr int Q_WARPS = 8, Q_THREADS = 32 * Q_WARPS;           // of a block at most
 struct Product4Params {
-  int rows, cols, act, kblocks, tiles, split, early, vec, k, token_rows;
-  int64_t tokens;
-  const void* x; int64_t ldx;
+  int rows, cols, act, kblocks, tiles, split, log_split, log_block, early, vec, k, token_rows, tokens;
+  const void* x; int64_t ldx, part_stride;
   const uint8_t* q[2]; const void* scale[2];
   int64_t q_stride, scale_stride;    // from expert to expert
-  void* d; int64_t ldd; int d32;
+  void* d; int64_t ldd, part_stride_d; int d32;
   const ExpertTile* list; const int* n_list; const int* pair_of;
 };
 
-template <class T> struct Half2Of { using type = __nv_bfloat162; };
-template <> struct Half2Of<__half> { using type = __half2; };
-// Columns 2 i and 2 i + 1 of a word, less 8.
-template <class T>
+// Columns 2 i and 2 i + 1 of a word, less 8: q + 128 in BF16's seven bits of fraction; in FP16's ten q + 1024, or q + 64 four bits up, which is a shift for two pairs.
+template <class O>
 __device__ __forceinline__ uint32_t quarter_pair(uint32_t w, int i) {
-  if constexpr (__is_same(T, __half)) {
-    const uint32_t v = ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u;
-    const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&v), __half2(__half_raw{0x6408}, __half_raw{0x6408}));
+  if constexpr (__is_same(O, __half)) {
+    const uint32_t x = i < 2 ? w : w >> 8, v = i & 1 ? (x & 0x00f000f0u) | 0x54005400u : (x & 0x000f000fu) | 0x64006400u, by = i & 1 ? 0xd480d480u : 0xe408e408u;
+    const __half2 h = __hadd2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&by));
     return *reinterpret_cast<const uint32_t*>(&h);
   } else {
-    const uint32_t v = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
-    const __nv_bfloat162 h = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), __nv_bfloat162(__nv_bfloat16_raw{0x4308}, __nv_bfloat16_raw{0x4308}));
+    const uint32_t v = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u, by = 0xc308c308u;
+    const __nv_bfloat162 h = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&by));
     return *reinterpret_cast<const uint32_t*>(&h);
   }
 }
-template <class T>
-__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  if constexpr (__is_same(T, __half))
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+// d = a b, or with `more` d += a b.
+template <class O>
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, bool more) {
+  const float c0 = more ? d[0] : 0.f, c1 = more ? d[1] : 0.f, c2 = more ? d[2] : 0.f, c3 = more ? d[3] : 0.f;
+  if constexpr (__is_same(O, __half))
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 
-// Eight neighbouring columns of a token as PARTS parts of four pairs.
-template <int PARTS> struct Eight { uint32_t w[PARTS][4]; };
-// The leading 8 bits of v as a BF16 (cut off), and what is left of it; infinities leave nothing.
-__device__ __forceinline__ uint32_t leading(float v, float& rest) {
-  const uint32_t high = __float_as_uint(v) & 0xffff0000u;
-  rest = fabsf(v) == __int_as_float(0x7f800000) ? 0.f : v - __uint_as_float(high);
-  return high >> 16;
-}
-template <class X, int PARTS>
-__device__ __forceinline__ Eight<PARTS> load_eight(const X* row, int c, int cols, bool vec) {
-  Eight<PARTS> r;
+// Eight neighbouring columns of a row of operands; zeros past its end, or without a row.  WHOLE: all of them are there, as 16 bytes.
+template <bool WHOLE, class O>
+__device__ __forceinline__ uint4 load_eight(const O* row, int c, int cols) {
+  if constexpr (WHOLE) return row ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
   const int left = row ? cols - c : 0;
-  if constexpr (sizeof(X) == 2) {
-    static_assert(PARTS == 1, "16-bit tokens are operands as they are");
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (vec && left >= 8) {
-      v = *reinterpret_cast<const uint4*>(row + c);
-    } else if (left > 0) {
-      uint32_t o[4] = {0u, 0u, 0u, 0u};
+  uint32_t o[4] = {0u, 0u, 0u, 0u};
+  if (left > 0) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < left) o[e >> 1] |= (uint32_t) * reinterpret_cast<const uint16_t*>(row + c + e) << (16 * (e & 1));
-      v = make_uint4(o[0], o[1], o[2], o[3]);
-    }
-    r.w[0][0] = v.x; r.w[0][1] = v.y; r.w[0][2] = v.z; r.w[0][3] = v.w;
-  } else {
-    float f[8];
-    if (vec && left >= 8) {
-      const float4 a = *reinterpret_cast<const float4*>(row + c), b = *reinterpret_cast<const float4*>(row + c + 4);
-      f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = e < left ? row[c + e] : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float a = f[2 * i], b = f[2 * i + 1];
-#pragma unroll
-      for (int part = 0; part < PARTS; ++part) {
-        if (part == PARTS - 1 && PARTS == 2) {
-          r.w[part][i] = pack2<__nv_bfloat16>(a, b);           // (the last of two is rounded)
-        } else {
-          float ra, rb;
-          const uint32_t lo = leading(a, ra), hi = leading(b, rb);
-          r.w[part][i] = lo | hi << 16;
-          a = ra; b = rb;
-        }
-      }
-    }
+    for (int e = 0; e < 8; ++e)
+      if (e < left) o[e >> 1] |= (uint32_t) * reinterpret_cast<const uint16_t*>(row + c + e) << (16 * (e & 1));
   }
-  return r;
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+// An FP32 number as PARTS BF16 numbers that add up to it: the leading 8 bits of what is left, cut off, three times (exact), or once and the rest rounded.
+// Infinities leave nothing.
+template <int PARTS>
+__device__ __forceinline__ void split_parts(float v, __nv_bfloat16 (&o)[PARTS]) {
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) {
+    if (i == 1 && PARTS == 2) { o[i] = __float2bfloat16_rn(v); break; }
+    const uint32_t high = __float_as_uint(v) & 0xffff0000u;
+    o[i] = __nv_bfloat16(__nv_bfloat16_raw{(unsigned short)(high >> 16)});
+    v = fabsf(v) == __int_as_float(0x7f800000) ? 0.f : v - __uint_as_float(high);
+  }
 }
 
-// G scales of a row for a record's groups.
-template <class T, int G> struct Scales { T s[G]; };
-template <class T, int G>
-__device__ __forceinline__ Scales<T, G> load_scales(const T* p) {
-  Scales<T, G> r;
-  constexpr int BYTES = G * (int)sizeof(T);
-  if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(r.s) = *reinterpret_cast<const uint4*>(p);
-  else if constexpr (BYTES == 8) *reinterpret_cast<uint2*>(r.s) = *reinterpret_cast<const uint2*>(p);
-  else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(r.s) = *reinterpret_cast<const uint32_t*>(p);
-  else r.s[0] = *p;
-  return r;
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// T: type of the scales and of the result; X: of the tokens; G groups of a record; NT tiles of eight tokens; M matrices (2: gate).
-template <class T, class X, int PARTS, int G, int NT, int M>
-__global__ void __launch_bounds__(Q_THREADS, NT == 1 && M == 1 ? 3 : 2) product4_kernel(const __grid_constant__ Product4Params p) {
-  using O = typename std::conditional<__is_same(X, __half), __half, __nv_bfloat16>::type;    // operands
-  constexpr int COLUMNS = 8 * NT, PITCH = 17;
-  __shared__ float sums[Q_WARPS][M][COLUMNS][PITCH];
+// A warp's ring: of each record, for each of M matrices, the 1 KB of weights and 16 rows' scales.
+template <class T, int G, int M> constexpr int q_piece = 1024 + 16 * G * (int)sizeof(T);
+template <int M> constexpr int q_stages = M == 2 ? 4 : 6;
+template <class T, int G, int M> constexpr int q_ring = q_stages<M> * M * q_piece<T, G, M>;
+constexpr int Q_PITCH = 17;          // of a column's 16 sums
+template <class T, int G, int NT, int M> constexpr int q_smem = q_ring<T, G, M> > M * 8 * NT * Q_PITCH * 4 ? q_ring<T, G, M> : M * 8 * NT * Q_PITCH * 4;     // of a warp
+
+// T: type of the scales and of the result; O: of the operands; PARTS columns to a token; G groups of a record; NT tiles of eight columns; M matrices (2: gate).
+template <class T, class O, int PARTS, int G, int NT, int M>
+__global__ void __launch_bounds__(Q_THREADS, NT * M <= 2 ? 3 : 2) product4_kernel(const __grid_constant__ Product4Params p) {
+  constexpr int COLUMNS = 8 * NT, TOKENS = COLUMNS / PARTS, STAGES = q_stages<M>, PIECE = q_piece<T, G, M>, SCALE_UNITS = G * (int)sizeof(T);
+  static_assert(M * SCALE_UNITS <= 32, "a lane copies one unit of the scales");
+  extern __shared__ __align__(16) uint8_t smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const int per_block = Q_WARPS / p.split, slice = warp % p.split;
-  const int tile = blockIdx.x * per_block + warp / p.split;
+  const int slice = warp & (p.split - 1), tile = (blockIdx.x << p.log_block) + (warp >> p.log_split);
   const bool on = tile < p.tiles;
-  struct Record { uint4 w[M][2]; Scales<T, G> s[M][2]; };
-  Record next;
-  int expert = 0;
-  const uint8_t* q[M];
-  const T* scale[M];
-  const auto base = [&] {
-#pragma unroll
-    for (int m = 0; m < M; ++m) {
-      q[m] = p.q[m] + expert * p.q_stride + (int64_t)tile * p.kblocks * 1024 + lane * 16;
-      scale[m] = (const T*)p.scale[m] + expert * p.scale_stride + (int64_t)tile * p.kblocks * (16 * G) + g * G;
+  uint8_t* const ring = smem + warp * q_ring<T, G, M>;
+  const uint32_t to = smem_u32(ring);
+  int expert = 0, tokens = 0, slot = 0;
+  // What a list says, and weights, need not wait for the kernel before this one where that has waited for what has written them.
+  const auto place = [&] {
+    if (p.list) {
+      if ((int)blockIdx.y >= *p.n_list) return false;
+      const int4 e = *reinterpret_cast<const int4*>(p.list + blockIdx.y);
+      expert = e.x; slot = e.y; tokens = e.z;
+    } else {
+      tokens = min(p.tokens - (int)blockIdx.y * TOKENS, TOKENS);
     }
+    return true;
   };
-  const auto fetch = [&](int kb) {
+  // This lane's 16 bytes of the next record to ask for, of each matrix, and of the scales.
+  const uint8_t *from[M], *from_scale = nullptr;
+  const uint32_t to_lane = to + lane * 16, to_scale = to + (M == 2 && lane >= SCALE_UNITS ? PIECE : 0) + 1024 + lane % SCALE_UNITS * 16;
+  const int step = p.split * 1024, step_scale = p.split * 16 * SCALE_UNITS;
+  int left = 0;                      // records to ask for
+  const auto request = [&](int stage) {
+    if (left > 0) {
 #pragma unroll
-    for (int m = 0; m < M; ++m)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        next.w[m][h] = *reinterpret_cast<const uint4*>(q[m] + (int64_t)kb * 1024 + h * 512);
-        next.s[m][h] = load_scales<T, G>(scale[m] + kb * (16 * G) + h * 8 * G);
+      for (int m = 0; m < M; ++m) {
+        cp_async16(to_lane + stage * (M * PIECE) + m * PIECE, from[m]);
+        cp_async16(to_lane + stage * (M * PIECE) + m * PIECE + 512, from[m] + 512);
+        from[m] += step;
       }
+      if (lane < M * SCALE_UNITS) cp_async16(to_scale + stage * (M * PIECE), from_scale);
+      from_scale += step_scale;
+      --left;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  // (weights of one matrix that nothing before this kernel can still be writing need not wait)
-  const bool ahead = p.early && !p.list && on && slice < p.kblocks;
-  if (ahead) { base(); fetch(slice); }
+  const auto begin = [&] {
+    const int64_t record = (int64_t)tile * p.kblocks + slice;
+    left = on && slice < p.kblocks ? (p.kblocks - slice + p.split - 1) / p.split : 0;
+#pragma unroll
+    for (int m = 0; m < M; ++m) from[m] = p.q[m] + expert * p.q_stride + record * 1024 + lane * 16;
+    from_scale = (const uint8_t*)p.scale[M == 2 && lane >= SCALE_UNITS && lane < 2 * SCALE_UNITS ? 1 : 0] +
+                 (expert * p.scale_stride + record * (16 * G)) * (int64_t)sizeof(T) + lane % SCALE_UNITS * 16;
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) request(i);
+  };
+  bool some = true;
+  if (p.early) {
+    some = place();
+    if (some) begin();
+  }
   grid_dep_wait();
   grid_dep_launch();
-  int columns, slot = 0;
-  if (p.list) {
-    if ((int)blockIdx.y >= *p.n_list) return;
-    const int4 e = *reinterpret_cast<const int4*>(p.list + blockIdx.y);
-    expert = e.x; slot = e.y; columns = e.z;
-  } else {
-    const int64_t left = p.tokens - (int64_t)blockIdx.y * COLUMNS;
-    columns = (int)(left < COLUMNS ? left : COLUMNS);
+  if (!p.early) {
+    some = place();
+    if (some) begin();
   }
-  const auto row_of = [&](int c) -> int64_t { return p.list ? p.pair_of[slot + c] : (int64_t)blockIdx.y * COLUMNS + c; };
-  const X* row[NT];
+  if (!some) return;
+  const auto row_of = [&](int c) { return p.list ? p.pair_of[slot + c] : (int)blockIdx.y * TOKENS + c; };
+  const int columns = tokens * PARTS;            // column PARTS i + j: part j of token i
+  const O* row[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     row[n] = nullptr;
-    if (8 * n + g < columns) {
-      const int64_t r = row_of(8 * n + g);
-      row[n] = (const X*)p.x + (p.token_rows ? r / p.k : r) * p.ldx;
+    const int c = 8 * n + g;
+    if (c < columns) {
+      int r = row_of(c / PARTS);
+      if (p.token_rows && p.k > 1) r = (int)((unsigned)r / (unsigned)p.k);
+      row[n] = (const O*)p.x + r * p.ldx + c % PARTS * p.part_stride;
     }
   }
   float acc[M][NT][4] = {};
-  if (on && slice < p.kblocks) {
-    if (!ahead) { base(); fetch(slice); }
-#pragma unroll 1
-    for (int kb = slice; kb < p.kblocks; kb += p.split) {
-      const Record r = next;
-      if (kb + p.split < p.kblocks) fetch(kb + p.split);
-      float part[M][NT][4];
+  if (on) {
+    int stage = 0;
+    // one record: its sums, group by group
+    const auto record = [&](int kb, auto whole) {
+      constexpr bool WHOLE = decltype(whole)::value != 0;
+      uint4 x[NT == 1 ? 4 : 1][NT];
+      const int c0 = kb * 128 + t * 8;
+      if constexpr (NT == 1) {       // (on their way while the record is)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) x[b][0] = load_eight<WHOLE>(row[0], c0 + b * 32, p.cols);
+      }
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+      __syncwarp();
+      request(stage == 0 ? STAGES - 1 : stage - 1);
+      const uint8_t* const at = ring + stage * (M * PIECE);
+      uint4 w[M][2];
+#pragma unroll
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[m][h] = *reinterpret_cast<const uint4*>(at + m * PIECE + h * 512 + lane * 16);
+      // (two chains of products side by side where a group is long enough and there is room)
+      constexpr int CHAINS = NT == 1 && G == 1 ? 2 : 1;
+      float part[CHAINS][M][NT][4];
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        if (b % (4 / G) == 0) {
+        if constexpr (NT > 1) {
 #pragma unroll
-          for (int m = 0; m < M; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) part[m][n][i] = 0.f;
+          for (int n = 0; n < NT; ++n) x[0][n] = load_eight<WHOLE>(row[n], c0 + b * 32, p.cols);
         }
+        const bool more = b % (4 / G) >= CHAINS;
         uint32_t a[M][2][4];
 #pragma unroll
         for (int m = 0; m < M; ++m)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t w = b == 0 ? r.w[m][h].x : b == 1 ? r.w[m][h].y : b == 2 ? r.w[m][h].z : r.w[m][h].w;
+            const uint32_t word = b == 0 ? w[m][h].x : b == 1 ? w[m][h].y : b == 2 ? w[m][h].z : w[m][h].w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[m][h][i] = quarter_pair<O>(w, i);
+            for (int i = 0; i < 4; ++i) a[m][h][i] = quarter_pair<O>(word, i);
           }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const Eight<PARTS> x = load_eight<X, PARTS>(row[n], kb * 128 + b * 32 + t * 8, p.cols, p.vec);
+          if (NT > 1 && 8 * n >= columns) break;
+          const uint4 y = x[NT == 1 ? b : 0][n];
 #pragma unroll
-          for (int m = 0; m < M; ++m)
-#pragma unroll
-            for (int part_x = PARTS - 1; part_x >= 0; --part_x) {
-              mma16816<O>(part[m][n], a[m][0][0], a[m][1][0], a[m][0][1], a[m][1][1], x.w[part_x][0], x.w[part_x][1]);
-              mma16816<O>(part[m][n], a[m][0][2], a[m][1][2], a[m][0][3], a[m][1][3], x.w[part_x][2], x.w[part_x][3]);
-            }
+          for (int m = 0; m < M; ++m) {
+            float (&sum)[4] = part[b % CHAINS][m][n];
+            mma16816<O>(sum, a[m][0][0], a[m][1][0], a[m][0][1], a[m][1][1], y.x, y.y, more);
+            mma16816<O>(sum, a[m][0][2], a[m][1][2], a[m][0][3], a[m][1][3], y.z, y.w, true);
+          }
         }
         if (b % (4 / G) == 4 / G - 1) {
 #pragma unroll
           for (int m = 0; m < M; ++m) {
-            const float low = to_f(r.s[m][0].s[b * G / 4]), high = to_f(r.s[m][1].s[b * G / 4]);
+            const T* const scale = reinterpret_cast<const T*>(at + m * PIECE + 1024) + g * G + b * G / 4;
+            const float low = to_f(scale[0]), high = to_f(scale[8 * G]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              acc[m][n][0] = fmaf(low, part[m][n][0], acc[m][n][0]); acc[m][n][1] = fmaf(low, part[m][n][1], acc[m][n][1]);
-              acc[m][n][2] = fmaf(high, part[m][n][2], acc[m][n][2]); acc[m][n][3] = fmaf(high, part[m][n][3], acc[m][n][3]);
+              if (NT > 1 && 8 * n >= columns) break;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float v = CHAINS == 2 ? part[0][m][n][i] + part[CHAINS - 1][m][n][i] : part[0][m][n][i];
+                acc[m][n][i] = fmaf(i < 2 ? low : high, v, acc[m][n][i]);
+              }
             }
           }
         }
       }
-    }
+      if (++stage == STAGES) stage = 0;
+    };
+    const int whole = p.vec ? p.cols / 128 : 0;            // records of whole columns that can be loaded as 16 bytes
+    int kb = slice;
+#pragma unroll 1
+    for (; kb < whole; kb += p.split) record(kb, ActIs<1>{});
+#pragma unroll 1
+    for (; kb < p.kblocks; kb += p.split) record(kb, ActIs<0>{});
   }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();                   // (the rings are free)
+  float* const sums = reinterpret_cast<float*>(smem);            // [warp][M][COLUMNS][Q_PITCH]
 #pragma unroll
   for (int m = 0; m < M; ++m)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sums[warp][m][8 * n + 2 * t + (i & 1)][g + 8 * (i >> 1)] = acc[m][n][i];
+      for (int i = 0; i < 4; ++i) sums[((warp * M + m) * COLUMNS + 8 * n + 2 * t + (i & 1)) * Q_PITCH + g + 8 * (i >> 1)] = acc[m][n][i];
   __syncthreads();
   // 16 rows of a tile to neighbouring threads
-  for (int i = threadIdx.x; i < per_block * 16 * columns; i += Q_THREADS) {
-    const int r = i & 15, in = (i >> 4) % per_block, c = (i >> 4) / per_block;
-    const int at = (blockIdx.x * per_block + in) * 16 + r;
+  for (int i = threadIdx.x; i < tokens << (4 + p.log_block); i += blockDim.x) {
+    const int r = i & 15, in = (i >> 4) & ((1 << p.log_block) - 1), c = i >> (4 + p.log_block);
+    const int at = ((blockIdx.x << p.log_block) + in) * 16 + r;
     if (at >= p.rows) continue;
     float s[M];
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      s[m] = sums[in * p.split][m][c][r];
-      for (int w = 1; w < p.split; ++w) s[m] += sums[in * p.split + w][m][c][r];
+      s[m] = 0.f;
+      for (int w = 0; w < p.split; ++w)
+#pragma unroll
+        for (int j = PARTS - 1; j >= 0; --j) s[m] += sums[((((in << p.log_split) + w) * M + m) * COLUMNS + c * PARTS + j) * Q_PITCH + r];
     }
-    const int64_t to = row_of(c) * p.ldd + at;
+    const int64_t d = row_of(c) * p.ldd + at;
     if constexpr (M == 2) {
+      // the parts that the second product takes
+      constexpr int OUT = sizeof(T) == 4 ? 3 : 2;
       with_activation(p.act, [&](auto act) {
         float h, unused;
         activation<decltype(act)::value, sizeof(T) == 2>(s[0], h, unused);
-        ((float*)p.d)[to] = h * s[1];
+        __nv_bfloat16 o[OUT];
+        split_parts<OUT>(h * s[1], o);
+#pragma unroll
+        for (int j = 0; j < OUT; ++j) ((__nv_bfloat16*)p.d)[d + j * p.part_stride_d] = o[j];
       });
     } else {
-      if (p.d32) ((float*)p.d)[to] = s[0];
-      else ((T*)p.d)[to] = from_f<T>(s[0]);
+      if (p.d32) ((float*)p.d)[d] = s[0];
+      else ((T*)p.d)[d] = from_f<T>(s[0]);
     }
   }
 }
 
-template <class T, class X, int PARTS, int G, int NT, int M>
+template <class T, class O, int PARTS, int G, int NT, int M>
 cudaError_t launch_product4_as(const Product4& a, cudaStream_t st) {
   Product4Params p = {};
   p.rows = a.rows; p.cols = a.cols; p.act = a.act; p.kblocks = (int)w4_blocks(a.cols); p.tiles = (int)w4_tiles(a.rows);
-  p.early = a.early; p.k = a.k; p.token_rows = a.token_rows; p.tokens = a.tokens; p.x = a.x; p.ldx = a.ldx; p.d = a.d; p.ldd = a.ldd; p.d32 = a.d32;
-  p.vec = ((uintptr_t)a.x & 15) == 0 && a.ldx * (int64_t)sizeof(X) % 16 == 0;
+  p.early = a.early; p.k = a.k; p.token_rows = a.token_rows; p.tokens = (int)a.tokens; p.x = a.x; p.ldx = a.ldx; p.part_stride = a.part_stride;
+  p.d = a.d; p.ldd = a.ldd; p.d32 = a.d32; p.part_stride_d = a.part_stride_d;
+  p.vec = ((uintptr_t)a.x & 15) == 0 && a.ldx % 8 == 0 && a.part_stride % 8 == 0;
   for (int m = 0; m < M; ++m) { p.q[m] = a.w[m].q; p.scale[m] = a.w[m].scale; }
   p.q_stride = w4_bytes(a.rows, a.cols); p.scale_stride = w4_scales(a.rows, a.cols, a.group);
-  int64_t columns;
+  int64_t columns, busy;             // tiles of columns, and how many of them there are about
   if (a.plan) {
     p.list = a.plan->tiles; p.n_list = a.plan->n_tiles; p.pair_of = a.plan->pair_of;
-    columns = plan_tiles(a.plan->pairs, a.plan->experts, 8 * NT);
+    columns = plan_tiles(a.plan->pairs, a.plan->experts, a.tile_tokens);
+    busy = a.plan->pairs < a.plan->experts ? a.plan->pairs : (int64_t)a.plan->experts;
   } else {
-    columns = (a.tokens + 8 * NT - 1) / (8 * NT);
+    busy = columns = (a.tokens + 8 * NT / PARTS - 1) / (8 * NT / PARTS);
   }
-  // Warps to a tile: two records each at least, eight warps at most.
-  p.split = 1;
-  while (p.split < Q_WARPS && p.split * 4 <= p.kblocks) p.split *= 2;
-  const int per_block = Q_WARPS / p.split;
+  // Warps to a tile: as many as the SMs have room for at once, 24 each (a few blocks too many would take as long again), of two records each at least.
+  int log_split = 0;
+  while ((2 << log_split) <= Q_WARPS && (4 << log_split) <= p.kblocks && p.tiles * busy * (2 << log_split) <= 24LL * num_sms()) ++log_split;
+  p.split = 1 << log_split;
+  const int warps = p.split > 4 ? p.split : 4, per_block = warps / p.split;
+  p.log_split = log_split; p.log_block = log_split >= 2 ? 0 : 2 - log_split;
   if (columns > 65535) return cudaErrorInvalidValue;
-  return launch_pdl_grid(product4_kernel<T, X, PARTS, G, NT, M>, dim3((unsigned)((p.tiles + per_block - 1) / per_block), (unsigned)columns), Q_THREADS, 0, st, p);
+  auto* const kernel = product4_kernel<T, O, PARTS, G, NT, M>;
+  constexpr int SMEM = q_smem<T, G, NT, M>;
+  static std::atomic<signed char> ready[64];
+  if (!once_per_device(ready, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Q_WARPS * SMEM) == cudaSuccess; })) return cudaErrorInvalidDevice;
+  return launch_pdl_grid(kernel, dim3((unsigned)((p.tiles + per_block - 1) / per_block), (unsigned)columns), 32 * warps, warps * SMEM, st, p);
 }
-template <class T, class X, int PARTS, int G>
-cudaError_t launch_product4_g(const Product4& a, cudaStream_t st) {
-  if constexpr (sizeof(X) == sizeof(T)) {
-    if (a.gate) return a.columns == 8 ? launch_product4_as<T, X, PARTS, G, 1, 2>(a, st) : launch_product4_as<T, X, PARTS, G, 4, 2>(a, st);
-  }
-  return a.columns == 8 ? launch_product4_as<T, X, PARTS, G, 1, 1>(a, st) : launch_product4_as<T, X, PARTS, G, 4, 1>(a, st);
+template <class T, class O, int PARTS, int G, int M>
+cudaError_t launch_product4_nt(const Product4& a, cudaStream_t st) {
+  // columns of a tile: those of the plan's tiles, or of all tokens up to 32
+  const int64_t columns = (a.plan ? (int64_t)a.tile_tokens : a.tokens) * PARTS;
+  if (columns <= 8 / PARTS * PARTS) return launch_product4_as<T, O, PARTS, G, 1, M>(a, st);
+  return columns <= 16 / PARTS * PARTS ? launch_product4_as<T, O, PARTS, G, 2, M>(a, st) : launch_product4_as<T, O, PARTS, G, 4, M>(a, st);
 }
-template <class T, class X, int PARTS>
-cudaError_t launch_product4_x(const Product4& a, cudaStream_t st) {
-  return a.group == 32 ? launch_product4_g<T, X, PARTS, 4>(a, st) : a.group == 64 ? launch_product4_g<T, X, PARTS, 2>(a, st) : launch_product4_g<T, X, PARTS, 1>(a, st);
+template <class T, class O, int PARTS, int M>
+cudaError_t launch_product4_of(const Product4& a, cudaStream_t st) {
+  return a.group == 32 ? launch_product4_nt<T, O, PARTS, 4, M>(a, st) : a.group == 64 ? launch_product4_nt<T, O, PARTS, 2, M>(a, st) : launch_product4_nt<T, O, PARTS, 1, M>(a, st);
 }
 
 }  // namespace

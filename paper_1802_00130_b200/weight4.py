@@ -138,8 +138,13 @@ def matvec4(x, w, stream=None):
         return out
     px, ldx = _matrix(x, "x", tokens, cols, dtype, dev)
     y = x.new_empty(tokens, w.rows)
+    ws, n = 0, 0
+    if dtype is torch.float32:
+        n = lib().gn_matvec4_workspace(0, tokens, cols)
+        room = x.new_empty(max(n, 16) // 4)
+        ws = room.data_ptr()
     err = _err()
-    status = lib().gn_matvec4(_TYPES[dtype], tokens, w.rows, cols, w.group, px, ldx, pq, ps, y.data_ptr(), w.rows, _raw_stream(dev), err, 200)
+    status = lib().gn_matvec4(_TYPES[dtype], tokens, w.rows, cols, w.group, px, ldx, pq, ps, y.data_ptr(), w.rows, ws, n, _raw_stream(dev), err, 200)
     if status:
         _checked(status, err)
     return y

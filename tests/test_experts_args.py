@@ -136,9 +136,10 @@ def test_layouts_refuse_misaligned_elements():
 
 
 @pytest.mark.parametrize("change,word", [c for c in SIZES4 if "experts" not in c[0]] + [
-    (dict(tokens=-1), "tokens"), (dict(tokens=1 << 20), "tokens"), (dict(x=None), "x:"), (dict(ldx=39), "x:"), (dict(q=C.c_void_p(8)), "packed"), (dict(y=None), "y:"), (dict(ldy=19), "y:")])
+    (dict(tokens=-1), "tokens"), (dict(tokens=1 << 20), "tokens"), (dict(x=None), "x:"), (dict(ldx=39), "x:"), (dict(q=C.c_void_p(8)), "packed"), (dict(y=None), "y:"), (dict(ldy=19), "y:"),
+    (dict(type=0, ws=None), "workspace"), (dict(type=0, ws=C.c_void_p(8)), "workspace"), (dict(type=0, n=719), "workspace")])
 def test_matvec4_refuses(change, word):
-    a = dict(type=1, tokens=3, rows=20, cols=40, group=32, x=P, ldx=40, q=P, scale=P, y=P, ldy=20, st=None)
+    a = dict(type=1, tokens=3, rows=20, cols=40, group=32, x=P, ldx=40, q=P, scale=P, y=P, ldy=20, ws=P, n=1 << 30, st=None)
     a.update(change)
     assert word in refused(gn.lib().gn_matvec4, *a.values())
 

@@ -32,7 +32,7 @@ struct RouteParams {
 // Keys that order as the values do; NaN below every number, and 0 is nobody.
 __device__ __forceinline__ uint32_t key_of(float v) {
   const uint32_t u = __float_as_uint(v + 0.f);             // (-0 is 0)
-  return v != v ? 1u : u >> 31 ? ~u : u | 0x80000000u;
+  return v != v ? 1u : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ uint64_t key_of(double v) {
   const uint64_t u = (uint64_t)__double_as_longlong(v + 0.0);
@@ -101,58 +101,101 @@ __device__ __forceinline__ float warp_max_nan(float x) {
 }
 __device__ __forceinline__ float exp_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f)); return y; }
 
+// Scores in FP64: of a row whose largest logit (0 if that is -inf) and sum of exponentials are known.
+struct Exact { float top; double sum; };
+template <class T>
+__device__ __forceinline__ Exact exact_of(const RouteParams& p, const T* row, int lane) {
+  Exact x{-__int_as_float(0x7f800000), 0.0};
+  if (!p.softmax) return x;
+  for (int e = lane; e < p.experts; e += 32) x.top = max_nan(x.top, to_f(row[e]));
+  x.top = warp_max_nan(x.top);
+  if (x.top == -__int_as_float(0x7f800000)) x.top = 0.f;
+#pragma unroll 4
+  for (int e = lane; e < p.experts; e += 32) x.sum += exp((double)to_f(row[e]) - (double)x.top);
+  x.sum = warp_sum(x.sum);
+  if (x.sum == 0.0) x.sum = 1.0;
+  return x;
+}
+__device__ __forceinline__ double exact_score(const RouteParams& p, const Exact& x, float l) {
+  return p.softmax ? exp((double)l - (double)x.top) / x.sum : 1.0 / (1.0 + exp(-(double)l));
+}
+
+// The order in FP64 of n experts (one to a lane, bias included): lane j < k returns the j-th.
+template <class T>
+__device__ __noinline__ int order_exactly(const RouteParams& p, const T* row, const float* bias, int index, int n, int lane) {
+  const Exact x = exact_of(p, row, lane);
+  const bool on = lane < n;
+  const uint64_t key = on ? key_of(exact_score(p, x, to_f(row[index])) + (double)bias[index]) : 0u;
+  int rank = 0, mine = -1;
+  for (int i = 0; i < n; ++i) {
+    const uint64_t k = __shfl_sync(0xffffffffu, key, i);
+    const int e = __shfl_sync(0xffffffffu, index, i);
+    rank += k > key || (k == key && e < index);
+  }
+  for (int i = 0; i < n; ++i) {
+    const int r = __shfl_sync(0xffffffffu, rank, i), e = __shfl_sync(0xffffffffu, index, i);
+    if (r == lane) mine = e;
+  }
+  return mine;
+}
+
 // The k experts of a row in FP64, by a warp, from and to shared memory (an element for each expert): lane j < k returns the j-th.  Rare: few registers, no speed.
 template <class T>
 __device__ __noinline__ int choose_exactly(const RouteParams& p, const T* row, const float* bias, double* order, int lane) {
   const double LOW = -(double)__int_as_float(0x7f800000);
-  float top = (float)LOW;
-  double sum = 0.0;
-  if (p.softmax) {
-    for (int e = lane; e < p.experts; e += 32) top = max_nan(top, to_f(row[e]));
-    top = warp_max_nan(top);
-    if (top == (float)LOW) top = 0.f;
-    for (int e = lane; e < p.experts; e += 32) sum += exp((double)to_f(row[e]) - (double)top);
-    sum = warp_sum(sum);
-    if (sum == 0.0) sum = 1.0;
-  }
-  const auto score = [&](int e) {
-    const double l = (double)to_f(row[e]);
-    return p.softmax ? exp(l - (double)top) / sum : 1.0 / (1.0 + exp(-l));
-  };
+  const Exact exact = exact_of(p, row, lane);
+  const auto score = [&](int e) { return exact_score(p, exact, to_f(row[e])); };
+#pragma unroll 4
   for (int e = lane; e < p.experts; e += 32) order[e] = bias ? score(e) + (double)bias[e] : (double)to_f(row[e]);
   __syncwarp();
-  uint32_t kept = 0xffffffffu;
+  const double TAKEN = __longlong_as_double(0x7fffffffffffffffll);       // (a NaN of its own: nobody any more)
   if (p.groups > 1) {
+    // Lanes in turn take a group's elements, two groups' halves at a time where there are lanes for it: here a power of two of lanes to a group.
+    int lanes = 1;
+    while (2 * lanes * p.groups <= 32) lanes *= 2;
+    const int group = lane / lanes, sub = lane % lanes;
     double first = LOW, second = LOW;
     int i1 = -1, i2 = -1;
-    bool any = false;                // an element that is no NaN
-    if (lane < p.groups)
-      for (int e = lane * p.each; e < (lane + 1) * p.each; ++e) {
-        const double x = order[e];
-        if (x > first || (i1 < 0 && x == x)) { second = first; i2 = i1; first = x; i1 = e; } else if (x > second || (i2 < 0 && x == x)) { second = x; i2 = e; }
-        any |= x == x;
+    const auto better = [](double x, int i, double y, int j) { return j < 0 || (i >= 0 && (x > y || (x == y && i < j))); };
+    const auto merge = [&](double x, int i) {
+      if (i < 0) return;
+      if (better(x, i, first, i1)) { second = first; i2 = i1; first = x; i1 = i; } else if (better(x, i, second, i2)) { second = x; i2 = i; }
+    };
+    if (group < p.groups)
+#pragma unroll 4
+      for (int i = sub; i < p.each; i += lanes) {
+        const double x = order[group * p.each + i];
+        merge(x, x == x ? group * p.each + i : -1);
       }
+    for (int o = 1; o < lanes; o <<= 1) {
+      const double f = __shfl_xor_sync(0xffffffffu, first, o), q = __shfl_xor_sync(0xffffffffu, second, o);
+      const int i = __shfl_xor_sync(0xffffffffu, i1, o), j = __shfl_xor_sync(0xffffffffu, i2, o);
+      merge(f, i); merge(q, j);
+    }
     double value = first;
     // Scores and biases by themselves: two groups that have the same ones in other pairs are equal, which roundings of four different values might not show.
     if (p.best == 2 && p.each > 1) value = i2 < 0 ? LOW : (score(i1) + score(i2)) + (bias ? (double)bias[i1] + (double)bias[i2] : 0.0);
-    uint64_t g = lane < p.groups ? (any ? key_of(value) : 1u) : 0u;
-    kept = 0;
+    uint64_t g = group < p.groups && sub == 0 ? key_of(value) : 0u;
+    uint32_t kept = 0;
     for (int j = 0; j < p.top; ++j) {
       const uint64_t m = warp_max(g);
       const int from = __ffs(__ballot_sync(0xffffffffu, g == m)) - 1;
-      kept |= 1u << from;
+      kept |= 1u << (from / lanes);
       if (lane == from) g = 0;
     }
+    for (int e = lane; e < p.experts; e += 32)
+      if (!(kept >> (e / p.each) & 1)) order[e] = TAKEN;
+    __syncwarp();
   }
   uint64_t best;
   int at, mine = -1;
   const auto look = [&] {
     best = 0; at = -1;
-#pragma unroll 1
+#pragma unroll 4
     for (int e = lane; e < p.experts; e += 32) {
-      if (p.groups > 1 && !(kept >> (e / p.each) & 1)) continue;
-      const uint64_t k = key_of(order[e]);
-      if (k > best && !(__double_as_longlong(order[e]) == 0x7fffffffffffffffll)) { best = k; at = e; }
+      const double x = order[e];
+      const uint64_t k = __double_as_longlong(x) == __double_as_longlong(TAKEN) ? 0u : key_of(x);
+      if (k > best) { best = k; at = e; }
     }
   };
   look();
@@ -161,7 +204,7 @@ __device__ __noinline__ int choose_exactly(const RouteParams& p, const T* row, c
     const uint64_t m = warp_max(best);
     const int e = (int)__reduce_min_sync(0xffffffffu, best == m ? (unsigned)at : 0xffffffffu);
     if (lane == j) mine = e;
-    if (best == m && at == e) { order[e] = __longlong_as_double(0x7fffffffffffffffll); look(); }      // (a NaN of its own: taken)
+    if (best == m && at == e) { order[e] = TAKEN; look(); }
   }
   __syncwarp();
   return mine;
@@ -205,27 +248,23 @@ __device__ __forceinline__ int choose(const RouteParams& p, const T* row, const 
     if (p.groups > 1) {
       const bool one = p.best == 1 || p.each == 1, plain = one && by_logit;
       float first = LOW, second = LOW;
-      bool any = false;              // an element that is no NaN
-      const auto take = [&](float x) { second = fmaxf(second, fminf(first, x)); first = fmaxf(first, x); any |= x == x; };
-      uint32_t g, kept = 0;
+      const auto take = [&](float x) {
+        x = x == x ? x : LOW;        // (a NaN is nobody's best)
+        second = fmaxf(second, fminf(first, x)); first = fmaxf(first, x);
+      };
+      uint32_t kept = 0;
       int lanes = 1;                 // to a group
+      bool mine;                     // a group is this lane's
       if (p.lanes) {                 // a power of two of whole lanes
         lanes = p.lanes;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const float x = plain ? l[v] : s[v];
-          if (x == x) take(x);
-        }
-        any = false;
-#pragma unroll
-        for (int v = 0; v < V; ++v) any |= (plain ? l[v] : s[v]) == (plain ? l[v] : s[v]);
+        for (int v = 0; v < V; ++v) take(plain ? l[v] : s[v]);
         for (int o = 1; o < lanes; o <<= 1) {
           const float f = __shfl_xor_sync(0xffffffffu, first, o), q = __shfl_xor_sync(0xffffffffu, second, o);
           second = fmaxf(fminf(first, f), fmaxf(second, q));
           first = fmaxf(first, f);
-          any |= __shfl_xor_sync(0xffffffffu, (int)any, o) != 0;
         }
-        g = lane * V < p.experts ? 2u : 0u;
+        mine = lane * V < p.experts;
       } else {                       // a lane each; rows of the stage are an odd number of elements apart
         const int pitch = p.each | 1;
 #pragma unroll
@@ -234,16 +273,13 @@ __device__ __forceinline__ int choose(const RouteParams& p, const T* row, const 
           if (x < p.experts) stage[x / p.each * pitch + x % p.each] = plain ? l[v] : s[v];
         }
         __syncwarp();
-        if (lane < p.groups)
-          for (int i = 0; i < p.each; ++i) {
-            const float x = stage[lane * pitch + i];
-            if (x == x) take(x);
-          }
+        mine = lane < p.groups;
+        if (mine)
+          for (int i = 0; i < p.each; ++i) take(stage[lane * pitch + i]);
         __syncwarp();
-        g = lane < p.groups ? 2u : 0u;
       }
       const float value = one ? first : first + second;
-      if (g) g = any ? key_of(value) : 1u;
+      uint32_t g = mine ? key_of(value) : 0u;
       float last = 0.f;
       const uint32_t span = lanes == 32 ? 0xffffffffu : (1u << lanes) - 1;
       for (int j = 0; j <= p.top && j < p.groups; ++j) {
@@ -280,31 +316,45 @@ __device__ __forceinline__ int choose(const RouteParams& p, const T* row, const 
       if (key[v] > best) { best = key[v]; at = v; }
   };
   look();
-  // ORDERED, and without a bias, the keys are the values; else the first one behind the last that is not its equal is looked at too.
+  // ORDERED, and without a bias, the keys are the values.  Else those behind the last are looked at until one is clearly less than it; if two neighbours are
+  // too near to tell, and not equal in any arithmetic, all that may be among the first k are put in order in FP64.
   const bool sure = ORDERED || !bias;
-  int mine = -1, last_index = 0;
-  float last = __int_as_float(0x7fffffff);
-  for (int j = 0; j < p.k || !sure; ++j) {
-    const uint32_t m = warp_max(best);
-    if (m == 0) break;                                     // (nobody is left)
-    const int from = __ffs(__ballot_sync(0xffffffffu, best == m)) - 1;
+  int mine = -1;
+  uint32_t my_key = 0, m = 0;
+  int from = 0;
+  const auto next = [&] {            // the best that is left: its key (0: nobody) and its lane
+    m = warp_max(best);
+    from = __ffs(__ballot_sync(0xffffffffu, best == m)) - 1;
+  };
+  const auto take = [&](int n) {
     const int index = __shfl_sync(0xffffffffu, lane * V + at, from);
-    if (!sure) {
-      const float value = value_of(m);
-      bool same = false;
-      if (last - value <= E * (2.f * off + fabsf(last) + fabsf(value))) {
-        same = to_f(row[index]) == to_f(row[last_index]) && bias[index] == bias[last_index];
-        if (!same) { certain = false; break; }
-      }
-      if (j >= p.k && !same) break;
-      last = value; last_index = index;
-    }
-    if (lane == j && j < p.k) mine = index;
+    if (lane == n) { mine = index; my_key = m; }
     if (lane == from) {
 #pragma unroll
       for (int v = 0; v < V; ++v)
         if (at == v) key[v] = 0;
       look();
+    }
+  };
+#pragma unroll 1
+  for (int n = 0; n < p.k; ++n) { next(); take(n); }
+  if constexpr (!ORDERED) {
+    if (sure) return mine;
+    const float kth = value_of(m);
+    int n = p.k;
+#pragma unroll 1
+    for (;; ++n) {
+      next();
+      if (m == 0 || !(kth - value_of(m) <= E * (2.f * off + fabsf(kth) + fabsf(value_of(m))))) break;
+      if (n == 32) { certain = false; return mine; }       // (too many for a lane each)
+      take(n);
+    }
+    const float value = value_of(my_key), after = __shfl_down_sync(0xffffffffu, value, 1);
+    const bool near = lane < n - 1 && value - after <= E * (2.f * off + fabsf(value) + fabsf(after));
+    if (__any_sync(0xffffffffu, near)) {
+      const int behind = __shfl_down_sync(0xffffffffu, mine, 1);
+      const bool differ = near && !(to_f(row[mine]) == to_f(row[behind]) && bias[mine] == bias[behind]);
+      if (__any_sync(0xffffffffu, differ)) mine = order_exactly<T>(p, row, bias, mine, n, lane);
     }
   }
   return mine;

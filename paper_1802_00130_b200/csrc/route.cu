@@ -361,7 +361,7 @@ __device__ __forceinline__ int choose(const RouteParams& p, const T* row, const 
 }
 
 template <class T, int V, bool ORDERED>
-__global__ void __launch_bounds__(32 * kRouteWarps) route_kernel(const __grid_constant__ RouteParams p) {
+__global__ void __launch_bounds__(32 * kRouteWarps, ORDERED ? 1 : V <= 8 ? 4 : 2) route_kernel(const __grid_constant__ RouteParams p) {
   extern __shared__ double stages[];                       // (an element for each expert and for each group)
   grid_dep_wait();
   grid_dep_launch();

@@ -31,18 +31,18 @@ ExpertPlan plan_at(int* mem, int64_t pairs, int experts, int height);           
 // The plan of an index table, with tiles of `height` slots (where `padded` is looked at, a multiple of kSlots).
 cudaError_t launch_plan(const int* index, const ExpertPlan& plan, int height, cudaStream_t st);
 
-// Rows of tokens to their pairs' slots: dst[slot of (t, j)] = src[t], empty slots zero.  `bytes` of an element (2 or 4); rows of dst are 16-byte aligned.
+// Rows of tokens to their pairs' slots: dst[slot of (t, j)] = src[t]; zero: empty slots are written too, zero.  `bytes` of an element (2 or 4); rows of dst are 16-byte aligned.
 struct RowCopy { const void* src; int64_t ld; void* dst; int64_t ld_dst; };
-cudaError_t launch_to_slots(const RowCopy* list, int n, int64_t tokens, int k, int cols, int bytes, const int* index, const ExpertPlan& plan, cudaStream_t st);
+cudaError_t launch_to_slots(const RowCopy* list, int n, int64_t tokens, int k, int cols, int bytes, bool zero, const ExpertPlan& plan, cudaStream_t st);
 
-// d[t] = sum over the choices j that are experts of weight[t k + j] (1 without weights) src[t k + j], src of type `from`, d of type `type`.  parts: with them,
+// d[t] = sum over the choices j that are experts of weight[t k + j] (1 without weights) src[t k + j], d of type `type` (NULL: not wanted).  parts: with them,
 // dweight[t k + j] = the sum of n_parts partial sums at parts[(slot of the pair) n_parts], in order; 0 for a choice that is no expert.
 struct Combine {
   int64_t tokens; int k, cols, experts; const int* index; const float* weight;
-  const void* src; int64_t ld; void* d; int64_t ld_d;
+  const float* src; int64_t ld; void* d; int64_t ld_d;
   const float* parts; int n_parts; const int* slot_of; float* dweight;
 };
-cudaError_t launch_combine(int type, int from, const Combine& c, cudaStream_t st);
+cudaError_t launch_combine(int type, const Combine& c, cudaStream_t st);
 
 // Copies of 16-bit matrices of every expert (or of one) with rows that TMA can address: [experts][rows][cols], rows `ld` and experts `stride` apart, to rows
 // ld_out apart without gaps between experts.
@@ -55,10 +55,10 @@ cudaError_t launch_pack_mats(const PackMats* list, int n, cudaStream_t st);
 struct Weights16 { const void* p = nullptr; int64_t ld = 0, stride = 0; };
 struct Grads16 { void* p = nullptr; int64_t ld = 0, stride = 0; };
 //   GROUP_GATE   slots: d = act(gate) * up with gate = x Wg^T, up = x Wu^T; pairs: gate, up (optional)
-//   GROUP_DOWN   pairs: d = h Wd^T
+//   GROUP_DOWN   pairs: rows = h Wd^T, FP32
 //   GROUP_GRAD   q = dy Wd; slots: d = weight act(gate) up, dgate = weight q up act'(gate), dup = weight q act(gate), from the pairs' gate and up;
 //                parts[slot][n_parts]: sums over columns of q act(gate) up
-//   GROUP_DX     pairs: d = dgate Wg + dup Wu
+//   GROUP_DX     pairs: rows = dgate Wg + dup Wu, FP32
 //   GROUP_WEIGHT experts: grads[i] = sum over the expert's slots of (left row)^T (right row)
 enum GroupKind { GROUP_GATE = 0, GROUP_DOWN = 1, GROUP_GRAD = 2, GROUP_DX = 3, GROUP_WEIGHT = 4 };
 struct GroupGemm {
@@ -67,6 +67,7 @@ struct GroupGemm {
   Mat16 A[2];                        // rows of slots
   Weights16 B[2];
   Out16 d, dgate, dup;
+  FfnOut rows;
   Mat16 gate, up; Out16 gate_out, up_out;
   const float* weight = nullptr; float* parts = nullptr;
   struct { int M = 0, N = 0; Mat16 left, right; Grads16 d; } grads[3];

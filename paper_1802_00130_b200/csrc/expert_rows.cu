@@ -132,10 +132,11 @@ int64_t plan_chunk(int64_t pairs) {
 constexpr int kCopies = 2;
 struct CopyParams {
   RowCopy c[kCopies]; int vec[kCopies];
-  int64_t tokens; int k, row_bytes, experts, units;
-  const int* index; ExpertPlan plan;
+  int64_t tokens; int k, row_bytes, zero, units;           // zero: experts whose empty slots are written
+  ExpertPlan plan;
 };
-// A warp takes 1 KB of a token's row at a time (two 16-byte units a lane) and writes it to the token's k slots; the warps behind the tokens' zero the experts' empty slots.
+// A warp takes 1 KB of a token's row at a time (two 16-byte units a lane) and writes it to the token's k slots; the warps behind the tokens' zero the experts' empty slots (where
+// they are terms of a sum).
 template <int BYTES>
 __global__ void __launch_bounds__(256) to_slots_kernel(const __grid_constant__ CopyParams p) {
   grid_dep_wait();
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(256) to_slots_kernel(const __grid_constant__ C
   const bool vec = p.vec[blockIdx.y] != 0;
   const int* const slot_of = dep(p.plan.slot_of);
   const int lane = threadIdx.x & 31;
-  const int64_t work = (p.tokens + p.experts) * p.units;
+  const int64_t work = (p.tokens + p.zero) * p.units;
   for (int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); w < work; w += (int64_t)gridDim.x * 8) {
     const int64_t t = w / p.units;
     const int unit = (int)(w - t * p.units), at = unit * 1024 + lane * 16;
@@ -191,34 +192,32 @@ __global__ void __launch_bounds__(256) to_slots_kernel(const __grid_constant__ C
 }
 
 // ---- pairs to tokens ----------------------------------------------------------------------------
-// A thread takes four columns of a token (rows of src start on 16 bytes and are whole units of four), all of its k rows' loads before the first addition.
-template <class T, class S>
+// A thread takes four columns of a token (rows of src start on 16 bytes and are whole units of four), four of its rows' loads before their additions.
+template <class T>
 __global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ Combine p, int units, int vec) {
   grid_dep_wait();
   grid_dep_launch();
-  const S* const src = (const S*)dep(p.src);
   const int* const index = dep(p.index);
   const float* const weight = dep(p.weight);
   const int64_t work = p.d ? p.tokens * units : 0;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < work; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = i / units;
+    const int64_t t = work <= 0x7fffffff ? (int64_t)((uint32_t)i / (uint32_t)units) : i / units;
     const int c = (int)(i - t * units) * 4;
+    const float* const src = dep(p.src) + t * p.k * p.ld + c;
+    const int* const mine = index + t * p.k;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int j = 0; j < p.k; ++j) {
-      const int64_t pair = t * p.k + j;
-      if ((unsigned)index[pair] >= (unsigned)p.experts) continue;
-      const float w = weight ? weight[pair] : 1.f;
-      if constexpr (sizeof(S) == 4) {
-        const float4 v = *reinterpret_cast<const float4*>(src + pair * p.ld + c);
-        s[0] = fmaf(w, v.x, s[0]); s[1] = fmaf(w, v.y, s[1]); s[2] = fmaf(w, v.z, s[2]); s[3] = fmaf(w, v.w, s[3]);
-      } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(src + pair * p.ld + c);
-        Pack<S> x;
-        x.w = make_uint4(v.x, v.y, 0u, 0u);
+    for (int j0 = 0; j0 < p.k; j0 += 4) {
+      float4 v[4];
+      float w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = fmaf(w, x.get(e), s[e]);
+      for (int j = 0; j < 4; ++j) {
+        const bool in = j0 + j < p.k && (unsigned)mine[min(j0 + j, p.k - 1)] < (unsigned)p.experts;
+        v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        w[j] = 0.f;
+        if (in) { v[j] = __ldcs(reinterpret_cast<const float4*>(src + (j0 + j) * p.ld)); w[j] = weight ? weight[t * p.k + j0 + j] : 1.f; }
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { s[0] = fmaf(w[j], v[j].x, s[0]); s[1] = fmaf(w[j], v[j].y, s[1]); s[2] = fmaf(w[j], v[j].z, s[2]); s[3] = fmaf(w[j], v[j].w, s[3]); }
     }
     T* const d = (T*)p.d + t * p.ld_d + c;
     if (vec && c + 4 <= p.cols) {
@@ -305,14 +304,14 @@ cudaError_t launch_plan(const int* index, const ExpertPlan& plan, int height, cu
   return e == cudaSuccess ? launch_pdl(plan_place_kernel<false>, blocks, kPlanThreads, smem, st, p) : e;
 }
 
-cudaError_t launch_to_slots(const RowCopy* list, int n, int64_t tokens, int k, int cols, int bytes, const int* index, const ExpertPlan& plan, cudaStream_t st) {
+cudaError_t launch_to_slots(const RowCopy* list, int n, int64_t tokens, int k, int cols, int bytes, bool zero, const ExpertPlan& plan, cudaStream_t st) {
   CopyParams p = {};
   for (int i = 0; i < n; ++i) {
     p.c[i] = list[i];
     p.vec[i] = ((uintptr_t)list[i].src & 15) == 0 && list[i].ld * bytes % 16 == 0;
   }
-  p.tokens = tokens; p.k = k; p.row_bytes = cols * bytes; p.experts = plan.experts; p.units = (p.row_bytes + 1023) / 1024; p.index = index; p.plan = plan;
-  const int64_t want = ((tokens + plan.experts) * p.units + 7) / 8, most = (int64_t)num_sms() * 8;
+  p.tokens = tokens; p.k = k; p.row_bytes = cols * bytes; p.zero = zero ? plan.experts : 0; p.units = (p.row_bytes + 1023) / 1024; p.plan = plan;
+  const int64_t want = ((tokens + p.zero) * p.units + 7) / 8, most = (int64_t)num_sms() * 8;
   const dim3 grid((unsigned)(want < most ? want : most), (unsigned)n);
   return bytes == 4 ? launch_pdl_grid(to_slots_kernel<4>, grid, 256, 0, st, p) : launch_pdl_grid(to_slots_kernel<2>, grid, 256, 0, st, p);
 }
@@ -330,17 +329,15 @@ cudaError_t launch_pack_mats(const PackMats* list, int n, cudaStream_t st) {
   return launch_pdl_grid(pack_mats_kernel, dim3((unsigned)(blocks < 1184 ? blocks : 1184), (unsigned)n), 256, 0, st, q);
 }
 
-template <class T, class S>
+template <class T>
 static cudaError_t combine_as(const Combine& c, int type, cudaStream_t st) {
   const int units = (c.cols + 3) / 4, each = 4 * type_bytes(type);
   const int vec = (uintptr_t)c.d % each == 0 && c.ld_d * type_bytes(type) % each == 0;
-  const int64_t want = (c.tokens * units + 255) / 256, most = (int64_t)num_sms() * 8;
-  return launch_pdl(combine_kernel<T, S>, (int)(want < most ? want : most), 256, 0, st, c, units, vec);
+  const int64_t want = (c.tokens * units + 255) / 256, most = (int64_t)num_sms() * 32;
+  return launch_pdl(combine_kernel<T>, (int)(want < most ? want : most), 256, 0, st, c, units, vec);
 }
-cudaError_t launch_combine(int type, int from, const Combine& c, cudaStream_t st) {
-  if (type == GN_F32) return combine_as<float, float>(c, type, st);
-  if (type == GN_BF16) return from == GN_F32 ? combine_as<__nv_bfloat16, float>(c, type, st) : combine_as<__nv_bfloat16, __nv_bfloat16>(c, type, st);
-  return from == GN_F32 ? combine_as<__half, float>(c, type, st) : combine_as<__half, __half>(c, type, st);
+cudaError_t launch_combine(int type, const Combine& c, cudaStream_t st) {
+  return type == GN_F32 ? combine_as<float>(c, type, st) : type == GN_BF16 ? combine_as<__nv_bfloat16>(c, type, st) : combine_as<__half>(c, type, st);
 }
 
 }  // namespace gn

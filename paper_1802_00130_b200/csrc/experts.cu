@@ -69,7 +69,7 @@ struct Half {
   PackMats packs[kPackMats]; int n_packs;
   Out16 h, dgate, dup;           // in slots
   float* parts;
-  Out16 out;                     // of the pairs
+  FfnOut out;                    // of the pairs
   int64_t slots;
 };
 Weights16 addressable(const gn_stack& m, int experts, int64_t rows, int cols, Workspace& ws, Half& w) {
@@ -109,7 +109,7 @@ int64_t lay_out_half(const gn_mixture& f, bool backward, char* base, Half& w) {
     w.dup = {ws.take(w.slots * lf * 2), lf};
     w.parts = (float*)ws.take(w.slots * group_parts(f.inner) * 4);
   }
-  if (!backward || f.dx.p) w.out = {ws.take(pairs * lc * 2), lc};
+  if (!backward || f.dx.p) w.out = {(float*)ws.take(pairs * lc * 4), lc};
   return ws.used;
 }
 
@@ -123,7 +123,7 @@ cudaError_t run_half(const gn_mixture& f, bool backward, const Half& w, int* err
   int n = 0;
   if (w.x.p) rows[n++] = {f.x.p, f.x.ld, const_cast<void*>(w.x.p), w.x.ld};
   if (backward) rows[n++] = {f.dy.p, f.dy.ld, const_cast<void*>(w.dy.p), w.dy.ld};
-  if (e == cudaSuccess) e = launch_to_slots(rows, n, f.tokens, f.k, f.cols, 2, f.index, w.plan, st);
+  if (e == cudaSuccess) e = launch_to_slots(rows, n, f.tokens, f.k, f.cols, 2, backward, w.plan, st);
   GroupGemm g;
   g.act = f.act; g.slots = w.slots;
   Combine c = {};
@@ -132,17 +132,17 @@ cudaError_t run_half(const gn_mixture& f, bool backward, const Half& w, int* err
     g.N = f.inner; g.K = f.cols; g.A[0] = w.x; g.B[0] = w.w_gate; g.B[1] = w.w_up; g.d = w.h; g.gate_out = {f.gate.p, f.gate.ld}; g.up_out = {f.up.p, f.up.ld};
     if (e == cudaSuccess) e = launch_group(GROUP_GATE, bf16, g, w.plan, err, st);
     GroupGemm q;
-    q.slots = w.slots; q.N = f.cols; q.K = f.inner; q.A[0] = in16(w.h); q.B[0] = w.w_down; q.d = w.out;
+    q.slots = w.slots; q.N = f.cols; q.K = f.inner; q.A[0] = in16(w.h); q.B[0] = w.w_down; q.rows = w.out;
     if (e == cudaSuccess) e = launch_group(GROUP_DOWN, bf16, q, w.plan, err, st);
     c.weight = f.weight; c.d = f.y.p; c.ld_d = f.y.ld;
-    return e == cudaSuccess ? launch_combine(f.type, f.type, c, st) : e;
+    return e == cudaSuccess ? launch_combine(f.type, c, st) : e;
   }
   g.N = f.inner; g.K = f.cols; g.A[0] = w.dy; g.B[0] = w.w_down; g.d = w.h; g.dgate = w.dgate; g.dup = w.dup; g.gate = w.gate; g.up = w.up;
   g.weight = f.weight; g.parts = w.parts;
   if (e == cudaSuccess) e = launch_group(GROUP_GRAD, bf16, g, w.plan, err, st);
   if (f.dx.p) {
     GroupGemm q;
-    q.slots = w.slots; q.N = f.cols; q.K = f.inner; q.A[0] = in16(w.dgate); q.A[1] = in16(w.dup); q.B[0] = w.w_gate; q.B[1] = w.w_up; q.d = w.out;
+    q.slots = w.slots; q.N = f.cols; q.K = f.inner; q.A[0] = in16(w.dgate); q.A[1] = in16(w.dup); q.B[0] = w.w_gate; q.B[1] = w.w_up; q.rows = w.out;
     if (e == cudaSuccess) e = launch_group(GROUP_DX, bf16, q, w.plan, err, st);
   }
   if (any_weights(f)) {
@@ -160,7 +160,7 @@ cudaError_t run_half(const gn_mixture& f, bool backward, const Half& w, int* err
   }
   c.d = f.dx.p; c.ld_d = f.dx.ld;
   if (f.dweight) { c.parts = w.parts; c.n_parts = group_parts(f.inner); c.slot_of = w.plan.slot_of; c.dweight = f.dweight; }
-  return e == cudaSuccess && (c.d || c.parts) ? launch_combine(f.type, f.type, c, st) : e;
+  return e == cudaSuccess && (c.d || c.parts) ? launch_combine(f.type, c, st) : e;
 }
 
 // ---- FP32 --------------------------------------------------------------------------------------
@@ -196,7 +196,7 @@ cudaError_t run_single(const gn_mixture& f, bool backward, const Single& w, cuda
     q.A[0] = of(w.h); q.B[0] = weights(f.w_down);
     if (e == cudaSuccess) e = launch_group_fma(GROUP_DOWN, q, w.plan, st);
     c.weight = f.weight; c.d = f.y.p; c.ld_d = f.y.ld;
-    return e == cudaSuccess ? launch_combine(GN_F32, GN_F32, c, st) : e;
+    return e == cudaSuccess ? launch_combine(GN_F32, c, st) : e;
   }
   g.A[0] = in(f.dy); g.B[0] = weights(f.w_down); g.dgate = w.dgate; g.dup = w.dup; g.gate = in(f.gate); g.up = in(f.up); g.weight = f.weight; g.parts = w.parts;
   if (e == cudaSuccess) e = launch_group_fma(GROUP_GRAD, g, w.plan, st);
@@ -219,7 +219,7 @@ cudaError_t run_single(const gn_mixture& f, bool backward, const Single& w, cuda
   }
   c.d = f.dx.p; c.ld_d = f.dx.ld;
   if (f.dweight) { c.parts = w.parts; c.n_parts = fma_parts(f.inner); c.slot_of = w.plan.slot_of; c.dweight = f.dweight; }
-  return e == cudaSuccess && (c.d || c.parts) ? launch_combine(GN_F32, GN_F32, c, st) : e;
+  return e == cudaSuccess && (c.d || c.parts) ? launch_combine(GN_F32, c, st) : e;
 }
 
 cudaError_t clear(const gn_stack& m, int experts, int64_t rows, int64_t cols, int type, cudaStream_t st) {

@@ -9,10 +9,11 @@
 // Weights are three-dimensional to TMA (expert, row, column), so that a box past the edge of an expert's matrix reads zeros, not its neighbour.
 // Warp roles as in gemm_pair16.cu: warp 0 TMA producer, warp 1 of the leader CTA issues the products, warps 2.. are the epilogue, beside the next tile's
 // products (two accumulators of 256 columns).  What belongs to the pairs of token and choice (gate, up, the products' results) is read and written
-// in the pairs' order, a row's place found by a shuffle from the lane that has the row.
+// in the pairs' order, a row's place found by a shuffle from the lane that has the row.  Results of GROUP_DOWN and GROUP_DX stay FP32 until a token's k rows are added.
 //
 // GROUP_GATE: the B tile is 128 rows of the gate's weights and the same 128 of the up projection's.  h, dgate and dup are rounded to the type: they are operands of the
-// next product; results of GROUP_DOWN and GROUP_DX are rounded before a token's k rows are added, which is one rounding more for y and dx, and half the bytes.
+// next product.  (Rows of GROUP_DOWN and GROUP_DX in the type would save 270 MB at 8192 tokens, 4 choices and 2048 columns, and make the error of y and dx 1.7 times
+// that of their own rounding instead of 1.4.)
 // GROUP_GRAD's sums for the gradient of the routing weights stay FP32: a thread has 64 columns of its row, their sums are added in order elsewhere.
 // Every wait is bounded; a role that gives up leaves a code in *err and the CTA drains.
 #include "expert_kernels.h"
@@ -34,10 +35,11 @@ constexpr int G_GRADS = 3;
 struct GroupGrad { int M, N, tiles_m, tiles_n, first, vec; Grads16 d; };
 struct GroupParams {
   int N, tiles_n, kb0, kb, act, pairs;
-  int vec, vec_gate, vec_up;
+  int vec_gate, vec_up;
   const ExpertTile* tiles; const int* n_tiles;
   const int *start, *count, *pair_of;
   Out16 d, dgate, dup, gate_out, up_out;
+  FfnOut rows;
   Mat16 gate, up;
   const float* weight; float* parts; int n_parts;
   GroupGrad grad[G_GRADS]; int n_grads, items;
@@ -186,7 +188,8 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
     }
   } else {
     // Epilogue: a quadrant's warps take its chunks of columns in turn.
-    constexpr int U = group_units<KIND>, COLS = 8 * U, STEP = EPI / 4;
+    constexpr bool ROWS = KIND == GROUP_DOWN || KIND == GROUP_DX;
+    constexpr int U = group_units<KIND>, COLS = ROWS ? 32 : 8 * U, STEP = EPI / 4;
     const int quad = warp & 3, first = (warp - 2) >> 2;
     const uint32_t stg = smem_u32(staging + (warp - 2) * (G_STG_ALL / EPI));
     const uint32_t acc_leader = map_to_cta(smem_u32(&acc_empty[0]), 0);
@@ -281,6 +284,13 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
             put_rows<U, 32>(o, stg, lane, p.d.p, p.d.ld, slot_row, nc, N, true);
             put_rows<U, 32>(gw, stg, lane, p.dgate.p, p.dgate.ld, slot_row, nc, N, true);
             put_rows<U, 32>(uw, stg, lane, p.dup.p, p.dup.ld, slot_row, nc, N, true);
+          } else if constexpr (KIND == GROUP_DOWN || KIND == GROUP_DX) {
+            // (32 columns of FP32 are 64 of 16 bits)
+            float v[32];
+            tmem_ld32(tq + (uint32_t)(c * COLS), v);
+#pragma unroll
+            for (int q = 0; q < 32; ++q) o[q] = __float_as_uint(v[q]);
+            put_rows<8, 32>(o, stg, lane, p.rows.p, 2 * p.rows.ld, pair_row, 2 * nc, 2 * N, true);
           } else {
 #pragma unroll
             for (int h = 0; h < COLS / 32; ++h) {
@@ -294,12 +304,8 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
 #pragma unroll
               for (int q = 0; q < 8; ++q) { o[16 * h + q] = pack2<T>(a[2 * q], a[2 * q + 1]); o[16 * h + 8 + q] = pack2<T>(b[2 * q], b[2 * q + 1]); }
             }
-            if constexpr (KIND == GROUP_WEIGHT) {
-              const GroupGrad& g = p.grad[w.grad];
-              put_chunk<U, 32>(o, stg, lane, reinterpret_cast<uint16_t*>(g.d.p) + w.expert * g.d.stride, g.d.ld, w.m0 + r0, g.M, nc, N, g.vec);
-            } else {
-              put_rows<U, 32>(o, stg, lane, p.d.p, p.d.ld, pair_row, nc, N, p.vec);
-            }
+            const GroupGrad& g = p.grad[w.grad];
+            put_chunk<U, 32>(o, stg, lane, reinterpret_cast<uint16_t*>(g.d.p) + w.expert * g.d.stride, g.d.ld, w.m0 + r0, g.M, nc, N, g.vec);
           }
         }
       };
@@ -366,7 +372,7 @@ cudaError_t launch_group_as(const GroupGemm& g, const ExpertPlan& plan, int* err
     p.N = g.N; p.tiles_n = (g.N + WIDTH - 1) / WIDTH;
     p.kb0 = (g.K + G_BK - 1) / G_BK; p.kb = KIND == GROUP_DX ? 2 * p.kb0 : p.kb0;
     p.d = g.d; p.dgate = g.dgate; p.dup = g.dup; p.gate_out = g.gate_out; p.up_out = g.up_out; p.gate = g.gate; p.up = g.up;
-    p.vec = vec16(p.d); p.vec_gate = vec16(p.gate_out); p.vec_up = vec16(p.up_out);
+    p.rows = g.rows; p.vec_gate = vec16(p.gate_out); p.vec_up = vec16(p.up_out);
     p.weight = g.weight; p.parts = g.parts; p.n_parts = group_parts(g.N);
     most = plan_tiles(plan.pairs, plan.experts, kGroupHeight) * p.tiles_n;
     if (most > 0x3fffffff) return cudaErrorInvalidValue;

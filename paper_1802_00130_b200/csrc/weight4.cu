@@ -185,7 +185,7 @@ cudaError_t run_ffn4(const gn_ffn4& f, const Few4& w, cudaStream_t st) {
   if (!f.index || e != cudaSuccess) return e;
   Combine c = {};
   c.tokens = f.tokens; c.k = f.k; c.cols = f.cols; c.experts = f.experts; c.index = f.index; c.weight = f.weight; c.src = w.out; c.ld = w.ld_out; c.d = f.y.p; c.ld_d = f.y.ld;
-  return launch_combine(f.type, GN_F32, c, st);
+  return launch_combine(f.type, c, st);
 }
 
 }  // namespace

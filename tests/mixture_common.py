@@ -35,8 +35,8 @@ def used(index, experts):
 
 
 def check_experts(got, x, index, weight, w, act, t, row=None, h_round=1.0):
-    """row: rounding of a pair's row of y (None: that of the type)."""
-    row = u(t) if row is None else row
+    """row: rounding of a pair's row of y (none: they are FP32)."""
+    row = 0.0 if row is None else row
     x64, (wg, wu, wd) = x.double(), (m.double() for m in w)
     tokens, k = index.shape
     y, y_err = torch.zeros(x.shape, dtype=torch.float64, device="cuda"), torch.zeros(x.shape, dtype=torch.float64, device="cuda")
@@ -81,7 +81,7 @@ def check_experts_grad(got, dy, x, index, weight, gate, up, w, act, t):
         dup_err = s * q_err * a.abs() + rel * dup.abs() + tiny(t) + slack * (s * q).abs()
         both, both_err = product(torch.cat([dgate, dup], 1), torch.cat([wg[e], wu[e]], 0).T, torch.cat([dgate_err, dup_err], 1), 0)
         dx.index_put_((at,), both, accumulate=True)
-        dx_err.index_put_((at,), both_err + rel * both.abs() + k * E * both.abs() + tiny(t), accumulate=True)
+        dx_err.index_put_((at,), both_err + (k + 2) * E * both.abs(), accumulate=True)
         xs = x64[at]
         for i, (ref, err) in enumerate((product(dgate.T, xs.T, dgate_err.T, 0), product(dup.T, xs.T, dup_err.T, 0), product(d.T, h_s.T, 0, h_err.T))):
             grads[i][e], errs[i][e] = ref, err

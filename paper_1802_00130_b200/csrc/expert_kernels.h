@@ -90,8 +90,9 @@ struct FmaGroup {
   struct { int M = 0, N = 0; FfnMat left, right; bool left_tokens = false, right_tokens = false; Grads32 d; } grads[3];
   int n_grads = 0;
 };
-constexpr int kFmaHeight = 64;       // slots of a plan's tile for these kernels
-int fma_parts(int N);
-cudaError_t launch_group_fma(GroupKind kind, const FmaGroup& g, const ExpertPlan& plan, cudaStream_t st);
+constexpr int kFmaHeight = 64, kFmaSmall = 32;       // slots of a plan's tile for these kernels, in large and small tiles
+bool fma_small(int64_t pairs, int experts, int cols, int inner);                     // which a call takes
+int fma_parts(int N, bool small);
+cudaError_t launch_group_fma(GroupKind kind, const FmaGroup& g, bool small, const ExpertPlan& plan, cudaStream_t st);
 
 }  // namespace gn

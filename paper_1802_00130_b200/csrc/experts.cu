@@ -164,17 +164,19 @@ cudaError_t run_half(const gn_mixture& f, bool backward, const Half& w, int* err
 }
 
 // ---- FP32 --------------------------------------------------------------------------------------
-struct Single { ExpertPlan plan; FfnOut h, dgate, dup, out; float* parts; };
+struct Single { ExpertPlan plan; bool small; int height; FfnOut h, dgate, dup, out; float* parts; };
 int64_t lay_out_single(const gn_mixture& f, bool backward, char* base, Single& w) {
   Workspace ws{base};
   w = Single{};
   const int64_t pairs = f.tokens * f.k, lc = up8(f.cols), lf = up8(f.inner);
-  w.plan = plan_at((int*)ws.take(plan_ints(pairs, f.experts, kFmaHeight) * 4), pairs, f.experts, kFmaHeight);
+  w.small = fma_small(pairs, f.experts, f.cols, f.inner);
+  w.height = w.small ? kFmaSmall : kFmaHeight;
+  w.plan = plan_at((int*)ws.take(plan_ints(pairs, f.experts, w.height) * 4), pairs, f.experts, w.height);
   w.h = {(float*)ws.take(pairs * lf * 4), lf};
   if (backward) {
     w.dgate = {(float*)ws.take(pairs * lf * 4), lf};
     w.dup = {(float*)ws.take(pairs * lf * 4), lf};
-    w.parts = (float*)ws.take(plan_slots(pairs, f.experts) * fma_parts(f.inner) * 4);
+    w.parts = (float*)ws.take(plan_slots(pairs, f.experts) * fma_parts(f.inner, w.small) * 4);
   }
   if (!backward || f.dx.p) w.out = {(float*)ws.take(pairs * lc * 4), lc};
   return ws.used;
@@ -183,7 +185,7 @@ cudaError_t run_single(const gn_mixture& f, bool backward, const Single& w, cuda
   const auto in = [](const gn_mat& m) { return FfnMat{(const float*)m.p, m.ld}; };
   const auto of = [](const FfnOut& m) { return FfnMat{m.p, m.ld}; };
   const auto weights = [](const gn_stack& m) { return Weights32{(const float*)m.p, m.ld, m.stride}; };
-  cudaError_t e = launch_plan(f.index, w.plan, kFmaHeight, st);
+  cudaError_t e = launch_plan(f.index, w.plan, w.height, st);
   FmaGroup g, q;
   g.act = f.act; g.k = q.k = f.k; g.N = f.inner; g.K = f.cols; g.token_rows = true; g.d = w.h;
   q.N = f.cols; q.K = f.inner; q.d = w.out;
@@ -192,17 +194,17 @@ cudaError_t run_single(const gn_mixture& f, bool backward, const Single& w, cuda
   if (!backward) {
     g.A[0] = in(f.x); g.B[0] = weights(f.w_gate); g.B[1] = weights(f.w_up);
     g.gate_out = {(float*)f.gate.p, f.gate.ld}; g.up_out = {(float*)f.up.p, f.up.ld};
-    if (e == cudaSuccess) e = launch_group_fma(GROUP_GATE, g, w.plan, st);
+    if (e == cudaSuccess) e = launch_group_fma(GROUP_GATE, g, w.small, w.plan, st);
     q.A[0] = of(w.h); q.B[0] = weights(f.w_down);
-    if (e == cudaSuccess) e = launch_group_fma(GROUP_DOWN, q, w.plan, st);
+    if (e == cudaSuccess) e = launch_group_fma(GROUP_DOWN, q, w.small, w.plan, st);
     c.weight = f.weight; c.d = f.y.p; c.ld_d = f.y.ld;
     return e == cudaSuccess ? launch_combine(GN_F32, c, st) : e;
   }
   g.A[0] = in(f.dy); g.B[0] = weights(f.w_down); g.dgate = w.dgate; g.dup = w.dup; g.gate = in(f.gate); g.up = in(f.up); g.weight = f.weight; g.parts = w.parts;
-  if (e == cudaSuccess) e = launch_group_fma(GROUP_GRAD, g, w.plan, st);
+  if (e == cudaSuccess) e = launch_group_fma(GROUP_GRAD, g, w.small, w.plan, st);
   if (f.dx.p) {
     q.A[0] = of(w.dgate); q.A[1] = of(w.dup); q.B[0] = weights(f.w_gate); q.B[1] = weights(f.w_up);
-    if (e == cudaSuccess) e = launch_group_fma(GROUP_DX, q, w.plan, st);
+    if (e == cudaSuccess) e = launch_group_fma(GROUP_DX, q, w.small, w.plan, st);
   }
   if (any_weights(f)) {
     FmaGroup r;
@@ -215,10 +217,10 @@ cudaError_t run_single(const gn_mixture& f, bool backward, const Single& w, cuda
     add(f.inner, f.cols, of(w.dgate), false, in(f.x), true, f.dw_gate);
     add(f.inner, f.cols, of(w.dup), false, in(f.x), true, f.dw_up);
     add(f.cols, f.inner, in(f.dy), true, of(w.h), false, f.dw_down);
-    if (e == cudaSuccess) e = launch_group_fma(GROUP_WEIGHT, r, w.plan, st);
+    if (e == cudaSuccess) e = launch_group_fma(GROUP_WEIGHT, r, w.small, w.plan, st);
   }
   c.d = f.dx.p; c.ld_d = f.dx.ld;
-  if (f.dweight) { c.parts = w.parts; c.n_parts = fma_parts(f.inner); c.slot_of = w.plan.slot_of; c.dweight = f.dweight; }
+  if (f.dweight) { c.parts = w.parts; c.n_parts = fma_parts(f.inner, w.small); c.slot_of = w.plan.slot_of; c.dweight = f.dweight; }
   return e == cudaSuccess && (c.d || c.parts) ? launch_combine(GN_F32, c, st) : e;
 }
 

@@ -95,4 +95,25 @@ bool fma_small(int64_t pairs, int experts, int cols, int inner);                
 int fma_parts(int N, bool small);
 cudaError_t launch_group_fma(GroupKind kind, const FmaGroup& g, bool small, const ExpertPlan& plan, cudaStream_t st);
 
+// ---- the same in FP32 on the tensor cores (gemm_group32.cu) -------------------------------------------------------------------
+// An FP32 matrix as three BF16 parts that add up to it, each with rows that TMA can address: [3][rows][ld], of every expert [3][experts][rows][ld].
+struct Parts { void* p = nullptr; int64_t ld = 0, rows = 0; };
+struct SplitMats { const float* src; int64_t ld, stride; Parts to; int64_t rows; int experts, cols; };
+cudaError_t launch_split_mats(const SplitMats* list, int n, cudaStream_t st);           // up to three
+// Rows of tokens to their pairs' slots, in parts; zero: the empty slots too.
+struct SplitRows { const float* src; int64_t ld; Parts to; };
+cudaError_t launch_split_to_slots(const SplitRows* list, int n, int64_t tokens, int k, int cols, bool zero, const ExpertPlan& plan, cudaStream_t st);
+struct TensorGroup {
+  int act = 0, N = 0, K = 0;
+  Parts A[2], B[2];                  // rows of slots; weights
+  Parts d, dgate, dup;               // in slots
+  FfnOut rows;                       // of pairs
+  FfnMat gate, up; FfnOut gate_out, up_out;
+  const float* weight = nullptr; float* parts = nullptr;
+  struct { int M = 0, N = 0; Parts left, right; Grads32 d; } grads[3];
+  int n_grads = 0;
+};
+int tensor_parts(int N);
+cudaError_t launch_group32(GroupKind kind, const TensorGroup& g, const ExpertPlan& plan, int* err, cudaStream_t st);
+
 }  // namespace gn

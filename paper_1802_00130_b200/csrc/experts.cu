@@ -3,7 +3,7 @@
 // 16-bit types, forward: the plan (which pairs of token and choice are whose), the tokens to the experts' slots, both projections with the gate, the product
 // with Wd, the weighted sums of each token's results.  Backward: the plan again (it is cheaper than to keep it), x and dy to the slots, q = dy Wd with the gate's
 // gradient, dx's two products, the three weight gradients as one launch, and each token's sums.
-// FP32: the same products on FMAs, rows read where they lie.
+// FP32: the same products on the tensor cores, operands in three parts, or on FMAs, rows read where they lie.
 // Nothing is read by the host: how many tokens an expert has only the device knows, and grids are for what there can be.
 #include <math.h>
 
@@ -224,6 +224,93 @@ cudaError_t run_single(const gn_mixture& f, bool backward, const Single& w, cuda
   return e == cudaSuccess && (c.d || c.parts) ? launch_combine(GN_F32, c, st) : e;
 }
 
+// ---- FP32 on the tensor cores --------------------------------------------------------------------
+struct Tensor { ExpertPlan plan; Parts x, dy, w_gate, w_up, w_down, h, dgate, dup; FfnOut out; float* parts; };
+// Where its estimated time, in us, is the smaller one.  FMAs: 26 TFLOP/s of tiles that are half empty at an expert's end, or the weights' bytes (backward their gradients'
+// too), and the chain of an expert's rows in its gradients.  Tensor cores: more launches, the parts of the weights (30 bytes for three), six products a term of tiles of 256 rows.
+// Measured, forward and backward, tensor cores and FMAs: 16 tokens, 2 of 8 experts, 512 x 512 65, 116 and 45, 92; 500, 2 of 8, 784 x 300 65, 131 and 98, 193; 2000, 4 of 32,
+// 1024 x 1024 592, 1048 and 1499, 3172; 64, 2 of 32, 1024 x 2048 893, 1202 and 394, 1557.
+bool on_tensor_cores(const gn_mixture& f, bool backward) {
+  const double pairs = (double)f.tokens * f.k, E = f.experts, used = pairs < E ? pairs : E, terms = (double)f.cols * f.inner * (backward ? 12 : 6);
+  const double flops = (pairs + 24.0 * used) * terms / 26e6, bytes = E * f.cols * f.inner * (backward ? 36 : 12) / 2.2e6;
+  const double fmas = (flops > bytes ? flops : bytes) + (backward ? 45.0 + 0.03 * pairs / E : 32.0);
+  const double tensor = (backward ? 80.0 : 50.0) + E * f.cols * f.inner * 30 / 5e6 + 6 * (pairs + 128.0 * used) * terms / 0.95e9;
+  return tensor < fmas;
+}
+int64_t lay_out_tensor(const gn_mixture& f, bool backward, char* base, Tensor& w) {
+  Workspace ws{base};
+  w = Tensor{};
+  const int64_t pairs = f.tokens * f.k, slots = plan_slots(pairs, f.experts), lc = up8(f.cols), lf = up8(f.inner);
+  w.plan = plan_at((int*)ws.take(plan_ints(pairs, f.experts, kGroupHeight) * 4), pairs, f.experts, kGroupHeight);
+  const auto parts = [&](int64_t rows, int64_t ld) { return Parts{ws.take(3 * rows * ld * 2), ld, rows}; };
+  if (!backward || any_weights(f)) w.x = parts(slots, lc);
+  if (backward) w.dy = parts(slots, lc);
+  if (!backward || f.dx.p) {
+    w.w_gate = parts((int64_t)f.experts * f.inner, lc);
+    w.w_up = parts((int64_t)f.experts * f.inner, lc);
+  }
+  w.w_down = parts((int64_t)f.experts * f.cols, lf);
+  w.h = parts(slots, lf);
+  if (backward) {
+    w.dgate = parts(slots, lf); w.dup = parts(slots, lf);
+    w.parts = (float*)ws.take(slots * tensor_parts(f.inner) * 4);
+  }
+  if (!backward || f.dx.p) w.out = {(float*)ws.take(pairs * lc * 4), lc};
+  return ws.used;
+}
+cudaError_t run_tensor(const gn_mixture& f, bool backward, const Tensor& w, int* err, cudaStream_t st) {
+  const auto in = [](const gn_mat& m) { return FfnMat{(const float*)m.p, m.ld}; };
+  SplitMats mats[3];
+  int n = 0;
+  const auto split = [&](const gn_stack& m, int64_t rows, int cols, const Parts& to) {
+    if (to.p) mats[n++] = {(const float*)m.p, m.ld, f.experts == 1 ? 0 : m.stride, to, rows, f.experts, cols};
+  };
+  split(f.w_gate, f.inner, f.cols, w.w_gate);
+  split(f.w_up, f.inner, f.cols, w.w_up);
+  split(f.w_down, f.cols, f.inner, w.w_down);
+  cudaError_t e = launch_split_mats(mats, n, st);
+  if (e == cudaSuccess) e = launch_plan(f.index, w.plan, kGroupHeight, st);
+  SplitRows rows[2];
+  n = 0;
+  if (w.x.p) rows[n++] = {(const float*)f.x.p, f.x.ld, w.x};
+  if (backward) rows[n++] = {(const float*)f.dy.p, f.dy.ld, w.dy};
+  if (e == cudaSuccess) e = launch_split_to_slots(rows, n, f.tokens, f.k, f.cols, backward, w.plan, st);
+  TensorGroup g, q;
+  g.act = f.act; g.N = f.inner; g.K = f.cols; g.d = w.h;
+  q.N = f.cols; q.K = f.inner; q.rows = w.out;
+  Combine c = {};
+  c.tokens = f.tokens; c.k = f.k; c.cols = f.cols; c.experts = f.experts; c.index = f.index; c.src = w.out.p; c.ld = w.out.ld;
+  if (!backward) {
+    g.A[0] = w.x; g.B[0] = w.w_gate; g.B[1] = w.w_up; g.gate_out = {(float*)f.gate.p, f.gate.ld}; g.up_out = {(float*)f.up.p, f.up.ld};
+    if (e == cudaSuccess) e = launch_group32(GROUP_GATE, g, w.plan, err, st);
+    q.A[0] = w.h; q.B[0] = w.w_down;
+    if (e == cudaSuccess) e = launch_group32(GROUP_DOWN, q, w.plan, err, st);
+    c.weight = f.weight; c.d = f.y.p; c.ld_d = f.y.ld;
+    return e == cudaSuccess ? launch_combine(GN_F32, c, st) : e;
+  }
+  g.A[0] = w.dy; g.B[0] = w.w_down; g.dgate = w.dgate; g.dup = w.dup; g.gate = in(f.gate); g.up = in(f.up); g.weight = f.weight; g.parts = w.parts;
+  if (e == cudaSuccess) e = launch_group32(GROUP_GRAD, g, w.plan, err, st);
+  if (f.dx.p) {
+    q.A[0] = w.dgate; q.A[1] = w.dup; q.B[0] = w.w_gate; q.B[1] = w.w_up;
+    if (e == cudaSuccess) e = launch_group32(GROUP_DX, q, w.plan, err, st);
+  }
+  if (any_weights(f)) {
+    TensorGroup r;
+    const auto add = [&](int M, int N, const Parts& left, const Parts& right, const gn_stack& d) {
+      if (!d.p) return;
+      auto& t = r.grads[r.n_grads++];
+      t.M = M; t.N = N; t.left = left; t.right = right; t.d = {(float*)d.p, d.ld, d.stride};
+    };
+    add(f.inner, f.cols, w.dgate, w.x, f.dw_gate);
+    add(f.inner, f.cols, w.dup, w.x, f.dw_up);
+    add(f.cols, f.inner, w.dy, w.h, f.dw_down);
+    if (e == cudaSuccess) e = launch_group32(GROUP_WEIGHT, r, w.plan, err, st);
+  }
+  c.d = f.dx.p; c.ld_d = f.dx.ld;
+  if (f.dweight) { c.parts = w.parts; c.n_parts = tensor_parts(f.inner); c.slot_of = w.plan.slot_of; c.dweight = f.dweight; }
+  return e == cudaSuccess && (c.d || c.parts) ? launch_combine(GN_F32, c, st) : e;
+}
+
 cudaError_t clear(const gn_stack& m, int experts, int64_t rows, int64_t cols, int type, cudaStream_t st) {
   const size_t b = (size_t)type_bytes(type);
   cudaError_t e = cudaSuccess;
@@ -232,17 +319,18 @@ cudaError_t clear(const gn_stack& m, int experts, int64_t rows, int64_t cols, in
   return e;
 }
 
-int64_t needed(const gn_mixture& f, bool backward, char* base, Half& h, Single& s) {
-  return (f.type == GN_F32 ? lay_out_single(f, backward, base, s) : lay_out_half(f, backward, base, h)) + 256;
+struct Layouts { Half half; Single single; Tensor tensor; };
+int64_t needed(const gn_mixture& f, bool backward, char* base, Layouts& w) {
+  if (f.type != GN_F32) return lay_out_half(f, backward, base, w.half) + 256;
+  return (on_tensor_cores(f, backward) ? lay_out_tensor(f, backward, base, w.tensor) : lay_out_single(f, backward, base, w.single)) + 256;
 }
 
 gn_status run(const gn_mixture* f, bool back, void* d_ws, int64_t ws_bytes, void* stream, char* errbuf, int64_t errbuf_len) {
   const char* why = mixture_args(f, back);
   if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
-  Half h;
-  Single s;
+  Layouts w;
   char* const base = (char*)(((uintptr_t)d_ws + 255) & ~(uintptr_t)255);
-  if (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < needed(*f, back, base, h, s))
+  if (!d_ws || ((uintptr_t)d_ws & 15) || ws_bytes < needed(*f, back, base, w))
     return op_fail(GN_EINVAL, "workspace: null, not 16-byte aligned or too small", errbuf, errbuf_len);
   cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e = cudaSuccess;
@@ -256,7 +344,9 @@ gn_status run(const gn_mixture* f, bool back, void* d_ws, int64_t ws_bytes, void
   }
   int* const err = ffn_error_word();
   if (!err) return op_done(cudaErrorNoDevice, errbuf, errbuf_len);
-  e = f->type == GN_F32 ? run_single(*f, back, s, st) : run_half(*f, back, h, err, st);
+  if (f->type != GN_F32) e = run_half(*f, back, w.half, err, st);
+  else if (on_tensor_cores(*f, back)) e = run_tensor(*f, back, w.tensor, err, st);
+  else e = run_single(*f, back, w.single, st);
   return op_done(e, errbuf, errbuf_len);
 }
 
@@ -266,9 +356,8 @@ gn_status run(const gn_mixture* f, bool back, void* d_ws, int64_t ws_bytes, void
 using namespace gn;
 
 extern "C" int64_t gn_experts_workspace(const gn_mixture* args, int32_t backward) {
-  Half h;
-  Single s;
-  return mixture_args(args, backward != 0) ? -1 : needed(*args, backward != 0, kNowhere, h, s);
+  Layouts w;
+  return mixture_args(args, backward != 0) ? -1 : needed(*args, backward != 0, kNowhere, w);
 }
 extern "C" gn_status gn_experts(const gn_mixture* args, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
   return run(args, false, d_ws, ws_bytes, cuda_stream, errbuf, errbuf_len);

@@ -74,6 +74,11 @@ __device__ __forceinline__ GroupItem group_item(const GroupParams& p, int i) {
   return w;
 }
 
+__device__ __forceinline__ GroupItem uniform_item(GroupItem w) {
+  w.expert = uniform(w.expert); w.slot = uniform(w.slot); w.m0 = uniform(w.m0); w.n0 = uniform(w.n0); w.kb = uniform(w.kb); w.grad = uniform(w.grad);
+  return w;
+}
+
 template <int KIND, class T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(group_threads<KIND>, 1)
 group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant__ GroupParams p) {
@@ -89,7 +94,7 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
   const int pair = blockIdx.x >> 1;
 
@@ -109,20 +114,20 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
   const uint32_t tmem_base = *tmem_slot;
   grid_dep_wait();
   grid_dep_launch();
-  const int items = KIND == GROUP_WEIGHT ? p.items : *dep(p.n_tiles) * p.tiles_n;
+  const int items = KIND == GROUP_WEIGHT ? p.items : uniform(*dep(p.n_tiles)) * p.tiles_n;
 
   if (warp == 0) {
-    if (lane == 0) {
-      int s = 0;
-      uint32_t ph = 0;
-      bool ok = true;
-      const uint32_t full_leader = map_to_cta(smem_u32(&full[0]), 0);
-      for (int i = pair; ok && i < items; i += p.pairs) {
-        const GroupItem w = group_item<KIND>(p, i);
-        const int m0 = (KIND == GROUP_WEIGHT ? w.m0 : w.slot) + (int)rank * G_BM, n0 = KIND == GROUP_GATE ? w.n0 : w.n0 + (int)rank * G_BM;
+    int s = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    const uint32_t full_leader = map_to_cta(smem_u32(&full[0]), 0);
+    for (int i = pair; ok && i < items; i += p.pairs) {
+      const GroupItem w = uniform_item(group_item<KIND>(p, i));
+      const int m0 = (KIND == GROUP_WEIGHT ? w.m0 : w.slot) + (int)rank * G_BM, n0 = KIND == GROUP_GATE ? w.n0 : w.n0 + (int)rank * G_BM;
 #pragma unroll 1
-        for (int kb = 0; kb < w.kb; ++kb) {
-          if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, p.err, 1)) { ok = false; break; }
+      for (int kb = 0; kb < w.kb; ++kb) {
+        if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, p.err, 1)) { ok = false; break; }
+        if (elect_one()) {
           if (rank == 0) mbar_expect_tx(&full[s], 2u * G_STAGE_BYTES);
           const uint32_t bar = full_leader + (uint32_t)s * 8u;
           uint8_t* const sa = smem + s * G_STAGE_BYTES;
@@ -145,12 +150,12 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
               tma2_load_3d(sb + 8192, mb, n0 + 64, k0, w.expert, bar);
             }
           }
-          if (++s == G_STAGES) { s = 0; ph ^= 1u; }
         }
+        if (++s == G_STAGES) { s = 0; ph ^= 1u; }
       }
     }
   } else if (warp == 1) {
-    if (rank == 0 && lane == 0) {
+    if (rank == 0) {
       constexpr bool BF16 = !__is_same(T, __half);
       const uint32_t base = smem_u32(smem);
       const uint32_t idesc = (1u << 4) | (BF16 ? (1u << 7) | (1u << 10) : 0u) | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(G_BN >> 3) << 17) |
@@ -162,7 +167,7 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
       uint32_t ph = 0;
       bool ok = true;
       for (int i = pair; ok && i < items; i += p.pairs) {
-        const GroupItem w = group_item<KIND>(p, i);
+        const GroupItem w = uniform_item(group_item<KIND>(p, i));
         if (KIND == GROUP_WEIGHT && w.kb == 0) continue;
         const int buf = ti & 1;
         if (!wait_or_abort(&acc_empty[buf], ((ti >> 1) & 1) ^ 1, abort_flag, p.err, 4)) break;
@@ -174,15 +179,17 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
           if (!wait_or_abort(&full[s], ph, abort_flag, p.err, 2)) { ok = false; break; }
           tc_fence_after();
           const uint64_t ad = a0 + (uint64_t)(s * (G_STAGE_BYTES >> 4)), bd = b0 + (uint64_t)(s * (G_STAGE_BYTES >> 4));
-          pair_mma<BF16>(tmem_d, ad, bd, idesc, acc);
+          if (elect_one()) {
+            pair_mma<BF16>(tmem_d, ad, bd, idesc, acc);
+            pair_mma<BF16>(tmem_d, ad + a_step, bd + b_step, idesc, 1u);
+            pair_mma<BF16>(tmem_d, ad + 2 * a_step, bd + 2 * b_step, idesc, 1u);
+            pair_mma<BF16>(tmem_d, ad + 3 * a_step, bd + 3 * b_step, idesc, 1u);
+            mma2_commit_both(&empty[s]);
+          }
           acc = 1u;
-          pair_mma<BF16>(tmem_d, ad + a_step, bd + b_step, idesc, 1u);
-          pair_mma<BF16>(tmem_d, ad + 2 * a_step, bd + 2 * b_step, idesc, 1u);
-          pair_mma<BF16>(tmem_d, ad + 3 * a_step, bd + 3 * b_step, idesc, 1u);
-          mma2_commit_both(&empty[s]);
           if (++s == G_STAGES) { s = 0; ph ^= 1u; }
         }
-        if (ok) mma2_commit_both(&acc_full[buf]);
+        if (ok && elect_one()) mma2_commit_both(&acc_full[buf]);
         ++ti;
       }
     }

@@ -586,12 +586,22 @@ typedef enum { GN_SOFTMAX = 0, GN_SIGMOID = 1 } gn_score;
  * Equal values go by the lower number (experts and groups).  The order is that of the exact values: no rounding of FP32 decides it.  -inf is the
  * logit of an expert that cannot be taken: it has the score 0, and comes last without a bias (with one, a bias of -inf keeps it out); a row of
  * nothing else has weights of 0.  NaN comes behind every number (and is not among a group's best); with softmax a NaN or +inf in a row makes its weights NaN.
- *   d_bias           [experts] floats or NULL.
+ *   bias             [experts] floats or NULL.
  * 1 <= k <= 32; k <= experts <= 1024; groups <= 32 divides experts; k <= experts / groups * top_groups; tokens < 2^31.
  */
-gn_status gn_route(gn_dtype type, gn_score score, int64_t tokens, int32_t experts, int32_t k, const void* d_logits, int64_t ld,
-                   const float* d_bias, int32_t groups, int32_t top_groups, int32_t group_best, int32_t renormalise, double scale,
-                   int32_t* d_index, float* d_weight, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+typedef struct {
+  int32_t type, score;        /* gn_dtype (of the logits), gn_score */
+  int64_t tokens;
+  int32_t experts, k, groups, top_groups, group_best, renormalise;
+  double scale;
+  gn_mat logits;              /* [tokens][experts] */
+  const float* bias;
+  int32_t* index;
+  float* weight;              /* gn_route_grad: the gradient of the weights, an input */
+  gn_mat dlogits;             /* gn_route_grad */
+} gn_router;
+
+gn_status gn_route(const gn_router* args, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 
 /*
  * gn_route_grad - the gradient of the weights to that of the logits (the choice itself has none).  With u_j = scale dweight_j, s_j the chosen experts' scores:
@@ -600,12 +610,10 @@ gn_status gn_route(gn_dtype type, gn_score score, int64_t tokens, int32_t expert
  *   and with `renormalise`, p_j = s_j / sum s:
  *     softmax                  dlogits_e = sum_{j: e_j = e} p_j (u_j - sum_i u_i p_i)
  *     sigmoid                  the same times 1 - s_e.
- * d_logits: those of the forward call.  d_index [tokens][k]: what it has written; entries outside [0, experts) take no part.
- * d_dlogits [tokens][ld_d] is written whole.
+ * logits, index: those of the forward call (inputs); entries of index outside [0, experts) take no part.  dlogits [tokens][experts] is written whole, and is
+ * not in the place of the logits.  bias and groups are not looked at.
  */
-gn_status gn_route_grad(gn_dtype type, gn_score score, int64_t tokens, int32_t experts, int32_t k, const float* d_dweight,
-                        const void* d_logits, int64_t ld, const int32_t* d_index, int32_t renormalise, double scale, void* d_dlogits,
-                        int64_t ld_d, void* cuda_stream, char* errbuf, int64_t errbuf_len);
+gn_status gn_route_grad(const gn_router* args, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 
 typedef struct { void* p; int64_t ld, stride; } gn_stack;   /* a matrix of every expert, `stride` elements apart */
 

@@ -76,8 +76,8 @@ _SIGNATURES = {
     "gn_matvec4": (_i32, [_i32, _i64, _i64, _i64, _i32, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, C.c_char_p, _i64]),
     "gn_gated_ffn4_workspace": (_i64, [_vp]),
     "gn_gated_ffn4": (_i32, [_vp, _vp, _i64, _vp, C.c_char_p, _i64]),
-    "gn_route": (_i32, [_i32, _i32, _i64, _i32, _i32, _vp, _i64, _vp, _i32, _i32, _i32, _i32, _dbl, _vp, _vp, _vp, C.c_char_p, _i64]),
-    "gn_route_grad": (_i32, [_i32, _i32, _i64, _i32, _i32, _vp, _vp, _i64, _vp, _i32, _dbl, _vp, _i64, _vp, C.c_char_p, _i64]),
+    "gn_route": (_i32, [_vp, _vp, C.c_char_p, _i64]),
+    "gn_route_grad": (_i32, [_vp, _vp, C.c_char_p, _i64]),
 }
 
 

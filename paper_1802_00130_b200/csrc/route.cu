@@ -546,65 +546,49 @@ cudaError_t run_route(RouteParams p, bool grad, cudaStream_t st) {
   }
 }
 
-const char* route_args(int type, int score, int64_t tokens, int experts, int k, double scale) {
-  if (!type_ok(type)) return "type is not a gn_dtype";
-  if (score != GN_SOFTMAX && score != GN_SIGMOID) return "score is not a gn_score";
-  if (tokens < 0 || tokens >= (int64_t(1) << 31)) return "tokens must be in [0, 2^31)";
-  if (experts < 1 || experts > kRouteExperts) return "experts must be in [1, 1024]";
-  if (k < 1 || k > kRouteChoices || k > experts) return "k must be in [1, 32] and not above the number of experts";
-  if (!(fabs(scale) <= 3.402823466e38)) return "scale must be a finite FP32 number";
+const char* route_args(const gn_router* f, bool grad) {
+  if (!f) return "no arguments";
+  if (!type_ok(f->type)) return "type is not a gn_dtype";
+  if (f->score != GN_SOFTMAX && f->score != GN_SIGMOID) return "score is not a gn_score";
+  if (f->tokens < 0 || f->tokens >= (int64_t(1) << 31)) return "tokens must be in [0, 2^31)";
+  if (f->experts < 1 || f->experts > kRouteExperts) return "experts must be in [1, 1024]";
+  if (f->k < 1 || f->k > kRouteChoices || f->k > f->experts) return "k must be in [1, 32] and not above the number of experts";
+  if (!(fabs(f->scale) <= 3.402823466e38)) return "scale must be a finite FP32 number";
+  if (!grad) {
+    if (f->groups < 1 || f->groups > 32 || f->experts % f->groups) return "groups must be in [1, 32] and divide the experts";
+    if (f->top_groups < 1 || f->top_groups > f->groups) return "top_groups must be in [1, groups]";
+    if (f->group_best != 1 && f->group_best != 2) return "group_best must be 1 or 2";
+    if (f->k > f->experts / f->groups * f->top_groups) return "k must not be above the experts of top_groups groups";
+    if ((uintptr_t)f->bias & 3) return "bias is not aligned to 4 bytes";
+  }
+  if (f->tokens == 0) return nullptr;
+  if (!mat_ok(f->logits.p, f->logits.ld, f->experts, f->type)) return "logits: null, misaligned, or a leading dimension below the number of experts";
+  if (!f->index || ((uintptr_t)f->index & 3) || !f->weight || ((uintptr_t)f->weight & 3)) return "index or weight: null or misaligned";
+  if (grad && !mat_ok(f->dlogits.p, f->dlogits.ld, f->experts, f->type)) return "dlogits: null, misaligned, or a leading dimension below the number of experts";
+  if (grad && f->dlogits.p == f->logits.p) return "dlogits must not be in the place of the logits";
   return nullptr;
 }
-bool words_ok(const void* p) { return p && ((uintptr_t)p & 3) == 0; }
+
+gn_status run(const gn_router* f, bool grad, void* stream, char* errbuf, int64_t errbuf_len) {
+  const char* why = route_args(f, grad);
+  if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
+  if (f->tokens == 0) return op_done(cudaSuccess, errbuf, errbuf_len);
+  RouteParams p = {};
+  p.tokens = f->tokens; p.experts = f->experts; p.k = f->k; p.softmax = f->score == GN_SOFTMAX; p.renormalise = f->renormalise != 0; p.scale = (float)f->scale;
+  // (where all groups are kept there is nothing to choose between)
+  p.groups = grad || f->top_groups == f->groups ? 1 : f->groups;
+  p.each = f->experts / p.groups; p.top = f->top_groups; p.best = f->group_best;
+  p.logits = f->logits.p; p.ld = f->logits.ld; p.bias = grad ? nullptr : f->bias; p.index = f->index; p.weight = f->weight; p.dweight = f->weight;
+  p.dlogits = f->dlogits.p; p.ld_d = f->dlogits.ld;
+  cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = f->type == GN_F32 ? run_route<float>(p, grad, st) : f->type == GN_BF16 ? run_route<__nv_bfloat16>(p, grad, st) : run_route<__half>(p, grad, st);
+  return op_done(e, errbuf, errbuf_len);
+}
 
 }  // namespace
 }  // namespace gn
 
 using namespace gn;
 
-extern "C" gn_status gn_route(gn_dtype type, gn_score score, int64_t tokens, int32_t experts, int32_t k, const void* d_logits, int64_t ld,
-                              const float* d_bias, int32_t groups, int32_t top_groups, int32_t group_best, int32_t renormalise, double scale,
-                              int32_t* d_index, float* d_weight, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
-  const char* why = route_args(type, score, tokens, experts, k, scale);
-  if (!why) {
-    if (groups < 1 || groups > 32 || experts % groups) why = "groups must be in [1, 32] and divide the experts";
-    else if (top_groups < 1 || top_groups > groups) why = "top_groups must be in [1, groups]";
-    else if (group_best != 1 && group_best != 2) why = "group_best must be 1 or 2";
-    else if (k > experts / groups * top_groups) why = "k must not be above the experts of top_groups groups";
-    else if ((uintptr_t)d_bias & 3) why = "bias is not aligned to 4 bytes";
-    else if (tokens > 0) {
-      if (!mat_ok(d_logits, ld, experts, type)) why = "logits: null, misaligned, or a leading dimension below the number of experts";
-      else if (!words_ok(d_index) || !words_ok(d_weight)) why = "index or weight: null or misaligned";
-    }
-  }
-  if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
-  if (tokens == 0) return op_done(cudaSuccess, errbuf, errbuf_len);
-  RouteParams p = {};
-  p.tokens = tokens; p.experts = experts; p.k = k; p.softmax = score == GN_SOFTMAX; p.renormalise = renormalise != 0;
-  // (all groups are kept: there is nothing to choose between)
-  p.groups = top_groups == groups ? 1 : groups; p.each = experts / p.groups; p.top = top_groups; p.best = group_best; p.scale = (float)scale;
-  p.logits = d_logits; p.ld = ld; p.bias = d_bias; p.index = d_index; p.weight = d_weight;
-  cudaStream_t st = (cudaStream_t)cuda_stream;
-  return op_done(type == GN_F32 ? run_route<float>(p, false, st) : type == GN_BF16 ? run_route<__nv_bfloat16>(p, false, st) : run_route<__half>(p, false, st),
-                 errbuf, errbuf_len);
-}
-
-extern "C" gn_status gn_route_grad(gn_dtype type, gn_score score, int64_t tokens, int32_t experts, int32_t k, const float* d_dweight,
-                                   const void* d_logits, int64_t ld, const int32_t* d_index, int32_t renormalise, double scale, void* d_dlogits,
-                                   int64_t ld_d, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
-  const char* why = route_args(type, score, tokens, experts, k, scale);
-  if (!why && tokens > 0) {
-    if (!mat_ok(d_logits, ld, experts, type)) why = "logits: null, misaligned, or a leading dimension below the number of experts";
-    else if (!mat_ok(d_dlogits, ld_d, experts, type)) why = "dlogits: null, misaligned, or a leading dimension below the number of experts";
-    else if (d_dlogits == d_logits) why = "dlogits must not be in the place of the logits";
-    else if (!words_ok(d_index) || !words_ok(d_dweight)) why = "index or dweight: null or misaligned";
-  }
-  if (why) return op_fail(GN_EINVAL, why, errbuf, errbuf_len);
-  if (tokens == 0) return op_done(cudaSuccess, errbuf, errbuf_len);
-  RouteParams p = {};
-  p.tokens = tokens; p.experts = experts; p.k = k; p.softmax = score == GN_SOFTMAX; p.renormalise = renormalise != 0; p.groups = 1; p.each = experts;
-  p.scale = (float)scale; p.logits = d_logits; p.ld = ld; p.index = const_cast<int*>(d_index); p.dweight = d_dweight; p.dlogits = d_dlogits; p.ld_d = ld_d;
-  cudaStream_t st = (cudaStream_t)cuda_stream;
-  return op_done(type == GN_F32 ? run_route<float>(p, true, st) : type == GN_BF16 ? run_route<__nv_bfloat16>(p, true, st) : run_route<__half>(p, true, st),
-                 errbuf, errbuf_len);
-}
+extern "C" gn_status gn_route(const gn_router* args, void* cuda_stream, char* errbuf, int64_t errbuf_len) { return run(args, false, cuda_stream, errbuf, errbuf_len); }
+extern "C" gn_status gn_route_grad(const gn_router* args, void* cuda_stream, char* errbuf, int64_t errbuf_len) { return run(args, true, cuda_stream, errbuf, errbuf_len); }

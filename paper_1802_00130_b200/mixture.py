@@ -8,6 +8,7 @@ float32, bfloat16 or float16 with unit stride inside a row, results are new tens
 """
 from __future__ import annotations
 
+import struct
 from array import array
 
 import torch
@@ -16,6 +17,7 @@ from .binding import lib
 from .feedforward import _TYPES, ACTIVATIONS, _checked, _device, _elsewhere, _err, _first, _matrix, _raw_stream, _vector
 
 SCORES = {"softmax": 0, "sigmoid": 1}
+_ONE = 0x3FF0000000000000                # 1.0 as a 64-bit word
 
 
 def _score(score):
@@ -43,6 +45,11 @@ def _choices(index, tokens):
     return index.shape[1]
 
 
+def _bits(scale):
+    """A float as a 64-bit word."""
+    return _ONE if scale == 1.0 else struct.unpack("q", struct.pack("d", scale))[0]
+
+
 def _whole(value, what):
     """A count, small enough for the library's 32-bit words."""
     if isinstance(value, bool) or not isinstance(value, int):
@@ -61,16 +68,18 @@ def route(logits, k, score="softmax", bias=None, groups=1, top_groups=1, group_b
     dtype, dev, tokens, n = _first(logits, "logits")
     if stream is not None or dev != _device():
         return _elsewhere(route, dev, stream, logits, k, score, bias, groups, top_groups, group_best, renormalise, scale)
-    pl, ld = _matrix(logits, "logits", tokens, n, dtype, dev)
-    pb = _vector(bias, "bias", n, dev, torch.float32)
-    kind, k = _score(score), _whole(k, "k")
-    if not 1 <= k <= n:
+    kind = _score(score)
+    if type(k) is not int or not 1 <= k <= n:
+        _whole(k, "k")
         raise ValueError(f"k: expected 1 to {n}, got {k}")
+    if not groups == top_groups == group_best == 1:
+        groups, top_groups, group_best = _whole(groups, "groups"), _whole(top_groups, "top_groups"), _whole(group_best, "group_best")
     index, weight = logits.new_empty(tokens, k, dtype=torch.int32), logits.new_empty(tokens, k, dtype=torch.float32)
+    args = array("q", (_TYPES[dtype] | kind << 32, tokens, n | k << 32, groups & 0xFFFFFFFF | top_groups << 32, group_best & 0xFFFFFFFF | (1 << 32 if renormalise else 0),
+                       _bits(scale), *_matrix(logits, "logits", tokens, n, dtype, dev), _vector(bias, "bias", n, dev, torch.float32) or 0, index.data_ptr(),
+                       weight.data_ptr(), 0, 0))
     err = _err()
-    status = lib().gn_route(_TYPES[dtype], kind, tokens, n, k, pl, ld, pb, _whole(groups, "groups"), _whole(top_groups, "top_groups"),
-                            _whole(group_best, "group_best"), 1 if renormalise else 0, float(scale), index.data_ptr(), weight.data_ptr(),
-                            _raw_stream(dev), err, 200)
+    status = lib().gn_route(args.buffer_info()[0], _raw_stream(dev), err, 200)
     if status:
         _checked(status, err)
     return index, weight
@@ -81,14 +90,15 @@ def route_grad(dweight, logits, index, score="softmax", renormalise=False, scale
     dtype, dev, tokens, n = _first(logits, "logits")
     if stream is not None or dev != _device():
         return _elsewhere(route_grad, dev, stream, dweight, logits, index, score, renormalise, scale)
-    pl, ld = _matrix(logits, "logits", tokens, n, dtype, dev)
     k = _choices(index, tokens)
-    pi, pw = _table(index, "index", tokens, k, torch.int32, dev), _table(dweight, "dweight", tokens, k, torch.float32, dev)
+    if k >= 1 << 31:
+        raise ValueError("index: expected a size below 2^31")
     kind = _score(score)
     dlogits = logits.new_empty(tokens, n)
+    args = array("q", (_TYPES[dtype] | kind << 32, tokens, n | k << 32, 0, 1 << 32 if renormalise else 0, _bits(scale), *_matrix(logits, "logits", tokens, n, dtype, dev), 0,
+                       _table(index, "index", tokens, k, torch.int32, dev), _table(dweight, "dweight", tokens, k, torch.float32, dev), dlogits.data_ptr(), n))
     err = _err()
-    status = lib().gn_route_grad(_TYPES[dtype], kind, tokens, n, k, pw, pl, ld, pi, 1 if renormalise else 0, float(scale), dlogits.data_ptr(), n,
-                                 _raw_stream(dev), err, 200)
+    status = lib().gn_route_grad(args.buffer_info()[0], _raw_stream(dev), err, 200)
     if status:
         _checked(status, err)
     return dlogits

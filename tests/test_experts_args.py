@@ -1,5 +1,6 @@
 """Refusals of the calls of a mixture of experts: nothing is launched, so no device is needed."""
 import ctypes as C
+import struct
 
 import pytest
 import torch
@@ -16,35 +17,38 @@ def refused(fn, *args):
     return err.value.decode()
 
 
-def route(**change):
-    a = dict(type=1, score=0, tokens=4, experts=16, k=4, logits=P, ld=16, bias=None, groups=4, top=2, best=2, renormalise=0, scale=1.0, index=P, weight=P, st=None)
+def router(**change):
+    """gn_router as 13 words."""
+    a = dict(type=1, score=0, tokens=4, experts=16, k=4, groups=4, top=2, best=2, renormalise=0, scale=1.0, logits=(1 << 20, 16), bias=0, index=1 << 20, weight=1 << 20,
+             dlogits=(1 << 21, 16))
     a.update(change)
-    return refused(gn.lib().gn_route, *a.values())
+    low = lambda x: x & 0xFFFFFFFF
+    words = [low(a["type"]) | a["score"] << 32, a["tokens"], low(a["experts"]) | a["k"] << 32, low(a["groups"]) | a["top"] << 32, low(a["best"]) | a["renormalise"] << 32,
+             struct.unpack("q", struct.pack("d", a["scale"]))[0], *a["logits"], a["bias"], a["index"], a["weight"], *a["dlogits"]]
+    return (C.c_int64 * 13)(*words)
 
 
-SHARED = [(dict(type=3), "type"), (dict(score=2), "score"), (dict(score=-1), "score"), (dict(tokens=-1), "tokens"), (dict(tokens=1 << 31), "tokens"), (dict(experts=0), "experts"),
-          (dict(experts=1025), "experts"), (dict(k=0), "k must"), (dict(k=33, experts=64), "k must"), (dict(k=17), "k must"), (dict(scale=float("nan")), "scale"),
-          (dict(scale=float("inf")), "scale"), (dict(scale=1e39), "scale"), (dict(logits=None), "logits"), (dict(ld=15), "logits"), (dict(logits=C.c_void_p(3)), "logits"),
-          (dict(index=None), "index"), (dict(index=C.c_void_p(2)), "index")]
+SHARED = [(dict(type=3), "type"), (dict(type=-1), "type"), (dict(score=2), "score"), (dict(score=-1), "score"), (dict(tokens=-1), "tokens"), (dict(tokens=1 << 31), "tokens"),
+          (dict(experts=0), "experts"), (dict(experts=1025), "experts"), (dict(k=0), "k must"), (dict(k=33, experts=64), "k must"), (dict(k=17), "k must"), (dict(k=-1), "k must"),
+          (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale"), (dict(scale=1e39), "scale"), (dict(logits=(0, 16)), "logits"), (dict(logits=(1 << 20, 15)), "logits"),
+          (dict(logits=(3, 16)), "logits"), (dict(index=0), "index"), (dict(index=2), "index"), (dict(weight=0), "weight"), (dict(weight=6), "weight")]
 
 
 @pytest.mark.parametrize("change,word", SHARED + [
     (dict(groups=0), "groups"), (dict(groups=3), "groups"), (dict(groups=33, experts=33), "groups"), (dict(top=0), "top_groups"), (dict(top=5), "top_groups"),
-    (dict(best=0), "group_best"), (dict(best=3), "group_best"), (dict(k=9), "k must"), (dict(bias=C.c_void_p(6)), "bias"), (dict(weight=None), "weight"),
-    (dict(weight=C.c_void_p(6)), "weight")])
+    (dict(best=0), "group_best"), (dict(best=3), "group_best"), (dict(k=9), "k must"), (dict(bias=6), "bias")])
 def test_route_refuses(change, word):
-    assert word in route(**change)
+    assert word in refused(gn.lib().gn_route, router(**change), None)
 
 
-def route_grad(**change):
-    a = dict(type=1, score=0, tokens=4, experts=16, k=4, dweight=P, logits=P, ld=16, index=P, renormalise=0, scale=1.0, dlogits=C.c_void_p(1 << 21), ld_d=16, st=None)
-    a.update(change)
-    return refused(gn.lib().gn_route_grad, *a.values())
-
-
-@pytest.mark.parametrize("change,word", SHARED + [(dict(dweight=None), "dweight"), (dict(dlogits=None), "dlogits"), (dict(ld_d=15), "dlogits"), (dict(dlogits=P), "place")])
+@pytest.mark.parametrize("change,word", SHARED + [(dict(dlogits=(0, 16)), "dlogits"), (dict(dlogits=(1 << 21, 15)), "dlogits"), (dict(dlogits=(1 << 20, 16)), "place")])
 def test_route_grad_refuses(change, word):
-    assert word in route_grad(**change)
+    assert word in refused(gn.lib().gn_route_grad, router(**change), None)
+
+
+def test_no_arguments():
+    for fn in (gn.lib().gn_route, gn.lib().gn_route_grad):
+        assert "no arguments" in refused(fn, None, None)
 
 
 def test_the_binding_refuses_tensors_that_are_not_on_a_device():

@@ -676,9 +676,9 @@ gn_status gn_unpack4(gn_dtype type, int32_t experts, int64_t rows, int64_t cols,
 /*
  * gn_matvec4 - y [tokens][rows] = x [tokens][cols] W^T of packed weights W [rows][cols].  Meant for a few tokens; any number below 2^20 is taken, 32 at a time.
  * Products of the type's numbers and whole q - 8, summed in FP32 group by group, times the scale; FP32 tokens lose nothing.
- * Workspace: gn_matvec4_workspace(type, tokens, cols) bytes, none for 16-bit types.
+ * Workspace: gn_matvec4_workspace(type, tokens, cols, d_x, ldx) bytes; none for 16-bit tokens whose rows start on 16 bytes and have a multiple of 8 columns.
  */
-int64_t gn_matvec4_workspace(gn_dtype type, int64_t tokens, int64_t cols);
+int64_t gn_matvec4_workspace(gn_dtype type, int64_t tokens, int64_t cols, const void* d_x, int64_t ldx);
 gn_status gn_matvec4(gn_dtype type, int64_t tokens, int64_t rows, int64_t cols, int32_t group, const void* d_x, int64_t ldx, const void* d_q,
                      const void* d_scale, void* d_y, int64_t ldy, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 

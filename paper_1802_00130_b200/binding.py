@@ -72,7 +72,7 @@ _SIGNATURES = {
     "gn_pack4": (_i32, [_i32, _i32, _i64, _i64, _i32, _vp, _i64, _i64, _vp, _vp, _vp, _vp, C.c_char_p, _i64]),
     "gn_quantize4": (_i32, [_i32, _i32, _i64, _i64, _i32, _vp, _i64, _i64, _vp, _vp, _vp, C.c_char_p, _i64]),
     "gn_unpack4": (_i32, [_i32, _i32, _i64, _i64, _i32, _vp, _vp, _vp, _i64, _i64, _vp, C.c_char_p, _i64]),
-    "gn_matvec4_workspace": (_i64, [_i32, _i64, _i64]),
+    "gn_matvec4_workspace": (_i64, [_i32, _i64, _i64, _vp, _i64]),
     "gn_matvec4": (_i32, [_i32, _i64, _i64, _i64, _i32, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, C.c_char_p, _i64]),
     "gn_gated_ffn4_workspace": (_i64, [_vp]),
     "gn_gated_ffn4": (_i32, [_vp, _vp, _i64, _vp, C.c_char_p, _i64]),

@@ -11,8 +11,8 @@ namespace {
 
 constexpr int kPlanThreads = 1024, kPlanWarps = 32;
 
-// Sum of a over the threads before this one, and over all of them.
-__device__ __forceinline__ int before_me(int a, int* warps, int& all) {
+// Sum of a over the threads before this one, and over all of them (n_warps full warps).
+__device__ __forceinline__ int before_me(int a, int* warps, int n_warps, int& all) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int x = a;
 #pragma unroll
@@ -21,7 +21,7 @@ __device__ __forceinline__ int before_me(int a, int* warps, int& all) {
   if (lane == 31) warps[warp] = x;
   __syncthreads();
   if (warp == 0) {
-    int s = warps[lane];
+    int s = lane < n_warps ? warps[lane] : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, s, o); if (lane >= o) s += y; }
     warps[lane] = s;
@@ -53,16 +53,16 @@ __global__ void __launch_bounds__(kPlanThreads) plan_count_kernel(const __grid_c
 // ONE: the grid is one block of up to kPlanThreads pairs, which counts for itself.
 template <bool ONE>
 __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const __grid_constant__ PlanParams p) {
-  extern __shared__ uint16_t of_warp[];          // [kPlanWarps][experts]: pairs of a round's warps, then of the warps before
+  extern __shared__ uint16_t of_warp[];          // [warps][experts]: pairs of a round's warps, then of the warps before
   __shared__ int base[kMostExperts], warps[kPlanWarps];
   grid_dep_wait();
   grid_dep_launch();
   const int* const index = dep(p.index);
-  const int E = p.plan.experts, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int E = p.plan.experts, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, threads = ONE ? (int)blockDim.x : kPlanThreads, n_warps = threads >> 5;
   const int64_t from = ONE ? 0 : blockIdx.x * p.chunk, to = ONE ? p.plan.pairs : min(from + p.chunk, p.plan.pairs);
   int before = 0, mine = 0;                      // thread e: pairs of expert e in the blocks before, in all
   const auto round = [&](int64_t i0, auto first) {
-    for (int i = threadIdx.x; i < kPlanWarps * E; i += kPlanThreads) of_warp[i] = 0;
+    for (int i = threadIdx.x; i < n_warps * E; i += threads) of_warp[i] = 0;
     __syncthreads();
     const int64_t i = i0 + threadIdx.x;
     int e = i < to ? index[i] : -1;
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const __grid_c
     __syncthreads();
     int sum = 0;
     if (threadIdx.x < E)
-      for (int w = 0; w < kPlanWarps; ++w) {
+      for (int w = 0; w < n_warps; ++w) {
         const int n = of_warp[w * E + threadIdx.x];
         of_warp[w * E + threadIdx.x] = (uint16_t)sum;
         sum += n;
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_place_kernel(const __grid_c
   const auto lay_out = [&] {
     int slots, tiles;
     const int padded = (mine + kSlots - 1) / kSlots * kSlots, n = (mine + p.height - 1) / p.height;
-    const int start = before_me(padded, warps, slots), tile = before_me(n, warps, tiles);
+    const int start = before_me(padded, warps, n_warps, slots), tile = before_me(n, warps, n_warps, tiles);
     if (threadIdx.x < E) base[threadIdx.x] = start + before;
     if (blockIdx.x == 0) {
       if (threadIdx.x < E) {
@@ -299,7 +299,10 @@ cudaError_t launch_plan(const int* index, const ExpertPlan& plan, int height, cu
     return cudaErrorInvalidDevice;
   const PlanParams p{index, plan, plan_chunk(plan.pairs), height};
   const int smem = kPlanWarps * plan.experts * 2, blocks = (int)((plan.pairs + p.chunk - 1) / p.chunk);
-  if (plan.pairs <= kPlanThreads) return launch_pdl(plan_place_kernel<true>, 1, kPlanThreads, smem, st, p);
+  if (plan.pairs <= kPlanThreads) {      // (a thread for each pair and each expert)
+    const int most = (int)plan.pairs > plan.experts ? (int)plan.pairs : plan.experts, threads = (most + 31) / 32 * 32;
+    return launch_pdl(plan_place_kernel<true>, 1, threads, threads / 32 * plan.experts * 2, st, p);
+  }
   const cudaError_t e = launch_pdl(plan_count_kernel, blocks, kPlanThreads, 0, st, p);
   return e == cudaSuccess ? launch_pdl(plan_place_kernel<false>, blocks, kPlanThreads, smem, st, p) : e;
 }

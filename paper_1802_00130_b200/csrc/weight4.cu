@@ -144,10 +144,12 @@ const char* ffn4_args(const gn_ffn4* f) {
   return nullptr;
 }
 struct Few4 { ExpertPlan plan; void *x, *h; float* out; int64_t ld_x, ld_h, ld_out; int tile; };
-// Tokens of a plan's tile: eight (five in FP32, whose operands are three rows each) where that is what the experts that can have one have on average, else twice as many.
+// Tokens of a plan's tile, whose operand rows (two a token in the second product, three in FP32) are eight columns of the tensor core, 16 or 32: for twice what the experts
+// that can have one have on average.
 int tile_tokens(int64_t pairs, int experts, bool f32) {
-  const bool few = pairs <= 4 * (pairs < experts ? pairs : (int64_t)experts);
-  return f32 ? (few ? 5 : 10) : few ? 8 : 16;
+  const int64_t some = pairs < experts ? pairs : (int64_t)experts;
+  if (f32) return pairs <= some ? 2 : 2 * pairs <= 5 * some ? 5 : 10;
+  return pairs <= 2 * some ? 4 : pairs <= 4 * some ? 8 : 16;
 }
 int64_t lay_out(const gn_ffn4& f, char* base, Few4& w) {
   Workspace ws{base};
@@ -156,7 +158,7 @@ int64_t lay_out(const gn_ffn4& f, char* base, Few4& w) {
   w = Few4{};
   w.tile = tile_tokens(pairs, f.experts, f32);
   w.ld_x = up8(f.cols); w.ld_h = up8(f.inner); w.ld_out = up8(f.cols);
-  if (f32) w.x = ws.take(3 * f.tokens * w.ld_x * 2);
+  if (!operands_ok(f.x.p, f.x.ld, f.cols, type_bytes(f.type))) w.x = ws.take((f32 ? 3 : 1) * f.tokens * w.ld_x * 2);
   w.h = ws.take((f32 ? 3 : 2) * pairs * w.ld_h * 2);
   if (f.index) {
     w.plan = plan_at((int*)ws.take(plan_ints(pairs, f.experts, w.tile) * 4), pairs, f.experts, w.tile);
@@ -171,7 +173,7 @@ cudaError_t run_ffn4(const gn_ffn4& f, const Few4& w, cudaStream_t st) {
   a.rows = f.inner; a.cols = f.cols; a.group = b.group = f.group; a.act = f.act; a.tokens = b.tokens = f.tokens; a.k = b.k = f.k; a.tile_tokens = b.tile_tokens = w.tile;
   a.gate = true; a.x = f.x.p; a.ldx = f.x.ld; a.token_rows = true;
   if (w.x) {
-    if (e == cudaSuccess) e = launch_parts((const float*)f.x.p, f.x.ld, f.tokens, f.cols, w.x, w.ld_x, st);
+    if (e == cudaSuccess) e = launch_operands(f.x.p, f.x.ld, f.tokens, f.cols, type_bytes(f.type), w.x, st);
     a.x = w.x; a.ldx = w.ld_x; a.part_stride = f.tokens * w.ld_x;
   }
   a.w[0] = {(const uint8_t*)f.q_gate, f.s_gate}; a.w[1] = {(const uint8_t*)f.q_up, f.s_up};
@@ -211,15 +213,15 @@ extern "C" gn_status gn_unpack4(gn_dtype type, int32_t experts, int64_t rows, in
                                 void* cuda_stream, char* errbuf, int64_t errbuf_len) {
   return layout4(2, type, experts, rows, cols, group, nullptr, ld, stride, nullptr, const_cast<void*>(d_q), const_cast<void*>(d_scale), d_w, cuda_stream, errbuf, errbuf_len);
 }
-extern "C" int64_t gn_matvec4_workspace(gn_dtype type, int64_t tokens, int64_t cols) {
+extern "C" int64_t gn_matvec4_workspace(gn_dtype type, int64_t tokens, int64_t cols, const void* d_x, int64_t ldx) {
   if (!type_ok(type) || tokens < 0 || tokens >= (1 << 20) || cols < 1 || cols > (1 << 20)) return -1;
-  return type == GN_F32 ? 3 * tokens * up8(cols) * 2 : 0;
+  return operands_ok(d_x, ldx, cols, type_bytes(type)) ? 0 : (type == GN_F32 ? 3 : 1) * tokens * up8(cols) * 2;
 }
 extern "C" gn_status gn_matvec4(gn_dtype type, int64_t tokens, int64_t rows, int64_t cols, int32_t group, const void* d_x, int64_t ldx, const void* d_q, const void* d_scale,
                                 void* d_y, int64_t ldy, void* d_ws, int64_t ws_bytes, void* cuda_stream, char* errbuf, int64_t errbuf_len) {
   const char* why = sizes4(type, 1, rows, cols, group);
   if (!why) {
-    const int64_t need = gn_matvec4_workspace(type, tokens, cols);
+    const int64_t need = gn_matvec4_workspace(type, tokens, cols, d_x, ldx);
     if (need < 0) why = "tokens must be in [0, 2^20)";
     else if (!packed_ok(d_q, d_scale)) why = kPackedWhy;
     else if (tokens > 0 && !mat_ok(d_x, ldx, cols, type)) why = "x: null, misaligned, or a leading dimension below cols";
@@ -232,8 +234,8 @@ extern "C" gn_status gn_matvec4(gn_dtype type, int64_t tokens, int64_t rows, int
   Product4 p;
   p.rows = (int)rows; p.cols = (int)cols; p.group = group; p.tokens = tokens; p.x = d_x; p.ldx = ldx; p.w[0] = {(const uint8_t*)d_q, d_scale}; p.d = d_y; p.ldd = ldy;
   cudaError_t e = cudaSuccess;
-  if (type == GN_F32) {
-    e = launch_parts((const float*)d_x, ldx, tokens, (int)cols, d_ws, up8(cols), st);
+  if (!operands_ok(d_x, ldx, cols, type_bytes(type))) {
+    e = launch_operands(d_x, ldx, tokens, (int)cols, type_bytes(type), d_ws, st);
     p.x = d_ws; p.ldx = up8(cols); p.part_stride = tokens * up8(cols);
   }
   return op_done(e == cudaSuccess ? launch_product4(type, p, st) : e, errbuf, errbuf_len);

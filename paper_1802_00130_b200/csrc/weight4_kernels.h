@@ -15,7 +15,7 @@ inline int64_t w4_bytes(int64_t rows, int64_t cols) { return w4_tiles(rows) * w4
 inline int64_t w4_scales(int64_t rows, int64_t cols, int group) { return w4_tiles(rows) * w4_blocks(cols) * 16 * (128 / group); }          // of an expert
 
 // d [tokens][rows] = x w^T.  gate: w[0] and w[1], d = act(.) * (.).
-//   x        16-bit operands: tokens of the type; or `parts` BF16 rows that add up to each token, part_stride apart
+//   x        16-bit operands in rows that start on 16 bytes and are whole eights, zero past `cols`: tokens of the type; or BF16 rows that add up to each token, part_stride apart
 //   d        of the type, or (d32) FP32; gate: BF16 parts that add up to it, two or (FP32) three, part_stride_d apart
 struct Product4 {
   int rows = 0, cols = 0, group = 128, act = 0;
@@ -31,7 +31,8 @@ inline int w4_parts(bool f32, bool in_parts) { return f32 ? 3 : in_parts ? 2 : 1
 cudaError_t launch_product4_f32(const Product4& p, cudaStream_t st);
 cudaError_t launch_product4_bf16(const Product4& p, cudaStream_t st);
 cudaError_t launch_product4_f16(const Product4& p, cudaStream_t st);
-// FP32 rows as three BF16 ones: to [3][rows][ld_out], ld_out a multiple of 8.
-cudaError_t launch_parts(const float* x, int64_t ldx, int64_t rows, int cols, void* to, int64_t ld_out, cudaStream_t st);
+// Rows of tokens as operands: 16-bit ones as they are, FP32 ones in three BF16 parts: to [1 or 3][rows][ld_out], ld_out = cols rounded up to 8.  operands_ok: they are that already.
+inline bool operands_ok(const void* x, int64_t ldx, int64_t cols, int bytes) { return bytes == 2 && ((uintptr_t)x & 15) == 0 && ldx % 8 == 0 && cols % 8 == 0; }
+cudaError_t launch_operands(const void* x, int64_t ldx, int64_t rows, int cols, int bytes, void* to, cudaStream_t st);
 
 }  // namespace gn

@@ -22,7 +22,7 @@ namespace {
 
 constexpr int Q_WARPS = 8, Q_THREADS = 32 * Q_WARPS;           // of a block at most
 struct Product4Params {
-  int rows, cols, act, kblocks, tiles, split, log_split, log_block, early, vec, k, token_rows, tokens;
+  int rows, cols, act, kblocks, tiles, split, log_split, log_block, early, k, token_rows, tokens;
   const void* x; int64_t ldx, part_stride;
   const uint8_t* q[2]; const void* scale[2];
   int64_t q_stride, scale_stride;    // from expert to expert
@@ -55,18 +55,10 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
 }
 
-// Eight neighbouring columns of a row of operands; zeros past its end, or without a row.  WHOLE: all of them are there, as 16 bytes.
-template <bool WHOLE, class O>
+// Eight neighbouring columns of a row of operands, which starts on 16 bytes and has whole eights (zero past its end).
+template <class O>
 __device__ __forceinline__ uint4 load_eight(const O* row, int c, int cols) {
-  if constexpr (WHOLE) return row ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
-  const int left = row ? cols - c : 0;
-  uint32_t o[4] = {0u, 0u, 0u, 0u};
-  if (left > 0) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < left) o[e >> 1] |= (uint32_t) * reinterpret_cast<const uint16_t*>(row + c + e) << (16 * (e & 1));
-  }
-  return make_uint4(o[0], o[1], o[2], o[3]);
+  return row && c < cols ? *reinterpret_cast<const uint4*>(row + c) : make_uint4(0u, 0u, 0u, 0u);
 }
 // An FP32 number as PARTS BF16 numbers that add up to it: the leading 8 bits of what is left, cut off, three times (exact), or once and the rest rounded.
 // Infinities leave nothing.
@@ -94,7 +86,7 @@ template <class T, int G, int NT, int M> constexpr int q_smem = q_ring<T, G, M> 
 
 // T: type of the scales and of the result; O: of the operands; PARTS columns to a token; G groups of a record; NT tiles of eight columns; M matrices (2: gate).
 template <class T, class O, int PARTS, int G, int NT, int M>
-__global__ void __launch_bounds__(Q_THREADS, NT * M <= 2 ? 3 : 2) product4_kernel(const __grid_constant__ Product4Params p) {
+__global__ void __launch_bounds__(Q_THREADS, NT * M == 1 ? 3 : 2) product4_kernel(const __grid_constant__ Product4Params p) {
   constexpr int COLUMNS = 8 * NT, TOKENS = COLUMNS / PARTS, STAGES = q_stages<M>, PIECE = q_piece<T, G, M>, SCALE_UNITS = G * (int)sizeof(T);
   static_assert(M * SCALE_UNITS <= 32, "a lane copies one unit of the scales");
   extern __shared__ __align__(16) uint8_t smem[];
@@ -172,15 +164,26 @@ __global__ void __launch_bounds__(Q_THREADS, NT * M <= 2 ? 3 : 2) product4_kerne
   float acc[M][NT][4] = {};
   if (on) {
     int stage = 0;
-    // one record: its sums, group by group
-    const auto record = [&](int kb, auto whole) {
-      constexpr bool WHOLE = decltype(whole)::value != 0;
-      uint4 x[NT == 1 ? 4 : 1][NT];
-      const int c0 = kb * 128 + t * 8;
-      if constexpr (NT == 1) {       // (on their way while the record is)
+    // Eight tokens' columns of the next record (of two matrices: with one the loads ahead took longer, 35 us instead of 25 for 16384 x 8192).
+    uint4 ahead[NT == 1 ? 4 : 1];
+    const auto look_ahead = [&](int kb) {
+      if constexpr (NT == 1 && M == 2) {
 #pragma unroll
-        for (int b = 0; b < 4; ++b) x[b][0] = load_eight<WHOLE>(row[0], c0 + b * 32, p.cols);
+        for (int b = 0; b < 4; ++b) ahead[b] = load_eight(row[0], kb * 128 + b * 32 + t * 8, p.cols);
       }
+    };
+    look_ahead(slice);
+#pragma unroll 1
+    for (int kb = slice; kb < p.kblocks; kb += p.split) {
+      // The tokens' columns: of the whole record, or (many tokens) of a quarter of it and the next.
+      constexpr int QUARTERS = NT <= 2 ? 4 : 2;
+      uint4 x[QUARTERS][NT];
+      const int c0 = kb * 128 + t * 8;
+#pragma unroll
+      for (int b = 0; b < (NT <= 2 ? 4 : 1); ++b)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) x[b][n] = NT == 1 && M == 2 ? ahead[b] : load_eight(row[n], c0 + b * 32, p.cols);
+      look_ahead(kb + p.split);
       asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
       __syncwarp();
       request(stage == 0 ? STAGES - 1 : stage - 1);
@@ -195,9 +198,9 @@ __global__ void __launch_bounds__(Q_THREADS, NT * M <= 2 ? 3 : 2) product4_kerne
       float part[CHAINS][M][NT][4];
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        if constexpr (NT > 1) {
+        if (NT > 2 && b < 3) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n) x[0][n] = load_eight<WHOLE>(row[n], c0 + b * 32, p.cols);
+          for (int n = 0; n < NT; ++n) x[(b + 1) % QUARTERS][n] = load_eight(row[n], c0 + (b + 1) * 32, p.cols);
         }
         const bool more = b % (4 / G) >= CHAINS;
         uint32_t a[M][2][4];
@@ -212,7 +215,7 @@ __global__ void __launch_bounds__(Q_THREADS, NT * M <= 2 ? 3 : 2) product4_kerne
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           if (NT > 1 && 8 * n >= columns) break;
-          const uint4 y = x[NT == 1 ? b : 0][n];
+          const uint4 y = x[b % QUARTERS][n];
 #pragma unroll
           for (int m = 0; m < M; ++m) {
             float (&sum)[4] = part[b % CHAINS][m][n];
@@ -238,13 +241,7 @@ __global__ void __launch_bounds__(Q_THREADS, NT * M <= 2 ? 3 : 2) product4_kerne
         }
       }
       if (++stage == STAGES) stage = 0;
-    };
-    const int whole = p.vec ? p.cols / 128 : 0;            // records of whole columns that can be loaded as 16 bytes
-    int kb = slice;
-#pragma unroll 1
-    for (; kb < whole; kb += p.split) record(kb, ActIs<1>{});
-#pragma unroll 1
-    for (; kb < p.kblocks; kb += p.split) record(kb, ActIs<0>{});
+    }
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   __syncthreads();                   // (the rings are free)
@@ -260,7 +257,7 @@ __global__ void __launch_bounds__(Q_THREADS, NT * M <= 2 ? 3 : 2) product4_kerne
   for (int i = threadIdx.x; i < tokens << (4 + p.log_block); i += blockDim.x) {
     const int r = i & 15, in = (i >> 4) & ((1 << p.log_block) - 1), c = i >> (4 + p.log_block);
     const int at = ((blockIdx.x << p.log_block) + in) * 16 + r;
-    if (at >= p.rows) continue;
+    if (at >= (M == 2 ? (p.rows + 7) / 8 * 8 : p.rows)) continue;     // (rows of operands are whole eights: what is past the end is 0, as its weights are)
     float s[M];
 #pragma unroll
     for (int m = 0; m < M; ++m) {
@@ -294,7 +291,7 @@ cudaError_t launch_product4_as(const Product4& a, cudaStream_t st) {
   p.rows = a.rows; p.cols = a.cols; p.act = a.act; p.kblocks = (int)w4_blocks(a.cols); p.tiles = (int)w4_tiles(a.rows);
   p.early = a.early; p.k = a.k; p.token_rows = a.token_rows; p.tokens = (int)a.tokens; p.x = a.x; p.ldx = a.ldx; p.part_stride = a.part_stride;
   p.d = a.d; p.ldd = a.ldd; p.d32 = a.d32; p.part_stride_d = a.part_stride_d;
-  p.vec = ((uintptr_t)a.x & 15) == 0 && a.ldx % 8 == 0 && a.part_stride % 8 == 0;
+  if (((uintptr_t)a.x & 15) || a.ldx % 8 || a.part_stride % 8) return cudaErrorInvalidValue;
   for (int m = 0; m < M; ++m) { p.q[m] = a.w[m].q; p.scale[m] = a.w[m].scale; }
   p.q_stride = w4_bytes(a.rows, a.cols); p.scale_stride = w4_scales(a.rows, a.cols, a.group);
   int64_t columns, busy;             // tiles of columns, and how many of them there are about
@@ -305,9 +302,9 @@ cudaError_t launch_product4_as(const Product4& a, cudaStream_t st) {
   } else {
     busy = columns = (a.tokens + 8 * NT / PARTS - 1) / (8 * NT / PARTS);
   }
-  // Warps to a tile: as many as the SMs have room for at once, 24 each (a few blocks too many would take as long again), of two records each at least.
+  // Warps to a tile: as many as the SMs have room for at once, 24 or 16 each (a few blocks too many would take as long again), of two records each at least.
   int log_split = 0;
-  while ((2 << log_split) <= Q_WARPS && (4 << log_split) <= p.kblocks && p.tiles * busy * (2 << log_split) <= 24LL * num_sms()) ++log_split;
+  while ((2 << log_split) <= Q_WARPS && (4 << log_split) <= p.kblocks && p.tiles * busy * (2 << log_split) <= (NT * M == 1 ? 24LL : 16LL) * num_sms()) ++log_split;
   p.split = 1 << log_split;
   const int warps = p.split > 4 ? p.split : 4, per_block = warps / p.split;
   p.log_split = log_split; p.log_block = log_split >= 2 ? 0 : 2 - log_split;

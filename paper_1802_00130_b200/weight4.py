@@ -139,9 +139,9 @@ def matvec4(x, w, stream=None):
     px, ldx = _matrix(x, "x", tokens, cols, dtype, dev)
     y = x.new_empty(tokens, w.rows)
     ws, n = 0, 0
-    if dtype is torch.float32:
-        n = lib().gn_matvec4_workspace(0, tokens, cols)
-        room = x.new_empty(max(n, 16) // 4)
+    if dtype is torch.float32 or cols & 7 or ldx & 7 or px & 15:
+        n = lib().gn_matvec4_workspace(_TYPES[dtype], tokens, cols, px, ldx)
+        room = x.new_empty(max(n, 16) // x.element_size())
         ws = room.data_ptr()
     err = _err()
     status = lib().gn_matvec4(_TYPES[dtype], tokens, w.rows, cols, w.group, px, ldx, pq, ps, y.data_ptr(), w.rows, ws, n, _raw_stream(dev), err, 200)

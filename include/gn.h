@@ -628,7 +628,9 @@ typedef struct { void* p; int64_t ld, stride; } gn_stack;   /* a matrix of every
  *     dWg_e = sum dgate x_t^T,   dWu_e = sum dup x_t^T,   dWd_e = sum weight dy_t h^T   over the pairs of expert e (zero without any).
  *   dy, x, index, weight, gate, up and the weights are inputs; dx, dweight [tokens][k] (0 where there is no expert), dw_gate, dw_up, dw_down are outputs, each NULL where
  *   it is not wanted.
- * GN_BF16, GN_F16: h, weight h, dup and dgate are rounded to the type on their way into the next product, everything else is FP32 until it is a result; what is said of GN_F16's range at gn_gated_ffn holds here.  GN_F32: sums of FP32 products.
+ * GN_BF16, GN_F16: h, weight h, dup and dgate are rounded to the type on their way into the next product, everything else is FP32 until it is a result; what is
+ * said of GN_F16's range at gn_gated_ffn holds here.  GN_F32: products at FP32 accuracy, by size on FMAs or on the tensor cores in three BF16 parts of each
+ * operand, where an infinite element gives NaN.
  * A bounded wait that ran out shows in gn_gated_ffn_status.
  * Workspace: gn_experts_workspace(args, backward) bytes for the same args; it depends on sizes, types, leading dimensions, strides and on the alignment of
  * the pointers, and is negative for bad arguments.

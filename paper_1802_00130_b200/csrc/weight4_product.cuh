@@ -7,6 +7,8 @@
 // again as 16-bit weights.  A second product, of the tokens with 136, in the place of the operands' subtractions took longer: 31 against 25 us for a token
 // through 4096 x 8192.)
 //
+// Measured in a graph: one BF16 token by 8192 x 4096 7.5 us (17 MB; the same stream without the products 3.8), by 16384 x 8192 25 (16), through a layer of 4096 x 8192 22 (13), 8
+// tokens through that layer 24, 16 tokens 33, 32 tokens 64; 8 FP16 tokens through 8 of 64 experts of 2048 x 1024 49 (140 MB).
 // FP32 tokens are columns of three BF16 parts of eight bits each, exact; the hidden units of a gated layer of two (17 bits) where the result is rounded to 16
 // bits, as the first kernel has written them.
 // Four or eight warps share a block: W of them a tile of 16 rows (of both matrices, gate), each with every W-th record; their sums are added in order in shared memory.  W is

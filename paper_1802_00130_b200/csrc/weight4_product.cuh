@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(Q_THREADS, NT * M == 1 ? 3 : 2) product4_kerne
   for (int i = threadIdx.x; i < tokens << (4 + p.log_block); i += blockDim.x) {
     const int r = i & 15, in = (i >> 4) & ((1 << p.log_block) - 1), c = i >> (4 + p.log_block);
     const int at = ((blockIdx.x << p.log_block) + in) * 16 + r;
-    if (at >= (M == 2 ? (p.rows + 7) / 8 * 8 : p.rows)) continue;     // (rows of operands are whole eights: what is past the end is 0, as its weights are)
+    if (at >= (M == 2 ? (p.rows + 7) / 8 * 8 : p.rows)) continue;     // (rows of operands are whole eights: what is past the end is 0, an infinite token's too)
     float s[M];
 #pragma unroll
     for (int m = 0; m < M; ++m) {
@@ -275,6 +275,7 @@ __global__ void __launch_bounds__(Q_THREADS, NT * M == 1 ? 3 : 2) product4_kerne
       with_activation(p.act, [&](auto act) {
         float h, unused;
         activation<decltype(act)::value, sizeof(T) == 2>(s[0], h, unused);
+        if (at >= p.rows) h = s[1] = 0.f;
         __nv_bfloat16 o[OUT];
         split_parts<OUT>(h * s[1], o);
 #pragma unroll

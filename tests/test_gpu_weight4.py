@@ -168,3 +168,18 @@ def test_refusals():
                  lambda: gn.quantize4(x.double()), lambda: gn.quantize4(x.cpu()), lambda: gn.unpack4(x)):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("inner", [1, 17, 64])
+def test_infinite_tokens_through_a_layer(t, inner):
+    """Positive weights alone, so that no infinity meets a zero or its opposite: the result is infinite too, whatever is past the last hidden unit."""
+    t = TYPES[t]
+    ones = lambda *shape: gn.pack4(torch.full(shape, 9, device="cuda", dtype=torch.uint8), torch.ones(*shape[:-1], -(-shape[-1] // 64), device="cuda", dtype=t), 64)
+    x = torch.full((3, 40), 0.25, device="cuda", dtype=t)
+    x[1, 7] = math.inf
+    y = gn.gated_ffn4(x, ones(inner, 40), ones(inner, 40), ones(40, inner), "relu")
+    assert bool((y[1] == math.inf).all()) and bool((y[::2] == torch.tensor(100.0 * inner, dtype=t)).all())
+    index, weight = torch.tensor([[0], [1], [1]], device="cuda", dtype=torch.int32), torch.ones(3, 1, device="cuda")
+    y = gn.gated_ffn4(x, ones(2, inner, 40), ones(2, inner, 40), ones(2, 40, inner), "relu", index, weight)
+    assert bool((y[1] == math.inf).all()) and bool(y[::2].isfinite().all())

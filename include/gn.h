@@ -676,7 +676,7 @@ gn_status gn_unpack4(gn_dtype type, int32_t experts, int64_t rows, int64_t cols,
                      int64_t ld, int64_t stride, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 
 /*
- * gn_matvec4 - y [tokens][rows] = x [tokens][cols] W^T of packed weights W [rows][cols].  Meant for a few tokens; any number below 2^20 is taken, 32 at a time.
+ * gn_matvec4 - y [tokens][rows] = x [tokens][cols] W^T of packed weights W [rows][cols].  Meant for a few tokens; any number below 2^19 is taken, 32 at a time.
  * Products of the type's numbers and whole q - 8, summed in FP32 group by group, times the scale; FP32 tokens lose nothing.
  * Workspace: gn_matvec4_workspace(type, tokens, cols, d_x, ldx) bytes; none for 16-bit tokens whose rows start on 16 bytes and have a multiple of 8 columns.
  */
@@ -687,7 +687,7 @@ gn_status gn_matvec4(gn_dtype type, int64_t tokens, int64_t rows, int64_t cols, 
 /*
  * gn_gated_ffn4 - gn_gated_ffn, or with an index gn_experts, on packed weights: q_gate, q_up [experts][inner][cols] and q_down [experts][cols][inner] with their scales.
  *   index, weight   [tokens][k] as in gn_experts, or both NULL with experts == 1 and k == 1: y = ffn(x).
- * The hidden units go to the second product as 17 bits of FP32 (24 in GN_F32) whatever the type; y is rounded once.  tokens * k < 2^20.
+ * The hidden units go to the second product as 17 bits of FP32 (24 in GN_F32) whatever the type; y is rounded once.  tokens * k < 2^19.
  */
 typedef struct {
   int32_t type, act;          /* gn_dtype, gn_act */

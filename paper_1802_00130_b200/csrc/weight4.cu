@@ -133,7 +133,7 @@ const char* ffn4_args(const gn_ffn4* f) {
   const char* why = sizes4(f->type, f->experts, f->inner, f->cols, f->group);
   if (why) return why;
   if (f->k < 1 || f->k > 32) return "k must be in [1, 32]";
-  if (f->tokens < 0 || f->tokens >= (1 << 20) / f->k) return "tokens times k must be in [0, 2^20)";
+  if (f->tokens < 0 || f->tokens >= kMostTokens4 / f->k) return "tokens times k must be in [0, 2^19)";
   if (f->tokens > 0 && !f->index && (f->experts != 1 || f->k != 1)) return "without an index there is one expert, and one choice";
   if (!packed_ok(f->q_gate, f->s_gate) || !packed_ok(f->q_up, f->s_up) || !packed_ok(f->q_down, f->s_down)) return kPackedWhy;
   if (f->tokens == 0) return nullptr;
@@ -214,7 +214,7 @@ extern "C" gn_status gn_unpack4(gn_dtype type, int32_t experts, int64_t rows, in
   return layout4(2, type, experts, rows, cols, group, nullptr, ld, stride, nullptr, const_cast<void*>(d_q), const_cast<void*>(d_scale), d_w, cuda_stream, errbuf, errbuf_len);
 }
 extern "C" int64_t gn_matvec4_workspace(gn_dtype type, int64_t tokens, int64_t cols, const void* d_x, int64_t ldx) {
-  if (!type_ok(type) || tokens < 0 || tokens >= (1 << 20) || cols < 1 || cols > (1 << 20)) return -1;
+  if (!type_ok(type) || tokens < 0 || tokens >= kMostTokens4 || cols < 1 || cols > (1 << 20)) return -1;
   return operands_ok(d_x, ldx, cols, type_bytes(type)) ? 0 : (type == GN_F32 ? 3 : 1) * tokens * up8(cols) * 2;
 }
 extern "C" gn_status gn_matvec4(gn_dtype type, int64_t tokens, int64_t rows, int64_t cols, int32_t group, const void* d_x, int64_t ldx, const void* d_q, const void* d_scale,
@@ -222,7 +222,7 @@ extern "C" gn_status gn_matvec4(gn_dtype type, int64_t tokens, int64_t rows, int
   const char* why = sizes4(type, 1, rows, cols, group);
   if (!why) {
     const int64_t need = gn_matvec4_workspace(type, tokens, cols, d_x, ldx);
-    if (need < 0) why = "tokens must be in [0, 2^20)";
+    if (need < 0) why = "tokens must be in [0, 2^19)";
     else if (!packed_ok(d_q, d_scale)) why = kPackedWhy;
     else if (tokens > 0 && !mat_ok(d_x, ldx, cols, type)) why = "x: null, misaligned, or a leading dimension below cols";
     else if (tokens > 0 && !mat_ok(d_y, ldy, rows, type)) why = "y: null, misaligned, or a leading dimension below rows";

@@ -7,6 +7,9 @@
 
 namespace gn {
 
+// Tokens of a call stay below this: ten to a tile (FP32), and two tiles for an expert's last, are fewer tiles than a grid has in its second dimension.
+constexpr int kMostTokens4 = 1 << 19;
+static_assert(kMostTokens4 / 10 + 1 + kMostExperts <= 65535, "tiles of tokens fit a grid");
 // 4-bit weights of one matrix [rows][cols], or of every expert's, as they are laid out: see gn.h.
 struct Weight4 { const uint8_t* q = nullptr; const void* scale = nullptr; };
 inline int64_t w4_tiles(int64_t rows) { return (rows + 15) / 16; }

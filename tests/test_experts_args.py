@@ -181,3 +181,13 @@ def test_4_bit_weights_without_a_device():
     for call in (lambda: gn.pack4(q, q.float()), lambda: gn.quantize4(q.float())):
         with pytest.raises(TypeError, match="CUDA"):
             call()
+
+
+def test_4_bit_calls_take_fewer_than_2_to_the_19_tokens():
+    """Their tiles are the second dimension of a grid: what is taken fits, whatever the type."""
+    lib, most = gn.lib(), 1 << 19
+    for type in (0, 1, 2):
+        assert lib.gn_matvec4_workspace(type, most - 1, 40, P, 40) >= 0 and lib.gn_matvec4_workspace(type, most, 40, P, 40) < 0
+        assert "tokens" in refused(lib.gn_matvec4, type, most, 20, 40, 32, P, 40, P, P, P, 20, P, 1 << 40, None)
+        for k in (1, 2):
+            assert lib.gn_gated_ffn4_workspace(ffn4(type=type, k=k, tokens=most // k - 1)) > 0 and lib.gn_gated_ffn4_workspace(ffn4(type=type, k=k, tokens=most // k)) < 0

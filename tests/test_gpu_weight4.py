@@ -183,3 +183,21 @@ def test_infinite_tokens_through_a_layer(t, inner):
     index, weight = torch.tensor([[0], [1], [1]], device="cuda", dtype=torch.int32), torch.ones(3, 1, device="cuda")
     y = gn.gated_ffn4(x, ones(2, inner, 40), ones(2, inner, 40), ones(2, 40, inner), "relu", index, weight)
     assert bool((y[1] == math.inf).all()) and bool(y[::2].isfinite().all())
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_the_most_tokens(t):
+    t, n = TYPES[t], (1 << 19) - 1
+    q, scale = quarters((24, 40), 32, t, 1)
+    x = rand((n, 40), t, 2)
+    ref, err = product(x.double(), values(q, scale, 32), 0, 0)
+    within(gn.matvec4(x, gn.pack4(q, scale, 32)), ref, err + u(t) * ref.abs() + tiny(t), "y")
+    # (one record a row, so that every token's sums have one order in any call)
+    w = [gn.pack4(*quarters(s, 32, t, 3), 32) for s in ((17, 40), (17, 40), (40, 17))]
+    y = gn.gated_ffn4(x, *w)
+    for part in (slice(0, 50), slice(n // 2, n // 2 + 50), slice(n - 50, n)):
+        assert torch.equal(y[part], gn.gated_ffn4(x[part], *w))
+    w, (index, weight) = [gn.pack4(*quarters((3, *s), 32, t, 3), 32) for s in ((17, 40), (17, 40), (40, 17))], choices(n // 2, 3, 2)
+    y = gn.gated_ffn4(x[: n // 2], *w, index=index, weight=weight)
+    for part in (slice(0, 50), slice(n // 2 - 50, n // 2)):
+        assert torch.equal(y[part], gn.gated_ffn4(x[part], *w, index=index[part], weight=weight[part]))

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import struct
 from array import array
+from numbers import Real
 
 import torch
 
@@ -47,7 +48,13 @@ def _choices(index, tokens):
 
 def _bits(scale):
     """A float as a 64-bit word."""
-    return _ONE if scale == 1.0 else struct.unpack("q", struct.pack("d", scale))[0]
+    if type(scale) is float and scale == 1.0:
+        return _ONE
+    if isinstance(scale, bool) or not isinstance(scale, Real):
+        raise TypeError(f"scale: expected a number, got {type(scale).__name__}")
+    if abs(scale) > 1e300:
+        scale = float("inf")         # (which the library refuses; a whole number may be too large for a float)
+    return struct.unpack("q", struct.pack("d", scale))[0]
 
 
 def _whole(value, what):

@@ -21,13 +21,24 @@ from .feedforward import _TYPES, ACTIVATIONS, _checked, _device, _elsewhere, _er
 
 @dataclass(frozen=True)
 class Weight4:
-    """4-bit weights of one matrix [rows][cols] (experts: None) or of every expert's, in the library's layout; made by pack4 and quantize4."""
+    """4-bit weights of one matrix [rows][cols] (experts: None) or of every expert's, in the library's layout; made by pack4 and quantize4, or of what they have made (a
+    copy on another device, a file)."""
     q: torch.Tensor
     scale: torch.Tensor
     experts: int | None
     rows: int
     cols: int
     group: int
+
+    def __post_init__(self):
+        """The products read as many bytes as the sizes say."""
+        if not isinstance(self.q, torch.Tensor) or self.q.dtype is not torch.uint8 or not isinstance(self.scale, torch.Tensor) or self.scale.dtype not in _TYPES:
+            raise TypeError("expected q as uint8 and scale as float32, bfloat16 or float16 tensors")
+        n, rows, cols = 1 if self.experts is None else _whole(self.experts, "experts"), _whole(self.rows, "rows"), _whole(self.cols, "cols")
+        bytes_, scales = lib().gn_weight4_bytes(n, rows, cols), lib().gn_weight4_scales(n, rows, cols, _whole(self.group, "group"))
+        if scales < 0 or (self.q.numel(), self.scale.numel()) != (bytes_, scales) or not self.q.is_contiguous() or not self.scale.is_contiguous():
+            raise ValueError(f"expected {bytes_} consecutive bytes and {scales} consecutive scales for {self.shape} in groups of {self.group}, "
+                             f"got {self.q.numel()} and {self.scale.numel()}")
 
     @property
     def shape(self):
@@ -100,6 +111,8 @@ def quantize4(w, group=128, stream=None):
 def _weight4(w, what, dtype=None, dev=None):
     if not isinstance(w, Weight4):
         raise TypeError(f"{what}: expected a Weight4, got {type(w).__name__}")
+    if dtype is None and not 0 <= w.q.get_device() == w.scale.get_device():
+        raise TypeError(f"{what}: expected CUDA tensors of one device, got {w.q.device} and {w.scale.device}")
     if dtype is not None and (w.scale.dtype is not dtype or w.q.get_device() != dev or w.scale.get_device() != dev):
         raise TypeError(f"{what}: expected scales of {dtype} on cuda:{dev}, got {w.scale.dtype} on {w.device}")
     return w.q.data_ptr(), w.scale.data_ptr()

@@ -191,3 +191,18 @@ def test_4_bit_calls_take_fewer_than_2_to_the_19_tokens():
         assert "tokens" in refused(lib.gn_matvec4, type, most, 20, 40, 32, P, 40, P, P, P, 20, P, 1 << 40, None)
         for k in (1, 2):
             assert lib.gn_gated_ffn4_workspace(ffn4(type=type, k=k, tokens=most // k - 1)) > 0 and lib.gn_gated_ffn4_workspace(ffn4(type=type, k=k, tokens=most // k)) < 0
+
+
+def test_4_bit_weights_have_the_bytes_of_their_sizes():
+    q, scale = torch.zeros(2 * 2 * 1024, dtype=torch.uint8), torch.zeros(2 * 2 * 64)
+    w = gn.Weight4(q, scale, None, 17, 129, 32)
+    assert w.shape == (17, 129) and gn.Weight4(q, scale, 2, 16, 129, 32).shape == (2, 16, 129)
+    for bad in ((q[1:], scale, None, 17, 129, 32), (q, scale[1:], None, 17, 129, 32), (q, scale, None, 33, 129, 32), (q, scale, None, 17, 257, 32), (q, scale, 2, 17, 129, 32), (q, scale, None, 17, 129, 64),
+                (q, scale, None, 17, 129, 48), (q, scale, None, 0, 129, 32), (q, scale, 0, 17, 129, 32), (q, scale, None, 1 << 40, 129, 32), (torch.zeros(4096, 2, dtype=torch.uint8)[:, 0], scale, None, 17, 129, 32)):
+        with pytest.raises(ValueError):
+            gn.Weight4(*bad)
+    for bad in ((q.int(), scale, None, 17, 129, 32), (q, scale.double(), None, 17, 129, 32), (q, None, None, 17, 129, 32), (q, scale, None, 17.0, 129, 32), (q, scale, 1.0, 17, 129, 32)):
+        with pytest.raises(TypeError):
+            gn.Weight4(*bad)
+    with pytest.raises(TypeError, match="CUDA"):
+        gn.unpack4(w)

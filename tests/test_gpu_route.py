@@ -281,3 +281,14 @@ def test_refusals():
                  lambda: gn.route(logits, 4, group_best=3), lambda: gn.route(logits, 4, scale=math.inf)):
         with pytest.raises(gn.GnError):
             call()
+
+
+def test_a_scale_is_a_number():
+    logits = rand((4, 16), torch.float32, 1)
+    assert torch.equal(gn.route(logits, 2, scale=2)[1], gn.route(logits, 2, scale=2.0)[1])
+    for bad in ("1", None, True, torch.ones(1), 1j):
+        with pytest.raises(TypeError, match="scale"):
+            gn.route(logits, 2, scale=bad)
+    for bad in (10 ** 400, -1e301, math.nan, math.inf):
+        with pytest.raises(gn.GnError, match="scale"):
+            gn.route(logits, 2, scale=bad)

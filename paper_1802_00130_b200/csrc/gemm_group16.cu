@@ -16,8 +16,8 @@
 // that of their own rounding instead of 1.4.)
 // GROUP_GRAD's sums for the gradient of the routing weights stay FP32: a thread has 64 columns of its row, their sums are added in order elsewhere.
 // Bound, with all pairs at work, by what L2 gives to shared memory: 32 KB a CTA for 64 terms, 0.37 us (13 TB/s), where the products take 0.27; and by the power cap.
-// 8192 tokens, 4 of 64 experts, 2048 x 1408: gate 361 us (1047 TFLOP/s, a fifth of the rows padding), with Wd 185; 4 of 32, 2048 x 1024: gate's gradient 212, dx 227, three
-// weight gradients 354.  16 tokens, 4 of 32 experts: 48 and 28, the weights at 4.7 TB/s (224 tiles are 3.03 rounds of the pairs).
+// 8192 tokens, 4 of 64 experts, 2048 x 1408: gate 361 us (1047 TFLOP/s, a fifth of the rows padding), with Wd 185; 4 of 32, 2048 x 1024: gate's gradient 172, dx 213, three
+// weight gradients 315.  16 tokens, 4 of 32 experts: 48 and 28, the weights at 4.7 TB/s (224 tiles are 3.03 rounds of the pairs).
 // Every wait is bounded; a role that gives up leaves a code in *err and the CTA drains.
 #include "expert_kernels.h"
 #include "pair_common.cuh"
@@ -30,9 +30,10 @@ constexpr int G_A_BYTES = G_BM * G_BK * 2, G_STAGE_BYTES = 2 * G_A_BYTES, G_STG_
 constexpr int G_SMEM = G_STAGES * G_STAGE_BYTES + G_STG_ALL + 1024 + 256;
 static_assert(G_SMEM <= 232448, "more shared memory than a block can have");
 static_assert(kGroupHeight == 2 * G_BM, "a tile of slots is a pair's rows");
-template <int KIND> constexpr int group_warps = KIND == GROUP_GRAD ? 16 : 8;
+// Epilogue warps: with 16 in GROUP_GRAD a thread has 96 registers and keeps 1.3 KB of its values in local memory, more than the L1 has beside the stages: 203 us where
+// eight take 172.
+constexpr int G_WARPS = 8, G_THREADS = 64 + 32 * G_WARPS;
 template <int KIND> constexpr int group_units = KIND == GROUP_GRAD ? 4 : 8;
-template <int KIND> constexpr int group_threads = 64 + 32 * group_warps<KIND>;
 constexpr int G_GRADS = 3;
 
 struct GroupGrad { int M, N, tiles_m, tiles_n, first, vec; Grads16 d; };
@@ -83,10 +84,10 @@ __device__ __forceinline__ GroupItem uniform_item(GroupItem w) {
 }
 
 template <int KIND, class T>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(group_threads<KIND>, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(G_THREADS, 1)
 group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant__ GroupParams p) {
   constexpr bool A_MN = KIND == GROUP_WEIGHT, B_MN = KIND == GROUP_GRAD || KIND == GROUP_DX || KIND == GROUP_WEIGHT;
-  constexpr int EPI = group_warps<KIND>;
+  constexpr int EPI = G_WARPS;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* staging = smem + G_STAGES * G_STAGE_BYTES;
@@ -398,7 +399,7 @@ cudaError_t launch_group_as(const GroupGemm& g, const ExpertPlan& plan, int* err
   if (!ok) return cudaErrorInvalidValue;
   const int pairs = num_sms() / 2;
   p.pairs = most < pairs ? (int)most : pairs;
-  return launch_pdl(kernel, 2 * p.pairs, group_threads<KIND>, G_SMEM, st, maps, p);
+  return launch_pdl(kernel, 2 * p.pairs, G_THREADS, G_SMEM, st, maps, p);
 }
 template <class T>
 cudaError_t launch_group_of(GroupKind kind, const GroupGemm& g, const ExpertPlan& plan, int* err, cudaStream_t st) {
@@ -413,7 +414,7 @@ cudaError_t launch_group_of(GroupKind kind, const GroupGemm& g, const ExpertPlan
 
 }  // namespace
 
-int group_parts(int N) { return (N + G_BN - 1) / G_BN * (group_warps<GROUP_GRAD> / 4); }
+int group_parts(int N) { return (N + G_BN - 1) / G_BN * (G_WARPS / 4); }
 
 cudaError_t launch_group(GroupKind kind, bool bf16, const GroupGemm& g, const ExpertPlan& plan, int* err, cudaStream_t st) {
   return bf16 ? launch_group_of<__nv_bfloat16>(kind, g, plan, err, st) : launch_group_of<__half>(kind, g, plan, err, st);

@@ -387,6 +387,9 @@ __global__ void __launch_bounds__(32 * kRouteWarps, ORDERED ? 1 : V <= 8 ? 4 : 2
 #pragma unroll
       for (int v = 1; v < V; ++v) top = max_nan(top, l[v]);
       top = warp_max_nan(top);
+      // Shares are of the chosen alone, which a bias or the groups may have taken far below the row's largest: from the largest of them on, as the backward pass has them.
+      // (a NaN or +inf anywhere in the row is one in its scores)
+      if (p.renormalise) top = top < __int_as_float(0x7f800000) ? value_of(warp_max(mine ? key_of(z) : 0u)) : __int_as_float(0x7fffffff);
       if (top == -__int_as_float(0x7f800000)) top = 0.f;
       w = mine ? expf(z - top) : 0.f;
       if (p.renormalise) {

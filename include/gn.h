@@ -585,7 +585,8 @@ typedef enum { GN_SOFTMAX = 0, GN_SIGMOID = 1 } gn_score;
  *   - weight [tokens][k]: scale s_e, with `renormalise` divided by the sum of the chosen experts' s_e.  (The bias takes part in the choice alone.)
  * Equal values go by the lower number (experts and groups).  The order is that of the exact values: no rounding of FP32 decides it.  -inf is the
  * logit of an expert that cannot be taken: it has the score 0, and comes last without a bias (with one, a bias of -inf keeps it out); a row of
- * nothing else has weights of 0.  NaN comes behind every number (and is not among a group's best); with softmax a NaN or +inf in a row makes its weights NaN.
+ * nothing else has weights of 0, and so with sigmoid has one whose chosen scores are all below exp(-700) (a mask by the type's lowest value, not one of -inf); above that
+ * the weights of `renormalise` add up to scale, however small the scores are.  NaN comes behind every number (and is not among a group's best); with softmax a NaN or +inf in a row makes its weights NaN.
  *   bias             [experts] floats or NULL.
  * 1 <= k <= 32; k <= experts <= 1024; groups <= 32 divides experts; k <= experts / groups * top_groups; tokens < 2^31.
  */

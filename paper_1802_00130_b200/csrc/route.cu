@@ -99,6 +99,13 @@ __device__ __forceinline__ float warp_max_nan(float x) {
   for (int o = 16; o; o >>= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
   return x;
 }
+// sigmoid(z) of the lanes that are `in`, 0 of the others, times exp(-m) where the largest z, m, is negative: numbers in the proportions of the scores, all of which may be below FP32's smallest.
+// From exp(-700) down, where 64 bits end too, they are 0 all the same: a row that is masked by a type's lowest value instead of -inf has no shares either.
+__device__ __forceinline__ float sigmoid_share(float z, bool in) {
+  float m = fminf(value_of(warp_max(in ? key_of(z) : 0u)), 0.f);       // (NaN: 0)
+  if (m < -700.f) m = 0.f;
+  return !in ? 0.f : z < 0.f ? expf(z - m) / (1.f + expf(z)) : 1.f / (1.f + expf(-z));
+}
 __device__ __forceinline__ float exp_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f)); return y; }
 
 // Scores in FP64: of a row whose largest logit (0 if that is -inf) and sum of exponentials are known.
@@ -401,7 +408,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps, ORDERED ? 1 : V <= 8 ? 4 : 2
       sum = warp_sum(sum);
       w = sum == 0.f ? 0.f : w / sum;
     } else {
-      w = mine ? 1.f / (1.f + expf(-z)) : 0.f;
+      w = p.renormalise ? sigmoid_share(z, mine) : mine ? 1.f / (1.f + expf(-z)) : 0.f;
       if (p.renormalise) {
         const float sum = warp_sum(w);
         w = sum == 0.f ? 0.f : w / sum;
@@ -455,8 +462,8 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_grad_kernel(const __gr
         sum = sum == 0.f ? 0.f : 1.f / sum;
         s *= sum;
       }
-    } else if (in) {
-      s = 1.f / (1.f + expf(-z));
+    } else {
+      s = p.renormalise ? sigmoid_share(z, in) : in ? 1.f / (1.f + expf(-z)) : 0.f;
     }
     float d;                         // dL/dlogit of this lane's expert, of this choice alone
     float dot = 0.f;

@@ -70,7 +70,8 @@ def route(logits, k, score="softmax", bias=None, groups=1, top_groups=1, group_b
     score: "softmax" or "sigmoid" of the logits.  bias: float32 [experts], added to the scores for the choice alone (balance); without one, experts are
     compared by their logits.  groups: neighbouring experts form so many groups, of which the top_groups with the largest sum of their
     group_best (1 or 2) best values remain.  Equal values go by the lower number, and no rounding decides an order.
-    weight: the scores of the chosen, divided by their sum with `renormalise`, times `scale`.  Logits of -inf have the score 0.
+    weight: the scores of the chosen, divided by their sum with `renormalise` (however small they are), times `scale`.  Logits of -inf have the score 0; a token that has
+    chosen nothing else (or, with sigmoid, nothing above -700) has weights of 0.
     """
     dtype, dev, tokens, n = _first(logits, "logits")
     if stream is not None or dev != _device():

@@ -12,11 +12,15 @@ INF = math.inf
 
 
 def shares64(logits, index, score):
-    """Scores of the chosen over their sum: exp(log s_j - the largest - log of the sum), for which no score is too small.  Zero where none of them has one."""
+    """Scores of the chosen over their sum: exp(log s_j - the largest - log of the sum), for which no score is too small.  Zero where none of them has one: with
+    softmax of -inf alone, with sigmoid where all are below exp(-700), which 64 bits cannot hold either."""
     z = logits.double().gather(1, index.long())
     log = -torch.nn.functional.softplus(-z) if score == "sigmoid" else z
     log = torch.where(z == -INF, -INF, log)
     top = log.amax(1, keepdim=True)
+    if score == "sigmoid":
+        log = torch.where(top < -700, -INF, log)
+        top = log.amax(1, keepdim=True)
     e = (log - top.masked_fill(top == -INF, 0)).exp()
     total = e.sum(1, keepdim=True)
     return e / total.masked_fill(total == 0, 1)
@@ -64,7 +68,22 @@ def check_gradient(got, dweight, logits, index, score, scale):
     within(got, ref, bound + ref.abs() * u(logits.dtype) + tiny(logits.dtype) + 1e-37, "dlogits")
 
 
-@pytest.mark.parametrize("score", ["softmax"])
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("experts,k", [(2, 2), (40, 5), (256, 8), (1000, 32)])
+@pytest.mark.parametrize("middle", [80.0, 0.0, -40.0, -80.0, -86.0, -90.0, -100.0, -300.0, -600.0, -30000.0])
+@pytest.mark.parametrize("spread", [1.5, 15.0])
+def test_shares_of_sigmoids_far_from_one(t, experts, k, middle, spread):
+    """Scores below FP32's smallest number still have shares."""
+    logits = rand((50, experts), TYPES[t], experts, spread, middle)
+    index, weight = gn.route(logits, k, "sigmoid", renormalise=True, scale=1.5)
+    assert torch.equal(index.long(), logits.double().sort(dim=1, descending=True, stable=True).indices[:, :k])
+    want = 1.5 * shares64(logits, index, "sigmoid")
+    within(weight, want, want * SHARE + 1e-37, "weight")
+    dweight = rand((50, k), torch.float32, 2)
+    check_gradient(gn.route_grad(dweight, logits, index, "sigmoid", True, 1.5), dweight, logits, index, "sigmoid", 1.5)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_some_of_the_chosen_are_masked(score):
     """A bias takes experts with logits of -inf: they have the share 0, and where there is nothing else so have all."""
     logits = torch.full((4, 24), -120.0, device="cuda")

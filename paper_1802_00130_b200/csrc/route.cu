@@ -285,22 +285,24 @@ __device__ __forceinline__ int choose(const RouteParams& p, const T* row, const 
           for (int i = 0; i < p.each; ++i) take(stage[lane * pitch + i]);
         __syncwarp();
       }
-      const float value = one ? first : first + second;
+      // (half the sum of two, which does not overflow)
+      const float value = one ? first : 0.5f * first + 0.5f * second;
       uint32_t g = mine ? key_of(value) : 0u;
-      float last = 0.f;
       const uint32_t span = lanes == 32 ? 0xffffffffu : (1u << lanes) - 1;
-      for (int j = 0; j <= p.top && j < p.groups; ++j) {
+      for (int j = 0; j < p.top; ++j) {
         const uint32_t m = warp_max(g);
         const int from = __ffs(__ballot_sync(0xffffffffu, g == m)) - 1;
-        const float v = value_of(m);
-        if (j == p.top) {
-          // two sums of two values, each a score and a bias, and their roundings
-          if (!plain && last - v <= E * (4.f * off + 4.f * (fabsf(last) + fabsf(v)))) certain = false;
-        } else {
-          kept |= span << from;
-          last = v;
-          if (kept >> lane & 1) g = 0;
-        }
+        kept |= span << from;
+        if (kept >> lane & 1) g = 0;
+      }
+      if (!plain) {
+        // What a group's value may be off: each of its scores and the rounding of each sum, which goes by what was added, since a score's bias and another's may cancel.  Certain is a choice
+        // whose lowest is above all that is left, or as far down or up as that, where no rounding is.
+        const float about = E * 1.25f * (off + fabsf(first) + (one ? 0.f : fabsf(second))), err = about < __int_as_float(0x7f800000) ? about : 0.f;
+        const bool in = kept >> lane & 1;
+        const uint32_t low = __reduce_min_sync(0xffffffffu, mine && in ? key_of(value - err) : 0xffffffffu);
+        const uint32_t high = warp_max(mine && !in ? key_of(value + err) : 0u);
+        if (!(low > high || (low == high && fabsf(value_of(low)) == __int_as_float(0x7f800000)))) certain = false;
       }
 #pragma unroll
       for (int v = 0; v < V; ++v)

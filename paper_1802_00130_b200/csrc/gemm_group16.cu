@@ -130,7 +130,7 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
       const int m0 = (KIND == GROUP_WEIGHT ? w.m0 : w.slot) + (int)rank * G_BM, n0 = KIND == GROUP_GATE ? w.n0 : w.n0 + (int)rank * G_BM;
 #pragma unroll 1
       for (int kb = 0; kb < w.kb; ++kb) {
-        if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, p.err, 1)) { ok = false; break; }
+        if (!warp_wait_or_abort(&empty[s], ph ^ 1, abort_flag, p.err, 1)) { ok = false; break; }
         if (elect_one()) {
           if (rank == 0) mbar_expect_tx(&full[s], 2u * G_STAGE_BYTES);
           const uint32_t bar = full_leader + (uint32_t)s * 8u;
@@ -174,13 +174,13 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
         const GroupItem w = uniform_item(group_item<KIND>(p, i));
         if (KIND == GROUP_WEIGHT && w.kb == 0) continue;
         const int buf = ti & 1;
-        if (!wait_or_abort(&acc_empty[buf], ((ti >> 1) & 1) ^ 1, abort_flag, p.err, 4)) break;
+        if (!warp_wait_or_abort(&acc_empty[buf], ((ti >> 1) & 1) ^ 1, abort_flag, p.err, 4)) break;
         tc_fence_after();
         const uint32_t tmem_d = tmem_base + (uint32_t)(buf * G_BN);
         uint32_t acc = 0u;
 #pragma unroll 1
         for (int kb = 0; kb < w.kb; ++kb) {
-          if (!wait_or_abort(&full[s], ph, abort_flag, p.err, 2)) { ok = false; break; }
+          if (!warp_wait_or_abort(&full[s], ph, abort_flag, p.err, 2)) { ok = false; break; }
           tc_fence_after();
           const uint64_t ad = a0 + (uint64_t)(s * (G_STAGE_BYTES >> 4)), bd = b0 + (uint64_t)(s * (G_STAGE_BYTES >> 4));
           if (elect_one()) {

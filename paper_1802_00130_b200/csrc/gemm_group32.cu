@@ -140,7 +140,7 @@ group32_kernel(const __grid_constant__ TensorMaps<KIND> maps, const __grid_const
         const int second = seg >= H_PRODUCTS ? 1 : 0, pa = kPartA[seg - second * H_PRODUCTS], pb = kPartB[seg - second * H_PRODUCTS];
 #pragma unroll 1
         for (int kb = 0; kb < w.kb; ++kb) {
-          if (!wait_or_abort(&empty[s], ph ^ 1, abort_flag, p.err, 1)) { ok = false; break; }
+          if (!warp_wait_or_abort(&empty[s], ph ^ 1, abort_flag, p.err, 1)) { ok = false; break; }
           if (elect_one()) {
             if (rank == 0) mbar_expect_tx(&full[s], 2u * H_STAGE_BYTES);
             const uint32_t bar = full_leader + (uint32_t)s * 8u;
@@ -181,14 +181,14 @@ group32_kernel(const __grid_constant__ TensorMaps<KIND> maps, const __grid_const
 #pragma unroll 1
         for (int kb = 0; kb < total && ok; kb += H_CHUNK, ++ci) {
           const int buf = ci % H_BUFS;
-          if (!wait_or_abort(&acc_empty[buf], ((ci / H_BUFS) & 1) ^ 1, abort_flag, p.err, 4)) { ok = false; break; }
+          if (!warp_wait_or_abort(&acc_empty[buf], ((ci / H_BUFS) & 1) ^ 1, abort_flag, p.err, 4)) { ok = false; break; }
           tc_fence_after();
           const uint32_t tmem_d = tmem_base + (uint32_t)(buf * H_BN);
           uint32_t acc = 0u;
           const int end = min(kb + H_CHUNK, total);
 #pragma unroll 1
           for (int j = kb; j < end; ++j) {
-            if (!wait_or_abort(&full[s], ph, abort_flag, p.err, 2)) { ok = false; break; }
+            if (!warp_wait_or_abort(&full[s], ph, abort_flag, p.err, 2)) { ok = false; break; }
             tc_fence_after();
             const uint64_t ad = a0 + (uint64_t)(s * (H_STAGE_BYTES >> 4)), bd = b0 + (uint64_t)(s * (H_STAGE_BYTES >> 4));
             if (elect_one()) {

@@ -183,6 +183,12 @@ __device__ __forceinline__ bool wait_or_abort(uint64_t* bar, uint32_t parity, vo
   return true;
 }
 
+// The same for a converged warp that stays one: whether all its lanes have seen the phase complete.  Each lane looks at the barrier, the clock and the flag by itself, and where one
+// gives up in the moment in which another gets through, lanes would part before the next instruction that waits for all of them (elect_one, a shuffle), and wait there for good.
+__device__ __forceinline__ bool warp_wait_or_abort(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* err, int code) {
+  return __all_sync(0xffffffffu, wait_or_abort(bar, parity, abort_flag, err, code)) != 0;
+}
+
 // One lane of a converged warp.  Products and copies that a whole warp comes to and one lane issues have their operands in uniform registers; under a branch on
 // the lane's number each is moved there before each instruction, which took longer than a product of 256 x 128 x 16 (155 cycles against 64).
 __device__ __forceinline__ bool elect_one() {

@@ -263,9 +263,9 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
                 uw[16 * h + q] = pack2<T>(uv[2 * q], uv[2 * q + 1]);
               }
             }
-            put_rows<U, 32>(o, stg, lane, p.d.p, p.d.ld, slot_row, nc, N, true);
-            if (p.gate_out.p) put_rows<U, 32>(gw, stg, lane, p.gate_out.p, p.gate_out.ld, pair_row, nc, N, p.vec_gate);
-            if (p.up_out.p) put_rows<U, 32>(uw, stg, lane, p.up_out.p, p.up_out.ld, pair_row, nc, N, p.vec_up);
+            put_rows<U>(o, stg, lane, p.d.p, p.d.ld, slot_row, nc, N, true);
+            if (p.gate_out.p) put_rows<U>(gw, stg, lane, p.gate_out.p, p.gate_out.ld, pair_row, nc, N, p.vec_gate);
+            if (p.up_out.p) put_rows<U>(uw, stg, lane, p.up_out.p, p.up_out.ld, pair_row, nc, N, p.vec_up);
           } else if constexpr (KIND == GROUP_GRAD) {
             uint32_t gw[4 * U], uw[4 * U];
             turn_chunk(gx, stg, lane, gw);
@@ -292,16 +292,16 @@ group_kernel(const __grid_constant__ GroupMaps<KIND> maps, const __grid_constant
               gw[q] = pack2<T>(d0 * up.x * s0, d1 * up.y * s1);
               uw[q] = pack2<T>(d0 * a0, d1 * a1);
             }
-            put_rows<U, 32>(o, stg, lane, p.d.p, p.d.ld, slot_row, nc, N, true);
-            put_rows<U, 32>(gw, stg, lane, p.dgate.p, p.dgate.ld, slot_row, nc, N, true);
-            put_rows<U, 32>(uw, stg, lane, p.dup.p, p.dup.ld, slot_row, nc, N, true);
+            put_rows<U>(o, stg, lane, p.d.p, p.d.ld, slot_row, nc, N, true);
+            put_rows<U>(gw, stg, lane, p.dgate.p, p.dgate.ld, slot_row, nc, N, true);
+            put_rows<U>(uw, stg, lane, p.dup.p, p.dup.ld, slot_row, nc, N, true);
           } else if constexpr (KIND == GROUP_DOWN || KIND == GROUP_DX) {
             // (32 columns of FP32 are 64 of 16 bits)
             float v[32];
             tmem_ld32(tq + (uint32_t)(c * COLS), v);
 #pragma unroll
             for (int q = 0; q < 32; ++q) o[q] = __float_as_uint(v[q]);
-            put_rows<8, 32>(o, stg, lane, p.rows.p, 2 * p.rows.ld, pair_row, 2 * nc, 2 * N, true);
+            put_rows<8>(o, stg, lane, p.rows.p, 2 * p.rows.ld, pair_row, 2 * nc, 2 * N, true);
           } else {
 #pragma unroll
             for (int h = 0; h < COLS / 32; ++h) {

@@ -258,7 +258,7 @@ group32_kernel(const __grid_constant__ TensorMaps<KIND> maps, const __grid_const
         uint32_t o[32];
 #pragma unroll
         for (int q = 0; q < 32; ++q) o[q] = __float_as_uint(v[q]);
-        put_rows<8, 32>(o, stg, lane, base, 2 * ld, row_of, 2 * n0, 2 * N, vec);
+        put_rows<8>(o, stg, lane, base, 2 * ld, row_of, 2 * n0, 2 * N, vec);
       };
       const auto put_parts = [&](const float (&v)[32], const Parts& to, int n0) {
         uint32_t o[3][16];
@@ -269,7 +269,7 @@ group32_kernel(const __grid_constant__ TensorMaps<KIND> maps, const __grid_const
           o[0][q] = t[0]; o[1][q] = t[1]; o[2][q] = t[2];
         }
 #pragma unroll
-        for (int j = 0; j < 3; ++j) put_rows<4, 32>(o[j], stg, lane, reinterpret_cast<uint16_t*>(to.p) + j * to.rows * to.ld, to.ld, slot_row, n0, N, true);
+        for (int j = 0; j < 3; ++j) put_rows<4>(o[j], stg, lane, reinterpret_cast<uint16_t*>(to.p) + j * to.rows * to.ld, to.ld, slot_row, n0, N, true);
       };
       if constexpr (KIND == GROUP_GATE) {
         const int nc = w.n0 + half * 32;

@@ -57,12 +57,59 @@ __device__ __forceinline__ uint16_t lds2(uint32_t a) {
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
   return v;
 }
-// This thread's row of a chunk, 8 U elements in 4 U words, to columns n0.. (of N) of row_of(its number of 0..31) of a matrix (negative: no such row), by way of the
-// staging tile, ROWS rows at a time, in stores of 16 bytes.  vec: the rows' chunks start where such a store may.  Else a store's 16 bytes are put together from
-// two units of the staging tile, and the up to seven elements before a row's first such place, and those after its last, go one by one.
+// A unit's part of a row of `cols` columns to where it does not start on 16 bytes: a store's 16 bytes are put together from two units of the staging tile, and the up to seven elements
+// before the row's first such place, and those after its last, go one by one.
 // 8000 tokens, 1001 columns, 3001 hidden units forward: 172 us where no matrix is aligned (228 in words of four bytes, a row at a time), 143 where all are.
-template <int U, int ROWS, class RowOf>
+template <int U>
+__device__ __forceinline__ void put_loose(uint16_t* p, uint32_t stg, int row, int unit, int cols) {
+  const int head = min(cols, (int)(-(reinterpret_cast<uintptr_t>(p) >> 1) & 7)), wholes = (cols - head) >> 3;
+  if (unit < wholes) {
+    const uint4 x = lds16(stg_at<U>(stg, row, unit)), y = lds16(stg_at<U>(stg, row, unit + (head > 0)));
+    const bool two = head & 4, one = head & 2;
+    const uint32_t a0 = two ? x.z : x.x, a1 = two ? x.w : x.y, a2 = two ? y.x : x.z, a3 = two ? y.y : x.w, a4 = two ? y.z : y.x, a5 = two ? y.w : y.y;
+    const uint32_t b0 = one ? a1 : a0, b1 = one ? a2 : a1, b2 = one ? a3 : a2, b3 = one ? a4 : a3, b4 = one ? a5 : a4;
+    const uint32_t by = (head & 1) * 16;
+    *reinterpret_cast<uint4*>(p + head + unit * 8) =
+        make_uint4(__funnelshift_r(b0, b1, by), __funnelshift_r(b1, b2, by), __funnelshift_r(b2, b3, by), __funnelshift_r(b3, b4, by));
+  }
+  for (int i = unit; i < cols - 8 * wholes; i += U) {
+    const int e = i < head ? i : 8 * wholes + i;
+    p[e] = lds2(stg_at<U>(stg, row, e >> 3) + (e & 7) * 2u);
+  }
+}
+// This thread's row of a chunk, 8 U elements in 4 U words, to columns n0.. (of N) of row_of(its number of 0..31) of a matrix (negative: no such row), by way of the
+// staging tile, in stores of 16 bytes.  vec: the rows' chunks start where such a store may.
+template <int U, class RowOf>
 __device__ __forceinline__ void put_rows(const uint32_t (&w)[4 * U], uint32_t stg, int lane, void* base, int64_t ld, RowOf row_of, int n0, int N, bool vec) {
+  const int cols = min(8 * U, N - n0), unit = lane % U;
+#pragma unroll
+  for (int q = 0; q < U; ++q) sts16(stg_at<U>(stg, lane, q), make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]));
+  __syncwarp();
+  uint16_t* const at = reinterpret_cast<uint16_t*>(base) + n0;
+  if (vec) {
+#pragma unroll
+    for (int it = 0; it < U; ++it) {
+      const int row = it * (32 / U) + lane / U, m = row_of(row);
+      if (m >= 0 && unit * 8 + 8 <= cols) *reinterpret_cast<uint4*>(at + m * ld + unit * 8) = lds16(stg_at<U>(stg, row, unit));
+    }
+    if (cols & 7) {
+      const int m = row_of(lane);
+      if (m >= 0)
+        for (int e = cols & ~7; e < cols; ++e) at[m * ld + e] = lds2(stg_at<U>(stg, lane, e >> 3) + (e & 7) * 2u);
+    }
+  } else {
+#pragma unroll 2
+    for (int it = 0; it < U; ++it) {
+      const int row = it * (32 / U) + lane / U, m = row_of(row);
+      if (m >= 0) put_loose<U>(at + m * ld, stg, row, unit, cols);
+    }
+  }
+  __syncwarp();
+}
+// The same to rows m0.. (of M), which follow one another, ROWS rows at a time.  (Taken for rows of a list they cost the backward passes of few tokens a microsecond, 28.9 instead of 28.0 us
+// for one token of 1024 columns and 4096 hidden units.)
+template <int U, int ROWS>
+__device__ __forceinline__ void put_chunk(const uint32_t (&w)[4 * U], uint32_t stg, int lane, void* base, int64_t ld, int m0, int M, int n0, int N, bool vec) {
   const int cols = min(8 * U, N - n0), unit = lane % U;
 #pragma unroll
   for (int r0 = 0; r0 < 32; r0 += ROWS) {
@@ -71,47 +118,28 @@ __device__ __forceinline__ void put_rows(const uint32_t (&w)[4 * U], uint32_t st
       for (int q = 0; q < U; ++q) sts16(stg_at<U>(stg, lane % ROWS, q), make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]));
     }
     __syncwarp();
-    uint16_t* const at = reinterpret_cast<uint16_t*>(base) + n0;
+    uint16_t* const at = reinterpret_cast<uint16_t*>(base) + (int64_t)(m0 + r0) * ld + n0;
     if (vec) {
+      if (unit * 8 + 8 <= cols) {
 #pragma unroll
-      for (int it = 0; it < ROWS * U / 32; ++it) {
-        const int row = it * (32 / U) + lane / U, m = row_of(r0 + row);
-        if (m >= 0 && unit * 8 + 8 <= cols) *reinterpret_cast<uint4*>(at + m * ld + unit * 8) = lds16(stg_at<U>(stg, row, unit));
+        for (int it = 0; it < ROWS * U / 32; ++it) {
+          const int row = it * (32 / U) + lane / U;
+          const uint4 v = lds16(stg_at<U>(stg, row, unit));
+          if (m0 + r0 + row < M) *reinterpret_cast<uint4*>(at + (int64_t)row * ld + unit * 8) = v;
+        }
       }
-      if (cols & 7) {
-        const int m = row_of(r0 + lane % ROWS);
-        if (lane < ROWS && m >= 0)
-          for (int e = cols & ~7; e < cols; ++e) at[m * ld + e] = lds2(stg_at<U>(stg, lane, e >> 3) + (e & 7) * 2u);
-      }
+      if (lane < ROWS && m0 + r0 + lane < M)
+        for (int e = cols & ~7; e < cols; ++e) at[(int64_t)lane * ld + e] = lds2(stg_at<U>(stg, lane, e >> 3) + (e & 7) * 2u);
     } else {
 #pragma unroll 2
       for (int it = 0; it < ROWS * U / 32; ++it) {
-        const int row = it * (32 / U) + lane / U, m = row_of(r0 + row);
-        if (m < 0) continue;
-        uint16_t* const p = at + m * ld;
-        const int head = min(cols, (int)(-(reinterpret_cast<uintptr_t>(p) >> 1) & 7)), wholes = (cols - head) >> 3;
-        if (unit < wholes) {
-          const uint4 x = lds16(stg_at<U>(stg, row, unit)), y = lds16(stg_at<U>(stg, row, unit + (head > 0)));
-          const bool two = head & 4, one = head & 2;
-          const uint32_t a0 = two ? x.z : x.x, a1 = two ? x.w : x.y, a2 = two ? y.x : x.z, a3 = two ? y.y : x.w, a4 = two ? y.z : y.x, a5 = two ? y.w : y.y;
-          const uint32_t b0 = one ? a1 : a0, b1 = one ? a2 : a1, b2 = one ? a3 : a2, b3 = one ? a4 : a3, b4 = one ? a5 : a4;
-          const uint32_t by = (head & 1) * 16;
-          *reinterpret_cast<uint4*>(p + head + unit * 8) =
-              make_uint4(__funnelshift_r(b0, b1, by), __funnelshift_r(b1, b2, by), __funnelshift_r(b2, b3, by), __funnelshift_r(b3, b4, by));
-        }
-        for (int i = unit; i < cols - 8 * wholes; i += U) {
-          const int e = i < head ? i : 8 * wholes + i;
-          p[e] = lds2(stg_at<U>(stg, row, e >> 3) + (e & 7) * 2u);
-        }
+        const int row = it * (32 / U) + lane / U;
+        if (m0 + r0 + row >= M) break;
+        put_loose<U>(at + (int64_t)row * ld, stg, row, unit, cols);
       }
     }
     __syncwarp();
   }
-}
-// The same to rows m0.. (of M).
-template <int U, int ROWS>
-__device__ __forceinline__ void put_chunk(const uint32_t (&w)[4 * U], uint32_t stg, int lane, void* base, int64_t ld, int m0, int M, int n0, int N, bool vec) {
-  put_rows<U, ROWS>(w, stg, lane, base, ld, [&](int r) { return m0 + r < M ? m0 + r : -1; }, n0, N, vec);
 }
 // A chunk of 32 columns, all of them there and addressable in units of 16 bytes.
 __device__ __forceinline__ void put_whole(const uint32_t* w, uint32_t stg, int lane, void* base, int64_t ld, int m0, int M, int n0) {

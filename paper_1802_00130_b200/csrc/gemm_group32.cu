@@ -1,6 +1,7 @@
 // Products of FP32 matrices over a mixture's experts on the tensor cores: the kernel of gemm_group16.cu on operands in three BF16 parts of eight bits each.
 //
-//   a b = sum of a_i b_j over the six pairs of parts with i + j <= 2 (0 the leading part); what is left out is below 2^-23 of |a b|.
+//   a b = sum of a_i b_j over the six pairs of parts with i + j <= 2 (0 the leading part).  Parts are rounded to nearest: |a_1| <= 2^-8 2^e, |a_2| <= 2^-16 2^e with 2^e <= |a|, so what is left out,
+//   a_1 b_2 + a_2 b_1 + a_2 b_2, is below 2^-23 of |a b|, and of either sign.  (Parts cut off left out up to 3.9 times that, always towards zero.)
 // Tiles of 256 x 128 of a CTA pair.  The tensor core cuts off what does not fit when it adds to a sum, always towards zero; so a sum is
 // taken out of tensor memory after 256 terms, added to registers in FP32, and begun anew: four accumulators of 128 columns take turns.  The parts of h, dgate and dup are
 // written by the epilogue that has them in FP32.  Taking the sums out costs a fifth of the time (dx of 16384 pairs, 1024 x 1024: 571 and 484 us before the elected lane, 353 now).
@@ -74,15 +75,21 @@ __device__ __forceinline__ float4 four32(const float* row, int c, int n, bool ve
   if (c + 3 < n) v.w = row[c + 3];
   return v;
 }
-// The three parts of v, and of w beside them.
+// The three parts of v, and of w beside them: the first two rounded to nearest (halves away from zero), so that what is left is half as large, and of either sign; the third is all that is left.  What
+// would be rounded to infinity is cut off; an infinity leaves nothing, and of a NaN one part at least is one.
+__device__ __forceinline__ uint32_t leading(float v) {
+  const uint32_t a = __float_as_uint(v);
+  return (a & 0x7fffffffu) < 0x7f7f8000u ? a + 0x8000u : a;
+}
+__device__ __forceinline__ float less(float v, uint32_t part) { return v - __uint_as_float(part & 0xffff0000u); }
 __device__ __forceinline__ void three(float v, float w, uint32_t (&o)[3]) {
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const uint32_t a = __float_as_uint(v), b = __float_as_uint(w);
-    o[i] = __byte_perm(a, b, 0x7632);
-    v = fabsf(v) == __int_as_float(0x7f800000) ? 0.f : v - __uint_as_float(a & 0xffff0000u);
-    w = fabsf(w) == __int_as_float(0x7f800000) ? 0.f : w - __uint_as_float(b & 0xffff0000u);
-  }
+  uint32_t a = leading(v), b = leading(w);
+  o[0] = __byte_perm(a, b, 0x7632);
+  v = fabsf(v) == __int_as_float(0x7f800000) ? 0.f : less(v, a);
+  w = fabsf(w) == __int_as_float(0x7f800000) ? 0.f : less(w, b);
+  a = __float_as_uint(v) + 0x8000u; b = __float_as_uint(w) + 0x8000u;
+  o[1] = __byte_perm(a, b, 0x7632);
+  o[2] = __byte_perm(__float_as_uint(less(v, a)), __float_as_uint(less(w, b)), 0x7632);
 }
 
 __device__ __forceinline__ TensorItem uniform_item(TensorItem w) {

@@ -31,9 +31,9 @@ ExpertPlan plan_at(int* mem, int64_t pairs, int experts, int height);           
 // The plan of an index table, with tiles of `height` slots (where `padded` is looked at, a multiple of kSlots).
 cudaError_t launch_plan(const int* index, const ExpertPlan& plan, int height, cudaStream_t st);
 
-// Rows of tokens to their pairs' slots: dst[slot of (t, j)] = src[t]; zero: empty slots are written too, zero.  `bytes` of an element (2 or 4); rows of dst are 16-byte aligned.
+// Rows of tokens, of 16-bit elements, to their pairs' slots: dst[slot of (t, j)] = src[t]; zero: empty slots are written too, zero.  Rows of dst are 16-byte aligned.
 struct RowCopy { const void* src; int64_t ld; void* dst; int64_t ld_dst; };
-cudaError_t launch_to_slots(const RowCopy* list, int n, int64_t tokens, int k, int cols, int bytes, bool zero, const ExpertPlan& plan, cudaStream_t st);
+cudaError_t launch_to_slots(const RowCopy* list, int n, int64_t tokens, int k, int cols, bool zero, const ExpertPlan& plan, cudaStream_t st);
 
 // d[t] = sum over the choices j that are experts of weight[t k + j] (1 without weights) src[t k + j], d of type `type` (NULL: not wanted).  parts: with them,
 // dweight[t k + j] = the sum of n_parts partial sums at parts[(slot of the pair) n_parts], in order; 0 for a choice that is no expert.

@@ -139,7 +139,6 @@ struct CopyParams {
 // Bound by its bytes: 8192 tokens of 2048 BF16 columns to 4 slots each, 168 MB, 27 us (6.3 TB/s).
 // A warp takes 1 KB of a token's row at a time (two 16-byte units a lane) and writes it to the token's k slots; the warps behind the tokens' zero the experts' empty slots (where
 // they are terms of a sum).
-template <int BYTES>
 __global__ void __launch_bounds__(256) to_slots_kernel(const __grid_constant__ CopyParams p) {
   grid_dep_wait();
   grid_dep_launch();
@@ -152,7 +151,7 @@ __global__ void __launch_bounds__(256) to_slots_kernel(const __grid_constant__ C
     const int64_t t = w / p.units;
     const int unit = (int)(w - t * p.units), at = unit * 1024 + lane * 16;
     char* const dst = (char*)c.dst;
-    const int64_t ld = c.ld_dst * BYTES;
+    const int64_t ld = c.ld_dst * 2;
     if (t >= p.tokens) {
       const int e = (int)(t - p.tokens), n = p.plan.count[e], end = (n + kSlots - 1) / kSlots * kSlots;
       for (int i = n; i < end; ++i) {
@@ -163,7 +162,7 @@ __global__ void __launch_bounds__(256) to_slots_kernel(const __grid_constant__ C
       }
       continue;
     }
-    const char* const src = (const char*)dep(c.src) + t * c.ld * BYTES + at;
+    const char* const src = (const char*)dep(c.src) + t * c.ld * 2 + at;
     uint4 v[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -175,11 +174,8 @@ __global__ void __launch_bounds__(256) to_slots_kernel(const __grid_constant__ C
       } else {
         uint32_t o[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int b = 0; b < 16; b += BYTES)
-          if (b < left) {
-            if constexpr (BYTES == 4) o[b >> 2] = *reinterpret_cast<const uint32_t*>(src + h * 512 + b);
-            else o[b >> 2] |= (uint32_t) * reinterpret_cast<const uint16_t*>(src + h * 512 + b) << (8 * (b & 3));
-          }
+        for (int b = 0; b < 16; b += 2)
+          if (b < left) o[b >> 2] |= (uint32_t) * reinterpret_cast<const uint16_t*>(src + h * 512 + b) << (8 * (b & 3));
         v[h] = make_uint4(o[0], o[1], o[2], o[3]);
       }
     }
@@ -310,16 +306,16 @@ cudaError_t launch_plan(const int* index, const ExpertPlan& plan, int height, cu
   return e == cudaSuccess ? launch_pdl(plan_place_kernel<false>, blocks, kPlanThreads, smem, st, p) : e;
 }
 
-cudaError_t launch_to_slots(const RowCopy* list, int n, int64_t tokens, int k, int cols, int bytes, bool zero, const ExpertPlan& plan, cudaStream_t st) {
+cudaError_t launch_to_slots(const RowCopy* list, int n, int64_t tokens, int k, int cols, bool zero, const ExpertPlan& plan, cudaStream_t st) {
   CopyParams p = {};
   for (int i = 0; i < n; ++i) {
     p.c[i] = list[i];
-    p.vec[i] = ((uintptr_t)list[i].src & 15) == 0 && list[i].ld * bytes % 16 == 0;
+    p.vec[i] = ((uintptr_t)list[i].src & 15) == 0 && list[i].ld % 8 == 0;
   }
-  p.tokens = tokens; p.k = k; p.row_bytes = cols * bytes; p.zero = zero ? plan.experts : 0; p.units = (p.row_bytes + 1023) / 1024; p.plan = plan;
+  p.tokens = tokens; p.k = k; p.row_bytes = cols * 2; p.zero = zero ? plan.experts : 0; p.units = (p.row_bytes + 1023) / 1024; p.plan = plan;
   const int64_t want = ((tokens + p.zero) * p.units + 7) / 8, most = (int64_t)num_sms() * 8;
   const dim3 grid((unsigned)(want < most ? want : most), (unsigned)n);
-  return bytes == 4 ? launch_pdl_grid(to_slots_kernel<4>, grid, 256, 0, st, p) : launch_pdl_grid(to_slots_kernel<2>, grid, 256, 0, st, p);
+  return launch_pdl_grid(to_slots_kernel, grid, 256, 0, st, p);
 }
 
 cudaError_t launch_pack_mats(const PackMats* list, int n, cudaStream_t st) {

@@ -91,10 +91,7 @@ int64_t lay_out_half(const gn_mixture& f, bool backward, char* base, Half& w) {
   const int64_t pairs = f.tokens * f.k, lc = up8(f.cols), lf = up8(f.inner);
   w.slots = plan_slots(pairs, f.experts);
   w.plan = plan_at((int*)ws.take(plan_ints(pairs, f.experts, kGroupHeight) * 4), pairs, f.experts, kGroupHeight);
-  if (!backward) {
-    w.w_gate = addressable(f.w_gate, f.experts, f.inner, f.cols, ws, w);
-    w.w_up = addressable(f.w_up, f.experts, f.inner, f.cols, ws, w);
-  } else if (f.dx.p) {
+  if (!backward || f.dx.p) {
     w.w_gate = addressable(f.w_gate, f.experts, f.inner, f.cols, ws, w);
     w.w_up = addressable(f.w_up, f.experts, f.inner, f.cols, ws, w);
   }
@@ -123,7 +120,7 @@ cudaError_t run_half(const gn_mixture& f, bool backward, const Half& w, int* err
   int n = 0;
   if (w.x.p) rows[n++] = {f.x.p, f.x.ld, const_cast<void*>(w.x.p), w.x.ld};
   if (backward) rows[n++] = {f.dy.p, f.dy.ld, const_cast<void*>(w.dy.p), w.dy.ld};
-  if (e == cudaSuccess) e = launch_to_slots(rows, n, f.tokens, f.k, f.cols, 2, backward, w.plan, st);
+  if (e == cudaSuccess) e = launch_to_slots(rows, n, f.tokens, f.k, f.cols, backward, w.plan, st);
   GroupGemm g;
   g.act = f.act; g.slots = w.slots;
   Combine c = {};

@@ -27,7 +27,7 @@ const char* mixture_args(const gn_mixture* f, bool backward) {
   if (f->act < GN_ACT_SIGMOID || f->act > GN_ACT_RELU) return "act is not a gn_act";
   if (f->experts < 1 || f->experts > kMostExperts) return "experts must be in [1, 1024]";
   if (f->k < 1 || f->k > 32) return "k must be in [1, 32]";
-  if (f->tokens < 0 || f->tokens >= (int64_t(1) << 28) / f->k) return "tokens times k must be in [0, 2^28)";
+  if (f->tokens < 0 || f->tokens >= (int64_t(1) << 28) || f->tokens * f->k >= (int64_t(1) << 28)) return "tokens times k must be in [0, 2^28)";
   if (f->cols < 1 || f->inner < 1 || f->cols > (1 << 20) || f->inner > (1 << 20) || (int64_t)f->cols * f->inner >= (int64_t(1) << 31))
     return "cols and inner must be in [1, 2^20] with a product below 2^31";
   const int64_t C = f->cols, F = f->inner;

@@ -133,7 +133,7 @@ const char* ffn4_args(const gn_ffn4* f) {
   const char* why = sizes4(f->type, f->experts, f->inner, f->cols, f->group);
   if (why) return why;
   if (f->k < 1 || f->k > 32) return "k must be in [1, 32]";
-  if (f->tokens < 0 || f->tokens >= kMostTokens4 / f->k) return "tokens times k must be in [0, 2^19)";
+  if (f->tokens < 0 || f->tokens >= kMostTokens4 || f->tokens * f->k >= kMostTokens4) return "tokens times k must be in [0, 2^19)";
   if (f->tokens > 0 && !f->index && (f->experts != 1 || f->k != 1)) return "without an index there is one expert, and one choice";
   if (!packed_ok(f->q_gate, f->s_gate) || !packed_ok(f->q_up, f->s_up) || !packed_ok(f->q_down, f->s_down)) return kPackedWhy;
   if (f->tokens == 0) return nullptr;

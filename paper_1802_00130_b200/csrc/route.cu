@@ -99,12 +99,14 @@ __device__ __forceinline__ float warp_max_nan(float x) {
   for (int o = 16; o; o >>= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
   return x;
 }
+// The largest z of the lanes that are `in` (NaN: none is a number).
+__device__ __forceinline__ float warp_largest(float z, bool in) { return value_of(warp_max(in ? key_of(z) : 0u)); }
 // sigmoid(z) of the lanes that are `in`, 0 of the others, times exp(-m) where the largest z, m, is negative: numbers in the proportions of the scores, all of which may be below FP32's smallest.
-// From exp(-700) down, where 64 bits end too, they are 0 all the same: a row that is masked by a type's lowest value instead of -inf has no shares either.
-__device__ __forceinline__ float sigmoid_share(float z, bool in) {
-  float m = fminf(value_of(warp_max(in ? key_of(z) : 0u)), 0.f);       // (NaN: 0)
-  if (m < -700.f) m = 0.f;
-  return !in ? 0.f : z < 0.f ? expf(z - m) / (1.f + expf(z)) : 1.f / (1.f + expf(-z));
+// From exp(-700) down, where 64 bits end too, they are 0 all the same: a row that is masked by a type's lowest value instead of -inf has no shares either.  rest = 1 - sigmoid(z).
+__device__ __forceinline__ float sigmoid_share(float z, float m, bool in, float& rest) {
+  const float e = expf(-fabsf(z)), r = 1.f / (1.f + e);
+  rest = z < 0.f ? r : e * r;
+  return !in ? 0.f : z < 0.f ? (m < 0.f && m >= -700.f ? expf(z - m) : e) * r : r;
 }
 __device__ __forceinline__ float exp_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f)); return y; }
 
@@ -397,8 +399,8 @@ __global__ void __launch_bounds__(32 * kRouteWarps, ORDERED ? 1 : V <= 8 ? 4 : 2
       for (int v = 1; v < V; ++v) top = max_nan(top, l[v]);
       top = warp_max_nan(top);
       // Shares are of the chosen alone, which a bias or the groups may have taken far below the row's largest: from the largest of them on, as the backward pass has them.
-      // (a NaN or +inf anywhere in the row is one in its scores)
-      if (p.renormalise) top = top < __int_as_float(0x7f800000) ? value_of(warp_max(mine ? key_of(z) : 0u)) : __int_as_float(0x7fffffff);
+      // (A NaN or +inf anywhere in the row is one in its scores.  ORDERED, the largest is the first chosen.)
+      if (!ORDERED && p.renormalise) top = top < __int_as_float(0x7f800000) ? warp_largest(z, mine) : __int_as_float(0x7fffffff);
       if (top == -__int_as_float(0x7f800000)) top = 0.f;
       w = mine ? expf(z - top) : 0.f;
       if (p.renormalise) {
@@ -410,10 +412,13 @@ __global__ void __launch_bounds__(32 * kRouteWarps, ORDERED ? 1 : V <= 8 ? 4 : 2
       sum = warp_sum(sum);
       w = sum == 0.f ? 0.f : w / sum;
     } else {
-      w = p.renormalise ? sigmoid_share(z, mine) : mine ? 1.f / (1.f + expf(-z)) : 0.f;
       if (p.renormalise) {
+        float rest;
+        w = sigmoid_share(z, ORDERED ? __shfl_sync(0xffffffffu, z, 0) : warp_largest(z, mine), mine, rest);
         const float sum = warp_sum(w);
         w = sum == 0.f ? 0.f : w / sum;
+      } else {
+        w = mine ? 1.f / (1.f + expf(-z)) : 0.f;
       }
     }
     if (mine) {
@@ -444,7 +449,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_grad_kernel(const __gr
     }
     const bool in = at >= 0 && at < p.experts;             // (an expert that there is not takes no part)
     if (in) z = to_f(row[at]);
-    float s = 0.f, l[V], top = 0.f, sum = 1.f;
+    float s = 0.f, l[V], top = 0.f, sum = 1.f, rest = 0.f;
     if (p.softmax) {
       top = z;
       if constexpr (WHOLE) {
@@ -464,8 +469,10 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_grad_kernel(const __gr
         sum = sum == 0.f ? 0.f : 1.f / sum;
         s *= sum;
       }
+    } else if (p.renormalise) {
+      s = sigmoid_share(z, warp_largest(z, in), in, rest);
     } else {
-      s = p.renormalise ? sigmoid_share(z, in) : in ? 1.f / (1.f + expf(-z)) : 0.f;
+      s = in ? 1.f / (1.f + expf(-z)) : 0.f;
     }
     float d;                         // dL/dlogit of this lane's expert, of this choice alone
     float dot = 0.f;
@@ -473,7 +480,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps) route_grad_kernel(const __gr
       const float total = warp_sum(s), share = total == 0.f ? 0.f : s / total;
       dot = warp_sum(in ? u * share : 0.f);
       const float g = share * (u - dot);
-      d = p.softmax ? g : g / (1.f + expf(z));             // (share (1 - s) (u - dot); 1 - s = 1 / (1 + exp(z)))
+      d = p.softmax ? g : g * rest;                        // (share (1 - s) (u - dot))
       dot = 0.f;
     } else if (p.softmax) {
       dot = warp_sum(in ? u * s : 0.f);

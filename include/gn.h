@@ -583,7 +583,8 @@ typedef enum { GN_SOFTMAX = 0, GN_SIGMOID = 1 } gn_score;
  *   - of `groups` groups of neighbouring experts those top_groups remain that have the largest sum of their group_best (1 or 2, or all they have) largest values;
  *   - index [tokens][k]: the k experts of the largest values, the largest first;
  *   - weight [tokens][k]: scale s_e, with `renormalise` divided by the sum of the chosen experts' s_e.  (The bias takes part in the choice alone.)
- * Equal values go by the lower number (experts and groups).  The order is that of the exact values: no rounding of FP32 decides it.  -inf is the
+ * Equal values go by the lower number (experts and groups).  The order is that of the values in 64 bits (of a group's two best, the scores' sum and the biases' each by itself): no
+ * rounding of FP32 decides it.  -inf is the
  * logit of an expert that cannot be taken: it has the score 0, and comes last without a bias (with one, a bias of -inf keeps it out); a row of
  * nothing else has weights of 0, and so with sigmoid has one whose chosen scores are all below exp(-700) (a mask by the type's lowest value, not one of -inf); above that
  * the weights of `renormalise` add up to scale, however small the scores are.  NaN comes behind every number (and is not among a group's best); with softmax a NaN or +inf in a row makes its weights NaN.
@@ -629,12 +630,14 @@ typedef struct { void* p; int64_t ld, stride; } gn_stack;   /* a matrix of every
  *     dWg_e = sum dgate x_t^T,   dWu_e = sum dup x_t^T,   dWd_e = sum weight dy_t h^T   over the pairs of expert e (zero without any).
  *   dy, x, index, weight, gate, up and the weights are inputs; dx, dweight [tokens][k] (0 where there is no expert), dw_gate, dw_up, dw_down are outputs, each NULL where
  *   it is not wanted.
- * GN_BF16, GN_F16: h, weight h, dup and dgate are rounded to the type on their way into the next product, everything else is FP32 until it is a result; what is
+ * GN_BF16, GN_F16: h, weight h, dup and dgate are rounded to the type on their way into the next product, everything else is FP32 until it is a result.  (A product's sum stays in the
+ * tensor core, which cuts off what does not fit, towards zero: dweight is 2e-6 of itself too small at 2048 columns.)  What is
  * said of GN_F16's range at gn_gated_ffn holds here.  GN_F32: products at FP32 accuracy, by size on FMAs or on the tensor cores in three BF16 parts of each
  * operand, where an infinite element gives NaN.
  * A bounded wait that ran out shows in gn_gated_ffn_status.
  * Workspace: gn_experts_workspace(args, backward) bytes for the same args; it depends on sizes, types, leading dimensions, strides and on the alignment of
- * the pointers, and is negative for bad arguments.
+ * the pointers, and is negative for bad arguments.  It can exceed the weights: GN_F32 on the tensor cores holds the three parts of every expert's weights (6 bytes an
+ * element of the matrices that the pass reads), GN_BF16 and GN_F16 a copy of matrices whose rows do not start on 16 bytes.
  * experts <= 1024; k <= 32; 1 <= cols, inner <= 2^20 with cols * inner < 2^31; tokens * k < 2^28; the matrices of the experts do not overlap.
  */
 typedef struct {
@@ -677,7 +680,9 @@ gn_status gn_unpack4(gn_dtype type, int32_t experts, int64_t rows, int64_t cols,
                      int64_t ld, int64_t stride, void* cuda_stream, char* errbuf, int64_t errbuf_len);
 
 /*
- * gn_matvec4 - y [tokens][rows] = x [tokens][cols] W^T of packed weights W [rows][cols].  Meant for a few tokens; any number below 2^19 is taken, 32 at a time.
+ * gn_matvec4 - y [tokens][rows] = x [tokens][cols] W^T of packed weights W [rows][cols].  Meant for a few tokens; any number below 2^19 is taken, 32 at a time, each
+ * of which reads and unpacks all weights again.  For a prompt gn_unpack4 and then gn_gated_ffn or gn_experts take less: in BF16 from 160 tokens on through a layer of 4096 x 8192,
+ * from 2600 through 4 of 64 experts of 2048 x 1024.
  * Products of the type's numbers and whole q - 8, summed in FP32 group by group, times the scale; FP32 tokens lose nothing.
  * Workspace: gn_matvec4_workspace(type, tokens, cols, d_x, ldx) bytes; none for 16-bit tokens whose rows start on 16 bytes and have a multiple of 8 columns.
  */

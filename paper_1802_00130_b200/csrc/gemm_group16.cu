@@ -14,7 +14,9 @@
 // GROUP_GATE: the B tile is 128 rows of the gate's weights and the same 128 of the up projection's.  h, dgate and dup are rounded to the type: they are operands of the
 // next product.  (Rows of GROUP_DOWN and GROUP_DX in the type would save 270 MB at 8192 tokens, 4 choices and 2048 columns, and make the error of y and dx 1.7 times
 // that of their own rounding instead of 1.4.)
-// GROUP_GRAD's sums for the gradient of the routing weights stay FP32: a thread has 64 columns of its row, their sums are added in order elsewhere.
+// GROUP_GRAD's sums for the gradient of the routing weights stay FP32: a thread has 64 columns of its row, their sums are added in order elsewhere.  They are of sums q that all their terms have
+// been added to in tensor memory, cut off towards zero each time: 2e-6 of dweight at 2048 columns, where FP32 operands (gemm_group32.cu) pay a fifth of their time for 5e-7.  Here gate and up
+// have come with 2^-9 or 2^-12 already.
 // Bound, with all pairs at work, by what L2 gives to shared memory: 32 KB a CTA for 64 terms, 0.37 us (13 TB/s), where the products take 0.27; and by the power cap.
 // 8192 tokens, 4 of 64 experts, 2048 x 1408: gate 361 us (1047 TFLOP/s, a fifth of the rows padding), with Wd 185; 4 of 32, 2048 x 1024: gate's gradient 172, dx 213, three
 // weight gradients 315.  16 tokens, 4 of 32 experts: 48 and 28, the weights at 4.7 TB/s (224 tiles are 3.03 rounds of the pairs).

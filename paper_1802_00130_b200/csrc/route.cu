@@ -3,14 +3,14 @@
 // A warp has a row of logits in registers, V neighbouring experts to a lane, so that the lowest lane that holds the largest value holds the lowest expert that
 // has it.  The k largest are taken one after the other: a warp's maximum of 32-bit keys is one instruction, and only the lane that gives an
 // expert away looks for its next best.  16384 rows of 256 FP32 logits are 17 MB, 2.8 us of the memory's time; the instructions of the choice bound the kernel, not
-// the bytes: 10 us for the best one without a bias, 15 for eight, 21 with a bias, 29 with groups as well (1240 instructions a row, half of them on the pipe of half the rate).
+// the bytes: 10 us for the best one without a bias, 15 for eight, 22 with a bias, 27 with groups as well, and 32 where the rows come from memory (1240 instructions a row, half of them on the pipe of half the rate).
 //
 // The order of two experts has to be that of their values, whatever FP32 makes of them.  Without a bias it is the order of the logits, which are at hand.
 // With one, and for sums of a group's two best, the values are computed in FP32 with a bound on what they may be off; where two neighbours in the
 // order are nearer than that (and not the same logit with the same bias, which are equal in any arithmetic), the row is done again in FP64, from shared memory, in a
 // function of its own that leaves the usual case its registers.
 //
-// The backward pass reads a whole row only where the scores are shares of all experts; else the chosen logits alone: 9 us for 16384 rows of 256, 17 MB written.
+// The backward pass reads a whole row only where the scores are shares of all experts; else the chosen logits alone: 8 us for 16384 rows of 256, 17 MB written.
 #include <math.h>
 
 #include "op_common.cuh"

@@ -630,8 +630,8 @@ typedef struct { void* p; int64_t ld, stride; } gn_stack;   /* a matrix of every
  *     dWg_e = sum dgate x_t^T,   dWu_e = sum dup x_t^T,   dWd_e = sum weight dy_t h^T   over the pairs of expert e (zero without any).
  *   dy, x, index, weight, gate, up and the weights are inputs; dx, dweight [tokens][k] (0 where there is no expert), dw_gate, dw_up, dw_down are outputs, each NULL where
  *   it is not wanted.
- * GN_BF16, GN_F16: h, weight h, dup and dgate are rounded to the type on their way into the next product, everything else is FP32 until it is a result.  (A product's sum stays in the
- * tensor core, which cuts off what does not fit, towards zero: dweight is 2e-6 of itself too small at 2048 columns.)  What is
+ * GN_BF16, GN_F16: h, weight h, dup and dgate are rounded to the type on their way into the next product, everything else is FP32 until it is a result (dweight
+ * is off by 5e-7 of it in GN_BF16, 7e-7 in GN_F16, in the mean over many pairs).  What is
  * said of GN_F16's range at gn_gated_ffn holds here.  GN_F32: products at FP32 accuracy, by size on FMAs or on the tensor cores in three BF16 parts of each
  * operand, where an infinite element gives NaN.
  * A bounded wait that ran out shows in gn_gated_ffn_status.

@@ -633,7 +633,7 @@ typedef struct { void* p; int64_t ld, stride; } gn_stack;   /* a matrix of every
  * GN_BF16, GN_F16: h, weight h, dup and dgate are rounded to the type on their way into the next product, everything else is FP32 until it is a result (dweight
  * is off by 5e-7 of it in GN_BF16, 7e-7 in GN_F16, in the mean over many pairs).  What is
  * said of GN_F16's range at gn_gated_ffn holds here.  GN_F32: products at FP32 accuracy, by size on FMAs or on the tensor cores in three BF16 parts of each
- * operand, where an infinite element gives NaN.
+ * operand, with infinities as on FMAs, but for the product of two, which is NaN there.
  * A bounded wait that ran out shows in gn_gated_ffn_status.
  * Workspace: gn_experts_workspace(args, backward) bytes for the same args; it depends on sizes, types, leading dimensions, strides and on the alignment of
  * the pointers, and is negative for bad arguments.  It can exceed the weights: GN_F32 on the tensor cores holds the three parts of every expert's weights (6 bytes an

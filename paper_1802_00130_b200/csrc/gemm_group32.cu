@@ -76,18 +76,20 @@ __device__ __forceinline__ float4 four32(const float* row, int c, int n, bool ve
   return v;
 }
 // The three parts of v, and of w beside them: the first two rounded to nearest (halves away from zero), so that what is left is half as large, and of either sign; the third is all that is left.  What
-// would be rounded to infinity is cut off; an infinity leaves nothing, and of a NaN one part at least is one.
-__device__ __forceinline__ uint32_t leading(float v) {
+// would be rounded to infinity is cut off.  An infinity is a third part alone, which meets the other number's first part and nothing else: its product is infinite (NaN with a zero, or with another
+// infinity, which has no first part).  Of a NaN one part at least is one.
+__device__ __forceinline__ uint32_t first_part(float v, bool infinite) {
   const uint32_t a = __float_as_uint(v);
-  return (a & 0x7fffffffu) < 0x7f7f8000u ? a + 0x8000u : a;
+  return infinite ? 0u : (a & 0x7fffffffu) < 0x7f7f8000u ? a + 0x8000u : a;
 }
+__device__ __forceinline__ uint32_t next_part(float v, bool infinite) { return infinite ? 0u : __float_as_uint(v) + 0x8000u; }
 __device__ __forceinline__ float less(float v, uint32_t part) { return v - __uint_as_float(part & 0xffff0000u); }
 __device__ __forceinline__ void three(float v, float w, uint32_t (&o)[3]) {
-  uint32_t a = leading(v), b = leading(w);
+  const bool iv = fabsf(v) == __int_as_float(0x7f800000), iw = fabsf(w) == __int_as_float(0x7f800000);
+  uint32_t a = first_part(v, iv), b = first_part(w, iw);
   o[0] = __byte_perm(a, b, 0x7632);
-  v = fabsf(v) == __int_as_float(0x7f800000) ? 0.f : less(v, a);
-  w = fabsf(w) == __int_as_float(0x7f800000) ? 0.f : less(w, b);
-  a = __float_as_uint(v) + 0x8000u; b = __float_as_uint(w) + 0x8000u;
+  v = less(v, a); w = less(w, b);
+  a = next_part(v, iv); b = next_part(w, iw);
   o[1] = __byte_perm(a, b, 0x7632);
   o[2] = __byte_perm(__float_as_uint(less(v, a)), __float_as_uint(less(w, b)), 0x7632);
 }

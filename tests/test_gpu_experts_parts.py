@@ -73,3 +73,26 @@ def test_largest_numbers_infinities_and_nan():
         assert not bool(other[5].isfinite().any())
         other[5] = gate[5]
         assert torch.equal(other, gate)
+
+
+@pytest.mark.parametrize("shape", [SHAPE, (300, 264, 136, 6, 2)])
+def test_infinities_are_those_of_the_formula(shape):
+    """An infinite token or weight: infinite projections of the formula's signs, NaN where it meets a zero, and the same on FMAs (the second shape) and on the tensor cores."""
+    tokens, cols, inner, experts, k = shape
+    assert path(*shape, False) == ("tensor" if shape == SHAPE else "small")
+    x, w_gate = numbers(tokens * cols, 1, True).view(tokens, cols).clone(), numbers(experts * inner * cols, 2, True).view(experts, inner, cols).clone()
+    w_up, w_down = w_gate.flip(1).clone(), torch.ones(experts, cols, inner, device="cuda")
+    x[5, 7], x[6, 9], x[8, cols - 1] = math.inf, -math.inf, math.inf
+    x[10, 3] = 0
+    w_gate[1, 4, 3] = math.inf
+    w_gate[2, 5, 7] = 0
+    w_up[0, 2, 11] = -math.inf
+    index = (torch.arange(tokens * k, device="cuda") % experts).to(torch.int32).view(tokens, k)
+    y, gate, up = gn.experts(x, index, torch.ones(tokens, k, device="cuda"), w_gate, w_up, w_down, "relu", save=True)
+    for got, w in ((gate, w_gate), (up, w_up)):
+        # (term by term, so that the 64-bit form meets infinities as the formula has them)
+        want = torch.stack([(x.double()[:, None, :] * w[e].double()[None]).sum(2) for e in range(experts)], 1).gather(1, index.long()[:, :, None].expand(-1, -1, inner))
+        got = got.view(tokens, k, inner)
+        assert bool(want.isinf().any()) and bool(want.isnan().any() or w is w_up)
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+        assert torch.equal(got[want.isinf()].double(), want[want.isinf()])
